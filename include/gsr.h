@@ -315,6 +315,57 @@ gsr_status_t gsr_sgd_update(float* w, const float* dw, int64_t count, float lr, 
 gsr_status_t gsr_adam_update(float* w, const float* dw, float* m, float* v, int64_t count, int64_t t, float lr,
                              float beta1, float beta2, float eps, float weight_decay, void* stream);
 
+/* ---- node embeddings: where X^0 comes from and what becomes of dL/dX^0 ----
+ *
+ * E: a table of `vocab` rows of d values, row stride ldt elements.  ids: device, n tokens (the cell type of every node, or any other
+ * number), int32, or int64 with ids_i64 = 1.  A token outside [0, vocab), such as -1, has no embedding: its row of x is zero and
+ * its row of dx has no part in the gradient (nor is it read).
+ * Planes (x, dx; device, n x d of `dtype`): ROW_MAJOR with row stride ldx elements, d at least; GROUP_PLANAR in c groups of d/c columns,
+ * row stride ldx, d/c at least, group stride n * ldx (ldx = d/c: what gsr_step takes).  Elements between rows are left as they are.
+ * 1 <= d <= 131072, c divides d, n < 2^31, 1 <= vocab < 2^31 - 1; pointers aligned to their elements.
+ * All tensors on the current device.  Calls only launch kernels and may be captured.
+ *
+ * gsr_embed_lookup: x[i, :] = scale * E[ids[i], :], rounded once to `dtype`; table and plane of either type. */
+gsr_status_t gsr_embed_lookup(const void* table, int64_t vocab, int64_t ldt, int32_t table_dtype, const void* ids, int32_t ids_i64,
+                              int64_t n, int32_t d, int32_t c, int32_t layout, int32_t dtype, float scale, void* x_out, int64_t ldx,
+                              void* stream);
+
+/* gsr_embed_grad: dE[t, :] = scale * sum of dx[i, :] over the rows i with ids[i] = t.  dtable_out: device, vocab rows of d floats,
+ * row stride ldt; every row is written, zeros where a token does not occur.  The positions are sorted by token and the sums taken in
+ * float32 in an order that the tokens alone fix: equal calls give equal bits.  workspace: device, 16-byte aligned, at least
+ * gsr_embed_grad_workspace() bytes (about n (16 + d / 8), the same for all types and layouts; 0 for sizes that are refused); it holds
+ * nothing between calls. */
+size_t gsr_embed_grad_workspace(int64_t n, int64_t vocab, int32_t d, int32_t c);
+gsr_status_t gsr_embed_grad(const void* ids, int32_t ids_i64, int64_t n, const void* dx, int64_t ldx, int32_t d, int32_t c, int32_t layout,
+                            int32_t dtype, float scale, int64_t vocab, float* dtable_out, int64_t ldt, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* ---- all tensors of a step at once: gradient norm, clipping, parameter update ----
+ *
+ * A list is `tensors` device addresses and `counts` sizes in elements, both host arrays that are read during the call; every tensor is a
+ * contiguous array on the current device, aligned to its elements, and may be empty.  At most 2^40 elements.  What a call writes may not
+ * overlap anything else in its lists (GSR_ERR_INVALID_ARG; a tensor named twice is such a case).  workspace: device, 8-byte aligned, at
+ * least gsr_grad_norm_workspace(counts, tensors) bytes; it holds nothing between calls.  Calls only launch kernels and may be captured;
+ * addresses, sizes and scalars are then those of the capture.
+ *
+ * gsr_grad_norm: norm_out (device, 1 float) = sqrt(sum g^2) over all elements of all tensors; squares and sums in float64.
+ *
+ * gsr_grad_clip: g <- c g with c = min(1, max_norm / (norm + 1e-6)), in place (out = NULL; with c = 1 nothing is written) or into the tensors
+ * `out` of the same sizes and of out_dtype.  max_norm >= 0 and finite.  norm_out: device, 1 float, the norm before clipping, or NULL.
+ * An infinite gradient makes the norm infinite and c zero (what was infinite becomes NaN, the rest zero), a NaN all of them NaN. */
+size_t gsr_grad_norm_workspace(const int64_t* counts, int32_t tensors);
+gsr_status_t gsr_grad_norm(const void* const* grads, const int64_t* counts, int32_t tensors, int32_t dtype, float* norm_out, void* workspace,
+                           size_t workspace_bytes, void* stream);
+gsr_status_t gsr_grad_clip(void* const* grads, const int64_t* counts, int32_t tensors, int32_t dtype, float max_norm, float* norm_out,
+                           void* const* out, int32_t out_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* gsr_adam_update on every tensor of a list: w, m, v float32, dw of dw_dtype.  norm (device, 1 float, as gsr_grad_norm leaves it, or NULL):
+ * the gradients count multiplied by c as above, without being changed; max_norm is read only with it.  Without norm, or with c = 1, the
+ * same bits as gsr_adam_update. */
+gsr_status_t gsr_adam_update_list(float* const* w, const void* const* dw, float* const* m, float* const* v, const int64_t* counts,
+                                  int32_t tensors, int32_t dw_dtype, const float* norm, float max_norm, int64_t t, float lr, float beta1,
+                                  float beta2, float eps, float weight_decay, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

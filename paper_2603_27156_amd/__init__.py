@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 from dataclasses import dataclass
 from typing import Optional, Tuple
 
@@ -34,6 +35,8 @@ EXPORTED = [
     "gsr_spmm_compressed", "gsr_workspace_size", "gsr_layer_forward", "gsr_layer_inverse", "gsr_layer_backward",
     "gsr_step", "gsr_step_tie_stats", "gsr_step_tie_export", "gsr_walkthrough_workspace", "gsr_slot_block", "gsr_alg1_layer_forward", "gsr_alg2_layer_backward",
     "gsr_sgd_update", "gsr_adam_update",
+    "gsr_embed_lookup", "gsr_embed_grad_workspace", "gsr_embed_grad",
+    "gsr_grad_norm_workspace", "gsr_grad_norm", "gsr_grad_clip", "gsr_adam_update_list",
 ]
 
 
@@ -72,6 +75,16 @@ def lib():
         l.gsr_spmm_compressed_workspace.argtypes = [C.c_void_p, C.c_int32, C.c_int32]
         l.gsr_walkthrough_workspace.restype = C.c_size_t
         l.gsr_walkthrough_workspace.argtypes = [C.c_void_p, C.c_int32]
+        p, i32, i64, f32, size = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_size_t
+        l.gsr_embed_lookup.argtypes = [p, i64, i64, i32, p, i32, i64, i32, i32, i32, i32, f32, p, i64, p]
+        l.gsr_embed_grad_workspace.restype = size
+        l.gsr_embed_grad_workspace.argtypes = [i64, i64, i32, i32]
+        l.gsr_embed_grad.argtypes = [p, i32, i64, p, i64, i32, i32, i32, i32, f32, i64, p, i64, p, size, p]
+        l.gsr_grad_norm_workspace.restype = size
+        l.gsr_grad_norm_workspace.argtypes = [p, i32]
+        l.gsr_grad_norm.argtypes = [p, p, i32, i32, p, p, size, p]
+        l.gsr_grad_clip.argtypes = [p, p, i32, i32, f32, p, p, i32, p, size, p]
+        l.gsr_adam_update_list.argtypes = [p, p, p, p, p, i32, i32, p, f32, i64, f32, f32, f32, f32, f32, p]
         _lib = l
     return _lib
 
@@ -313,6 +326,135 @@ def gsr_adam_update(w, dw, m, v, t: int, lr: float, beta1: float = 0.9, beta2: f
         assert x.is_cuda and x.dtype == torch.float32 and x.is_contiguous() and x.numel() == w.numel()
     _check(lib().gsr_adam_update(_dp(w), _dp(dw), _dp(m), _dp(v), C.c_int64(w.numel()), C.c_int64(t), C.c_float(lr),
                                  C.c_float(beta1), C.c_float(beta2), C.c_float(eps), C.c_float(weight_decay), _stream()))
+
+
+def _plane(x):
+    """(rows, D, groups, layout, row stride) of a plane [n, D] (rows may be strided) or [C, n, D/C]."""
+    assert x.is_cuda and x.device.index == _current_device() and x.dim() in (2, 3) and (x.stride(-1) == 1 or x.shape[-1] == 1)
+    if x.dim() == 2:
+        n, d = x.shape
+        return n, d, 1, GSR_LAYOUT_ROW_MAJOR, x.stride(0) if n > 1 else d
+    c, n, dg = x.shape
+    ld = x.stride(1) if n > 1 else x.stride(0) if n and c > 1 else dg
+    assert c == 1 or n == 0 or x.stride(0) == n * ld, "the groups of a plane follow each other"
+    return n, c * dg, c, GSR_LAYOUT_GROUP_PLANAR, ld
+
+
+def _current_device() -> int:
+    import torch
+    return torch.cuda.current_device()
+
+
+def _tokens(ids, n: int) -> int:
+    import torch
+    assert ids.device.index == _current_device() and ids.is_cuda and ids.is_contiguous() and ids.dim() == 1 and len(ids) == n
+    assert ids.dtype in (torch.int32, torch.int64)
+    return 1 if ids.dtype == torch.int64 else 0
+
+
+def gsr_embed_lookup(table, ids, x_out, scale: float = 1.0) -> None:
+    """x_out[i] = scale * table[ids[i]], zeros where a token lies outside the table.  table: [vocab, D], rows may be strided; x_out: a
+    plane [n, D] or [C, n, D/C]; either of both float32 or bfloat16.  ids: [n] int32 or int64."""
+    n, d, c, layout, ldx = _plane(x_out)
+    vocab, dt, _, _, ldt = _plane(table)
+    assert dt == d and table.dim() == 2
+    _check(lib().gsr_embed_lookup(table.data_ptr(), vocab, ldt, _dtype_of(table), ids.data_ptr(), _tokens(ids, n), n, d, c, layout,
+                                  _dtype_of(x_out), scale, x_out.data_ptr(), ldx, _stream()))
+
+
+def gsr_embed_grad_workspace(n: int, vocab: int, d: int, c: int = 1) -> int:
+    return lib().gsr_embed_grad_workspace(n, vocab, d, c)
+
+
+def gsr_embed_grad(ids, dx, dtable_out, scale: float = 1.0, workspace=None) -> None:
+    """dtable_out[t] = scale * sum of dx[i] over ids[i] == t (float32 [vocab, D], rows may be strided; written whole).  dx: a plane as
+    gsr_embed_lookup's x_out; workspace: device tensor of gsr_embed_grad_workspace(n, vocab, D, C) bytes, or None."""
+    import torch
+    n, d, c, layout, ldx = _plane(dx)
+    vocab, dt, _, _, ldt = _plane(dtable_out)
+    assert dt == d and dtable_out.dim() == 2 and dtable_out.dtype == torch.float32
+    if workspace is None:
+        workspace = torch.empty(gsr_embed_grad_workspace(n, vocab, d, c), dtype=torch.uint8, device=dx.device)
+    _check(lib().gsr_embed_grad(ids.data_ptr(), _tokens(ids, n), n, dx.data_ptr(), ldx, d, c, layout, _dtype_of(dx), scale, vocab,
+                                dtable_out.data_ptr(), ldt, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
+
+
+def _addresses(tensors, dtype, counts=None) -> array:
+    """The addresses of contiguous tensors of one type on the current device, as many elements each as `counts` says."""
+    dev = _current_device()
+    for t in tensors:
+        assert t.get_device() == dev and t.dtype is dtype and t.is_contiguous()
+    assert counts is None or array("q", [t.numel() for t in tensors]) == counts, "lists of different sizes"
+    return array("Q", [t.data_ptr() for t in tensors])
+
+
+def _counts(tensors) -> array:
+    return array("q", [t.numel() for t in tensors])
+
+
+def _at(a: array) -> int:
+    return a.buffer_info()[0]
+
+
+def _list_type(tensors):
+    """(torch type, library's type) of a list of gradients."""
+    import torch
+    return (tensors[0].dtype, _dtype_of(tensors[0])) if len(tensors) else (torch.float32, GSR_F32)
+
+
+def _norm_workspace(counts, workspace):
+    import torch
+    if workspace is None:
+        workspace = torch.empty(lib().gsr_grad_norm_workspace(_at(counts), len(counts)), dtype=torch.uint8, device="cuda")
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def gsr_grad_norm_workspace(grads) -> int:
+    counts = _counts(grads)
+    return lib().gsr_grad_norm_workspace(_at(counts), len(counts))
+
+
+def _scalar(t) -> int:
+    import torch
+    if t is None:
+        return 0
+    assert t.get_device() == _current_device() and t.dtype == torch.float32 and t.numel() == 1
+    return t.data_ptr()
+
+
+def gsr_grad_norm(grads, norm_out, workspace=None) -> None:
+    """norm_out (float32, one element) = the 2-norm over all elements of a list of tensors (float32, or all bfloat16)."""
+    kind, dtype = _list_type(grads)
+    counts, at = _counts(grads), _addresses(grads, kind)
+    ws, nb = _norm_workspace(counts, workspace)
+    _check(lib().gsr_grad_norm(_at(at), _at(counts), len(counts), dtype, _scalar(norm_out), ws.data_ptr(), nb, _stream()))
+
+
+def gsr_grad_clip(grads, max_norm: float, norm_out=None, out=None, workspace=None) -> None:
+    """Multiplies the tensors of a list by min(1, max_norm / (norm + 1e-6)), in place or into the tensors of `out` (of the same sizes, of
+    one type); norm_out (float32, one element): the norm before clipping."""
+    kind, dtype = _list_type(grads)
+    counts, at = _counts(grads), _addresses(grads, kind)
+    to, out_dtype = None, dtype
+    if out is not None:
+        out_kind, out_dtype = _list_type(out)
+        to = _addresses(out, out_kind, counts)
+    ws, nb = _norm_workspace(counts, workspace)
+    _check(lib().gsr_grad_clip(_at(at), _at(counts), len(counts), dtype, max_norm, _scalar(norm_out), None if to is None else _at(to),
+                               out_dtype, ws.data_ptr(), nb, _stream()))
+
+
+def gsr_adam_update_list(w, dw, m, v, t: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                         weight_decay: float = 0.0, norm=None, max_norm: float = 0.0) -> None:
+    """gsr_adam_update on every tensor of four lists, dw (float32, or all bfloat16) multiplied by min(1, max_norm / (norm + 1e-6)) where
+    norm, as gsr_grad_norm leaves it on the device, is given."""
+    import torch
+    kind, dtype = _list_type(dw)
+    counts = _counts(w)
+    ptrs = [_addresses(w, torch.float32), _addresses(dw, kind, counts), _addresses(m, torch.float32, counts),
+            _addresses(v, torch.float32, counts)]
+    _check(lib().gsr_adam_update_list(*map(_at, ptrs), _at(counts), len(counts), dtype, _scalar(norm), max_norm, t, lr, beta1, beta2, eps,
+                                      weight_decay, _stream()))
 
 
 def gsr_spmm_compressed(g: Graph, vals, idx, dg: int):

@@ -1,0 +1,679 @@
+// Node embeddings: the plane a stack of layers starts from, looked up by token, and the gradient of the table.
+//
+//   gsr_embed_lookup   x[n, :] = scale * E[id_n, :]
+//   gsr_embed_grad     dE[v, :] = scale * sum over the rows n with id_n = v of dx[n, :]
+//
+// A token outside [0, vocab) has no embedding: its row of x is zero, its row of dx is not read.
+#include "gsr_internal.h"
+#include "gsr_device.h"
+
+#include <algorithm>
+
+namespace gsr {
+
+// ---- pieces of a row ------------------------------------------------------------------------------------
+// Rows move in pieces of 16 bytes of the plane's type (V = 4 floats or 8 16-bit values).  The last piece of a row whose width
+// is no multiple of V starts V elements before the row's end and overlaps the one before it: both lanes load, sum and store the
+// same numbers, so nothing is predicated.  Rows narrower than a piece are taken element by element (V = 1).  Pieces are aligned
+// to their elements only.
+typedef uint32_t u32x2h __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x4h __attribute__((ext_vector_type(4), aligned(2)));
+
+template <typename T, int V>
+struct Piece {                       // V elements as they lie in memory
+    static constexpr int NW = (V * (int)sizeof(T) + 3) / 4;
+    uint32_t w[NW];
+    __device__ __forceinline__ void load(const T* p) {
+        if constexpr (V == 1) {
+            if constexpr (sizeof(T) == 4) w[0] = *reinterpret_cast<const uint32_t*>(p);
+            else w[0] = (uint32_t)*reinterpret_cast<const uint16_t*>(p) << 16;
+        } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < NW; i += 4) {
+                const u32x4a t = *reinterpret_cast<const u32x4a*>(p + i);
+                w[i] = t[0]; w[i + 1] = t[1]; w[i + 2] = t[2]; w[i + 3] = t[3];
+            }
+        } else if constexpr (NW == 2) {
+            const u32x2h t = *reinterpret_cast<const u32x2h*>(p);
+            w[0] = t[0]; w[1] = t[1];
+        } else {
+            const u32x4h t = *reinterpret_cast<const u32x4h*>(p);
+            w[0] = t[0]; w[1] = t[1]; w[2] = t[2]; w[3] = t[3];
+        }
+    }
+    __device__ __forceinline__ float at(int i) const {
+        if constexpr (V == 1 || sizeof(T) == 4) return __uint_as_float(w[i]);
+        else return __uint_as_float((i & 1) ? (w[i >> 1] & 0xFFFF0000u) : (w[i >> 1] << 16));
+    }
+};
+
+// rounded to the nearest 16-bit value, NaN stays NaN
+__device__ __forceinline__ uint32_t bf16_bits(float v) { return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v)); }
+
+template <int V, typename T>
+__device__ __forceinline__ void store_piece(T* p, const float (&v)[V]) {
+    if constexpr (sizeof(T) == 4) {
+        if constexpr (V == 1) {
+            *p = v[0];
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; i += 4) {
+                u32x4a t;
+                t[0] = __float_as_uint(v[i]); t[1] = __float_as_uint(v[i + 1]);
+                t[2] = __float_as_uint(v[i + 2]); t[3] = __float_as_uint(v[i + 3]);
+                *reinterpret_cast<u32x4a*>(p + i) = t;
+            }
+        }
+    } else {
+        if constexpr (V == 1) {
+            p->bits = (uint16_t)bf16_bits(v[0]);
+        } else {
+            static_assert(V == 8, "16-bit pieces hold eight values");
+            u32x4h t;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t[i] = bf16_bits(v[2 * i]) | (bf16_bits(v[2 * i + 1]) << 16);
+            *reinterpret_cast<u32x4h*>(p) = t;
+        }
+    }
+}
+
+// a token's row of the table, or `vocab` where it has none
+template <typename I>
+__device__ __forceinline__ int32_t token_row(I id, int32_t vocab) { return id >= 0 && id < (I)vocab ? (int32_t)id : vocab; }
+
+// ---- lookup ---------------------------------------------------------------------------------------------
+// blockIdx.y: the group (planes) or 0 (rows); a workgroup writes whole rows of it, about 1,024 pieces.  `magic` divides a piece's
+// number by the pieces per row (ceil(2^32 / pg), 0 for one piece; exact below 2^16).
+template <typename TT, typename T, typename I, int V>
+__global__ __launch_bounds__(256) void k_embed_lookup(const TT* __restrict__ table, int64_t ldt, int32_t vocab,
+                                                      const I* __restrict__ ids, int64_t n, int dg, int pg, uint32_t magic,
+                                                      int rows_per_wg, float scale, T* __restrict__ x, int64_t ldx, int64_t gs) {
+    const int group = blockIdx.y;
+    const TT* tab = table + (int64_t)group * dg;
+    T* plane = x + group * gs;
+    for (int64_t row0 = (int64_t)blockIdx.x * rows_per_wg; row0 < n; row0 += (int64_t)gridDim.x * rows_per_wg) {
+        const int rows = n - row0 < rows_per_wg ? (int)(n - row0) : rows_per_wg;
+        const uint32_t count = (uint32_t)rows * (uint32_t)pg;
+        for (uint32_t t0 = threadIdx.x; t0 < count; t0 += 4 * 256) {
+            uint32_t row[4], col[4];
+            int32_t id[4];
+            Piece<TT, V> p[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const uint32_t t = t0 + 256 * u < count ? t0 + 256 * u : count - 1;
+                row[u] = magic ? __umulhi(t, magic) : t;
+                const uint32_t q = (t - row[u] * (uint32_t)pg) * V;
+                col[u] = q + V <= (uint32_t)dg ? q : (uint32_t)(dg - V);
+                id[u] = token_row(ids[row0 + row[u]], vocab);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) p[u].load(tab + (id[u] < vocab ? id[u] : 0) * ldt + col[u]);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (t0 + 256 * u >= count) break;
+                float v[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[i] = id[u] < vocab ? scale * p[u].at(i) : 0.0f;
+                store_piece<V>(plane + (row0 + row[u]) * ldx + col[u], v);
+            }
+        }
+    }
+}
+
+// ---- positions sorted by token ----------------------------------------------------------------------------
+// A stable counting sort, so that the sums are taken in an order that the tokens alone fix.  Digits of up to 11 bits: tokens of a
+// vocabulary below 2,048 take one pass, below 4M two.  A pass is three launches: every workgroup counts the digits of its
+// stretch; a wave per digit turns the counts into places; every workgroup hands its elements out.  Within a workgroup each
+// wave owns a stretch and takes it 64 elements at a time; lanes of equal digits find their order from one ballot per bit.
+constexpr int kDigitBits = 11;
+constexpr int kSortWaves = 4;
+constexpr int kSmallSort = 4096;     // elements that one workgroup sorts in LDS
+constexpr int kSmallBits = 8;
+
+// What the sort moves: (row of the table or vocab, position).  The first pass reads tokens, positions are their own numbers.
+template <typename I>
+struct SortSource {
+    const I* ids;
+    const uint32_t* pos;             // nullptr: the first pass
+    int32_t vocab;
+    __device__ __forceinline__ int32_t key(int64_t i) const { return token_row(ids[i], vocab); }
+    __device__ __forceinline__ uint32_t place(int64_t i) const { return pos ? pos[i] : (uint32_t)i; }
+};
+
+// lanes of the wave that hold this lane's digit (valid lanes only)
+__device__ __forceinline__ uint64_t same_digit(uint32_t digit, int bits, bool valid) {
+    uint64_t m = ballot(valid);
+    for (int b = 0; b < bits; ++b) {
+        const bool one = (digit >> b) & 1;
+        const uint64_t o = ballot(one);
+        m &= one ? o : ~o;
+    }
+    return m;
+}
+__device__ __forceinline__ int lanes_below(uint64_t m) {
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+}
+// inclusive sum over the wave
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+    const int lane = lane_id();
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t t = __shfl_up(v, o);
+        if (lane >= o) v += t;
+    }
+    return v;
+}
+
+// The table's gradient is cleared by workgroups of the sort's first launch, beside it: sums are stored later, over the zeros.
+__device__ __forceinline__ void clear_rows(float* out, int64_t ldt, int64_t vocab, int d, int64_t wg, int64_t wgs) {
+    const int64_t first = wg * blockDim.x + threadIdx.x, step = wgs * blockDim.x;
+    if (ldt == d) {
+        const int64_t total = vocab * d, quads = total / 4;
+        const u32x4a z = {0, 0, 0, 0};
+        for (int64_t i = first; i < quads; i += step) *reinterpret_cast<u32x4a*>(out + 4 * i) = z;
+        for (int64_t i = 4 * quads + first; i < total; i += step) out[i] = 0.0f;
+    } else {
+        for (int64_t i = first; i < vocab * d; i += step) out[i / d * ldt + i % d] = 0.0f;
+    }
+}
+
+template <typename I>
+__global__ __launch_bounds__(256) void k_embed_count(SortSource<I> src, int64_t n, int stretch, int wgs, int shift, int bits,
+                                                     uint32_t* __restrict__ hist, float* out, int64_t ldt, int d) {
+    __shared__ uint32_t s_count[1 << kDigitBits];
+    if ((int)blockIdx.x >= wgs) {
+        clear_rows(out, ldt, src.vocab, d, blockIdx.x - wgs, gridDim.x - wgs);
+        return;
+    }
+    const int digits = 1 << bits;
+    for (int i = threadIdx.x; i < digits; i += 256) s_count[i] = 0;
+    __syncthreads();
+    const int64_t a = (int64_t)blockIdx.x * stretch, b = a + stretch < n ? a + stretch : n;
+    for (int64_t i = a + threadIdx.x; i < b; i += 256) atomicAdd(&s_count[((uint32_t)src.key(i) >> shift) & (digits - 1)], 1u);
+    __syncthreads();
+    for (int i = threadIdx.x; i < digits; i += 256) hist[(int64_t)i * wgs + blockIdx.x] = s_count[i];
+}
+
+// counts of a digit -> elements of that digit in the workgroups before; total[digit]
+__global__ __launch_bounds__(256) void k_embed_places(uint32_t* __restrict__ hist, int wgs, int digits, uint32_t* __restrict__ total) {
+    const int digit = blockIdx.x * 4 + (threadIdx.x >> 6), lane = lane_id();
+    if (digit >= digits) return;
+    uint32_t* h = hist + (int64_t)digit * wgs;
+    uint32_t before = 0;
+    for (int i = 0; i < wgs; i += 64) {
+        const uint32_t c = i + lane < wgs ? h[i + lane] : 0;
+        const uint32_t s = wave_scan(c);
+        if (i + lane < wgs) h[i + lane] = before + s - c;
+        before += __shfl(s, 63);
+    }
+    if (lane == 0) total[digit] = before;
+}
+
+// s_start[w * digits + digit]: the place of the next element of that digit in wave w's stretch [a, b)
+template <typename I, typename Put>
+__device__ __forceinline__ void hand_out(const SortSource<I>& src, int64_t a, int64_t b, int shift, int bits, uint32_t* start, Put put) {
+    const uint32_t mask = (1u << bits) - 1;
+    for (int64_t i = a; i < b; i += 64) {
+        const bool valid = i + lane_id() < b;
+        const int64_t e = valid ? i + lane_id() : b - 1;
+        const int32_t key = src.key(e);
+        const uint32_t place = src.place(e), digit = ((uint32_t)key >> shift) & mask;
+        const uint64_t m = same_digit(digit, bits, valid);
+        const int rank = lanes_below(m);
+        const uint32_t to = start[digit] + rank;
+        wave_sync();
+        if (valid && rank == 0) start[digit] += (uint32_t)__popcll(m);
+        wave_sync();
+        if (valid) put(to, key, place);
+    }
+}
+
+// exclusive sums of v[0 .. count) for a workgroup of `waves` waves; s_wave: a word per wave
+__device__ __forceinline__ void wg_scan(uint32_t* v, int count, uint32_t* s_wave, int waves) {
+    const int per = (count + 64 * waves - 1) / (64 * waves), a = threadIdx.x * per;
+    uint32_t sum = 0;
+    for (int i = a; i < a + per && i < count; ++i) sum += v[i];
+    const uint32_t s = wave_scan(sum);
+    if (lane_id() == 63) s_wave[threadIdx.x >> 6] = s;
+    __syncthreads();
+    uint32_t at = s - sum;
+    for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) at += s_wave[w];
+    for (int i = a; i < a + per && i < count; ++i) {
+        const uint32_t c = v[i];
+        v[i] = at;
+        at += c;
+    }
+    __syncthreads();
+}
+
+template <typename I>
+__global__ __launch_bounds__(256) void k_embed_hand_out(SortSource<I> src, int64_t n, int stretch, int wgs, int shift, int bits,
+                                                        const uint32_t* __restrict__ hist, const uint32_t* __restrict__ total,
+                                                        int32_t* __restrict__ keys, uint32_t* __restrict__ pos) {
+    __shared__ uint32_t s_start[kSortWaves << kDigitBits];
+    __shared__ uint32_t s_first[1 << kDigitBits];
+    __shared__ uint32_t s_wave[kSortWaves];
+    const int digits = 1 << bits, w = threadIdx.x >> 6;
+    for (int i = threadIdx.x; i < digits; i += 256) s_first[i] = total[i];
+    for (int i = threadIdx.x; i < kSortWaves * digits; i += 256) s_start[i] = 0;
+    __syncthreads();
+    wg_scan(s_first, digits, s_wave, kSortWaves);
+    // a workgroup's stretch is a multiple of 256 elements: each wave's a multiple of 64
+    const int64_t a0 = (int64_t)blockIdx.x * stretch, b0 = a0 + stretch < n ? a0 + stretch : n;
+    const int64_t a = a0 + (int64_t)w * (stretch / kSortWaves) < b0 ? a0 + (int64_t)w * (stretch / kSortWaves) : b0;
+    const int64_t b = a + stretch / kSortWaves < b0 ? a + stretch / kSortWaves : b0;
+    uint32_t* start = s_start + w * digits;
+    for (int64_t i = a + lane_id(); i < b; i += 64) atomicAdd(&start[((uint32_t)src.key(i) >> shift) & (digits - 1)], 1u);
+    __syncthreads();
+    for (int i = threadIdx.x; i < digits; i += 256) {
+        uint32_t at = s_first[i] + hist[(int64_t)i * wgs + blockIdx.x];
+        for (int v = 0; v < kSortWaves; ++v) {
+            const uint32_t c = s_start[v * digits + i];
+            s_start[v * digits + i] = at;
+            at += c;
+        }
+    }
+    __syncthreads();
+    hand_out(src, a, b, shift, bits, start, [&](uint32_t to, int32_t key, uint32_t place) {
+        keys[to] = key;
+        pos[to] = place;
+    });
+}
+
+// Up to kSmallSort elements: workgroup 0 sorts them in LDS, digits of up to 8 bits, the others clear the gradient.
+template <typename I>
+__global__ __launch_bounds__(1024) void k_embed_sort_small(SortSource<I> ids, int n, int bits, int passes, int32_t* __restrict__ keys,
+                                                           uint32_t* __restrict__ pos, float* out, int64_t ldt, int d) {
+    constexpr int W = 16;
+    __shared__ int32_t s_key[2][kSmallSort];
+    __shared__ uint32_t s_pos[2][kSmallSort];
+    __shared__ uint32_t s_start[W << kSmallBits];
+    __shared__ uint32_t s_first[1 << kSmallBits];
+    __shared__ uint32_t s_wave[W];
+    if (blockIdx.x) {
+        clear_rows(out, ldt, ids.vocab, d, blockIdx.x - 1, gridDim.x - 1);
+        return;
+    }
+    for (int i = threadIdx.x; i < n; i += 1024) {
+        s_key[0][i] = ids.key(i);
+        s_pos[0][i] = (uint32_t)i;
+    }
+    const int digits = 1 << bits, w = threadIdx.x >> 6, per = (n + 64 * W - 1) / (64 * W) * 64;
+    const int a = w * per < n ? w * per : n, b = a + per < n ? a + per : n;
+    for (int p = 0; p < passes; ++p) {
+        const SortSource<int32_t> src{s_key[p & 1], s_pos[p & 1], ids.vocab};
+        uint32_t* start = s_start + w * digits;
+        for (int i = threadIdx.x; i < W * digits; i += 1024) s_start[i] = 0;
+        __syncthreads();
+        for (int i = a + lane_id(); i < b; i += 64) atomicAdd(&start[((uint32_t)src.key(i) >> (p * bits)) & (digits - 1)], 1u);
+        __syncthreads();
+        if ((int)threadIdx.x < digits) {
+            uint32_t sum = 0;
+            for (int v = 0; v < W; ++v) {
+                const uint32_t c = s_start[v * digits + threadIdx.x];
+                s_start[v * digits + threadIdx.x] = sum;
+                sum += c;
+            }
+            s_first[threadIdx.x] = sum;
+        }
+        __syncthreads();
+        wg_scan(s_first, digits, s_wave, W);
+        for (int i = threadIdx.x; i < W * digits; i += 1024) s_start[i] += s_first[i & (digits - 1)];
+        __syncthreads();
+        int32_t* kto = s_key[(p + 1) & 1];
+        uint32_t* pto = s_pos[(p + 1) & 1];
+        hand_out(src, a, b, p * bits, bits, start, [&](uint32_t to, int32_t key, uint32_t place) {
+            kto[to] = key;
+            pto[to] = place;
+        });
+        __syncthreads();
+    }
+    for (int i = threadIdx.x; i < n; i += 1024) {
+        keys[i] = s_key[passes & 1][i];
+        pos[i] = s_pos[passes & 1][i];
+    }
+}
+
+// ---- sums over the rows of a token ------------------------------------------------------------------------
+// The sorted list is cut into chunks of equal length, one per sub-wave of as many lanes as a row has pieces (up to 64), so that a
+// token of a million rows and a million tokens of one row cost the same.  A run of equal tokens that lies in one chunk is stored as it
+// is; of a run that goes on beyond its chunk the sum is left in one of the chunk's two places of a list of partial rows (0: the run goes
+// on from the chunk before, 1: it begins here), whose tokens are ascending again: the same kernel joins that list, until one chunk holds it.
+struct EmbedSums {
+    const void* src;            // FIRST: the plane dx; else partial rows
+    int64_t ld, gs;             // FIRST: its row and group stride
+    const int32_t* keys;        // ascending rows of the table; FIRST: vocab and above, else negative: nothing
+    const uint32_t* pos;        // FIRST: rows of dx
+    int32_t entries, chunks;
+    int chunk;                  // entries per chunk, a multiple of kSumBatch
+    int lanes_log2;             // lanes per chunk
+    int pieces, pg, dg;         // of a whole row; of a group; columns of a group
+    int32_t vocab;
+    float scale;
+    float* out;
+    int64_t ldt;
+    float* part;                // [2 chunks][pieces * V], nullptr if there is one chunk
+    int32_t* part_keys;         // [2 chunks], negative: nothing
+};
+constexpr int kSumBatch = 8, kSumChunkMax = 64, kSumLanesMin = 3;      // (lanes per chunk as a logarithm)
+
+template <typename S, int V, bool FIRST>
+__global__ __launch_bounds__(256) void k_embed_sums(EmbedSums a) {
+    constexpr int U = kSumBatch;
+    __shared__ int32_t s_key[(256 >> kSumLanesMin) * (kSumChunkMax + 4)];
+    __shared__ int32_t s_pos[(256 >> kSumLanesMin) * (kSumChunkMax + 4)];
+    const int subs = 256 >> a.lanes_log2, sub = threadIdx.x >> a.lanes_log2, stride = a.chunk + 4;
+    const int64_t e0 = (int64_t)blockIdx.x * subs * a.chunk;
+    for (int i = threadIdx.x; i < subs * a.chunk; i += 256) {
+        const int64_t e = e0 + i;
+        int32_t key = -1, pos = 0;
+        if (e < a.entries) {
+            key = a.keys[e];
+            if constexpr (FIRST) {
+                pos = (int32_t)a.pos[e];
+                if (key >= a.vocab) key = -1;
+            } else {
+                pos = (int32_t)e;
+            }
+        }
+        const int at = i / a.chunk * stride + i % a.chunk;
+        s_key[at] = key;
+        s_pos[at] = pos;
+    }
+    __syncthreads();
+    const int64_t c = (int64_t)blockIdx.x * subs + sub;
+    if (c >= a.chunks) return;
+    const int32_t* keys = s_key + sub * stride;
+    const int32_t* rows = s_pos + sub * stride;
+    const int piece = blockIdx.y * (1 << a.lanes_log2) + (threadIdx.x & ((1 << a.lanes_log2) - 1));
+    const bool mine = piece < a.pieces;
+    const int q = mine ? piece : a.pieces - 1, group = q / a.pg;
+    const int in_group = (q - group * a.pg) * V, col = in_group + V <= a.dg ? in_group : a.dg - V;
+    const int64_t width = (int64_t)a.pieces * V;
+    const S* src = static_cast<const S*>(a.src) + (FIRST ? group * a.gs + col : (int64_t)q * V);
+    const int64_t ld = FIRST ? a.ld : width;
+    float* out = a.out + group * a.dg + col;
+
+    const int64_t s = c * a.chunk, e = s + a.chunk;
+    const int32_t first = keys[0];
+    bool left = false, right = false;           // whether the first run goes on from before, the last one beyond
+    if (first >= 0 && s > 0) left = !FIRST || a.keys[s - 1] == first;
+    if (e < a.entries) right = FIRST ? keys[a.chunk - 1] >= 0 && a.keys[e] == keys[a.chunk - 1] : a.keys[e] >= 0;
+
+    float acc[V];
+    int32_t cur = -1;
+    bool open = left;                           // the present run is the one that goes on from before
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] = 0.0f;
+    auto store = [&](bool to_part, int64_t place) {
+        if (!mine) return;
+        float v[V];
+        if (to_part) {
+            store_piece<V>(a.part + place * width + (int64_t)q * V, acc);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = a.scale * acc[i];
+            store_piece<V>(out + (int64_t)cur * a.ldt, v);
+        }
+    };
+    for (int b = 0; b < a.chunk; b += U) {
+        int32_t k[U];
+        Piece<S, V> p[U];
+        bool any = false;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            k[u] = keys[b + u];
+            any |= k[u] >= 0;
+        }
+        if (!__any(any)) continue;
+#pragma unroll
+        for (int u = 0; u < U; ++u) p[u].load(src + rows[b + u] * ld);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (k[u] < 0) continue;
+            if (k[u] != cur) {
+                if (cur >= 0) store(open, 2 * c);
+                open = open && cur < 0;
+                cur = k[u];
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[i] = 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i) acc[i] += p[u].at(i);
+        }
+    }
+    if (cur >= 0) store(open || right, open ? 2 * c : 2 * c + 1);
+    if (a.part_keys && piece == 0) {
+        a.part_keys[2 * c] = left ? first : -1;
+        a.part_keys[2 * c + 1] = right && !open ? cur : -1;
+    }
+}
+
+// ---- host side ----------------------------------------------------------------------------------------------
+namespace {
+
+constexpr int kMaxWidth = 1 << 17;
+
+struct EmbedShape {             // a plane as the kernels take it: one group, or one per plane
+    int64_t n, ldx, gs;
+    int dg, c;
+};
+
+gsr_status_t embed_shape(int64_t n, int32_t d, int32_t c, int32_t layout, int64_t ldx, int64_t vocab, int64_t ldt, EmbedShape* s) {
+    if (n < 0) return fail(GSR_ERR_INVALID_ARG, "negative n");
+    if (n >= ((int64_t)1 << 31)) return fail(GSR_ERR_UNSUPPORTED, "n=%lld at or above 2^31", (long long)n);
+    if (d < 1 || d > kMaxWidth) return fail(GSR_ERR_UNSUPPORTED, "d=%d outside [1, %d]", d, kMaxWidth);
+    if (c < 1 || d % c) return fail(GSR_ERR_UNSUPPORTED, "c=%d does not divide d=%d", c, d);
+    if (layout != GSR_LAYOUT_ROW_MAJOR && layout != GSR_LAYOUT_GROUP_PLANAR) return fail(GSR_ERR_INVALID_ARG, "layout %d", layout);
+    s->n = n;
+    s->c = layout == GSR_LAYOUT_GROUP_PLANAR ? c : 1;       // the groups of a row-major plane are its columns in order
+    s->dg = d / s->c;
+    s->ldx = ldx;
+    s->gs = n * ldx;
+    if (s->c > 65535) return fail(GSR_ERR_UNSUPPORTED, "c=%d above 65535", c);
+    if (ldx < s->dg || ldx >= ((int64_t)1 << 31)) return fail(GSR_ERR_INVALID_ARG, "row stride %lld outside [%d, 2^31)", (long long)ldx, s->dg);
+    if (vocab < 1) return fail(GSR_ERR_INVALID_ARG, "vocab=%lld below 1", (long long)vocab);
+    if (vocab >= ((int64_t)1 << 31) - 1) return fail(GSR_ERR_UNSUPPORTED, "vocab=%lld at or above 2^31 - 1", (long long)vocab);
+    if (ldt < d || ldt >= ((int64_t)1 << 31)) return fail(GSR_ERR_INVALID_ARG, "row stride %lld of the table outside [%d, 2^31)", (long long)ldt, d);
+    return GSR_OK;
+}
+gsr_status_t plane_dtype(int32_t dtype) {
+    if (dtype != GSR_F32 && dtype != GSR_BF16) return fail(GSR_ERR_UNSUPPORTED, "dtype %d", dtype);
+    return GSR_OK;
+}
+bool aligned_to(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+
+template <typename TT, typename T, typename I, int V>
+void launch_lookup(const EmbedShape& s, const void* table, int64_t ldt, int32_t vocab, const void* ids, float scale, void* x, hipStream_t st) {
+    const int pg = (s.dg + V - 1) / V, rows = std::max(1, 1024 / pg);
+    const unsigned wgs = (unsigned)std::min<int64_t>((s.n + rows - 1) / rows, 1 << 20);
+    const uint32_t magic = pg == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + pg - 1) / pg);
+    hipLaunchKernelGGL((k_embed_lookup<TT, T, I, V>), dim3(wgs, s.c), dim3(256), 0, st, (const TT*)table, ldt, vocab, (const I*)ids, s.n, s.dg,
+                       pg, magic, rows, scale, (T*)x, s.ldx, s.gs);
+}
+template <typename TT, typename T, typename I>
+void launch_lookup(const EmbedShape& s, const void* table, int64_t ldt, int32_t vocab, const void* ids, float scale, void* x, hipStream_t st) {
+    constexpr int V = 16 / (int)sizeof(T);
+    if (s.dg >= V) launch_lookup<TT, T, I, V>(s, table, ldt, vocab, ids, scale, x, st);
+    else launch_lookup<TT, T, I, 1>(s, table, ldt, vocab, ids, scale, x, st);
+}
+template <typename TT, typename T>
+void launch_lookup(const EmbedShape& s, const void* table, int64_t ldt, int32_t vocab, const void* ids, bool i64, float scale, void* x, hipStream_t st) {
+    if (i64) launch_lookup<TT, T, int64_t>(s, table, ldt, vocab, ids, scale, x, st);
+    else launch_lookup<TT, T, int32_t>(s, table, ldt, vocab, ids, scale, x, st);
+}
+
+// How gsr_embed_grad sorts and cuts, and where its workspace holds what.  Depends on the sizes alone.
+struct EmbedPlan {
+    int bits, passes;               // bits of a digit
+    bool small;
+    int wgs, stretch;               // workgroups of a pass and elements of each
+    int chunk;
+    size_t keys[2], pos[2], hist, total;
+    struct Level { int64_t entries, chunks; size_t part, part_keys; } level[8];
+    int levels;
+    size_t bytes;
+};
+EmbedPlan embed_plan(int64_t n, int64_t vocab, int d, int c) {
+    EmbedPlan p{};
+    int bits = 1;
+    while (((int64_t)1 << bits) <= vocab) ++bits;           // keys are 0 .. vocab
+    p.small = n <= kSmallSort;
+    const int most = p.small ? kSmallBits : kDigitBits;
+    p.passes = (bits + most - 1) / most;
+    p.bits = (bits + p.passes - 1) / p.passes;
+    p.wgs = (int)std::min<int64_t>(256, std::max<int64_t>(1, (n + 4095) / 4096));
+    p.stretch = (int)(((n + p.wgs - 1) / p.wgs + 255) / 256 * 256);
+    p.chunk = n > 65536 ? kSumChunkMax : 16;
+    const size_t width = (size_t)c * ((d / c + 7) / 8 * 8);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += align_up(bytes);
+        return here;
+    };
+    for (int i = 0; i < 2; ++i) {
+        p.keys[i] = i < p.passes ? take(4 * (size_t)n) : p.keys[0];
+        p.pos[i] = i < p.passes ? take(4 * (size_t)n) : p.pos[0];
+    }
+    p.hist = take(((size_t)p.wgs << p.bits) * 4);
+    p.total = take(((size_t)1 << p.bits) * 4);
+    int64_t entries = n;
+    do {
+        EmbedPlan::Level& l = p.level[p.levels++];
+        l.entries = entries;
+        l.chunks = (entries + p.chunk - 1) / p.chunk;
+        if (l.chunks <= 1) break;
+        l.part_keys = take((size_t)l.chunks * 2 * 4);
+        l.part = take((size_t)l.chunks * 2 * width * 4);
+        entries = 2 * l.chunks;
+    } while (true);
+    p.bytes = at;
+    return p;
+}
+
+template <typename S, int V>
+void launch_sums(const EmbedPlan& p, const EmbedShape& s, const void* dx, float scale, int64_t vocab, float* out, int64_t ldt, int last,
+                 char* ws, hipStream_t st) {
+    const int pg = (s.dg + V - 1) / V, pieces = pg * s.c;
+    int log2 = kSumLanesMin;
+    while (log2 < 6 && (1 << log2) < pieces) ++log2;
+    for (int l = 0; l < p.levels; ++l) {
+        const EmbedPlan::Level& v = p.level[l];
+        EmbedSums a{};
+        a.src = l ? (const void*)(ws + p.level[l - 1].part) : dx;
+        a.ld = s.ldx;
+        a.gs = s.gs;
+        a.keys = (const int32_t*)(ws + (l ? p.level[l - 1].part_keys : p.keys[last]));
+        a.pos = (const uint32_t*)(ws + p.pos[last]);
+        a.entries = (int32_t)v.entries;
+        a.chunks = (int32_t)v.chunks;
+        a.chunk = p.chunk;
+        a.lanes_log2 = log2;
+        a.pieces = pieces; a.pg = pg; a.dg = s.dg;
+        a.vocab = (int32_t)vocab;
+        a.scale = scale;
+        a.out = out;
+        a.ldt = ldt;
+        a.part = v.chunks > 1 ? (float*)(ws + v.part) : nullptr;
+        a.part_keys = v.chunks > 1 ? (int32_t*)(ws + v.part_keys) : nullptr;
+        const int subs = 256 >> log2;
+        const dim3 grid((unsigned)((v.chunks + subs - 1) / subs), (unsigned)((pieces + (1 << log2) - 1) >> log2));
+        if (l == 0) hipLaunchKernelGGL((k_embed_sums<S, V, true>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((k_embed_sums<float, V, false>), grid, dim3(256), 0, st, a);
+    }
+}
+
+template <typename I>
+int launch_sort(const EmbedPlan& p, const void* ids, int64_t n, int64_t vocab, float* out, int64_t ldt, int d, char* ws, hipStream_t st) {
+    const SortSource<I> src{(const I*)ids, nullptr, (int32_t)vocab};
+    // workgroups that clear: up to 4,096, 16 KB or more each
+    const unsigned clear = (unsigned)std::min<int64_t>(4096, (vocab * d + 4095) / 4096);
+    auto at = [&](size_t o) { return ws + o; };
+    if (p.small) {
+        hipLaunchKernelGGL((k_embed_sort_small<I>), dim3(1 + clear), dim3(1024), 0, st, src, (int)n, p.bits, p.passes,
+                           (int32_t*)at(p.keys[0]), (uint32_t*)at(p.pos[0]), out, ldt, d);
+        return 0;
+    }
+    uint32_t *hist = (uint32_t*)at(p.hist), *total = (uint32_t*)at(p.total);
+    const int digits = 1 << p.bits;
+    for (int i = 0; i < p.passes; ++i) {
+        const int to = i & 1;
+        int32_t* keys = (int32_t*)at(p.keys[to]);
+        uint32_t* pos = (uint32_t*)at(p.pos[to]);
+        const SortSource<int32_t> again{(const int32_t*)at(p.keys[to ^ 1]), (const uint32_t*)at(p.pos[to ^ 1]), (int32_t)vocab};
+        if (i == 0)
+            hipLaunchKernelGGL((k_embed_count<I>), dim3(p.wgs + clear), dim3(256), 0, st, src, n, p.stretch, p.wgs, 0, p.bits, hist, out, ldt, d);
+        else
+            hipLaunchKernelGGL((k_embed_count<int32_t>), dim3(p.wgs), dim3(256), 0, st, again, n, p.stretch, p.wgs, i * p.bits, p.bits, hist,
+                               (float*)nullptr, ldt, d);
+        hipLaunchKernelGGL(k_embed_places, dim3((digits + 3) / 4), dim3(256), 0, st, hist, p.wgs, digits, total);
+        if (i == 0)
+            hipLaunchKernelGGL((k_embed_hand_out<I>), dim3(p.wgs), dim3(256), 0, st, src, n, p.stretch, p.wgs, 0, p.bits, hist, total, keys, pos);
+        else
+            hipLaunchKernelGGL((k_embed_hand_out<int32_t>), dim3(p.wgs), dim3(256), 0, st, again, n, p.stretch, p.wgs, i * p.bits, p.bits, hist,
+                               total, keys, pos);
+    }
+    return (p.passes - 1) & 1;
+}
+
+}  // namespace
+}  // namespace gsr
+
+using namespace gsr;
+
+extern "C" {
+
+gsr_status_t gsr_embed_lookup(const void* table, int64_t vocab, int64_t ldt, int32_t table_dtype, const void* ids, int32_t ids_i64,
+                              int64_t n, int32_t d, int32_t c, int32_t layout, int32_t dtype, float scale, void* x_out, int64_t ldx,
+                              void* stream) {
+    EmbedShape s;
+    GSR_TRY(embed_shape(n, d, c, layout, ldx, vocab, ldt, &s));
+    GSR_TRY(plane_dtype(table_dtype));
+    GSR_TRY(plane_dtype(dtype));
+    if (n == 0) return GSR_OK;
+    if (!table || !ids || !x_out) return fail(GSR_ERR_INVALID_ARG, "null pointer");
+    if (!aligned_to(table, dtype_size(table_dtype)) || !aligned_to(x_out, dtype_size(dtype)) || !aligned_to(ids, ids_i64 ? 8 : 4))
+        return fail(GSR_ERR_INVALID_ARG, "a pointer is not aligned to its elements");
+    hipStream_t st = (hipStream_t)stream;
+    const int32_t v = (int32_t)vocab;
+    if (table_dtype == GSR_F32 && dtype == GSR_F32) launch_lookup<float, float>(s, table, ldt, v, ids, ids_i64, scale, x_out, st);
+    else if (table_dtype == GSR_F32) launch_lookup<float, bf16_t>(s, table, ldt, v, ids, ids_i64, scale, x_out, st);
+    else if (dtype == GSR_F32) launch_lookup<bf16_t, float>(s, table, ldt, v, ids, ids_i64, scale, x_out, st);
+    else launch_lookup<bf16_t, bf16_t>(s, table, ldt, v, ids, ids_i64, scale, x_out, st);
+    GSR_HIP_CHECK(hipGetLastError());
+    return GSR_OK;
+}
+
+size_t gsr_embed_grad_workspace(int64_t n, int64_t vocab, int32_t d, int32_t c) {
+    if (n < 0 || n >= ((int64_t)1 << 31) || vocab < 1 || vocab >= ((int64_t)1 << 31) - 1 || d < 1 || d > kMaxWidth || c < 1 || d % c) return 0;
+    return embed_plan(n, vocab, d, c).bytes;
+}
+
+gsr_status_t gsr_embed_grad(const void* ids, int32_t ids_i64, int64_t n, const void* dx, int64_t ldx, int32_t d, int32_t c, int32_t layout,
+                            int32_t dtype, float scale, int64_t vocab, float* dtable_out, int64_t ldt, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+    EmbedShape s;
+    GSR_TRY(embed_shape(n, d, c, layout, ldx, vocab, ldt, &s));
+    GSR_TRY(plane_dtype(dtype));
+    if (!dtable_out || (n > 0 && (!ids || !dx))) return fail(GSR_ERR_INVALID_ARG, "null pointer");
+    const EmbedPlan p = embed_plan(n, vocab, d, c);
+    if (workspace_bytes < p.bytes) return fail(GSR_ERR_WORKSPACE_TOO_SMALL, "workspace of %zu bytes, %zu needed", workspace_bytes, p.bytes);
+    if (p.bytes && !workspace) return fail(GSR_ERR_INVALID_ARG, "null workspace");
+    if (!aligned_to(dx, dtype_size(dtype)) || !aligned_to(dtable_out, 4) || !aligned_to(ids, ids_i64 ? 8 : 4) || !aligned_to(workspace, 16))
+        return fail(GSR_ERR_INVALID_ARG, "a pointer is not aligned to its elements (the workspace: to 16 bytes)");
+    hipStream_t st = (hipStream_t)stream;
+    char* ws = (char*)workspace;
+    const int last = ids_i64 ? launch_sort<int64_t>(p, ids, n, vocab, dtable_out, ldt, d, ws, st)
+                             : launch_sort<int32_t>(p, ids, n, vocab, dtable_out, ldt, d, ws, st);
+    if (n > 0) {
+        if (dtype == GSR_F32 && s.dg >= 4) launch_sums<float, 4>(p, s, dx, scale, vocab, dtable_out, ldt, last, ws, st);
+        else if (dtype == GSR_F32) launch_sums<float, 1>(p, s, dx, scale, vocab, dtable_out, ldt, last, ws, st);
+        else if (s.dg >= 8) launch_sums<bf16_t, 8>(p, s, dx, scale, vocab, dtable_out, ldt, last, ws, st);
+        else launch_sums<bf16_t, 1>(p, s, dx, scale, vocab, dtable_out, ldt, last, ws, st);
+    }
+    GSR_HIP_CHECK(hipGetLastError());
+    return GSR_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,407 @@
+// Operators over a list of tensors: the norm of all gradients of a step, clipping by it, and Adam on every tensor.
+//
+//   norm = sqrt(sum over all tensors and elements of g^2)
+//   c    = min(1, max_norm / (norm + 1e-6))
+//   gsr_grad_clip: out = c g          gsr_adam_update_list: gsr_adam_update with c g in the place of the gradient
+//
+// Tensors are contiguous arrays anywhere in device memory.  Their addresses and sizes go to the kernels as arguments, so a call
+// leaves nothing behind on the device and can be captured; lists longer than an argument block holds take several launches.
+#include "gsr_internal.h"
+#include "gsr_device.h"
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <vector>
+
+namespace gsr {
+
+constexpr int kArgBytes = 4096 - 256;           // tensor table of a launch (kernel arguments: 4 KB)
+constexpr int kChunk = 4096;                    // elements that a workgroup takes at a time
+constexpr int kMaxPartials = 2048;              // workgroups, hence partial sums, of one launch of the norm
+constexpr double kClipEps = 1e-6;
+
+// The tensors of one launch: P addresses each (gradient; gradient and output; w, dw, m, v).
+template <int P>
+struct TensorTable {
+    static constexpr int kMax = (kArgBytes - 16) / (8 * P + 8 + 4);
+    int32_t count, chunks;
+    void* at[P][kMax];
+    int64_t size[kMax];
+    int32_t first[kMax];                        // chunks of the tensors before
+};
+
+// the tensor that chunk c belongs to
+template <int P>
+__device__ __forceinline__ int tensor_of(const TensorTable<P>& t, int c) {
+    int lo = 0, hi = t.count;                   // first[lo] <= c < first[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (t.first[mid] <= c) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// ---- four elements at a time, aligned to their elements only ------------------------------------------------
+typedef uint32_t u32x2h __attribute__((ext_vector_type(2), aligned(2)));
+
+__device__ __forceinline__ uint32_t to_bits16(float v) { return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v)); }   // NaN stays NaN
+
+__device__ __forceinline__ void load4(const float* p, float (&v)[4]) {
+    const u32x4a t = *reinterpret_cast<const u32x4a*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(t[i]);
+}
+__device__ __forceinline__ void load4(const bf16_t* p, float (&v)[4]) {
+    const u32x2h t = *reinterpret_cast<const u32x2h*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __uint_as_float((i & 1) ? (t[i >> 1] & 0xFFFF0000u) : (t[i >> 1] << 16));
+}
+__device__ __forceinline__ void store4(float* p, const float (&v)[4]) {
+    u32x4a t;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = __float_as_uint(v[i]);
+    *reinterpret_cast<u32x4a*>(p) = t;
+}
+__device__ __forceinline__ void store4(bf16_t* p, const float (&v)[4]) {
+    u32x2h t;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) t[i] = to_bits16(v[2 * i]) | (to_bits16(v[2 * i + 1]) << 16);
+    *reinterpret_cast<u32x2h*>(p) = t;
+}
+__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store1(bf16_t* p, float v) { p->bits = (uint16_t)to_bits16(v); }
+
+// ---- norm -------------------------------------------------------------------------------------------------
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+// the sum over a workgroup of 256, in thread 0
+__device__ __forceinline__ double wg_sum(double v) {
+    __shared__ double s_sum[4];
+    v = wave_sum(v);
+    if (lane_id() == 0) s_sum[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return threadIdx.x == 0 ? (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]) : 0.0;
+}
+
+// Squares and sums in 64 bits: no float's square overflows or vanishes there, and how elements are dealt out hardly matters. It costs one
+// 64-bit multiply-add per element, of which the chip does some thirty for every float that memory delivers.
+template <typename T>
+__global__ __launch_bounds__(256) void k_norm_partial(TensorTable<1> t, double* __restrict__ partial) {
+    double sum = 0.0;
+    for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+        const int i = tensor_of(t, c);
+        const int64_t a = (int64_t)(c - t.first[i]) * kChunk;
+        const int left = (int)(t.size[i] - a < kChunk ? t.size[i] - a : kChunk);
+        const T* g = static_cast<const T*>(t.at[0][i]) + a;
+        if (left == kChunk) {
+            float v[4][4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) load4(g + 1024 * u + 4 * threadIdx.x, v[u]);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum = fma((double)v[u][j], (double)v[u][j], sum);
+        } else {
+            for (int e = threadIdx.x; e < left; e += 256) {
+                const double x = to_float(g[e]);
+                sum = fma(x, x, sum);
+            }
+        }
+    }
+    sum = wg_sum(sum);
+    if (threadIdx.x == 0) partial[blockIdx.x] = sum;
+}
+__global__ __launch_bounds__(256) void k_norm_final(const double* __restrict__ partial, int count, double* __restrict__ norm,
+                                                    float* __restrict__ norm_out) {
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < count; i += 256) sum += partial[i];
+    sum = wg_sum(sum);
+    if (threadIdx.x == 0) {
+        const double r = sqrt(sum);
+        *norm = r;
+        if (norm_out) *norm_out = (float)r;
+    }
+}
+
+// NaN stays NaN (a comparison with it is false), an infinite norm gives 0
+__device__ __forceinline__ double clip_coefficient(double norm, double max_norm) {
+    const double c = max_norm / (norm + kClipEps);
+    return c >= 1.0 ? 1.0 : c;
+}
+
+// ---- clipping ---------------------------------------------------------------------------------------------
+// The product is taken in 64 bits, so a gradient is rounded once (16-bit output: twice).
+template <typename T, typename O>
+__global__ __launch_bounds__(256) void k_clip(TensorTable<2> t, const double* __restrict__ norm, double max_norm, bool in_place) {
+    const double k = clip_coefficient(*norm, max_norm);
+    if (in_place && k == 1.0) return;           // multiplied by one: already there
+    const int c = blockIdx.x, i = tensor_of(t, c);
+    const int64_t a = (int64_t)(c - t.first[i]) * kChunk;
+    const int left = (int)(t.size[i] - a < kChunk ? t.size[i] - a : kChunk);
+    const T* g = static_cast<const T*>(t.at[0][i]) + a;
+    O* out = static_cast<O*>(t.at[1][i]) + a;
+    if (left == kChunk) {
+        float v[4][4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) load4(g + 1024 * u + 4 * threadIdx.x, v[u]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[u][j] = (float)(k * (double)v[u][j]);
+            store4(out + 1024 * u + 4 * threadIdx.x, v[u]);
+        }
+    } else {
+        for (int e = threadIdx.x; e < left; e += 256) store1(out + e, (float)(k * (double)to_float(g[e])));
+    }
+}
+
+// ---- Adam -------------------------------------------------------------------------------------------------
+struct AdamParams {
+    float lr, b1, b2, eps, wd, inv_c1, inv_c2;
+};
+// the arithmetic of k_adam, the gradient multiplied by the clipping coefficient first (by one, exactly, without clipping)
+__device__ __forceinline__ void adam_one(const AdamParams& p, float k, float& w, float dw, float& m, float& v) {
+    const float x = w;
+    const float gk = k * dw;
+    const float g = gk + p.wd * x;
+    const float mi = p.b1 * m + (1.0f - p.b1) * g;
+    const float vi = p.b2 * v + (1.0f - p.b2) * g * g;
+    m = mi;
+    v = vi;
+    w = x - p.lr * (mi * p.inv_c1) / (sqrtf(vi * p.inv_c2) + p.eps);
+}
+template <typename T>
+__global__ __launch_bounds__(256) void k_adam_list(TensorTable<4> t, const float* __restrict__ norm, double max_norm, AdamParams p) {
+    const float k = norm ? (float)clip_coefficient((double)*norm, max_norm) : 1.0f;
+    const int c = blockIdx.x, i = tensor_of(t, c);
+    const int64_t a = (int64_t)(c - t.first[i]) * kChunk;
+    const int left = (int)(t.size[i] - a < kChunk ? t.size[i] - a : kChunk);
+    float* w = static_cast<float*>(t.at[0][i]) + a;
+    const T* dw = static_cast<const T*>(t.at[1][i]) + a;
+    float* m = static_cast<float*>(t.at[2][i]) + a;
+    float* v = static_cast<float*>(t.at[3][i]) + a;
+    if (left == kChunk) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int e = 1024 * u + 4 * threadIdx.x;
+            float x[4], g[4], y[4], z[4];
+            load4(w + e, x);
+            load4(dw + e, g);
+            load4(m + e, y);
+            load4(v + e, z);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) adam_one(p, k, x[j], g[j], y[j], z[j]);
+            store4(w + e, x);
+            store4(m + e, y);
+            store4(v + e, z);
+        }
+    } else {
+        for (int e = threadIdx.x; e < left; e += 256) {
+            float x = w[e], y = m[e], z = v[e];
+            adam_one(p, k, x, to_float(dw[e]), y, z);
+            w[e] = x;
+            m[e] = y;
+            v[e] = z;
+        }
+    }
+}
+
+// ---- host side ----------------------------------------------------------------------------------------------
+namespace {
+
+constexpr int64_t kMaxLaunchChunks = (int64_t)1 << 23;         // (a grid holds fewer than 2^32 threads)
+
+// Calls launch(table) for the tensors of the list, an argument block at a time; empty tensors are left out.  A tensor of more chunks
+// than one launch takes goes on in the next.
+template <int P, typename Launch>
+void over_list(void* const* const (&lists)[P], const size_t (&width)[P], const int64_t* counts, int32_t tensors, Launch launch) {
+    TensorTable<P> t;
+    t.count = t.chunks = 0;
+    for (int32_t i = 0; i < tensors; ++i) {
+        for (int64_t at = 0; at < counts[i];) {
+            const int64_t room = kMaxLaunchChunks - t.chunks, size = std::min(counts[i] - at, room * kChunk);
+            for (int p = 0; p < P; ++p) t.at[p][t.count] = (char*)lists[p][i] + at * (int64_t)width[p];
+            t.size[t.count] = size;
+            t.first[t.count] = t.chunks;
+            t.chunks += (int32_t)((size + kChunk - 1) / kChunk);
+            at += size;
+            if (++t.count == TensorTable<P>::kMax || t.chunks == kMaxLaunchChunks) {
+                launch(t);
+                t.count = t.chunks = 0;
+            }
+        }
+    }
+    if (t.count) launch(t);
+}
+
+// Launches that over_list makes at most: some end with a full table, some with a full grid (of tensors that are cut there, each of which
+// takes a place in a second table), the last with neither.
+int64_t list_launches(int64_t tensors, int64_t elements, int per_launch) {
+    const int64_t full_grids = elements / ((kMaxLaunchChunks - per_launch) * kChunk);
+    return (tensors + full_grids) / per_launch + full_grids + 1;
+}
+
+struct Range {
+    uintptr_t from, to;
+    bool written;
+};
+
+// Sizes and addresses of a list: P arrays of `tensors` pointers, bit p of `written` set where array p is written.  What a call
+// writes may overlap nothing else of it (a tensor named twice would be updated twice, in no fixed order).
+template <int P>
+gsr_status_t check_list(void* const* const (&lists)[P], const size_t (&width)[P], unsigned written, const int64_t* counts, int32_t tensors,
+                        int64_t* elements) {
+    if (tensors < 0) return fail(GSR_ERR_INVALID_ARG, "negative number of tensors");
+    *elements = 0;
+    if (tensors == 0) return GSR_OK;
+    if (!counts) return fail(GSR_ERR_INVALID_ARG, "null pointer");
+    for (int p = 0; p < P; ++p)
+        if (!lists[p]) return fail(GSR_ERR_INVALID_ARG, "null pointer");
+    try {
+        std::vector<Range> r;
+        if (written) r.reserve((size_t)tensors * P);
+        for (int32_t i = 0; i < tensors; ++i) {
+            if (counts[i] < 0) return fail(GSR_ERR_INVALID_ARG, "tensor %d has a negative size", i);
+            if (counts[i] > ((int64_t)1 << 40) - *elements) return fail(GSR_ERR_UNSUPPORTED, "more than 2^40 elements");
+            *elements += counts[i];
+            if (counts[i] == 0) continue;
+            for (int p = 0; p < P; ++p) {
+                const uintptr_t at = (uintptr_t)lists[p][i];
+                if (!at) return fail(GSR_ERR_INVALID_ARG, "tensor %d is a null pointer", i);
+                if (at & (width[p] - 1)) return fail(GSR_ERR_INVALID_ARG, "tensor %d is not aligned to its elements", i);
+                if (written) r.push_back({at, at + (uintptr_t)counts[i] * width[p], ((written >> p) & 1) != 0});
+            }
+        }
+        auto before = [](const Range& a, const Range& b) { return a.from < b.from; };
+        if (!std::is_sorted(r.begin(), r.end(), before)) std::sort(r.begin(), r.end(), before);
+        uintptr_t read_to = 0, written_to = 0;              // ends of what lies before
+        for (const Range& x : r) {
+            if (x.from < written_to || (x.written && x.from < read_to))
+                return fail(GSR_ERR_INVALID_ARG, "tensors overlap, one of them is written");
+            if (x.written) written_to = std::max(written_to, x.to);
+            else read_to = std::max(read_to, x.to);
+        }
+    } catch (const std::bad_alloc&) {
+        return fail(GSR_ERR_INVALID_ARG, "out of host memory for a list of %d tensors", tensors);
+    }
+    return GSR_OK;
+}
+
+gsr_status_t list_dtype(int32_t dtype) {
+    if (dtype != GSR_F32 && dtype != GSR_BF16) return fail(GSR_ERR_UNSUPPORTED, "dtype %d", dtype);
+    return GSR_OK;
+}
+
+// workspace of the norm: the norm in 64 bits, then the partial sums
+size_t norm_workspace(int64_t tensors, int64_t elements) {
+    return 256 + sizeof(double) * kMaxPartials * (size_t)list_launches(tensors, elements, TensorTable<1>::kMax);
+}
+
+void launch_norm(void* const* grads, const int64_t* counts, int32_t tensors, int32_t dtype, float* norm_out, void* workspace, hipStream_t s) {
+    double *norm = (double*)workspace, *partial = (double*)((char*)workspace + 256);
+    int made = 0;
+    over_list<1>({grads}, {dtype_size(dtype)}, counts, tensors, [&](const TensorTable<1>& t) {
+        const int wgs = std::min(t.chunks, kMaxPartials);
+        if (dtype == GSR_F32) hipLaunchKernelGGL((k_norm_partial<float>), dim3(wgs), dim3(256), 0, s, t, partial + made);
+        else hipLaunchKernelGGL((k_norm_partial<bf16_t>), dim3(wgs), dim3(256), 0, s, t, partial + made);
+        made += wgs;
+    });
+    hipLaunchKernelGGL(k_norm_final, dim3(1), dim3(256), 0, s, partial, made, norm, norm_out);
+}
+
+gsr_status_t check_norm_workspace(int64_t tensors, int64_t elements, const void* workspace, size_t bytes) {
+    const size_t need = norm_workspace(tensors, elements);
+    if (bytes < need) return fail(GSR_ERR_WORKSPACE_TOO_SMALL, "workspace of %zu bytes, %zu needed", bytes, need);
+    if (!workspace) return fail(GSR_ERR_INVALID_ARG, "null workspace");
+    if ((uintptr_t)workspace & 7) return fail(GSR_ERR_INVALID_ARG, "workspace not aligned to 8 bytes");
+    return GSR_OK;
+}
+
+}  // namespace
+}  // namespace gsr
+
+using namespace gsr;
+
+extern "C" {
+
+size_t gsr_grad_norm_workspace(const int64_t* counts, int32_t tensors) {
+    int64_t elements = 0;
+    for (int32_t i = 0; counts && i < tensors; ++i) {
+        if (counts[i] < 0 || counts[i] > ((int64_t)1 << 40) - elements) return 0;
+        elements += counts[i];
+    }
+    return tensors < 0 ? 0 : norm_workspace(tensors, elements);
+}
+
+gsr_status_t gsr_grad_norm(const void* const* grads, const int64_t* counts, int32_t tensors, int32_t dtype, float* norm_out, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+    int64_t elements;
+    GSR_TRY(list_dtype(dtype));
+    void* const* g = (void* const*)grads;
+    GSR_TRY(check_list<1>({g}, {dtype_size(dtype)}, 0, counts, tensors, &elements));
+    if (!norm_out || ((uintptr_t)norm_out & 3)) return fail(GSR_ERR_INVALID_ARG, "norm_out is null or not aligned");
+    GSR_TRY(check_norm_workspace(tensors, elements, workspace, workspace_bytes));
+    launch_norm(g, counts, tensors, dtype, norm_out, workspace, (hipStream_t)stream);
+    GSR_HIP_CHECK(hipGetLastError());
+    return GSR_OK;
+}
+
+gsr_status_t gsr_grad_clip(void* const* grads, const int64_t* counts, int32_t tensors, int32_t dtype, float max_norm, float* norm_out,
+                           void* const* out, int32_t out_dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    int64_t elements;
+    GSR_TRY(list_dtype(dtype));
+    if (out) GSR_TRY(list_dtype(out_dtype));
+    else out_dtype = dtype;
+    if (!(max_norm >= 0.0f) || std::isinf(max_norm)) return fail(GSR_ERR_INVALID_ARG, "max_norm=%g is negative or not finite", (double)max_norm);
+    const size_t w = dtype_size(dtype), wo = dtype_size(out_dtype);
+    if (out) GSR_TRY(check_list<2>({grads, out}, {w, wo}, 2u, counts, tensors, &elements));
+    else GSR_TRY(check_list<1>({grads}, {w}, 1u, counts, tensors, &elements));
+    if ((uintptr_t)norm_out & 3) return fail(GSR_ERR_INVALID_ARG, "norm_out is not aligned");
+    GSR_TRY(check_norm_workspace(tensors, elements, workspace, workspace_bytes));
+    hipStream_t s = (hipStream_t)stream;
+    launch_norm(grads, counts, tensors, dtype, norm_out, workspace, s);
+    const double* norm = (const double*)workspace;
+    const bool in_place = !out;
+    over_list<2>({grads, out ? out : grads}, {w, wo}, counts, tensors, [&](const TensorTable<2>& t) {
+        const dim3 grid(t.chunks), wg(256);
+        if (dtype == GSR_F32 && out_dtype == GSR_F32) hipLaunchKernelGGL((k_clip<float, float>), grid, wg, 0, s, t, norm, (double)max_norm, in_place);
+        else if (dtype == GSR_F32) hipLaunchKernelGGL((k_clip<float, bf16_t>), grid, wg, 0, s, t, norm, (double)max_norm, in_place);
+        else if (out_dtype == GSR_F32) hipLaunchKernelGGL((k_clip<bf16_t, float>), grid, wg, 0, s, t, norm, (double)max_norm, in_place);
+        else hipLaunchKernelGGL((k_clip<bf16_t, bf16_t>), grid, wg, 0, s, t, norm, (double)max_norm, in_place);
+    });
+    GSR_HIP_CHECK(hipGetLastError());
+    return GSR_OK;
+}
+
+gsr_status_t gsr_adam_update_list(float* const* w, const void* const* dw, float* const* m, float* const* v, const int64_t* counts,
+                                  int32_t tensors, int32_t dw_dtype, const float* norm, float max_norm, int64_t t, float lr, float beta1,
+                                  float beta2, float eps, float weight_decay, void* stream) {
+    int64_t elements;
+    GSR_TRY(list_dtype(dw_dtype));
+    if (t < 1) return fail(GSR_ERR_INVALID_ARG, "Adam's step counter starts at 1");
+    if (!(beta1 >= 0.f && beta1 < 1.f) || !(beta2 >= 0.f && beta2 < 1.f)) return fail(GSR_ERR_INVALID_ARG, "beta outside [0,1)");
+    if (norm && (!(max_norm >= 0.0f) || std::isinf(max_norm)))
+        return fail(GSR_ERR_INVALID_ARG, "max_norm=%g is negative or not finite", (double)max_norm);
+    if ((uintptr_t)norm & 3) return fail(GSR_ERR_INVALID_ARG, "norm is not aligned");
+    void* const* lists[4] = {(void* const*)w, (void* const*)dw, (void* const*)m, (void* const*)v};
+    const size_t width[4] = {4, dtype_size(dw_dtype), 4, 4};
+    GSR_TRY(check_list<4>(lists, width, 13u, counts, tensors, &elements));
+    if (elements == 0) return GSR_OK;
+    const double c1 = 1.0 - std::pow((double)beta1, (double)t), c2 = 1.0 - std::pow((double)beta2, (double)t);
+    const AdamParams p{lr, beta1, beta2, eps, weight_decay, (float)(1.0 / c1), (float)(1.0 / c2)};
+    hipStream_t s = (hipStream_t)stream;
+    over_list<4>(lists, width, counts, tensors, [&](const TensorTable<4>& table) {
+        const dim3 grid(table.chunks), wg(256);
+        if (dw_dtype == GSR_F32) hipLaunchKernelGGL((k_adam_list<float>), grid, wg, 0, s, table, norm, (double)max_norm, p);
+        else hipLaunchKernelGGL((k_adam_list<bf16_t>), grid, wg, 0, s, table, norm, (double)max_norm, p);
+    });
+    GSR_HIP_CHECK(hipGetLastError());
+    return GSR_OK;
+}
+
+}  // extern "C"
