@@ -78,7 +78,7 @@ def lib():
         p, i32, i64, f32, size = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_size_t
         l.gsr_embed_lookup.argtypes = [p, i64, i64, i32, p, i32, i64, i32, i32, i32, i32, f32, p, i64, p]
         l.gsr_embed_grad_workspace.restype = size
-        l.gsr_embed_grad_workspace.argtypes = [i64, i64, i32, i32]
+        l.gsr_embed_grad_workspace.argtypes = [i64, i64, i32]
         l.gsr_embed_grad.argtypes = [p, i32, i64, p, i64, i32, i32, i32, i32, f32, i64, p, i64, p, size, p]
         l.gsr_grad_norm_workspace.restype = size
         l.gsr_grad_norm_workspace.argtypes = [p, i32]
@@ -362,19 +362,19 @@ def gsr_embed_lookup(table, ids, x_out, scale: float = 1.0) -> None:
                                   _dtype_of(x_out), scale, x_out.data_ptr(), ldx, _stream()))
 
 
-def gsr_embed_grad_workspace(n: int, vocab: int, d: int, c: int = 1) -> int:
-    return lib().gsr_embed_grad_workspace(n, vocab, d, c)
+def gsr_embed_grad_workspace(n: int, vocab: int, d: int) -> int:
+    return lib().gsr_embed_grad_workspace(n, vocab, d)
 
 
 def gsr_embed_grad(ids, dx, dtable_out, scale: float = 1.0, workspace=None) -> None:
     """dtable_out[t] = scale * sum of dx[i] over ids[i] == t (float32 [vocab, D], rows may be strided; written whole).  dx: a plane as
-    gsr_embed_lookup's x_out; workspace: device tensor of gsr_embed_grad_workspace(n, vocab, D, C) bytes, or None."""
+    gsr_embed_lookup's x_out; workspace: device tensor of gsr_embed_grad_workspace(n, vocab, D) bytes, or None."""
     import torch
     n, d, c, layout, ldx = _plane(dx)
     vocab, dt, _, _, ldt = _plane(dtable_out)
     assert dt == d and dtable_out.dim() == 2 and dtable_out.dtype == torch.float32
     if workspace is None:
-        workspace = torch.empty(gsr_embed_grad_workspace(n, vocab, d, c), dtype=torch.uint8, device=dx.device)
+        workspace = torch.empty(gsr_embed_grad_workspace(n, vocab, d), dtype=torch.uint8, device=dx.device)
     _check(lib().gsr_embed_grad(ids.data_ptr(), _tokens(ids, n), n, dx.data_ptr(), ldx, d, c, layout, _dtype_of(dx), scale, vocab,
                                 dtable_out.data_ptr(), ldt, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
 

@@ -127,6 +127,9 @@ __global__ __launch_bounds__(256) void k_embed_lookup(const TT* __restrict__ tab
 // wave owns a stretch and takes it 64 elements at a time; lanes of equal digits find their order from one ballot per bit.
 constexpr int kDigitBits = 11;
 constexpr int kSortWaves = 4;
+constexpr int kSortBatch = 8;        // elements that a lane has in flight
+constexpr int kSortStretch = 256 * kSortBatch;   // elements of a workgroup, or a multiple of them beyond kSortWgs workgroups
+constexpr int kSortWgs = 1024;
 constexpr int kSmallSort = 4096;     // elements that one workgroup sorts in LDS
 constexpr int kSmallBits = 8;
 
@@ -177,6 +180,19 @@ __device__ __forceinline__ void clear_rows(float* out, int64_t ldt, int64_t voca
     }
 }
 
+// adds elements i, i + step, .. below b to the counts of their digits
+template <typename I>
+__device__ __forceinline__ void count_digits(const SortSource<I>& src, int64_t i, int64_t b, int step, int shift, uint32_t mask, uint32_t* count) {
+    for (; i < b; i += kSortBatch * step) {
+        int32_t key[kSortBatch];
+#pragma unroll
+        for (int u = 0; u < kSortBatch; ++u) key[u] = src.key(i + u * step < b ? i + u * step : b - 1);
+#pragma unroll
+        for (int u = 0; u < kSortBatch; ++u)
+            if (i + u * step < b) atomicAdd(&count[((uint32_t)key[u] >> shift) & mask], 1u);
+    }
+}
+
 template <typename I>
 __global__ __launch_bounds__(256) void k_embed_count(SortSource<I> src, int64_t n, int stretch, int wgs, int shift, int bits,
                                                      uint32_t* __restrict__ hist, float* out, int64_t ldt, int d) {
@@ -189,22 +205,31 @@ __global__ __launch_bounds__(256) void k_embed_count(SortSource<I> src, int64_t 
     for (int i = threadIdx.x; i < digits; i += 256) s_count[i] = 0;
     __syncthreads();
     const int64_t a = (int64_t)blockIdx.x * stretch, b = a + stretch < n ? a + stretch : n;
-    for (int64_t i = a + threadIdx.x; i < b; i += 256) atomicAdd(&s_count[((uint32_t)src.key(i) >> shift) & (digits - 1)], 1u);
+    count_digits(src, a + threadIdx.x, b, 256, shift, digits - 1, s_count);
     __syncthreads();
     for (int i = threadIdx.x; i < digits; i += 256) hist[(int64_t)i * wgs + blockIdx.x] = s_count[i];
 }
 
-// counts of a digit -> elements of that digit in the workgroups before; total[digit]
+// counts of a digit -> elements of that digit in the workgroups before; total[digit].  A wave per digit.
 __global__ __launch_bounds__(256) void k_embed_places(uint32_t* __restrict__ hist, int wgs, int digits, uint32_t* __restrict__ total) {
     const int digit = blockIdx.x * 4 + (threadIdx.x >> 6), lane = lane_id();
     if (digit >= digits) return;
     uint32_t* h = hist + (int64_t)digit * wgs;
     uint32_t before = 0;
-    for (int i = 0; i < wgs; i += 64) {
-        const uint32_t c = i + lane < wgs ? h[i + lane] : 0;
-        const uint32_t s = wave_scan(c);
-        if (i + lane < wgs) h[i + lane] = before + s - c;
-        before += __shfl(s, 63);
+    for (int i = 0; i < wgs; i += 64 * kSortBatch) {
+        uint32_t c[kSortBatch];
+#pragma unroll
+        for (int u = 0; u < kSortBatch; ++u) {
+            const int at = i + 64 * u + lane;
+            c[u] = h[at < wgs ? at : wgs - 1];
+            if (at >= wgs) c[u] = 0;
+        }
+#pragma unroll
+        for (int u = 0; u < kSortBatch; ++u) {
+            const uint32_t s = wave_scan(c[u]);
+            if (i + 64 * u + lane < wgs) h[i + 64 * u + lane] = before + s - c[u];
+            before += __shfl(s, 63);
+        }
     }
     if (lane == 0) total[digit] = before;
 }
@@ -213,18 +238,27 @@ __global__ __launch_bounds__(256) void k_embed_places(uint32_t* __restrict__ his
 template <typename I, typename Put>
 __device__ __forceinline__ void hand_out(const SortSource<I>& src, int64_t a, int64_t b, int shift, int bits, uint32_t* start, Put put) {
     const uint32_t mask = (1u << bits) - 1;
-    for (int64_t i = a; i < b; i += 64) {
-        const bool valid = i + lane_id() < b;
-        const int64_t e = valid ? i + lane_id() : b - 1;
-        const int32_t key = src.key(e);
-        const uint32_t place = src.place(e), digit = ((uint32_t)key >> shift) & mask;
-        const uint64_t m = same_digit(digit, bits, valid);
-        const int rank = lanes_below(m);
-        const uint32_t to = start[digit] + rank;
-        wave_sync();
-        if (valid && rank == 0) start[digit] += (uint32_t)__popcll(m);
-        wave_sync();
-        if (valid) put(to, key, place);
+    for (int64_t i = a + lane_id(); i < b + lane_id(); i += 64 * kSortBatch) {          // (uniform: i - lane < b)
+        int32_t key[kSortBatch];
+        uint32_t place[kSortBatch];
+#pragma unroll
+        for (int u = 0; u < kSortBatch; ++u) {
+            const int64_t e = i + 64 * u < b ? i + 64 * u : b - 1;
+            key[u] = src.key(e);
+            place[u] = src.place(e);
+        }
+#pragma unroll
+        for (int u = 0; u < kSortBatch; ++u) {
+            const bool valid = i + 64 * u < b;
+            const uint32_t digit = ((uint32_t)key[u] >> shift) & mask;
+            const uint64_t m = same_digit(digit, bits, valid);
+            const int rank = lanes_below(m);
+            const uint32_t to = start[digit] + rank;
+            wave_sync();
+            if (valid && rank == 0) start[digit] = to + (uint32_t)__popcll(m);
+            wave_sync();
+            if (valid) put(to, key[u], place[u]);
+        }
     }
 }
 
@@ -263,7 +297,7 @@ __global__ __launch_bounds__(256) void k_embed_hand_out(SortSource<I> src, int64
     const int64_t a = a0 + (int64_t)w * (stretch / kSortWaves) < b0 ? a0 + (int64_t)w * (stretch / kSortWaves) : b0;
     const int64_t b = a + stretch / kSortWaves < b0 ? a + stretch / kSortWaves : b0;
     uint32_t* start = s_start + w * digits;
-    for (int64_t i = a + lane_id(); i < b; i += 64) atomicAdd(&start[((uint32_t)src.key(i) >> shift) & (digits - 1)], 1u);
+    count_digits(src, a + lane_id(), b, 64, shift, digits - 1, start);
     __syncthreads();
     for (int i = threadIdx.x; i < digits; i += 256) {
         uint32_t at = s_first[i] + hist[(int64_t)i * wgs + blockIdx.x];
@@ -338,28 +372,31 @@ __global__ __launch_bounds__(1024) void k_embed_sort_small(SortSource<I> ids, in
 // The sorted list is cut into chunks of equal length, one per sub-wave of as many lanes as a row has pieces (up to 64), so that a
 // token of a million rows and a million tokens of one row cost the same.  A run of equal tokens that lies in one chunk is stored as it
 // is; of a run that goes on beyond its chunk the sum is left in one of the chunk's two places of a list of partial rows (0: the run goes
-// on from the chunk before, 1: it begins here), whose tokens are ascending again: the same kernel joins that list, until one chunk holds it.
+// on from the chunk before, 1: it begins here), whose tokens are ascending again.  The same kernel shortens that list 32-fold at a time, and
+// where few chunks are left, k_embed_join adds up each run that began in one of them.
 struct EmbedSums {
-    const void* src;            // FIRST: the plane dx; else partial rows
-    int64_t ld, gs;             // FIRST: its row and group stride
+    const void* src;            // FIRST: the plane dx; else partial rows of d floats
+    int64_t ld, gs;             // row and group stride
     const int32_t* keys;        // ascending rows of the table; FIRST: vocab and above, else negative: nothing
     const uint32_t* pos;        // FIRST: rows of dx
     int32_t entries, chunks;
     int chunk;                  // entries per chunk, a multiple of kSumBatch
+    int d;                      // columns of a row of the table
     int lanes_log2;             // lanes per chunk
     int pieces, pg, dg;         // of a whole row; of a group; columns of a group
     int32_t vocab;
     float scale;
     float* out;
     int64_t ldt;
-    float* part;                // [2 chunks][pieces * V], nullptr if there is one chunk
+    float* part;                // [2 chunks][d], nullptr if there is one chunk
     int32_t* part_keys;         // [2 chunks], negative: nothing
 };
-constexpr int kSumBatch = 8, kSumChunkMax = 64, kSumLanesMin = 3;      // (lanes per chunk as a logarithm)
+constexpr int kSumBatch = 16, kSumChunkMax = 64, kSumLanesMin = 3;     // (lanes per chunk as a logarithm)
+constexpr int kJoinChunks = 1024;                                      // chunks from which k_embed_join takes over
 
 template <typename S, int V, bool FIRST>
 __global__ __launch_bounds__(256) void k_embed_sums(EmbedSums a) {
-    constexpr int U = kSumBatch;
+    constexpr int U = FIRST ? kSumBatch / 2 : kSumBatch;       // partial rows: few waves, each with more in flight
     __shared__ int32_t s_key[(256 >> kSumLanesMin) * (kSumChunkMax + 4)];
     __shared__ int32_t s_pos[(256 >> kSumLanesMin) * (kSumChunkMax + 4)];
     const int subs = 256 >> a.lanes_log2, sub = threadIdx.x >> a.lanes_log2, stride = a.chunk + 4;
@@ -389,10 +426,9 @@ __global__ __launch_bounds__(256) void k_embed_sums(EmbedSums a) {
     const bool mine = piece < a.pieces;
     const int q = mine ? piece : a.pieces - 1, group = q / a.pg;
     const int in_group = (q - group * a.pg) * V, col = in_group + V <= a.dg ? in_group : a.dg - V;
-    const int64_t width = (int64_t)a.pieces * V;
-    const S* src = static_cast<const S*>(a.src) + (FIRST ? group * a.gs + col : (int64_t)q * V);
-    const int64_t ld = FIRST ? a.ld : width;
-    float* out = a.out + group * a.dg + col;
+    const S* src = static_cast<const S*>(a.src) + group * a.gs + col;
+    const int column = group * a.dg + col;
+    float* out = a.out + column;
 
     const int64_t s = c * a.chunk, e = s + a.chunk;
     const int32_t first = keys[0];
@@ -409,7 +445,7 @@ __global__ __launch_bounds__(256) void k_embed_sums(EmbedSums a) {
         if (!mine) return;
         float v[V];
         if (to_part) {
-            store_piece<V>(a.part + place * width + (int64_t)q * V, acc);
+            store_piece<V>(a.part + place * a.d + column, acc);
         } else {
 #pragma unroll
             for (int i = 0; i < V; ++i) v[i] = a.scale * acc[i];
@@ -427,7 +463,7 @@ __global__ __launch_bounds__(256) void k_embed_sums(EmbedSums a) {
         }
         if (!__any(any)) continue;
 #pragma unroll
-        for (int u = 0; u < U; ++u) p[u].load(src + rows[b + u] * ld);
+        for (int u = 0; u < U; ++u) p[u].load(src + rows[b + u] * a.ld);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (k[u] < 0) continue;
@@ -447,6 +483,53 @@ __global__ __launch_bounds__(256) void k_embed_sums(EmbedSums a) {
         a.part_keys[2 * c] = left ? first : -1;
         a.part_keys[2 * c + 1] = right && !open ? cur : -1;
     }
+}
+
+// Partial rows of `chunks` chunks: workgroup (i, j) adds up the run that began in chunk i, if one did, in columns 16 V j to 16 V (j + 1): the place
+// where it begins and the first places of the chunks after it that carry on its token.  Sixteen lanes take a row, sixteen rows side by side.
+template <int V>
+__global__ __launch_bounds__(256) void k_embed_join(const float* __restrict__ part, const int32_t* __restrict__ keys, int chunks, int d,
+                                                    float scale, float* __restrict__ out, int64_t ldt) {
+    constexpr int U = 8;
+    __shared__ float s_sum[16][16 * V];
+    const int i = blockIdx.x;
+    const int32_t key = keys[2 * i + 1];
+    if (key < 0) return;
+    int more = 0, found;
+    do {                                        // every thread looks at a chunk: those that carry on come first
+        const int j = i + 1 + more + (int)threadIdx.x;
+        found = __syncthreads_count(j < chunks && keys[2 * (j < chunks ? j : chunks - 1)] == key);
+        more += found;
+    } while (found == 256);
+    const int sub = threadIdx.x >> 4, lane = threadIdx.x & 15, piece = blockIdx.y * 16 + lane;
+    const int col = piece * V + V <= d ? piece * V : d - V;
+    float acc[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+    for (int r = sub; r <= more; r += 16 * U) {
+        Piece<float, V> p[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int row = r + 16 * u <= more ? r + 16 * u : more;
+            p[u].load(part + (int64_t)(row ? 2 * (i + row) : 2 * i + 1) * d + col);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (r + 16 * u <= more) acc[e] += p[u].at(e);
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) s_sum[sub][lane * V + e] = acc[e];
+    __syncthreads();
+    if (threadIdx.x >= 16 || piece * V >= d) return;
+    const int rows = more + 1 < 16 ? more + 1 : 16;
+    for (int s = 1; s < rows; ++s)
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] += s_sum[s][lane * V + e];
+#pragma unroll
+    for (int e = 0; e < V; ++e) acc[e] *= scale;
+    store_piece<V>(out + (int64_t)key * ldt + col, acc);
 }
 
 // ---- host side ----------------------------------------------------------------------------------------------
@@ -514,7 +597,7 @@ struct EmbedPlan {
     int levels;
     size_t bytes;
 };
-EmbedPlan embed_plan(int64_t n, int64_t vocab, int d, int c) {
+EmbedPlan embed_plan(int64_t n, int64_t vocab, int d) {
     EmbedPlan p{};
     int bits = 1;
     while (((int64_t)1 << bits) <= vocab) ++bits;           // keys are 0 .. vocab
@@ -522,10 +605,10 @@ EmbedPlan embed_plan(int64_t n, int64_t vocab, int d, int c) {
     const int most = p.small ? kSmallBits : kDigitBits;
     p.passes = (bits + most - 1) / most;
     p.bits = (bits + p.passes - 1) / p.passes;
-    p.wgs = (int)std::min<int64_t>(256, std::max<int64_t>(1, (n + 4095) / 4096));
-    p.stretch = (int)(((n + p.wgs - 1) / p.wgs + 255) / 256 * 256);
+    const int64_t stretches = std::max<int64_t>(1, (n + kSortStretch - 1) / kSortStretch);
+    p.stretch = kSortStretch * (int)((stretches + kSortWgs - 1) / kSortWgs);
+    p.wgs = (int)std::max<int64_t>(1, (n + p.stretch - 1) / p.stretch);
     p.chunk = n > 65536 ? kSumChunkMax : 16;
-    const size_t width = (size_t)c * ((d / c + 7) / 8 * 8);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -539,49 +622,72 @@ EmbedPlan embed_plan(int64_t n, int64_t vocab, int d, int c) {
     p.hist = take(((size_t)p.wgs << p.bits) * 4);
     p.total = take(((size_t)1 << p.bits) * 4);
     int64_t entries = n;
+    int chunk = p.chunk;
     do {
         EmbedPlan::Level& l = p.level[p.levels++];
         l.entries = entries;
-        l.chunks = (entries + p.chunk - 1) / p.chunk;
+        l.chunks = (entries + chunk - 1) / chunk;
         if (l.chunks <= 1) break;
         l.part_keys = take((size_t)l.chunks * 2 * 4);
-        l.part = take((size_t)l.chunks * 2 * width * 4);
+        l.part = take((size_t)l.chunks * 2 * d * 4);
         entries = 2 * l.chunks;
-    } while (true);
+        chunk = kSumChunkMax;
+    } while (entries > 2 * kJoinChunks);
     p.bytes = at;
     return p;
 }
 
-template <typename S, int V>
-void launch_sums(const EmbedPlan& p, const EmbedShape& s, const void* dx, float scale, int64_t vocab, float* out, int64_t ldt, int last,
-                 char* ws, hipStream_t st) {
-    const int pg = (s.dg + V - 1) / V, pieces = pg * s.c;
-    int log2 = kSumLanesMin;
-    while (log2 < 6 && (1 << log2) < pieces) ++log2;
-    for (int l = 0; l < p.levels; ++l) {
-        const EmbedPlan::Level& v = p.level[l];
-        EmbedSums a{};
-        a.src = l ? (const void*)(ws + p.level[l - 1].part) : dx;
-        a.ld = s.ldx;
-        a.gs = s.gs;
-        a.keys = (const int32_t*)(ws + (l ? p.level[l - 1].part_keys : p.keys[last]));
-        a.pos = (const uint32_t*)(ws + p.pos[last]);
-        a.entries = (int32_t)v.entries;
-        a.chunks = (int32_t)v.chunks;
-        a.chunk = p.chunk;
-        a.lanes_log2 = log2;
-        a.pieces = pieces; a.pg = pg; a.dg = s.dg;
-        a.vocab = (int32_t)vocab;
-        a.scale = scale;
-        a.out = out;
-        a.ldt = ldt;
-        a.part = v.chunks > 1 ? (float*)(ws + v.part) : nullptr;
-        a.part_keys = v.chunks > 1 ? (int32_t*)(ws + v.part_keys) : nullptr;
-        const int subs = 256 >> log2;
-        const dim3 grid((unsigned)((v.chunks + subs - 1) / subs), (unsigned)((pieces + (1 << log2) - 1) >> log2));
-        if (l == 0) hipLaunchKernelGGL((k_embed_sums<S, V, true>), grid, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((k_embed_sums<float, V, false>), grid, dim3(256), 0, st, a);
+template <typename S, int V, bool FIRST>
+void launch_level(const EmbedPlan& p, int level, EmbedSums a, char* ws, hipStream_t st) {
+    const EmbedPlan::Level& v = p.level[level];
+    a.entries = (int32_t)v.entries;
+    a.chunks = (int32_t)v.chunks;
+    a.part = v.chunks > 1 ? (float*)(ws + v.part) : nullptr;
+    a.part_keys = v.chunks > 1 ? (int32_t*)(ws + v.part_keys) : nullptr;
+    a.chunk = FIRST ? p.chunk : kSumChunkMax;
+    a.pg = (a.dg + V - 1) / V;
+    a.pieces = a.pg * (a.d / a.dg);
+    a.lanes_log2 = kSumLanesMin;
+    while (a.lanes_log2 < 6 && (1 << a.lanes_log2) < a.pieces) ++a.lanes_log2;
+    const int subs = 256 >> a.lanes_log2, lanes = 1 << a.lanes_log2;
+    const dim3 grid((unsigned)((v.chunks + subs - 1) / subs), (unsigned)((a.pieces + lanes - 1) / lanes));
+    hipLaunchKernelGGL((k_embed_sums<S, V, FIRST>), grid, dim3(256), 0, st, a);
+}
+
+void launch_sums(const EmbedPlan& p, const EmbedShape& s, const void* dx, int32_t dtype, int d, float scale, int64_t vocab, float* out, int64_t ldt,
+                 int last, char* ws, hipStream_t st) {
+    EmbedSums a{};
+    a.vocab = (int32_t)vocab;
+    a.scale = scale;
+    a.out = out;
+    a.ldt = ldt;
+    a.d = d;
+    a.src = dx;
+    a.ld = s.ldx;
+    a.gs = s.gs;
+    a.dg = s.dg;
+    a.keys = (const int32_t*)(ws + p.keys[last]);
+    a.pos = (const uint32_t*)(ws + p.pos[last]);
+    if (dtype == GSR_F32 && s.dg >= 4) launch_level<float, 4, true>(p, 0, a, ws, st);
+    else if (dtype == GSR_F32) launch_level<float, 1, true>(p, 0, a, ws, st);
+    else if (s.dg >= 8) launch_level<bf16_t, 8, true>(p, 0, a, ws, st);
+    else launch_level<bf16_t, 1, true>(p, 0, a, ws, st);
+    a.ld = a.dg = d;
+    a.gs = 0;
+    for (int l = 1; l < p.levels; ++l) {
+        a.src = ws + p.level[l - 1].part;
+        a.keys = (const int32_t*)(ws + p.level[l - 1].part_keys);
+        if (d >= 4) launch_level<float, 4, false>(p, l, a, ws, st);
+        else launch_level<float, 1, false>(p, l, a, ws, st);
     }
+    const EmbedPlan::Level& v = p.level[p.levels - 1];
+    if (v.chunks <= 1) return;
+    const float* part = (const float*)(ws + v.part);
+    const int32_t* keys = (const int32_t*)(ws + v.part_keys);
+    if (d >= 4)
+        hipLaunchKernelGGL((k_embed_join<4>), dim3((unsigned)v.chunks, (d + 63) / 64), dim3(256), 0, st, part, keys, (int)v.chunks, d, scale, out, ldt);
+    else
+        hipLaunchKernelGGL((k_embed_join<1>), dim3((unsigned)v.chunks, 1), dim3(256), 0, st, part, keys, (int)v.chunks, d, scale, out, ldt);
 }
 
 template <typename I>
@@ -645,9 +751,9 @@ gsr_status_t gsr_embed_lookup(const void* table, int64_t vocab, int64_t ldt, int
     return GSR_OK;
 }
 
-size_t gsr_embed_grad_workspace(int64_t n, int64_t vocab, int32_t d, int32_t c) {
-    if (n < 0 || n >= ((int64_t)1 << 31) || vocab < 1 || vocab >= ((int64_t)1 << 31) - 1 || d < 1 || d > kMaxWidth || c < 1 || d % c) return 0;
-    return embed_plan(n, vocab, d, c).bytes;
+size_t gsr_embed_grad_workspace(int64_t n, int64_t vocab, int32_t d) {
+    if (n < 0 || n >= ((int64_t)1 << 31) || vocab < 1 || vocab >= ((int64_t)1 << 31) - 1 || d < 1 || d > kMaxWidth) return 0;
+    return embed_plan(n, vocab, d).bytes;
 }
 
 gsr_status_t gsr_embed_grad(const void* ids, int32_t ids_i64, int64_t n, const void* dx, int64_t ldx, int32_t d, int32_t c, int32_t layout,
@@ -657,7 +763,7 @@ gsr_status_t gsr_embed_grad(const void* ids, int32_t ids_i64, int64_t n, const v
     GSR_TRY(embed_shape(n, d, c, layout, ldx, vocab, ldt, &s));
     GSR_TRY(plane_dtype(dtype));
     if (!dtable_out || (n > 0 && (!ids || !dx))) return fail(GSR_ERR_INVALID_ARG, "null pointer");
-    const EmbedPlan p = embed_plan(n, vocab, d, c);
+    const EmbedPlan p = embed_plan(n, vocab, d);
     if (workspace_bytes < p.bytes) return fail(GSR_ERR_WORKSPACE_TOO_SMALL, "workspace of %zu bytes, %zu needed", workspace_bytes, p.bytes);
     if (p.bytes && !workspace) return fail(GSR_ERR_INVALID_ARG, "null workspace");
     if (!aligned_to(dx, dtype_size(dtype)) || !aligned_to(dtable_out, 4) || !aligned_to(ids, ids_i64 ? 8 : 4) || !aligned_to(workspace, 16))
@@ -666,12 +772,7 @@ gsr_status_t gsr_embed_grad(const void* ids, int32_t ids_i64, int64_t n, const v
     char* ws = (char*)workspace;
     const int last = ids_i64 ? launch_sort<int64_t>(p, ids, n, vocab, dtable_out, ldt, d, ws, st)
                              : launch_sort<int32_t>(p, ids, n, vocab, dtable_out, ldt, d, ws, st);
-    if (n > 0) {
-        if (dtype == GSR_F32 && s.dg >= 4) launch_sums<float, 4>(p, s, dx, scale, vocab, dtable_out, ldt, last, ws, st);
-        else if (dtype == GSR_F32) launch_sums<float, 1>(p, s, dx, scale, vocab, dtable_out, ldt, last, ws, st);
-        else if (s.dg >= 8) launch_sums<bf16_t, 8>(p, s, dx, scale, vocab, dtable_out, ldt, last, ws, st);
-        else launch_sums<bf16_t, 1>(p, s, dx, scale, vocab, dtable_out, ldt, last, ws, st);
-    }
+    if (n > 0) launch_sums(p, s, dx, dtype, d, scale, vocab, dtable_out, ldt, last, ws, st);
     GSR_HIP_CHECK(hipGetLastError());
     return GSR_OK;
 }

@@ -245,7 +245,7 @@ class Training:
         self.x0, self.dx0 = torch.zeros(groups, **f32), torch.zeros(groups, **f32)
         self.loss, self.norm, self.target = torch.zeros(1, **f32), torch.zeros(1, **f32), torch.from_numpy(c.inp.target).to(dev())
         self.ws = torch.empty(gsr.gsr_workspace_size(c.gg, c.gcfg)[1], dtype=torch.uint8, device=dev())
-        self.ews = torch.empty(gsr.gsr_embed_grad_workspace(n, vocab, w.d, w.c), dtype=torch.uint8, device=dev())
+        self.ews = torch.empty(gsr.gsr_embed_grad_workspace(n, vocab, w.d), dtype=torch.uint8, device=dev())
         self.nws = torch.empty(gsr.gsr_grad_norm_workspace(self.grads), dtype=torch.uint8, device=dev())
 
     def gradients(self):
