@@ -23,6 +23,8 @@ template <typename T, int V>
 struct Piece {                       // V elements as they lie in memory
     static constexpr int NW = (V * (int)sizeof(T) + 3) / 4;
     uint32_t w[NW];
+    // STREAM: read once, not to be kept in the caches
+    template <bool STREAM = false>
     __device__ __forceinline__ void load(const T* p) {
         if constexpr (V == 1) {
             if constexpr (sizeof(T) == 4) w[0] = *reinterpret_cast<const uint32_t*>(p);
@@ -30,14 +32,16 @@ struct Piece {                       // V elements as they lie in memory
         } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
             for (int i = 0; i < NW; i += 4) {
-                const u32x4a t = *reinterpret_cast<const u32x4a*>(p + i);
+                const u32x4a* q = reinterpret_cast<const u32x4a*>(p + i);
+                const u32x4a t = STREAM ? __builtin_nontemporal_load(q) : *q;
                 w[i] = t[0]; w[i + 1] = t[1]; w[i + 2] = t[2]; w[i + 3] = t[3];
             }
         } else if constexpr (NW == 2) {
             const u32x2h t = *reinterpret_cast<const u32x2h*>(p);
             w[0] = t[0]; w[1] = t[1];
         } else {
-            const u32x4h t = *reinterpret_cast<const u32x4h*>(p);
+            const u32x4h* q = reinterpret_cast<const u32x4h*>(p);
+            const u32x4h t = STREAM ? __builtin_nontemporal_load(q) : *q;
             w[0] = t[0]; w[1] = t[1]; w[2] = t[2]; w[3] = t[3];
         }
     }
@@ -132,6 +136,7 @@ constexpr int kSortStretch = 256 * kSortBatch;   // elements of a workgroup, or 
 constexpr int kSortWgs = 1024;
 constexpr int kSmallSort = 4096;     // elements that one workgroup sorts in LDS
 constexpr int kSmallBits = 8;
+static_assert(kSmallSort <= 16 * 64 * kSortBatch, "a wave of the small sort takes one batch");
 
 // What the sort moves: (row of the table or vocab, position).  The first pass reads tokens, positions are their own numbers.
 template <typename I>
@@ -234,21 +239,26 @@ __global__ __launch_bounds__(256) void k_embed_places(uint32_t* __restrict__ his
     if (lane == 0) total[digit] = before;
 }
 
-// s_start[w * digits + digit]: the place of the next element of that digit in wave w's stretch [a, b)
-template <typename I, typename Put>
-__device__ __forceinline__ void hand_out(const SortSource<I>& src, int64_t a, int64_t b, int shift, int bits, uint32_t* start, Put put) {
-    const uint32_t mask = (1u << bits) - 1;
-    for (int64_t i = a + lane_id(); i < b + lane_id(); i += 64 * kSortBatch) {          // (uniform: i - lane < b)
-        int32_t key[kSortBatch];
-        uint32_t place[kSortBatch];
+// The elements of a wave's stretch [i - lane, b), the batch that a lane holds of them.
+template <typename I>
+struct SortBatch {
+    int32_t key[kSortBatch];
+    uint32_t place[kSortBatch];
+    __device__ __forceinline__ void load(const SortSource<I>& src, int64_t i, int64_t b) {
 #pragma unroll
         for (int u = 0; u < kSortBatch; ++u) {
             const int64_t e = i + 64 * u < b ? i + 64 * u : b - 1;
             key[u] = src.key(e);
             place[u] = src.place(e);
         }
+    }
+    // start[digit]: the place of the wave's next element of that digit
+    template <typename Put>
+    __device__ __forceinline__ void hand_out(int64_t i, int64_t b, int shift, int bits, uint32_t* start, Put put) const {
+        const uint32_t mask = (1u << bits) - 1;
 #pragma unroll
         for (int u = 0; u < kSortBatch; ++u) {
+            if (i - lane_id() + 64 * u >= b) break;
             const bool valid = i + 64 * u < b;
             const uint32_t digit = ((uint32_t)key[u] >> shift) & mask;
             const uint64_t m = same_digit(digit, bits, valid);
@@ -260,7 +270,7 @@ __device__ __forceinline__ void hand_out(const SortSource<I>& src, int64_t a, in
             if (valid) put(to, key[u], place[u]);
         }
     }
-}
+};
 
 // exclusive sums of v[0 .. count) for a workgroup of `waves` waves; s_wave: a word per wave
 __device__ __forceinline__ void wg_scan(uint32_t* v, int count, uint32_t* s_wave, int waves) {
@@ -284,23 +294,45 @@ template <typename I>
 __global__ __launch_bounds__(256) void k_embed_hand_out(SortSource<I> src, int64_t n, int stretch, int wgs, int shift, int bits,
                                                         const uint32_t* __restrict__ hist, const uint32_t* __restrict__ total,
                                                         int32_t* __restrict__ keys, uint32_t* __restrict__ pos) {
+    constexpr int PER = (1 << kDigitBits) / 256;             // digits of a thread
     __shared__ uint32_t s_start[kSortWaves << kDigitBits];
     __shared__ uint32_t s_first[1 << kDigitBits];
     __shared__ uint32_t s_wave[kSortWaves];
     const int digits = 1 << bits, w = threadIdx.x >> 6;
-    for (int i = threadIdx.x; i < digits; i += 256) s_first[i] = total[i];
-    for (int i = threadIdx.x; i < kSortWaves * digits; i += 256) s_start[i] = 0;
-    __syncthreads();
-    wg_scan(s_first, digits, s_wave, kSortWaves);
-    // a workgroup's stretch is a multiple of 256 elements: each wave's a multiple of 64
+    // a workgroup's stretch is a multiple of 2,048 elements: each wave's a multiple of its batch
     const int64_t a0 = (int64_t)blockIdx.x * stretch, b0 = a0 + stretch < n ? a0 + stretch : n;
     const int64_t a = a0 + (int64_t)w * (stretch / kSortWaves) < b0 ? a0 + (int64_t)w * (stretch / kSortWaves) : b0;
     const int64_t b = a + stretch / kSortWaves < b0 ? a + stretch / kSortWaves : b0;
-    uint32_t* start = s_start + w * digits;
-    count_digits(src, a + lane_id(), b, 64, shift, digits - 1, start);
+    // what comes from memory is asked for at once: the first batch, the digits' totals and places
+    SortBatch<I> batch;
+    if (a < b) batch.load(src, a + lane_id(), b);
+    uint32_t tot[PER], before[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const int i = threadIdx.x + 256 * j < digits ? threadIdx.x + 256 * j : digits - 1;
+        if (256 * j < digits) {
+            tot[j] = total[i];
+            before[j] = hist[(int64_t)i * wgs + blockIdx.x];
+        }
+    }
+    for (int i = threadIdx.x; i < kSortWaves * digits; i += 256) s_start[i] = 0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+        if (threadIdx.x + 256 * j < digits) s_first[threadIdx.x + 256 * j] = tot[j];
     __syncthreads();
-    for (int i = threadIdx.x; i < digits; i += 256) {
-        uint32_t at = s_first[i] + hist[(int64_t)i * wgs + blockIdx.x];
+    uint32_t* start = s_start + w * digits;
+    if (a < b) {
+#pragma unroll
+        for (int u = 0; u < kSortBatch; ++u)
+            if (a + lane_id() + 64 * u < b) atomicAdd(&start[((uint32_t)batch.key[u] >> shift) & (digits - 1)], 1u);
+        count_digits(src, a + 64 * kSortBatch + lane_id(), b, 64, shift, digits - 1, start);
+    }
+    wg_scan(s_first, digits, s_wave, kSortWaves);
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const int i = threadIdx.x + 256 * j;
+        if (i >= digits) break;
+        uint32_t at = s_first[i] + before[j];
         for (int v = 0; v < kSortWaves; ++v) {
             const uint32_t c = s_start[v * digits + i];
             s_start[v * digits + i] = at;
@@ -308,10 +340,13 @@ __global__ __launch_bounds__(256) void k_embed_hand_out(SortSource<I> src, int64
         }
     }
     __syncthreads();
-    hand_out(src, a, b, shift, bits, start, [&](uint32_t to, int32_t key, uint32_t place) {
-        keys[to] = key;
-        pos[to] = place;
-    });
+    for (int64_t i = a + lane_id(); i - lane_id() < b; i += 64 * kSortBatch) {
+        if (i - lane_id() > a) batch.load(src, i, b);
+        batch.hand_out(i, b, shift, bits, start, [&](uint32_t to, int32_t key, uint32_t place) {
+            keys[to] = key;
+            pos[to] = place;
+        });
+    }
 }
 
 // Up to kSmallSort elements: workgroup 0 sorts them in LDS, digits of up to 8 bits, the others clear the gradient.
@@ -356,10 +391,14 @@ __global__ __launch_bounds__(1024) void k_embed_sort_small(SortSource<I> ids, in
         __syncthreads();
         int32_t* kto = s_key[(p + 1) & 1];
         uint32_t* pto = s_pos[(p + 1) & 1];
-        hand_out(src, a, b, p * bits, bits, start, [&](uint32_t to, int32_t key, uint32_t place) {
-            kto[to] = key;
-            pto[to] = place;
-        });
+        SortBatch<int32_t> batch;                // (at most 256 elements per wave: one batch)
+        if (a < b) {
+            batch.load(src, a + lane_id(), b);
+            batch.hand_out(a + lane_id(), b, p * bits, bits, start, [&](uint32_t to, int32_t key, uint32_t place) {
+                kto[to] = key;
+                pto[to] = place;
+            });
+        }
         __syncthreads();
     }
     for (int i = threadIdx.x; i < n; i += 1024) {
@@ -391,14 +430,16 @@ struct EmbedSums {
     float* part;                // [2 chunks][d], nullptr if there is one chunk
     int32_t* part_keys;         // [2 chunks], negative: nothing
 };
-constexpr int kSumBatch = 16, kSumChunkMax = 64, kSumLanesMin = 3;     // (lanes per chunk as a logarithm)
+constexpr int kSumBatch = 16, kSumLanesMin = 3;                        // (lanes per chunk as a logarithm)
+constexpr int kSumEntries = 2048;                                      // of a workgroup, at most
+constexpr int kPartChunk = 32;                                         // partial rows per chunk
 constexpr int kJoinChunks = 1024;                                      // chunks from which k_embed_join takes over
 
 template <typename S, int V, bool FIRST>
 __global__ __launch_bounds__(256) void k_embed_sums(EmbedSums a) {
     constexpr int U = FIRST ? kSumBatch / 2 : kSumBatch;       // partial rows: few waves, each with more in flight
-    __shared__ int32_t s_key[(256 >> kSumLanesMin) * (kSumChunkMax + 4)];
-    __shared__ int32_t s_pos[(256 >> kSumLanesMin) * (kSumChunkMax + 4)];
+    __shared__ int32_t s_key[kSumEntries + 4 * (256 >> kSumLanesMin)];
+    __shared__ int32_t s_pos[kSumEntries + 4 * (256 >> kSumLanesMin)];
     const int subs = 256 >> a.lanes_log2, sub = threadIdx.x >> a.lanes_log2, stride = a.chunk + 4;
     const int64_t e0 = (int64_t)blockIdx.x * subs * a.chunk;
     for (int i = threadIdx.x; i < subs * a.chunk; i += 256) {
@@ -463,7 +504,24 @@ __global__ __launch_bounds__(256) void k_embed_sums(EmbedSums a) {
         }
         if (!__any(any)) continue;
 #pragma unroll
-        for (int u = 0; u < U; ++u) p[u].load(src + rows[b + u] * a.ld);
+        for (int u = 0; u < U; ++u) p[u].template load<FIRST>(src + rows[b + u] * a.ld);
+        bool same = cur >= 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) same &= k[u] == cur;
+        if (same) {                             // a batch within a run, added up by pairs: a sum of 256 rows is 35 additions deep
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                float v[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) v[u] = p[u].at(i);
+#pragma unroll
+                for (int w = U / 2; w; w /= 2)
+#pragma unroll
+                    for (int u = 0; u < w; ++u) v[u] += v[u + w];
+                acc[i] += v[0];
+            }
+            continue;
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (k[u] < 0) continue;
@@ -608,7 +666,8 @@ EmbedPlan embed_plan(int64_t n, int64_t vocab, int d) {
     const int64_t stretches = std::max<int64_t>(1, (n + kSortStretch - 1) / kSortStretch);
     p.stretch = kSortStretch * (int)((stretches + kSortWgs - 1) / kSortWgs);
     p.wgs = (int)std::max<int64_t>(1, (n + p.stretch - 1) / p.stretch);
-    p.chunk = n > 65536 ? kSumChunkMax : 16;
+    p.chunk = 16;
+    while (p.chunk < 256 && p.chunk < (n * d) >> 20 && p.chunk < d) p.chunk *= 2;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -631,7 +690,7 @@ EmbedPlan embed_plan(int64_t n, int64_t vocab, int d) {
         l.part_keys = take((size_t)l.chunks * 2 * 4);
         l.part = take((size_t)l.chunks * 2 * d * 4);
         entries = 2 * l.chunks;
-        chunk = kSumChunkMax;
+        chunk = kPartChunk;
     } while (entries > 2 * kJoinChunks);
     p.bytes = at;
     return p;
@@ -644,7 +703,7 @@ void launch_level(const EmbedPlan& p, int level, EmbedSums a, char* ws, hipStrea
     a.chunks = (int32_t)v.chunks;
     a.part = v.chunks > 1 ? (float*)(ws + v.part) : nullptr;
     a.part_keys = v.chunks > 1 ? (int32_t*)(ws + v.part_keys) : nullptr;
-    a.chunk = FIRST ? p.chunk : kSumChunkMax;
+    a.chunk = FIRST ? p.chunk : kPartChunk;
     a.pg = (a.dg + V - 1) / V;
     a.pieces = a.pg * (a.d / a.dg);
     a.lanes_log2 = kSumLanesMin;
