@@ -54,7 +54,7 @@ struct Piece {                       // V elements as they lie in memory
 // rounded to the nearest 16-bit value, NaN stays NaN
 __device__ __forceinline__ uint32_t bf16_bits(float v) { return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v)); }
 
-template <int V, typename T>
+template <int V, bool STREAM = false, typename T>
 __device__ __forceinline__ void store_piece(T* p, const float (&v)[V]) {
     if constexpr (sizeof(T) == 4) {
         if constexpr (V == 1) {
@@ -65,7 +65,8 @@ __device__ __forceinline__ void store_piece(T* p, const float (&v)[V]) {
                 u32x4a t;
                 t[0] = __float_as_uint(v[i]); t[1] = __float_as_uint(v[i + 1]);
                 t[2] = __float_as_uint(v[i + 2]); t[3] = __float_as_uint(v[i + 3]);
-                *reinterpret_cast<u32x4a*>(p + i) = t;
+                if constexpr (STREAM) __builtin_nontemporal_store(t, reinterpret_cast<u32x4a*>(p + i));
+                else *reinterpret_cast<u32x4a*>(p + i) = t;
             }
         }
     } else {
@@ -76,7 +77,8 @@ __device__ __forceinline__ void store_piece(T* p, const float (&v)[V]) {
             u32x4h t;
 #pragma unroll
             for (int i = 0; i < 4; ++i) t[i] = bf16_bits(v[2 * i]) | (bf16_bits(v[2 * i + 1]) << 16);
-            *reinterpret_cast<u32x4h*>(p) = t;
+            if constexpr (STREAM) __builtin_nontemporal_store(t, reinterpret_cast<u32x4h*>(p));
+            else *reinterpret_cast<u32x4h*>(p) = t;
         }
     }
 }
@@ -86,8 +88,12 @@ template <typename I>
 __device__ __forceinline__ int32_t token_row(I id, int32_t vocab) { return id >= 0 && id < (I)vocab ? (int32_t)id : vocab; }
 
 // ---- lookup ---------------------------------------------------------------------------------------------
-// blockIdx.y: the group (planes) or 0 (rows); a workgroup writes whole rows of it, about 1,024 pieces.  `magic` divides a piece's
-// number by the pieces per row (ceil(2^32 / pg), 0 for one piece; exact below 2^16).
+// blockIdx.y: the group (planes) or 0 (rows); a workgroup writes whole rows of it, about 512 pieces, two a thread.  `magic` divides a piece's
+// number by the pieces per row (ceil(2^32 / pg), 0 for one piece; exact below 2^16).  Bound by the writes (the table comes from the caches
+// unless it is larger than the plane).  They are streamed past the caches: 1M rows of 256 floats 217 -> 181 us, and with two pieces a thread
+// instead of four 143 us (7.2 TB/s; a fill by itself reaches 6.8).  gsr_step on the plane right after it, lookup included: 4,990 us cached,
+// 4,908 and 4,899 streamed; planes of 4 to 128 MB are as fast or faster streamed too.
+constexpr int kLookupPieces = 2;                // of a thread
 template <typename TT, typename T, typename I, int V>
 __global__ __launch_bounds__(256) void k_embed_lookup(const TT* __restrict__ table, int64_t ldt, int32_t vocab,
                                                       const I* __restrict__ ids, int64_t n, int dg, int pg, uint32_t magic,
@@ -98,12 +104,13 @@ __global__ __launch_bounds__(256) void k_embed_lookup(const TT* __restrict__ tab
     for (int64_t row0 = (int64_t)blockIdx.x * rows_per_wg; row0 < n; row0 += (int64_t)gridDim.x * rows_per_wg) {
         const int rows = n - row0 < rows_per_wg ? (int)(n - row0) : rows_per_wg;
         const uint32_t count = (uint32_t)rows * (uint32_t)pg;
-        for (uint32_t t0 = threadIdx.x; t0 < count; t0 += 4 * 256) {
-            uint32_t row[4], col[4];
-            int32_t id[4];
-            Piece<TT, V> p[4];
+        for (uint32_t t0 = threadIdx.x; t0 < count; t0 += kLookupPieces * 256) {
+            constexpr int U = kLookupPieces;
+            uint32_t row[U], col[U];
+            int32_t id[U];
+            Piece<TT, V> p[U];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
+            for (int u = 0; u < U; ++u) {
                 const uint32_t t = t0 + 256 * u < count ? t0 + 256 * u : count - 1;
                 row[u] = magic ? __umulhi(t, magic) : t;
                 const uint32_t q = (t - row[u] * (uint32_t)pg) * V;
@@ -111,14 +118,14 @@ __global__ __launch_bounds__(256) void k_embed_lookup(const TT* __restrict__ tab
                 id[u] = token_row(ids[row0 + row[u]], vocab);
             }
 #pragma unroll
-            for (int u = 0; u < 4; ++u) p[u].load(tab + (id[u] < vocab ? id[u] : 0) * ldt + col[u]);
+            for (int u = 0; u < U; ++u) p[u].load(tab + (id[u] < vocab ? id[u] : 0) * ldt + col[u]);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
+            for (int u = 0; u < U; ++u) {
                 if (t0 + 256 * u >= count) break;
                 float v[V];
 #pragma unroll
                 for (int i = 0; i < V; ++i) v[i] = id[u] < vocab ? scale * p[u].at(i) : 0.0f;
-                store_piece<V>(plane + (row0 + row[u]) * ldx + col[u], v);
+                store_piece<V, true>(plane + (row0 + row[u]) * ldx + col[u], v);
             }
         }
     }
@@ -626,7 +633,7 @@ bool aligned_to(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1
 
 template <typename TT, typename T, typename I, int V>
 void launch_lookup(const EmbedShape& s, const void* table, int64_t ldt, int32_t vocab, const void* ids, float scale, void* x, hipStream_t st) {
-    const int pg = (s.dg + V - 1) / V, rows = std::max(1, 1024 / pg);
+    const int pg = (s.dg + V - 1) / V, rows = std::max(1, 256 * kLookupPieces / pg);
     const unsigned wgs = (unsigned)std::min<int64_t>((s.n + rows - 1) / rows, 1 << 20);
     const uint32_t magic = pg == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + pg - 1) / pg);
     hipLaunchKernelGGL((k_embed_lookup<TT, T, I, V>), dim3(wgs, s.c), dim3(256), 0, st, (const TT*)table, ldt, vocab, (const I*)ids, s.n, s.dg,
