@@ -17,8 +17,12 @@
 namespace gsr {
 
 constexpr int kArgBytes = 4096 - 256;           // tensor table of a launch (kernel arguments: 4 KB)
-constexpr int kChunk = 4096;                    // elements that a workgroup takes at a time
-constexpr int kMaxPartials = 2048;              // workgroups, hence partial sums, of one launch of the norm
+// Elements that a workgroup takes at a time.  Every kernel here is bound by memory, reads and writes past the caches, and was timed with 2,048 to
+// 16,384: norm of 400M 16-bit values (up to 16,384 workgroups, several chunks each) 152 us at 16,384, 139 at 8,192, 130 at 4,096 (6.2 TB/s),
+// 175 at 2,048; clipping 201M floats (one chunk per workgroup) 472, 426, 412, 402 us at 2,048; clipped Adam on 120M weights with 16-bit
+// gradients 706, 662, 617, 593 us (5.3 TB/s, the norm before it included).  With cached accesses at 8,192: 161, 488 and 726 us.
+constexpr int kNormChunk = 4096, kUpdateChunk = 2048;
+constexpr int kMaxPartials = 16384;             // workgroups, hence partial sums, of one launch of the norm
 constexpr double kClipEps = 1e-6;
 
 // The tensors of one launch: P addresses each (gradient; gradient and output; w, dw, m, v).
@@ -43,32 +47,43 @@ __device__ __forceinline__ int tensor_of(const TensorTable<P>& t, int c) {
     return lo;
 }
 
-// ---- four elements at a time, aligned to their elements only ------------------------------------------------
+// ---- V elements at a time, past the caches, aligned to their elements only -------------------------------------
 typedef uint32_t u32x2h __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x4h __attribute__((ext_vector_type(4), aligned(2)));
 
 __device__ __forceinline__ uint32_t to_bits16(float v) { return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v)); }   // NaN stays NaN
 
-__device__ __forceinline__ void load4(const float* p, float (&v)[4]) {
-    const u32x4a t = *reinterpret_cast<const u32x4a*>(p);
+__device__ __forceinline__ void load_v(const float* p, float (&v)[4]) {
+    const u32x4a* q = reinterpret_cast<const u32x4a*>(p);
+    const u32x4a t = __builtin_nontemporal_load(q);
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(t[i]);
 }
-__device__ __forceinline__ void load4(const bf16_t* p, float (&v)[4]) {
-    const u32x2h t = *reinterpret_cast<const u32x2h*>(p);
+__device__ __forceinline__ void load_v(const bf16_t* p, float (&v)[4]) {
+    const u32x2h* q = reinterpret_cast<const u32x2h*>(p);
+    const u32x2h t = __builtin_nontemporal_load(q);
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = __uint_as_float((i & 1) ? (t[i >> 1] & 0xFFFF0000u) : (t[i >> 1] << 16));
 }
-__device__ __forceinline__ void store4(float* p, const float (&v)[4]) {
+__device__ __forceinline__ void load_v(const bf16_t* p, float (&v)[8]) {
+    const u32x4h* q = reinterpret_cast<const u32x4h*>(p);
+    const u32x4h t = __builtin_nontemporal_load(q);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float((i & 1) ? (t[i >> 1] & 0xFFFF0000u) : (t[i >> 1] << 16));
+}
+__device__ __forceinline__ void store_v(float* p, const float (&v)[4]) {
     u32x4a t;
 #pragma unroll
     for (int i = 0; i < 4; ++i) t[i] = __float_as_uint(v[i]);
-    *reinterpret_cast<u32x4a*>(p) = t;
+    __builtin_nontemporal_store(t, reinterpret_cast<u32x4a*>(p));
 }
-__device__ __forceinline__ void store4(bf16_t* p, const float (&v)[4]) {
-    u32x2h t;
+template <int V>
+__device__ __forceinline__ void store_v(bf16_t* p, const float (&v)[V]) {
+    typedef uint32_t words __attribute__((ext_vector_type(V / 2), aligned(2)));
+    words t;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) t[i] = to_bits16(v[2 * i]) | (to_bits16(v[2 * i + 1]) << 16);
-    *reinterpret_cast<u32x2h*>(p) = t;
+    for (int i = 0; i < V / 2; ++i) t[i] = to_bits16(v[2 * i]) | (to_bits16(v[2 * i + 1]) << 16);
+    __builtin_nontemporal_store(t, reinterpret_cast<words*>(p));
 }
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(bf16_t* p, float v) { p->bits = (uint16_t)to_bits16(v); }
@@ -79,13 +94,14 @@ __device__ __forceinline__ double wave_sum(double v) {
     for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
     return v;
 }
-// the sum over a workgroup of 256, in thread 0
+// the sum over a workgroup of W waves, in the lanes of the first
+template <int W>
 __device__ __forceinline__ double wg_sum(double v) {
-    __shared__ double s_sum[4];
+    __shared__ double s_sum[W];
     v = wave_sum(v);
     if (lane_id() == 0) s_sum[threadIdx.x >> 6] = v;
     __syncthreads();
-    return threadIdx.x == 0 ? (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]) : 0.0;
+    return threadIdx.x < 64 ? wave_sum(lane_id() < W ? s_sum[lane_id()] : 0.0) : 0.0;
 }
 
 // Squares and sums in 64 bits: no float's square overflows or vanishes there, and how elements are dealt out hardly matters. It costs one
@@ -95,17 +111,18 @@ __global__ __launch_bounds__(256) void k_norm_partial(TensorTable<1> t, double* 
     double sum = 0.0;
     for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
         const int i = tensor_of(t, c);
-        const int64_t a = (int64_t)(c - t.first[i]) * kChunk;
-        const int left = (int)(t.size[i] - a < kChunk ? t.size[i] - a : kChunk);
+        const int64_t a = (int64_t)(c - t.first[i]) * kNormChunk;
+        const int left = (int)(t.size[i] - a < kNormChunk ? t.size[i] - a : kNormChunk);
         const T* g = static_cast<const T*>(t.at[0][i]) + a;
-        if (left == kChunk) {
-            float v[4][4];
+        if (left == kNormChunk) {
+            constexpr int V = 16 / sizeof(T), U = kNormChunk / (256 * V);
+            float v[U][V];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) load4(g + 1024 * u + 4 * threadIdx.x, v[u]);
+            for (int u = 0; u < U; ++u) load_v(g + 256 * V * u + V * threadIdx.x, v[u]);
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) sum = fma((double)v[u][j], (double)v[u][j], sum);
+                for (int j = 0; j < V; ++j) sum = fma((double)v[u][j], (double)v[u][j], sum);
         } else {
             for (int e = threadIdx.x; e < left; e += 256) {
                 const double x = to_float(g[e]);
@@ -113,14 +130,20 @@ __global__ __launch_bounds__(256) void k_norm_partial(TensorTable<1> t, double* 
             }
         }
     }
-    sum = wg_sum(sum);
+    sum = wg_sum<4>(sum);
     if (threadIdx.x == 0) partial[blockIdx.x] = sum;
 }
-__global__ __launch_bounds__(256) void k_norm_final(const double* __restrict__ partial, int count, double* __restrict__ norm,
-                                                    float* __restrict__ norm_out) {
+__global__ __launch_bounds__(1024) void k_norm_final(const double* __restrict__ partial, int count, double* __restrict__ norm,
+                                                     float* __restrict__ norm_out) {
     double sum = 0.0;
-    for (int i = threadIdx.x; i < count; i += 256) sum += partial[i];
-    sum = wg_sum(sum);
+    for (int i = threadIdx.x; i < count; i += 4 * 1024) {
+        double p[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) p[u] = partial[i + 1024 * u < count ? i + 1024 * u : i];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) sum += i + 1024 * u < count ? p[u] : 0.0;
+    }
+    sum = wg_sum<16>(sum);
     if (threadIdx.x == 0) {
         const double r = sqrt(sum);
         *norm = r;
@@ -140,20 +163,21 @@ template <typename T, typename O>
 __global__ __launch_bounds__(256) void k_clip(TensorTable<2> t, const double* __restrict__ norm, double max_norm, bool in_place) {
     const double k = clip_coefficient(*norm, max_norm);
     if (in_place && k == 1.0) return;           // multiplied by one: already there
-    const int c = blockIdx.x, i = tensor_of(t, c);
-    const int64_t a = (int64_t)(c - t.first[i]) * kChunk;
-    const int left = (int)(t.size[i] - a < kChunk ? t.size[i] - a : kChunk);
+    const int c = t.chunks - 1 - blockIdx.x, i = tensor_of(t, c);       // backwards: what the norm read last may still be cached
+    const int64_t a = (int64_t)(c - t.first[i]) * kUpdateChunk;
+    const int left = (int)(t.size[i] - a < kUpdateChunk ? t.size[i] - a : kUpdateChunk);
     const T* g = static_cast<const T*>(t.at[0][i]) + a;
     O* out = static_cast<O*>(t.at[1][i]) + a;
-    if (left == kChunk) {
-        float v[4][4];
+    if (left == kUpdateChunk) {
+        constexpr int V = sizeof(T) == 2 && sizeof(O) == 2 ? 8 : 4, U = kUpdateChunk / (256 * V);
+        float v[U][V];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) load4(g + 1024 * u + 4 * threadIdx.x, v[u]);
+        for (int u = 0; u < U; ++u) load_v(g + 256 * V * u + V * threadIdx.x, v[u]);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < U; ++u) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[u][j] = (float)(k * (double)v[u][j]);
-            store4(out + 1024 * u + 4 * threadIdx.x, v[u]);
+            for (int j = 0; j < V; ++j) v[u][j] = (float)(k * (double)v[u][j]);
+            store_v(out + 256 * V * u + V * threadIdx.x, v[u]);
         }
     } else {
         for (int e = threadIdx.x; e < left; e += 256) store1(out + e, (float)(k * (double)to_float(g[e])));
@@ -178,27 +202,27 @@ __device__ __forceinline__ void adam_one(const AdamParams& p, float k, float& w,
 template <typename T>
 __global__ __launch_bounds__(256) void k_adam_list(TensorTable<4> t, const float* __restrict__ norm, double max_norm, AdamParams p) {
     const float k = norm ? (float)clip_coefficient((double)*norm, max_norm) : 1.0f;
-    const int c = blockIdx.x, i = tensor_of(t, c);
-    const int64_t a = (int64_t)(c - t.first[i]) * kChunk;
-    const int left = (int)(t.size[i] - a < kChunk ? t.size[i] - a : kChunk);
+    const int c = t.chunks - 1 - blockIdx.x, i = tensor_of(t, c);       // backwards, as k_clip
+    const int64_t a = (int64_t)(c - t.first[i]) * kUpdateChunk;
+    const int left = (int)(t.size[i] - a < kUpdateChunk ? t.size[i] - a : kUpdateChunk);
     float* w = static_cast<float*>(t.at[0][i]) + a;
     const T* dw = static_cast<const T*>(t.at[1][i]) + a;
     float* m = static_cast<float*>(t.at[2][i]) + a;
     float* v = static_cast<float*>(t.at[3][i]) + a;
-    if (left == kChunk) {
+    if (left == kUpdateChunk) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < kUpdateChunk / 1024; ++u) {
             const int e = 1024 * u + 4 * threadIdx.x;
             float x[4], g[4], y[4], z[4];
-            load4(w + e, x);
-            load4(dw + e, g);
-            load4(m + e, y);
-            load4(v + e, z);
+            load_v(w + e, x);
+            load_v(dw + e, g);
+            load_v(m + e, y);
+            load_v(v + e, z);
 #pragma unroll
             for (int j = 0; j < 4; ++j) adam_one(p, k, x[j], g[j], y[j], z[j]);
-            store4(w + e, x);
-            store4(m + e, y);
-            store4(v + e, z);
+            store_v(w + e, x);
+            store_v(m + e, y);
+            store_v(v + e, z);
         }
     } else {
         for (int e = threadIdx.x; e < left; e += 256) {
@@ -218,7 +242,7 @@ constexpr int64_t kMaxLaunchChunks = (int64_t)1 << 23;         // (a grid holds 
 
 // Calls launch(table) for the tensors of the list, an argument block at a time; empty tensors are left out.  A tensor of more chunks
 // than one launch takes goes on in the next.
-template <int P, typename Launch>
+template <int P, int kChunk, typename Launch>
 void over_list(void* const* const (&lists)[P], const size_t (&width)[P], const int64_t* counts, int32_t tensors, Launch launch) {
     TensorTable<P> t;
     t.count = t.chunks = 0;
@@ -242,7 +266,7 @@ void over_list(void* const* const (&lists)[P], const size_t (&width)[P], const i
 // Launches that over_list makes at most: some end with a full table, some with a full grid (of tensors that are cut there, each of which
 // takes a place in a second table), the last with neither.
 int64_t list_launches(int64_t tensors, int64_t elements, int per_launch) {
-    const int64_t full_grids = elements / ((kMaxLaunchChunks - per_launch) * kChunk);
+    const int64_t full_grids = elements / ((kMaxLaunchChunks - per_launch) * (int64_t)kNormChunk);
     return (tensors + full_grids) / per_launch + full_grids + 1;
 }
 
@@ -299,19 +323,20 @@ gsr_status_t list_dtype(int32_t dtype) {
 
 // workspace of the norm: the norm in 64 bits, then the partial sums
 size_t norm_workspace(int64_t tensors, int64_t elements) {
-    return 256 + sizeof(double) * kMaxPartials * (size_t)list_launches(tensors, elements, TensorTable<1>::kMax);
+    const int64_t launches = list_launches(tensors, elements, TensorTable<1>::kMax);
+    return 256 + sizeof(double) * (size_t)std::min(kMaxPartials * launches, elements / kNormChunk + tensors + launches);
 }
 
 void launch_norm(void* const* grads, const int64_t* counts, int32_t tensors, int32_t dtype, float* norm_out, void* workspace, hipStream_t s) {
     double *norm = (double*)workspace, *partial = (double*)((char*)workspace + 256);
     int made = 0;
-    over_list<1>({grads}, {dtype_size(dtype)}, counts, tensors, [&](const TensorTable<1>& t) {
+    over_list<1, kNormChunk>({grads}, {dtype_size(dtype)}, counts, tensors, [&](const TensorTable<1>& t) {
         const int wgs = std::min(t.chunks, kMaxPartials);
         if (dtype == GSR_F32) hipLaunchKernelGGL((k_norm_partial<float>), dim3(wgs), dim3(256), 0, s, t, partial + made);
         else hipLaunchKernelGGL((k_norm_partial<bf16_t>), dim3(wgs), dim3(256), 0, s, t, partial + made);
         made += wgs;
     });
-    hipLaunchKernelGGL(k_norm_final, dim3(1), dim3(256), 0, s, partial, made, norm, norm_out);
+    hipLaunchKernelGGL(k_norm_final, dim3(1), dim3(1024), 0, s, partial, made, norm, norm_out);
 }
 
 gsr_status_t check_norm_workspace(int64_t tensors, int64_t elements, const void* workspace, size_t bytes) {
@@ -367,7 +392,7 @@ gsr_status_t gsr_grad_clip(void* const* grads, const int64_t* counts, int32_t te
     launch_norm(grads, counts, tensors, dtype, norm_out, workspace, s);
     const double* norm = (const double*)workspace;
     const bool in_place = !out;
-    over_list<2>({grads, out ? out : grads}, {w, wo}, counts, tensors, [&](const TensorTable<2>& t) {
+    over_list<2, kUpdateChunk>({grads, out ? out : grads}, {w, wo}, counts, tensors, [&](const TensorTable<2>& t) {
         const dim3 grid(t.chunks), wg(256);
         if (dtype == GSR_F32 && out_dtype == GSR_F32) hipLaunchKernelGGL((k_clip<float, float>), grid, wg, 0, s, t, norm, (double)max_norm, in_place);
         else if (dtype == GSR_F32) hipLaunchKernelGGL((k_clip<float, bf16_t>), grid, wg, 0, s, t, norm, (double)max_norm, in_place);
@@ -395,7 +420,7 @@ gsr_status_t gsr_adam_update_list(float* const* w, const void* const* dw, float*
     const double c1 = 1.0 - std::pow((double)beta1, (double)t), c2 = 1.0 - std::pow((double)beta2, (double)t);
     const AdamParams p{lr, beta1, beta2, eps, weight_decay, (float)(1.0 / c1), (float)(1.0 / c2)};
     hipStream_t s = (hipStream_t)stream;
-    over_list<4>(lists, width, counts, tensors, [&](const TensorTable<4>& table) {
+    over_list<4, kUpdateChunk>(lists, width, counts, tensors, [&](const TensorTable<4>& table) {
         const dim3 grid(table.chunks), wg(256);
         if (dw_dtype == GSR_F32) hipLaunchKernelGGL((k_adam_list<float>), grid, wg, 0, s, table, norm, (double)max_norm, p);
         else hipLaunchKernelGGL((k_adam_list<bf16_t>), grid, wg, 0, s, table, norm, (double)max_norm, p);
