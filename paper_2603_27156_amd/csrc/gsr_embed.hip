@@ -141,7 +141,7 @@ constexpr int kSortWaves = 4;
 constexpr int kSortBatch = 8;        // elements that a lane has in flight
 constexpr int kSortStretch = 256 * kSortBatch;   // elements of a workgroup, or a multiple of them beyond kSortWgs workgroups
 constexpr int kSortWgs = 1024;
-constexpr int kSmallSort = 4096;     // elements that one workgroup sorts in LDS
+constexpr int kSmallSort = 4096;     // elements that one workgroup sorts in LDS, at most
 constexpr int kSmallBits = 8;
 static_assert(kSmallSort <= 16 * 64 * kSortBatch, "a wave of the small sort takes one batch");
 
@@ -288,7 +288,7 @@ __device__ __forceinline__ void wg_scan(uint32_t* v, int count, uint32_t* s_wave
     if (lane_id() == 63) s_wave[threadIdx.x >> 6] = s;
     __syncthreads();
     uint32_t at = s - sum;
-    for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) at += s_wave[w];
+    for (int w = 0; a < count && w < (int)(threadIdx.x >> 6); ++w) at += s_wave[w];
     for (int i = a; i < a + per && i < count; ++i) {
         const uint32_t c = v[i];
         v[i] = at;
@@ -353,64 +353,6 @@ __global__ __launch_bounds__(256) void k_embed_hand_out(SortSource<I> src, int64
             keys[to] = key;
             pos[to] = place;
         });
-    }
-}
-
-// Up to kSmallSort elements: workgroup 0 sorts them in LDS, digits of up to 8 bits, the others clear the gradient.
-template <typename I>
-__global__ __launch_bounds__(1024) void k_embed_sort_small(SortSource<I> ids, int n, int bits, int passes, int32_t* __restrict__ keys,
-                                                           uint32_t* __restrict__ pos, float* out, int64_t ldt, int d) {
-    constexpr int W = 16;
-    __shared__ int32_t s_key[2][kSmallSort];
-    __shared__ uint32_t s_pos[2][kSmallSort];
-    __shared__ uint32_t s_start[W << kSmallBits];
-    __shared__ uint32_t s_first[1 << kSmallBits];
-    __shared__ uint32_t s_wave[W];
-    if (blockIdx.x) {
-        clear_rows(out, ldt, ids.vocab, d, blockIdx.x - 1, gridDim.x - 1);
-        return;
-    }
-    for (int i = threadIdx.x; i < n; i += 1024) {
-        s_key[0][i] = ids.key(i);
-        s_pos[0][i] = (uint32_t)i;
-    }
-    const int digits = 1 << bits, w = threadIdx.x >> 6, per = (n + 64 * W - 1) / (64 * W) * 64;
-    const int a = w * per < n ? w * per : n, b = a + per < n ? a + per : n;
-    for (int p = 0; p < passes; ++p) {
-        const SortSource<int32_t> src{s_key[p & 1], s_pos[p & 1], ids.vocab};
-        uint32_t* start = s_start + w * digits;
-        for (int i = threadIdx.x; i < W * digits; i += 1024) s_start[i] = 0;
-        __syncthreads();
-        for (int i = a + lane_id(); i < b; i += 64) atomicAdd(&start[((uint32_t)src.key(i) >> (p * bits)) & (digits - 1)], 1u);
-        __syncthreads();
-        if ((int)threadIdx.x < digits) {
-            uint32_t sum = 0;
-            for (int v = 0; v < W; ++v) {
-                const uint32_t c = s_start[v * digits + threadIdx.x];
-                s_start[v * digits + threadIdx.x] = sum;
-                sum += c;
-            }
-            s_first[threadIdx.x] = sum;
-        }
-        __syncthreads();
-        wg_scan(s_first, digits, s_wave, W);
-        for (int i = threadIdx.x; i < W * digits; i += 1024) s_start[i] += s_first[i & (digits - 1)];
-        __syncthreads();
-        int32_t* kto = s_key[(p + 1) & 1];
-        uint32_t* pto = s_pos[(p + 1) & 1];
-        SortBatch<int32_t> batch;                // (at most 256 elements per wave: one batch)
-        if (a < b) {
-            batch.load(src, a + lane_id(), b);
-            batch.hand_out(a + lane_id(), b, p * bits, bits, start, [&](uint32_t to, int32_t key, uint32_t place) {
-                kto[to] = key;
-                pto[to] = place;
-            });
-        }
-        __syncthreads();
-    }
-    for (int i = threadIdx.x; i < n; i += 1024) {
-        keys[i] = s_key[passes & 1][i];
-        pos[i] = s_pos[passes & 1][i];
     }
 }
 
@@ -597,10 +539,194 @@ __global__ __launch_bounds__(256) void k_embed_join(const float* __restrict__ pa
     store_piece<V>(out + (int64_t)key * ldt + col, acc);
 }
 
+// ---- few rows: one launch ----------------------------------------------------------------------------------
+// Up to kSmallSort rows.  Every workgroup sorts all positions by itself in LDS (digits of up to 8 bits; the others do the same at the same
+// time), then takes the runs that begin among its kSmallSpan sorted entries, in 64 columns (16 without pieces): 64 sub-waves cut those
+// entries evenly, a run that goes on in the next sub-wave's part is joined through LDS.  Rows of the table without a token are cleared by the
+// workgroups too, each its share, unless they are too many for that (`clear`).
+constexpr int kSmallSpan = 512, kSmallSubs = 64;
+
+template <typename S, int V, typename I>
+__global__ __launch_bounds__(1024) void k_embed_small(SortSource<I> ids, int n, int bits, int passes, EmbedSums a, int clear) {
+    constexpr int W = 16, U = kSumBatch / 2, FLAGS = W << kSmallBits;
+    __shared__ int32_t s_key[2][kSmallSort];
+    __shared__ uint32_t s_pos[2][kSmallSort];
+    __shared__ uint32_t s_start[W << kSmallBits];
+    __shared__ uint32_t s_first[1 << kSmallBits];
+    __shared__ uint32_t s_wave[W];
+    __shared__ float s_part[kSmallSubs][16 * V];             // sums of runs that go on from the sub-wave before
+    __shared__ int32_t s_on[kSmallSubs + 8];                 // their tokens, or -1 (8 more: read ahead)
+    __shared__ int s_bound[3];
+    const int digits = 1 << bits, w = threadIdx.x >> 6, share = (n + 64 * W - 1) / (64 * W) * 64;
+    const int wa = w * share < n ? w * share : n, wb = wa + share < n ? wa + share : n;
+    for (int p = 0; p < passes; ++p) {
+        uint32_t* start = s_start + w * digits;
+        SortBatch<int32_t> batch;                            // (at most 256 elements per wave: one batch)
+        if (wa < wb) {
+            if (p == 0) {
+                SortBatch<I> first;
+                first.load(ids, wa + lane_id(), wb);
+#pragma unroll
+                for (int u = 0; u < kSortBatch; ++u) {
+                    batch.key[u] = first.key[u];
+                    batch.place[u] = first.place[u];
+                }
+            } else {
+                batch.load(SortSource<int32_t>{s_key[p & 1], s_pos[p & 1], ids.vocab}, wa + lane_id(), wb);
+            }
+        }
+        for (int i = threadIdx.x; i < W * digits; i += 1024) s_start[i] = 0;
+        __syncthreads();
+        if (wa < wb) {
+#pragma unroll
+            for (int u = 0; u < kSortBatch; ++u)
+                if (wa + lane_id() + 64 * u < wb) atomicAdd(&start[((uint32_t)batch.key[u] >> (p * bits)) & (digits - 1)], 1u);
+        }
+        __syncthreads();
+        if ((int)threadIdx.x < digits) {
+            uint32_t c[W], sum = 0;
+#pragma unroll
+            for (int v = 0; v < W; ++v) c[v] = s_start[v * digits + threadIdx.x];
+#pragma unroll
+            for (int v = 0; v < W; ++v) {
+                s_start[v * digits + threadIdx.x] = sum;
+                sum += c[v];
+            }
+            s_first[threadIdx.x] = sum;
+        }
+        __syncthreads();
+        wg_scan(s_first, digits, s_wave, W);
+        for (int i = threadIdx.x; i < W * digits; i += 1024) s_start[i] += s_first[i & (digits - 1)];
+        __syncthreads();
+        int32_t* kto = s_key[(p + 1) & 1];
+        uint32_t* pto = s_pos[(p + 1) & 1];
+        if (wa < wb)
+            batch.hand_out(wa + lane_id(), wb, p * bits, bits, start, [&](uint32_t to, int32_t key, uint32_t place) {
+                kto[to] = key;
+                pto[to] = place;
+            });
+        __syncthreads();
+    }
+    const int32_t* keys = s_key[passes & 1];
+    const uint32_t* rows = s_pos[passes & 1];
+    // s_bound[i] = the entries of tokens up to `key`: the thread at the border writes it
+    auto bound = [&](int i, int32_t key) {
+        for (int at = threadIdx.x; at <= n; at += 1024)
+            if ((at == 0 || keys[at - 1] <= key) && (at == n || keys[at] > key)) s_bound[i] = at;
+    };
+    bound(0, a.vocab - 1);
+    __syncthreads();
+    const int valid = s_bound[0], b = (int)blockIdx.x * kSmallSpan, e = b + kSmallSpan < valid ? b + kSmallSpan : valid;
+    int from = 0, to = 0;                                    // the runs that begin in [b, e)
+    if (b < e) {                                             // (uniform)
+        if (b) bound(1, keys[b - 1]);
+        bound(2, keys[e - 1]);
+        __syncthreads();
+        from = b ? s_bound[1] : 0;
+        to = from < e ? s_bound[2] : from;
+    }
+    const int sub = threadIdx.x >> 4, lane = threadIdx.x & 15, piece = blockIdx.y * 16 + lane;
+    const bool mine = piece < a.pieces;
+    const int q = mine ? piece : a.pieces - 1, group = q / a.pg;
+    const int in_group = (q - group * a.pg) * V, col = in_group + V <= a.dg ? in_group : a.dg - V;
+    const S* src = static_cast<const S*>(a.src) + group * a.gs + col;
+    float* out = a.out + group * a.dg + col;
+
+    const int part = (to - from + kSmallSubs - 1) / kSmallSubs, s = from + sub * part, t = s + part < to ? s + part : to;
+    float acc[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] = 0.0f;
+    int32_t cur = -1;
+    bool open = false, right = false;
+    auto store = [&]() {
+        float v[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = a.scale * acc[i];
+        if (mine) store_piece<V>(out + (int64_t)cur * a.ldt, v);
+    };
+    auto leave = [&]() {
+#pragma unroll
+        for (int i = 0; i < V; ++i) s_part[sub][lane * V + i] = acc[i];
+    };
+    if (lane == 0) s_on[sub] = -1;
+    if (threadIdx.x < 8) s_on[kSmallSubs + threadIdx.x] = -1;
+    if (s < t) {
+        open = s > from && keys[s - 1] == keys[s];
+        right = t < to && keys[t] == keys[t - 1];
+        if (open && lane == 0) s_on[sub] = keys[s];
+        for (int i0 = s; i0 < t; i0 += U) {
+            int32_t k[U];
+            Piece<S, V> p[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int at = i0 + u < t ? i0 + u : t - 1;
+                k[u] = keys[at];
+                p[u].load(src + (int64_t)rows[at] * a.ld);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (i0 + u >= t) break;
+                if (k[u] != cur) {
+                    if (cur >= 0) {
+                        if (open) leave();
+                        else store();
+                        open = false;
+                    }
+                    cur = k[u];
+#pragma unroll
+                    for (int i = 0; i < V; ++i) acc[i] = 0.0f;
+                }
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[i] += p[u].at(i);
+            }
+        }
+        if (open) leave();
+    }
+    __syncthreads();
+    if (cur >= 0 && !open) {                                 // the last run began here: what follows of it is in the next places
+        for (int j = sub + 1; right && j < kSmallSubs; j += 8) {
+            float v[8][V];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                right = right && s_on[j + x] == cur;
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[x][i] = right ? s_part[j + x < kSmallSubs ? j + x : j][lane * V + i] : 0.0f;
+            }
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[i] += v[x][i];
+        }
+        store();
+    }
+    if (!clear) return;
+    uint8_t* has = reinterpret_cast<uint8_t*>(s_start);      // whether a token occurs, FLAGS rows of the table at a time
+    const int64_t each = ((int64_t)a.vocab + gridDim.x - 1) / gridDim.x, v0 = blockIdx.x * each;
+    const int64_t v1 = v0 + each < a.vocab ? v0 + each : a.vocab;
+    for (int64_t base = v0; base < v1; base += FLAGS) {
+        const int count = v1 - base < FLAGS ? (int)(v1 - base) : FLAGS;
+        for (int i = threadIdx.x; i < count; i += 1024) has[i] = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < valid; i += 1024)
+            if (keys[i] >= base && keys[i] < base + count) has[keys[i] - base] = 1;
+        __syncthreads();
+        const float zero[V] = {};
+        for (int r = sub; r < count; r += kSmallSubs)
+            if (!has[r] && mine) store_piece<V>(out + (base + r) * a.ldt, zero);
+        __syncthreads();
+    }
+}
+__global__ __launch_bounds__(256) void k_embed_clear(float* out, int64_t ldt, int64_t vocab, int d) {
+    clear_rows(out, ldt, vocab, d, blockIdx.x, gridDim.x);
+}
+
 // ---- host side ----------------------------------------------------------------------------------------------
 namespace {
 
 constexpr int kMaxWidth = 1 << 17;
+// Elements of the table that k_embed_small clears beside its sums; a launch of its own before it costs 2.5 us (1,000 rows, 64 columns, calls of
+// 0.3 / 4 / 15 MB: 13.6 / 14.7 / 16.5 us beside the sums, 15.7 / 16.2 / 16.9 before) but has the whole chip.
+constexpr int64_t kSmallClear = 1 << 22;
 
 struct EmbedShape {             // a plane as the kernels take it: one group, or one per plane
     int64_t n, ldx, gs;
@@ -666,13 +792,16 @@ EmbedPlan embed_plan(int64_t n, int64_t vocab, int d) {
     EmbedPlan p{};
     int bits = 1;
     while (((int64_t)1 << bits) <= vocab) ++bits;           // keys are 0 .. vocab
-    p.small = n <= kSmallSort;
+    // one launch against five: 2,000 rows of 64 floats, 40 tokens 15 us / 20; 4,096 rows 24 / 20, but against eight launches, with a second pass
+    // of the sort, 24 / 36 (a call from Python: 24 / 37)
+    p.small = n <= kSmallSort / 2 || (n <= kSmallSort && bits > kDigitBits);
     const int most = p.small ? kSmallBits : kDigitBits;
     p.passes = (bits + most - 1) / most;
     p.bits = (bits + p.passes - 1) / p.passes;
     const int64_t stretches = std::max<int64_t>(1, (n + kSortStretch - 1) / kSortStretch);
     p.stretch = kSortStretch * (int)((stretches + kSortWgs - 1) / kSortWgs);
     p.wgs = (int)std::max<int64_t>(1, (n + p.stretch - 1) / p.stretch);
+    if (p.small) return p;                                  // the workspace is not used
     p.chunk = 16;
     while (p.chunk < 256 && p.chunk < (n * d) >> 20 && p.chunk < d) p.chunk *= 2;
     size_t at = 0;
@@ -703,6 +832,43 @@ EmbedPlan embed_plan(int64_t n, int64_t vocab, int d) {
     return p;
 }
 
+// workgroups of 256 that clear the gradient: up to 4,096, 16 KB or more each
+unsigned clear_wgs(int64_t vocab, int d) { return (unsigned)std::min<int64_t>(4096, (vocab * d + 4095) / 4096); }
+
+EmbedSums sums_of(const EmbedShape& s, const void* dx, int d, float scale, int64_t vocab, float* out, int64_t ldt) {
+    EmbedSums a{};
+    a.vocab = (int32_t)vocab;
+    a.scale = scale;
+    a.out = out;
+    a.ldt = ldt;
+    a.d = d;
+    a.src = dx;
+    a.ld = s.ldx;
+    a.gs = s.gs;
+    a.dg = s.dg;
+    return a;
+}
+
+template <typename S, int V, typename I>
+void launch_small(const EmbedPlan& p, const void* ids, int64_t n, EmbedSums a, hipStream_t st) {
+    a.pg = (a.dg + V - 1) / V;
+    a.pieces = a.pg * (a.d / a.dg);
+    const int slabs = (a.pieces + 15) / 16;
+    const bool clear = (int64_t)a.vocab * a.d <= kSmallClear;
+    int64_t wgs = std::max<int64_t>(1, (n + kSmallSpan - 1) / kSmallSpan);
+    if (clear) wgs = std::max(wgs, std::min<int64_t>(std::max(1, 256 / slabs), ((int64_t)a.vocab + 511) / 512));
+    else hipLaunchKernelGGL(k_embed_clear, dim3(clear_wgs(a.vocab, a.d)), dim3(256), 0, st, a.out, a.ldt, (int64_t)a.vocab, a.d);
+    const SortSource<I> src{(const I*)ids, nullptr, a.vocab};
+    hipLaunchKernelGGL((k_embed_small<S, V, I>), dim3((unsigned)wgs, slabs), dim3(1024), 0, st, src, (int)n, p.bits, p.passes, a, (int)clear);
+}
+template <typename I>
+void launch_small(const EmbedPlan& p, const void* ids, int64_t n, int32_t dtype, const EmbedSums& a, hipStream_t st) {
+    if (dtype == GSR_F32 && a.dg >= 4) launch_small<float, 4, I>(p, ids, n, a, st);
+    else if (dtype == GSR_F32) launch_small<float, 1, I>(p, ids, n, a, st);
+    else if (a.dg >= 4) launch_small<bf16_t, 4, I>(p, ids, n, a, st);
+    else launch_small<bf16_t, 1, I>(p, ids, n, a, st);
+}
+
 template <typename S, int V, bool FIRST>
 void launch_level(const EmbedPlan& p, int level, EmbedSums a, char* ws, hipStream_t st) {
     const EmbedPlan::Level& v = p.level[level];
@@ -720,23 +886,13 @@ void launch_level(const EmbedPlan& p, int level, EmbedSums a, char* ws, hipStrea
     hipLaunchKernelGGL((k_embed_sums<S, V, FIRST>), grid, dim3(256), 0, st, a);
 }
 
-void launch_sums(const EmbedPlan& p, const EmbedShape& s, const void* dx, int32_t dtype, int d, float scale, int64_t vocab, float* out, int64_t ldt,
-                 int last, char* ws, hipStream_t st) {
-    EmbedSums a{};
-    a.vocab = (int32_t)vocab;
-    a.scale = scale;
-    a.out = out;
-    a.ldt = ldt;
-    a.d = d;
-    a.src = dx;
-    a.ld = s.ldx;
-    a.gs = s.gs;
-    a.dg = s.dg;
+void launch_sums(const EmbedPlan& p, EmbedSums a, int32_t dtype, int last, char* ws, hipStream_t st) {
+    const int d = a.d;
     a.keys = (const int32_t*)(ws + p.keys[last]);
     a.pos = (const uint32_t*)(ws + p.pos[last]);
-    if (dtype == GSR_F32 && s.dg >= 4) launch_level<float, 4, true>(p, 0, a, ws, st);
+    if (dtype == GSR_F32 && a.dg >= 4) launch_level<float, 4, true>(p, 0, a, ws, st);
     else if (dtype == GSR_F32) launch_level<float, 1, true>(p, 0, a, ws, st);
-    else if (s.dg >= 8) launch_level<bf16_t, 8, true>(p, 0, a, ws, st);
+    else if (a.dg >= 8) launch_level<bf16_t, 8, true>(p, 0, a, ws, st);
     else launch_level<bf16_t, 1, true>(p, 0, a, ws, st);
     a.ld = a.dg = d;
     a.gs = 0;
@@ -751,22 +907,16 @@ void launch_sums(const EmbedPlan& p, const EmbedShape& s, const void* dx, int32_
     const float* part = (const float*)(ws + v.part);
     const int32_t* keys = (const int32_t*)(ws + v.part_keys);
     if (d >= 4)
-        hipLaunchKernelGGL((k_embed_join<4>), dim3((unsigned)v.chunks, (d + 63) / 64), dim3(256), 0, st, part, keys, (int)v.chunks, d, scale, out, ldt);
+        hipLaunchKernelGGL((k_embed_join<4>), dim3((unsigned)v.chunks, (d + 63) / 64), dim3(256), 0, st, part, keys, (int)v.chunks, d, a.scale, a.out, a.ldt);
     else
-        hipLaunchKernelGGL((k_embed_join<1>), dim3((unsigned)v.chunks, 1), dim3(256), 0, st, part, keys, (int)v.chunks, d, scale, out, ldt);
+        hipLaunchKernelGGL((k_embed_join<1>), dim3((unsigned)v.chunks, 1), dim3(256), 0, st, part, keys, (int)v.chunks, d, a.scale, a.out, a.ldt);
 }
 
 template <typename I>
 int launch_sort(const EmbedPlan& p, const void* ids, int64_t n, int64_t vocab, float* out, int64_t ldt, int d, char* ws, hipStream_t st) {
     const SortSource<I> src{(const I*)ids, nullptr, (int32_t)vocab};
-    // workgroups that clear: up to 4,096, 16 KB or more each
-    const unsigned clear = (unsigned)std::min<int64_t>(4096, (vocab * d + 4095) / 4096);
+    const unsigned clear = clear_wgs(vocab, d);
     auto at = [&](size_t o) { return ws + o; };
-    if (p.small) {
-        hipLaunchKernelGGL((k_embed_sort_small<I>), dim3(1 + clear), dim3(1024), 0, st, src, (int)n, p.bits, p.passes,
-                           (int32_t*)at(p.keys[0]), (uint32_t*)at(p.pos[0]), out, ldt, d);
-        return 0;
-    }
     uint32_t *hist = (uint32_t*)at(p.hist), *total = (uint32_t*)at(p.total);
     const int digits = 1 << p.bits;
     for (int i = 0; i < p.passes; ++i) {
@@ -836,9 +986,15 @@ gsr_status_t gsr_embed_grad(const void* ids, int32_t ids_i64, int64_t n, const v
         return fail(GSR_ERR_INVALID_ARG, "a pointer is not aligned to its elements (the workspace: to 16 bytes)");
     hipStream_t st = (hipStream_t)stream;
     char* ws = (char*)workspace;
-    const int last = ids_i64 ? launch_sort<int64_t>(p, ids, n, vocab, dtable_out, ldt, d, ws, st)
-                             : launch_sort<int32_t>(p, ids, n, vocab, dtable_out, ldt, d, ws, st);
-    if (n > 0) launch_sums(p, s, dx, dtype, d, scale, vocab, dtable_out, ldt, last, ws, st);
+    const EmbedSums a = sums_of(s, dx, d, scale, vocab, dtable_out, ldt);
+    if (p.small) {
+        if (ids_i64) launch_small<int64_t>(p, ids, n, dtype, a, st);
+        else launch_small<int32_t>(p, ids, n, dtype, a, st);
+    } else {
+        const int last = ids_i64 ? launch_sort<int64_t>(p, ids, n, vocab, dtable_out, ldt, d, ws, st)
+                                 : launch_sort<int32_t>(p, ids, n, vocab, dtable_out, ldt, d, ws, st);
+        launch_sums(p, a, dtype, last, ws, st);
+    }
     GSR_HIP_CHECK(hipGetLastError());
     return GSR_OK;
 }

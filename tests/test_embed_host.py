@@ -13,7 +13,7 @@ def lookup(table=P, vocab=10, ldt=8, table_dtype=0, ids=P, i64=0, n=4, d=8, c=2,
     return gsr.lib().gsr_embed_lookup(table, vocab, ldt, table_dtype, ids, i64, n, d, c, layout, dtype, scale, x, ldx, None)
 
 
-def grad(ids=P, i64=0, n=4, dx=P, ldx=8, d=8, c=2, layout=0, dtype=0, scale=1.0, vocab=10, out=P, ldt=8, ws=P, nbytes=1 << 20):
+def grad(ids=P, i64=0, n=5000, dx=P, ldx=8, d=8, c=2, layout=0, dtype=0, scale=1.0, vocab=10, out=P, ldt=8, ws=P, nbytes=1 << 24):
     return gsr.lib().gsr_embed_grad(ids, i64, n, dx, ldx, d, c, layout, dtype, scale, vocab, out, ldt, ws, nbytes, None)
 
 
@@ -42,11 +42,11 @@ def test_grad_refuses(change, status):
 
 def test_grad_workspace_is_monotonic_and_refuses_the_same_sizes():
     size = gsr.gsr_embed_grad_workspace
-    assert 0 < size(0, 1, 1) <= size(1, 1, 1) <= size(100_000, 1, 1) <= size(100_000, 5_000, 1) <= size(100_000, 5_000, 256)
+    assert size(0, 1, 1) == size(2048, 100, 64) == 0 < size(4097, 1, 1) <= size(100_000, 1, 1) <= size(100_000, 5_000, 1) <= size(100_000, 5_000, 256)
     assert size(1_000_000, 5_000, 256) < 1_000_000 * (20 + 256 // 8 + 2)
     for bad in ((-1, 1, 1), (2 ** 31, 1, 1), (1, 0, 1), (1, 2 ** 31 - 1, 1), (1, 1, 0), (1, 1, 131_073)):
         assert size(*bad) == 0
-    need = size(4, 10, 8)
+    need = size(5000, 10, 8)
     assert grad(nbytes=need - 1) == SMALL
 
 
