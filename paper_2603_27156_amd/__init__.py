@@ -19,6 +19,7 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 # GSR_LIB names another build of the library (kernel variants under measurement); default: the one built in-tree
 LIB_PATH = os.environ.get("GSR_LIB") or os.path.join(_HERE, "libgsr.so")
+MARSHAL_PATH = os.path.join(_HERE, "libgsr_marshal.so")     # reads lists of torch tensors for the entry points that take lists
 
 GSR_OK, GSR_ERR_INVALID_ARG, GSR_ERR_BAD_CSR, GSR_ERR_UNSUPPORTED, GSR_ERR_WORKSPACE_TOO_SMALL, GSR_ERR_HIP = range(6)
 GSR_F32, GSR_BF16 = 0, 1
@@ -380,27 +381,39 @@ def gsr_embed_grad(ids, dx, dtable_out, scale: float = 1.0, workspace=None) -> N
                                 dtable_out.data_ptr(), ldt, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
 
 
-def _addresses(tensors, dtype, counts=None) -> array:
-    """The addresses of contiguous tensors of one type on the current device, as many elements each as `counts` says."""
-    dev = _current_device()
-    for t in tensors:
-        assert t.get_device() == dev and t.dtype is dtype and t.is_contiguous()
-    assert counts is None or array("q", [t.numel() for t in tensors]) == counts, "lists of different sizes"
-    return array("Q", [t.data_ptr() for t in tensors])
+_marshal = None
+_REFUSED = ("", "a list or tuple of tensors", "a tensor", "a tensor on the current device", "a tensor of the list's type (float32, or bfloat16)",
+            "contiguous", "of the size that the other lists have there")
 
 
-def _counts(tensors) -> array:
-    return array("q", [t.numel() for t in tensors])
+def _addresses(tensors, dtype: int, counts=None):
+    """(addresses, sizes) of a list of contiguous tensors of one type on the current device; `counts`: the sizes that they must have."""
+    global _marshal
+    if _marshal is None:
+        import torch  # noqa: F401  (the helper uses its libraries)
+        if not os.path.exists(MARSHAL_PATH):
+            raise GsrError(-1, f"{MARSHAL_PATH} is missing: build it with `python -m paper_2603_27156_amd.build`")
+        f = C.PyDLL(MARSHAL_PATH).gsr_marshal_list
+        f.restype = C.c_int
+        f.argtypes = [C.py_object, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]
+        _marshal = f
+    n = len(tensors)
+    if counts is not None and len(counts) != n:
+        raise TypeError("lists of different lengths")
+    at, which = array("Q", bytes(8 * n)), array("q", (0,))
+    sizes = array("q", bytes(8 * n)) if counts is None else counts
+    why = _marshal(tensors, n, _current_device(), dtype, counts is not None, _at(at), _at(sizes), _at(which))
+    if why:
+        raise TypeError(f"tensor {which[0]} of the list is not {_REFUSED[why]}")
+    return at, sizes
 
 
 def _at(a: array) -> int:
     return a.buffer_info()[0]
 
 
-def _list_type(tensors):
-    """(torch type, library's type) of a list of gradients."""
-    import torch
-    return (tensors[0].dtype, _dtype_of(tensors[0])) if len(tensors) else (torch.float32, GSR_F32)
+def _list_type(tensors) -> int:
+    return _dtype_of(tensors[0]) if len(tensors) else GSR_F32
 
 
 def _norm_workspace(counts, workspace):
@@ -411,7 +424,7 @@ def _norm_workspace(counts, workspace):
 
 
 def gsr_grad_norm_workspace(grads) -> int:
-    counts = _counts(grads)
+    counts = array("q", [t.numel() for t in grads])
     return lib().gsr_grad_norm_workspace(_at(counts), len(counts))
 
 
@@ -425,8 +438,8 @@ def _scalar(t) -> int:
 
 def gsr_grad_norm(grads, norm_out, workspace=None) -> None:
     """norm_out (float32, one element) = the 2-norm over all elements of a list of tensors (float32, or all bfloat16)."""
-    kind, dtype = _list_type(grads)
-    counts, at = _counts(grads), _addresses(grads, kind)
+    dtype = _list_type(grads)
+    at, counts = _addresses(grads, dtype)
     ws, nb = _norm_workspace(counts, workspace)
     _check(lib().gsr_grad_norm(_at(at), _at(counts), len(counts), dtype, _scalar(norm_out), ws.data_ptr(), nb, _stream()))
 
@@ -434,12 +447,12 @@ def gsr_grad_norm(grads, norm_out, workspace=None) -> None:
 def gsr_grad_clip(grads, max_norm: float, norm_out=None, out=None, workspace=None) -> None:
     """Multiplies the tensors of a list by min(1, max_norm / (norm + 1e-6)), in place or into the tensors of `out` (of the same sizes, of
     one type); norm_out (float32, one element): the norm before clipping."""
-    kind, dtype = _list_type(grads)
-    counts, at = _counts(grads), _addresses(grads, kind)
+    dtype = _list_type(grads)
+    at, counts = _addresses(grads, dtype)
     to, out_dtype = None, dtype
     if out is not None:
-        out_kind, out_dtype = _list_type(out)
-        to = _addresses(out, out_kind, counts)
+        out_dtype = _list_type(out)
+        to, _ = _addresses(out, out_dtype, counts)
     ws, nb = _norm_workspace(counts, workspace)
     _check(lib().gsr_grad_clip(_at(at), _at(counts), len(counts), dtype, max_norm, _scalar(norm_out), None if to is None else _at(to),
                                out_dtype, ws.data_ptr(), nb, _stream()))
@@ -449,13 +462,11 @@ def gsr_adam_update_list(w, dw, m, v, t: int, lr: float, beta1: float = 0.9, bet
                          weight_decay: float = 0.0, norm=None, max_norm: float = 0.0) -> None:
     """gsr_adam_update on every tensor of four lists, dw (float32, or all bfloat16) multiplied by min(1, max_norm / (norm + 1e-6)) where
     norm, as gsr_grad_norm leaves it on the device, is given."""
-    import torch
-    kind, dtype = _list_type(dw)
-    counts = _counts(w)
-    ptrs = [_addresses(w, torch.float32), _addresses(dw, kind, counts), _addresses(m, torch.float32, counts),
-            _addresses(v, torch.float32, counts)]
-    _check(lib().gsr_adam_update_list(*map(_at, ptrs), _at(counts), len(counts), dtype, _scalar(norm), max_norm, t, lr, beta1, beta2, eps,
-                                      weight_decay, _stream()))
+    dtype = _list_type(dw)
+    aw, counts = _addresses(w, GSR_F32)
+    ag, am, av = (_addresses(x, k, counts)[0] for x, k in ((dw, dtype), (m, GSR_F32), (v, GSR_F32)))
+    _check(lib().gsr_adam_update_list(_at(aw), _at(ag), _at(am), _at(av), _at(counts), len(counts), dtype, _scalar(norm), max_norm, t, lr,
+                                      beta1, beta2, eps, weight_decay, _stream()))
 
 
 def gsr_spmm_compressed(g: Graph, vals, idx, dg: int):

@@ -1,9 +1,11 @@
-"""Builds libgsr.so (the C-ABI HIP library) in-tree with hipcc for gfx950."""
+"""Builds libgsr.so (the C-ABI HIP library) in-tree with hipcc for gfx950, and the binding's helper that reads lists of torch tensors
+(host code) with the host compiler."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -11,6 +13,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libgsr.so")
+MARSHAL = os.path.join(HERE, "libgsr_marshal.so")
 SOURCES = ["gsr_graph.hip", "gsr_ops.hip", "gsr_layer.hip", "gsr_literal.hip", "gsr_optim.hip", "gsr_embed.hip",
            "gsr_lists.hip"]
 
@@ -32,6 +35,21 @@ def _hipcc() -> str:
     return "hipcc"
 
 
+def build_marshal(verbose: bool = True) -> str:
+    """Compile gsr_marshal.cpp against the installed torch."""
+    import torch
+    from torch.utils import cpp_extension
+    includes = [*cpp_extension.include_paths(), sysconfig.get_paths()["include"]]
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *(f"-I{i}" for i in includes),
+           os.path.join(CSRC, "gsr_marshal.cpp"), "-o", MARSHAL, *(f"-L{i}" for i in cpp_extension.library_paths()),
+           "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.check_call(cmd)
+    return MARSHAL
+
+
 def build_library(verbose: bool = True) -> str:
     """Compile every HIP source for gfx950 and link libgsr.so.  Always recompiles."""
     objdir = os.path.join(HERE, "_build")
@@ -46,8 +64,10 @@ def build_library(verbose: bool = True) -> str:
         subprocess.check_call(cmd)
         return obj
 
-    with ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        marshal = ex.submit(build_marshal, verbose)
         objs = list(ex.map(compile_one, SOURCES))
+        marshal.result()
     cmd = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs]
     if verbose:
         print(" ".join(cmd), flush=True)

@@ -116,3 +116,30 @@ def test_empty_lists_and_tensors():
     assert lib.gsr_grad_norm_workspace(None, 0) > 0 and lib.gsr_grad_norm_workspace(None, -1) == 0
     a = Lists((5, -1), g=())
     assert lib.gsr_grad_norm_workspace(a.sizes, 2) == 0
+
+
+def test_lists_of_tensors_are_read_as_they_are():
+    """The binding's helper on host tensors: what it refuses, and that it does so before an address is used."""
+    torch = pytest.importorskip("torch")
+    f, counts, which = gsr_marshal(), array("q", [0, 0]), array("q", [0])
+    at = array("Q", [0, 0])
+
+    def read(tensors, n=2, dtype=0, device=-1, compare=0):
+        return f(tensors, n, device, dtype, compare, at.buffer_info()[0], counts.buffer_info()[0], which.buffer_info()[0]), which[0]
+
+    a, b = torch.zeros(4), torch.zeros(3, 2)
+    for good in ([a, b], (a, b), [torch.nn.Parameter(a), b]):
+        assert read(good) == (3, 0)                          # host tensors: not on the GPU
+    assert read([a]) == (1, 0) and read(iter([a, b])) == (1, 0) and read([1, a]) == (2, 0) and read([a.to_sparse(), a]) == (2, 0)
+    assert at == array("Q", [0, 0])
+    with pytest.raises((TypeError, RuntimeError, AssertionError)):
+        gsr.gsr_grad_norm([a, b], a)
+    assert read([], n=0) == (0, 0)
+
+
+def gsr_marshal():
+    import ctypes as C
+    f = C.PyDLL(gsr.MARSHAL_PATH).gsr_marshal_list
+    f.restype = C.c_int
+    f.argtypes = [C.py_object, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]
+    return f

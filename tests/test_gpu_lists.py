@@ -220,7 +220,13 @@ def test_binding_refuses_what_does_not_fit():
                 lambda: gsr.gsr_grad_norm([a], one, workspace=one)):
         with pytest.raises(gsr.GsrError):
             bad()
+    for bad in (lambda: gsr.gsr_grad_norm([a, 1], one), lambda: gsr.gsr_grad_norm([a, None], one), lambda: gsr.gsr_grad_norm(a, one),
+                lambda: gsr.gsr_grad_norm(iter([a]), one), lambda: gsr.gsr_grad_clip([a], 1.0, out=[b[::2]]),
+                lambda: gsr.gsr_grad_clip([a, b], 1.0, out=[b.clone()])):
+        with pytest.raises((AssertionError, TypeError)):
+            bad()
     gsr.gsr_grad_norm([a, a], one)                           # only read: a tensor may count twice
+    gsr.gsr_grad_norm((torch.nn.Parameter(a), b.view(2, 4)), one)
 
 
 # ---- a training step with all of them, as a program makes it ---------------------------------------------------------
