@@ -24,6 +24,12 @@ constexpr int kArgBytes = 4096 - 256;           // tensor table of a launch (ker
 constexpr int kNormChunk = 4096, kUpdateChunk = 2048;
 constexpr int kMaxPartials = 16384;             // workgroups, hence partial sums, of one launch of the norm
 constexpr double kClipEps = 1e-6;
+// Chunks of which one workgroup takes the norm in one launch. In a captured graph, 4 chunks 4.0 us against 5.0 with two launches, 8: 4.8 / 5.5,
+// 16: 7.1 / 5.6; a call from Python 9.5 / 12.5.
+constexpr int kSmallNorm = 8;
+// Partial sums that every workgroup of the clipping adds up by itself instead of waiting for a launch that does: 115 tensors of 25,000 (805 partial
+// sums, 1,495 workgroups) 11.7 us against 12.9 in a captured graph, 18 / 21 from Python.
+constexpr int kClipPartials = 1024;
 
 // The tensors of one launch: P addresses each (gradient; gradient and output; w, dw, m, v).
 template <int P>
@@ -107,31 +113,47 @@ __device__ __forceinline__ double wg_sum(double v) {
 // Squares and sums in 64 bits: no float's square overflows or vanishes there, and how elements are dealt out hardly matters. It costs one
 // 64-bit multiply-add per element, of which the chip does some thirty for every float that memory delivers.
 template <typename T>
-__global__ __launch_bounds__(256) void k_norm_partial(TensorTable<1> t, double* __restrict__ partial) {
+__device__ __forceinline__ double chunk_squares(const TensorTable<1>& t, int c, int thread) {     // a share of chunk c for each of 256 threads
     double sum = 0.0;
-    for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
-        const int i = tensor_of(t, c);
-        const int64_t a = (int64_t)(c - t.first[i]) * kNormChunk;
-        const int left = (int)(t.size[i] - a < kNormChunk ? t.size[i] - a : kNormChunk);
-        const T* g = static_cast<const T*>(t.at[0][i]) + a;
-        if (left == kNormChunk) {
-            constexpr int V = 16 / sizeof(T), U = kNormChunk / (256 * V);
-            float v[U][V];
+    const int i = tensor_of(t, c);
+    const int64_t a = (int64_t)(c - t.first[i]) * kNormChunk;
+    const int left = (int)(t.size[i] - a < kNormChunk ? t.size[i] - a : kNormChunk);
+    const T* g = static_cast<const T*>(t.at[0][i]) + a;
+    if (left == kNormChunk) {
+        constexpr int V = 16 / sizeof(T), U = kNormChunk / (256 * V);
+        float v[U][V];
 #pragma unroll
-            for (int u = 0; u < U; ++u) load_v(g + 256 * V * u + V * threadIdx.x, v[u]);
+        for (int u = 0; u < U; ++u) load_v(g + 256 * V * u + V * thread, v[u]);
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int j = 0; j < V; ++j) sum = fma((double)v[u][j], (double)v[u][j], sum);
-        } else {
-            for (int e = threadIdx.x; e < left; e += 256) {
-                const double x = to_float(g[e]);
-                sum = fma(x, x, sum);
-            }
+            for (int j = 0; j < V; ++j) sum = fma((double)v[u][j], (double)v[u][j], sum);
+    } else {
+        for (int e = thread; e < left; e += 256) {
+            const double x = to_float(g[e]);
+            sum = fma(x, x, sum);
         }
     }
+    return sum;
+}
+template <typename T>
+__global__ __launch_bounds__(256) void k_norm_partial(TensorTable<1> t, double* __restrict__ partial) {
+    double sum = 0.0;
+    for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) sum += chunk_squares<T>(t, c, threadIdx.x);
     sum = wg_sum<4>(sum);
     if (threadIdx.x == 0) partial[blockIdx.x] = sum;
+}
+// the whole norm of up to kSmallNorm chunks, four at a time
+template <typename T>
+__global__ __launch_bounds__(1024) void k_norm_small(TensorTable<1> t, double* __restrict__ norm, float* __restrict__ norm_out) {
+    double sum = 0.0;
+    for (int c = threadIdx.x >> 8; c < t.chunks; c += 4) sum += chunk_squares<T>(t, c, threadIdx.x & 255);
+    sum = wg_sum<16>(sum);
+    if (threadIdx.x == 0) {
+        const double r = sqrt(sum);
+        *norm = r;
+        if (norm_out) *norm_out = (float)r;
+    }
 }
 __global__ __launch_bounds__(1024) void k_norm_final(const double* __restrict__ partial, int count, double* __restrict__ norm,
                                                      float* __restrict__ norm_out) {
@@ -159,9 +181,35 @@ __device__ __forceinline__ double clip_coefficient(double norm, double max_norm)
 
 // ---- clipping ---------------------------------------------------------------------------------------------
 // The product is taken in 64 bits, so a gradient is rounded once (16-bit output: twice).
+struct ClipNorm {
+    const double* norm;         // the norm, or, with partials, the sums of squares that every workgroup adds up by itself
+    int partials;
+    float* norm_out;            // written by the first workgroup if it added them up
+    double max_norm;
+};
 template <typename T, typename O>
-__global__ __launch_bounds__(256) void k_clip(TensorTable<2> t, const double* __restrict__ norm, double max_norm, bool in_place) {
-    const double k = clip_coefficient(*norm, max_norm);
+__global__ __launch_bounds__(256) void k_clip(TensorTable<2> t, ClipNorm n, bool in_place) {
+    double norm;
+    if (n.partials) {
+        __shared__ double s_norm;
+        double sum = 0.0;
+#pragma unroll
+        for (int u = 0; u < kClipPartials / 256; ++u) {
+            const int i = threadIdx.x + 256 * u;
+            const double p = n.norm[i < n.partials ? i : 0];
+            sum += i < n.partials ? p : 0.0;
+        }
+        sum = wg_sum<4>(sum);
+        if (threadIdx.x == 0) {
+            s_norm = sqrt(sum);
+            if (n.norm_out && blockIdx.x == 0) *n.norm_out = (float)s_norm;
+        }
+        __syncthreads();
+        norm = s_norm;
+    } else {
+        norm = *n.norm;
+    }
+    const double k = clip_coefficient(norm, n.max_norm);
     if (in_place && k == 1.0) return;           // multiplied by one: already there
     const int c = t.chunks - 1 - blockIdx.x, i = tensor_of(t, c);       // backwards: what the norm read last may still be cached
     const int64_t a = (int64_t)(c - t.first[i]) * kUpdateChunk;
@@ -327,16 +375,30 @@ size_t norm_workspace(int64_t tensors, int64_t elements) {
     return 256 + sizeof(double) * (size_t)std::min(kMaxPartials * launches, elements / kNormChunk + tensors + launches);
 }
 
-void launch_norm(void* const* grads, const int64_t* counts, int32_t tensors, int32_t dtype, float* norm_out, void* workspace, hipStream_t s) {
+// Leaves the norm at workspace and at norm_out, or, if clip is given and the partial sums are few, only the partial sums: ClipNorm says which.
+ClipNorm launch_norm(void* const* grads, const int64_t* counts, int32_t tensors, int32_t dtype, float* norm_out, bool clip, void* workspace,
+                     hipStream_t s) {
     double *norm = (double*)workspace, *partial = (double*)((char*)workspace + 256);
     int made = 0;
+    bool done = false;
+    int64_t chunks = 0;
+    for (int32_t i = 0; i < tensors; ++i) chunks += (counts[i] + kNormChunk - 1) / kNormChunk;
+    const bool small = chunks <= kSmallNorm;
     over_list<1, kNormChunk>({grads}, {dtype_size(dtype)}, counts, tensors, [&](const TensorTable<1>& t) {
+        if (small) {            // (chunks are of one tensor each: no more tables than one)
+            if (dtype == GSR_F32) hipLaunchKernelGGL((k_norm_small<float>), dim3(1), dim3(1024), 0, s, t, norm, norm_out);
+            else hipLaunchKernelGGL((k_norm_small<bf16_t>), dim3(1), dim3(1024), 0, s, t, norm, norm_out);
+            done = true;
+            return;
+        }
         const int wgs = std::min(t.chunks, kMaxPartials);
         if (dtype == GSR_F32) hipLaunchKernelGGL((k_norm_partial<float>), dim3(wgs), dim3(256), 0, s, t, partial + made);
         else hipLaunchKernelGGL((k_norm_partial<bf16_t>), dim3(wgs), dim3(256), 0, s, t, partial + made);
         made += wgs;
     });
-    hipLaunchKernelGGL(k_norm_final, dim3(1), dim3(1024), 0, s, partial, made, norm, norm_out);
+    if (clip && made && made <= kClipPartials) return {partial, made, norm_out, 0.0};
+    if (!done) hipLaunchKernelGGL(k_norm_final, dim3(1), dim3(1024), 0, s, partial, made, norm, norm_out);
+    return {norm, 0, nullptr, 0.0};
 }
 
 gsr_status_t check_norm_workspace(int64_t tensors, int64_t elements, const void* workspace, size_t bytes) {
@@ -371,7 +433,7 @@ gsr_status_t gsr_grad_norm(const void* const* grads, const int64_t* counts, int3
     GSR_TRY(check_list<1>({g}, {dtype_size(dtype)}, 0, counts, tensors, &elements));
     if (!norm_out || ((uintptr_t)norm_out & 3)) return fail(GSR_ERR_INVALID_ARG, "norm_out is null or not aligned");
     GSR_TRY(check_norm_workspace(tensors, elements, workspace, workspace_bytes));
-    launch_norm(g, counts, tensors, dtype, norm_out, workspace, (hipStream_t)stream);
+    launch_norm(g, counts, tensors, dtype, norm_out, false, workspace, (hipStream_t)stream);
     GSR_HIP_CHECK(hipGetLastError());
     return GSR_OK;
 }
@@ -389,15 +451,16 @@ gsr_status_t gsr_grad_clip(void* const* grads, const int64_t* counts, int32_t te
     if ((uintptr_t)norm_out & 3) return fail(GSR_ERR_INVALID_ARG, "norm_out is not aligned");
     GSR_TRY(check_norm_workspace(tensors, elements, workspace, workspace_bytes));
     hipStream_t s = (hipStream_t)stream;
-    launch_norm(grads, counts, tensors, dtype, norm_out, workspace, s);
-    const double* norm = (const double*)workspace;
+    ClipNorm n = launch_norm(grads, counts, tensors, dtype, norm_out, true, workspace, s);
+    n.max_norm = (double)max_norm;
     const bool in_place = !out;
     over_list<2, kUpdateChunk>({grads, out ? out : grads}, {w, wo}, counts, tensors, [&](const TensorTable<2>& t) {
         const dim3 grid(t.chunks), wg(256);
-        if (dtype == GSR_F32 && out_dtype == GSR_F32) hipLaunchKernelGGL((k_clip<float, float>), grid, wg, 0, s, t, norm, (double)max_norm, in_place);
-        else if (dtype == GSR_F32) hipLaunchKernelGGL((k_clip<float, bf16_t>), grid, wg, 0, s, t, norm, (double)max_norm, in_place);
-        else if (out_dtype == GSR_F32) hipLaunchKernelGGL((k_clip<bf16_t, float>), grid, wg, 0, s, t, norm, (double)max_norm, in_place);
-        else hipLaunchKernelGGL((k_clip<bf16_t, bf16_t>), grid, wg, 0, s, t, norm, (double)max_norm, in_place);
+        if (dtype == GSR_F32 && out_dtype == GSR_F32) hipLaunchKernelGGL((k_clip<float, float>), grid, wg, 0, s, t, n, in_place);
+        else if (dtype == GSR_F32) hipLaunchKernelGGL((k_clip<float, bf16_t>), grid, wg, 0, s, t, n, in_place);
+        else if (out_dtype == GSR_F32) hipLaunchKernelGGL((k_clip<bf16_t, float>), grid, wg, 0, s, t, n, in_place);
+        else hipLaunchKernelGGL((k_clip<bf16_t, bf16_t>), grid, wg, 0, s, t, n, in_place);
+        n.norm_out = nullptr;           // written by the first launch
     });
     GSR_HIP_CHECK(hipGetLastError());
     return GSR_OK;
