@@ -85,7 +85,7 @@ def lib():
         l.gsr_grad_norm_workspace.argtypes = [p, i32]
         l.gsr_grad_norm.argtypes = [p, p, i32, i32, p, p, size, p]
         l.gsr_grad_clip.argtypes = [p, p, i32, i32, f32, p, p, i32, p, size, p]
-        l.gsr_adam_update_list.argtypes = [p, p, p, p, p, i32, i32, p, f32, i64, f32, f32, f32, f32, f32, p]
+        l.gsr_adam_update_list.argtypes = [p, p, p, p, p, i32, i32, p, f32, i64, *[C.c_double] * 5, p]
         _lib = l
     return _lib
 

@@ -234,15 +234,15 @@ __global__ __launch_bounds__(256) void k_clip(TensorTable<2> t, ClipNorm n, bool
 
 // ---- Adam -------------------------------------------------------------------------------------------------
 struct AdamParams {
-    float lr, b1, b2, eps, wd, inv_c1, inv_c2;
+    float lr, b1, b2, r1, r2, eps, wd, inv_c1, inv_c2;          // r = 1 - b, rounded once (1.0f - 0.999f is off by 1.3e-5 of itself)
 };
-// the arithmetic of k_adam, the gradient multiplied by the clipping coefficient first (by one, exactly, without clipping)
+// the arithmetic of k_adam but for r1 and r2, the gradient multiplied by the clipping coefficient first (by one, exactly, without clipping)
 __device__ __forceinline__ void adam_one(const AdamParams& p, float k, float& w, float dw, float& m, float& v) {
     const float x = w;
     const float gk = k * dw;
     const float g = gk + p.wd * x;
-    const float mi = p.b1 * m + (1.0f - p.b1) * g;
-    const float vi = p.b2 * v + (1.0f - p.b2) * g * g;
+    const float mi = p.b1 * m + p.r1 * g;
+    const float vi = p.b2 * v + p.r2 * g * g;
     m = mi;
     v = vi;
     w = x - p.lr * (mi * p.inv_c1) / (sqrtf(vi * p.inv_c2) + p.eps);
@@ -467,12 +467,12 @@ gsr_status_t gsr_grad_clip(void* const* grads, const int64_t* counts, int32_t te
 }
 
 gsr_status_t gsr_adam_update_list(float* const* w, const void* const* dw, float* const* m, float* const* v, const int64_t* counts,
-                                  int32_t tensors, int32_t dw_dtype, const float* norm, float max_norm, int64_t t, float lr, float beta1,
-                                  float beta2, float eps, float weight_decay, void* stream) {
+                                  int32_t tensors, int32_t dw_dtype, const float* norm, float max_norm, int64_t t, double lr, double beta1,
+                                  double beta2, double eps, double weight_decay, void* stream) {
     int64_t elements;
     GSR_TRY(list_dtype(dw_dtype));
     if (t < 1) return fail(GSR_ERR_INVALID_ARG, "Adam's step counter starts at 1");
-    if (!(beta1 >= 0.f && beta1 < 1.f) || !(beta2 >= 0.f && beta2 < 1.f)) return fail(GSR_ERR_INVALID_ARG, "beta outside [0,1)");
+    if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return fail(GSR_ERR_INVALID_ARG, "beta outside [0,1)");
     if (norm && (!(max_norm >= 0.0f) || std::isinf(max_norm)))
         return fail(GSR_ERR_INVALID_ARG, "max_norm=%g is negative or not finite", (double)max_norm);
     if ((uintptr_t)norm & 3) return fail(GSR_ERR_INVALID_ARG, "norm is not aligned");
@@ -480,8 +480,9 @@ gsr_status_t gsr_adam_update_list(float* const* w, const void* const* dw, float*
     const size_t width[4] = {4, dtype_size(dw_dtype), 4, 4};
     GSR_TRY(check_list<4>(lists, width, 13u, counts, tensors, &elements));
     if (elements == 0) return GSR_OK;
-    const double c1 = 1.0 - std::pow((double)beta1, (double)t), c2 = 1.0 - std::pow((double)beta2, (double)t);
-    const AdamParams p{lr, beta1, beta2, eps, weight_decay, (float)(1.0 / c1), (float)(1.0 / c2)};
+    const double c1 = 1.0 - std::pow(beta1, (double)t), c2 = 1.0 - std::pow(beta2, (double)t);
+    const AdamParams p{(float)lr, (float)beta1, (float)beta2, (float)(1.0 - beta1), (float)(1.0 - beta2), (float)eps, (float)weight_decay,
+                       (float)(1.0 / c1), (float)(1.0 / c2)};
     hipStream_t s = (hipStream_t)stream;
     over_list<4, kUpdateChunk>(lists, width, counts, tensors, [&](const TensorTable<4>& table) {
         const dim3 grid(table.chunks), wg(256);

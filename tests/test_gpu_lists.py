@@ -2,7 +2,7 @@
 
 The norm is summed in 64 bits and rounded once (2^-24; 2^-23 leaves room for the sums of 2^-53 each).  A clipped gradient is the product with a
 coefficient in 64 bits, rounded once in float32 (2^-24, subnormal results 2^-150) and, for 16 bits, again (2^-8, 2^-134).  Adam's float32
-arithmetic is bit for bit that of gsr_adam_update where nothing is clipped; where something is, the clipped gradient is rounded twice more
+arithmetic is bit for bit that of gsr_adam_update where nothing is clipped (and 1 - beta comes to the same number); where something is, the clipped gradient is rounded twice more
 (the coefficient, from a rounded norm, and the product: under 2^-22 of the gradient)."""
 import numpy as np
 import pytest
@@ -131,7 +131,8 @@ def test_clip_of_what_is_not_finite(dtype):
     assert bool(norm.isnan()) and all(bool(t.isnan().all()) for t in g)
 
 
-ADAM = dict(t=7, lr=1e-2, beta1=0.9, beta2=0.99, eps=1e-8, weight_decay=1e-2)
+ADAM = dict(t=7, lr=1e-2, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=1e-2)
+EXACT = dict(ADAM, beta1=0.875, beta2=0.96875)               # 1 - beta is a float32 whatever way it is rounded
 
 
 def adam_lists(sizes, dw_dtype, seed=0):
@@ -146,15 +147,15 @@ def test_adam_list_is_adam_on_every_tensor(sizes):
     (wb, w), (gb, g), (mb, m), (vb, v) = adam_lists(sizes, F32)
     alone = [[t.clone() for t in x] for x in (w, g, m, v)]
     guards = wb.clone(), gb.clone()
-    gsr.gsr_adam_update_list(w, g, m, v, **ADAM)
+    gsr.gsr_adam_update_list(w, g, m, v, **EXACT)
     for a, b, c, d in zip(*alone):
-        gsr.gsr_adam_update(a, b, c, d, **ADAM)
+        gsr.gsr_adam_update(a, b, c, d, **EXACT)
     for got, want in zip((w, g, m, v), alone):
         assert all(torch.equal(x, y) for x, y in zip(got, want))
     assert gaps_untouched(wb, sizes) and gaps_untouched(mb, sizes, 2) and gaps_untouched(vb, sizes, 1, 3) and torch.equal(gb, guards[1])
     # a norm that needs no clipping changes nothing either
     again = adam_lists(sizes, F32)
-    gsr.gsr_adam_update_list(*(x[1] for x in again), norm=torch.full((1,), 3.0, device=dev()), max_norm=4.0, **ADAM)
+    gsr.gsr_adam_update_list(*(x[1] for x in again), norm=torch.full((1,), 3.0, device=dev()), max_norm=4.0, **EXACT)
     assert torch.equal(again[0][0], wb) and torch.equal(again[2][0], mb) and torch.equal(again[3][0], vb)
 
 
@@ -167,12 +168,22 @@ def test_clipped_adam(sizes, dw_dtype):
     gsr.gsr_grad_norm(g, norm)
     gsr.gsr_adam_update_list(w, g, m, v, norm=norm, max_norm=0.5, **ADAM)
     c = min(1.0, 0.5 / (float(np.sqrt((g0 ** 2).sum())) + 1e-6))
-    b1, b2, lr, eps, wd = (float(np.float32(ADAM[k])) for k in ("beta1", "beta2", "lr", "eps", "weight_decay"))
+    b1, b2, lr, eps, wd = (ADAM[k] for k in ("beta1", "beta2", "lr", "eps", "weight_decay"))
     rw, rm, rv = optim.adam(w0, c * g0, m0, v0, ADAM["t"], lr, b1, b2, eps, wd)
     assert_close("w", flat(w).numpy(), rw)
     assert_close("m", flat(m).numpy(), rm)
     assert_close("v", flat(v).numpy(), rv)
     assert np.array_equal(flat(g).numpy(), g0)
+
+
+def test_first_step_with_state_of_zeros_keeps_every_digit():
+    """m and v of the first step are (1 - beta) g and (1 - beta2) g^2: three roundings each (1 - beta, and one or two products)."""
+    g = randn(5000, 4)
+    w, m, v = torch.zeros_like(g), torch.zeros_like(g), torch.zeros_like(g)
+    gsr.gsr_adam_update_list([w], [g], [m], [v], 1, 1e-3)
+    x = g.double()
+    assert bool(((m.double() - 0.1 * x).abs() <= 3 * 2.0 ** -24 * (0.1 * x).abs()).all())
+    assert bool(((v.double() - 0.001 * x * x).abs() <= 3 * 2.0 ** -24 * 0.001 * x * x).all())
 
 
 def test_captured_calls_of_two_graphs_on_one_workspace():
@@ -294,7 +305,7 @@ def test_training_step_against_the_oracle(layout):
     before = [p.double().cpu().numpy() for p in s.params]
     gsr.gsr_adam_update_list(s.params, s.grads, s.m, s.v, 1, s.lr, norm=s.norm, max_norm=s.max_norm)
     for i, p in enumerate(s.params):
-        w, m, v = optim.adam(before[i], c * got[i], 0.0, 0.0, 1, s.lr, b1=float(np.float32(0.9)), b2=float(np.float32(0.999)))
+        w, m, v = optim.adam(before[i], c * got[i], 0.0, 0.0, 1, s.lr)
         assert_close("m", s.m[i].cpu().numpy(), m)
         assert_close("v", s.v[i].cpu().numpy(), v)
         assert_close("w", p.cpu().numpy(), w)
@@ -344,7 +355,8 @@ def test_clip_then_update_is_the_clipped_update():
     a.gradients()
     gsr.gsr_grad_clip(a.grads, a.max_norm)
     for p, g, m, v in zip(a.params, a.grads, a.m, a.v):
-        gsr.gsr_adam_update(p, g, m, v, 1, a.lr)
-    b.step(1)
+        gsr.gsr_adam_update(p, g, m, v, 1, a.lr, 0.875, 0.96875)
+    b.gradients()
+    gsr.gsr_adam_update_list(b.params, b.grads, b.m, b.v, 1, b.lr, 0.875, 0.96875, norm=b.norm, max_norm=b.max_norm)
     for x, y in zip(a.m + a.v, b.m + b.v):
         assert bool(((x - y).abs() <= 2.0 ** -20 * x.abs() + 1e-30).all())
