@@ -143,31 +143,24 @@ constexpr int kSortStretch = 256 * kSortBatch;   // elements of a workgroup, or 
 constexpr int kSortWgs = 1024;
 constexpr int kSmallSort = 4096;     // elements that one workgroup sorts in LDS, at most
 constexpr int kSmallBits = 8;
-static_assert(kSmallSort <= 16 * 64 * kSortBatch, "a wave of the small sort takes one batch");
+static_assert(kSmallSort <= 16 * 64 * 4, "a wave of the small sort takes four elements a lane");
 
-// What the sort moves: (row of the table or vocab, position).  The first pass reads tokens, positions are their own numbers.
+// What the sort moves: pairs of a row of the table (or vocab) and a position.  The first pass makes them of the tokens.
+struct SortPair {
+    int32_t key;
+    uint32_t place;
+};
 template <typename I>
-struct SortSource {
+struct TokenSource {
     const I* ids;
-    const uint32_t* pos;             // nullptr: the first pass
     int32_t vocab;
-    __device__ __forceinline__ int32_t key(int64_t i) const { return token_row(ids[i], vocab); }
-    __device__ __forceinline__ uint32_t place(int64_t i) const { return pos ? pos[i] : (uint32_t)i; }
+    __device__ __forceinline__ SortPair get(int64_t i) const { return {token_row(ids[i], vocab), (uint32_t)i}; }
+};
+struct PairSource {
+    const SortPair* pairs;
+    __device__ __forceinline__ SortPair get(int64_t i) const { return pairs[i]; }
 };
 
-// lanes of the wave that hold this lane's digit (valid lanes only)
-__device__ __forceinline__ uint64_t same_digit(uint32_t digit, int bits, bool valid) {
-    uint64_t m = ballot(valid);
-    for (int b = 0; b < bits; ++b) {
-        const bool one = (digit >> b) & 1;
-        const uint64_t o = ballot(one);
-        m &= one ? o : ~o;
-    }
-    return m;
-}
-__device__ __forceinline__ int lanes_below(uint64_t m) {
-    return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
-}
 // inclusive sum over the wave
 __device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
     const int lane = lane_id();
@@ -192,32 +185,26 @@ __device__ __forceinline__ void clear_rows(float* out, int64_t ldt, int64_t voca
     }
 }
 
-// adds elements i, i + step, .. below b to the counts of their digits
-template <typename I>
-__device__ __forceinline__ void count_digits(const SortSource<I>& src, int64_t i, int64_t b, int step, int shift, uint32_t mask, uint32_t* count) {
-    for (; i < b; i += kSortBatch * step) {
-        int32_t key[kSortBatch];
-#pragma unroll
-        for (int u = 0; u < kSortBatch; ++u) key[u] = src.key(i + u * step < b ? i + u * step : b - 1);
-#pragma unroll
-        for (int u = 0; u < kSortBatch; ++u)
-            if (i + u * step < b) atomicAdd(&count[((uint32_t)key[u] >> shift) & mask], 1u);
-    }
-}
-
-template <typename I>
-__global__ __launch_bounds__(256) void k_embed_count(SortSource<I> src, int64_t n, int stretch, int wgs, int shift, int bits,
-                                                     uint32_t* __restrict__ hist, float* out, int64_t ldt, int d) {
+template <typename Src>
+__global__ __launch_bounds__(256) void k_embed_count(Src src, int64_t n, int stretch, int wgs, int shift, int bits, uint32_t* __restrict__ hist,
+                                                     float* out, int64_t ldt, int64_t vocab, int d) {
     __shared__ uint32_t s_count[1 << kDigitBits];
     if ((int)blockIdx.x >= wgs) {
-        clear_rows(out, ldt, src.vocab, d, blockIdx.x - wgs, gridDim.x - wgs);
+        clear_rows(out, ldt, vocab, d, blockIdx.x - wgs, gridDim.x - wgs);
         return;
     }
     const int digits = 1 << bits;
     for (int i = threadIdx.x; i < digits; i += 256) s_count[i] = 0;
     __syncthreads();
     const int64_t a = (int64_t)blockIdx.x * stretch, b = a + stretch < n ? a + stretch : n;
-    count_digits(src, a + threadIdx.x, b, 256, shift, digits - 1, s_count);
+    for (int64_t i = a + threadIdx.x; i < b; i += kSortBatch * 256) {
+        int32_t key[kSortBatch];
+#pragma unroll
+        for (int u = 0; u < kSortBatch; ++u) key[u] = src.get(i + u * 256 < b ? i + u * 256 : b - 1).key;
+#pragma unroll
+        for (int u = 0; u < kSortBatch; ++u)
+            if (i + u * 256 < b) atomicAdd(&s_count[((uint32_t)key[u] >> shift) & (digits - 1)], 1u);
+    }
     __syncthreads();
     for (int i = threadIdx.x; i < digits; i += 256) hist[(int64_t)i * wgs + blockIdx.x] = s_count[i];
 }
@@ -246,35 +233,52 @@ __global__ __launch_bounds__(256) void k_embed_places(uint32_t* __restrict__ his
     if (lane == 0) total[digit] = before;
 }
 
-// The elements of a wave's stretch [i - lane, b), the batch that a lane holds of them.
-template <typename I>
+// Up to 64 kSortBatch elements from i - lane on, below b: the batch that a lane holds of them.
 struct SortBatch {
-    int32_t key[kSortBatch];
-    uint32_t place[kSortBatch];
-    __device__ __forceinline__ void load(const SortSource<I>& src, int64_t i, int64_t b) {
+    SortPair e[kSortBatch];
+    template <typename Src>
+    __device__ __forceinline__ void load(const Src& src, int64_t i, int64_t b) {
 #pragma unroll
-        for (int u = 0; u < kSortBatch; ++u) {
-            const int64_t e = i + 64 * u < b ? i + 64 * u : b - 1;
-            key[u] = src.key(e);
-            place[u] = src.place(e);
-        }
+        for (int u = 0; u < kSortBatch; ++u) e[u] = src.get(i + 64 * u < b ? i + 64 * u : b - 1);
     }
-    // start[digit]: the place of the wave's next element of that digit
-    template <typename Put>
-    __device__ __forceinline__ void hand_out(int64_t i, int64_t b, int shift, int bits, uint32_t* start, Put put) const {
-        const uint32_t mask = (1u << bits) - 1;
+    __device__ __forceinline__ void count(int64_t i, int64_t b, int shift, int bits, uint32_t* counts) const {
 #pragma unroll
-        for (int u = 0; u < kSortBatch; ++u) {
+        for (int u = 0; u < kSortBatch; ++u)
+            if (i + 64 * u < b) atomicAdd(&counts[((uint32_t)e[u].key >> shift) & ((1u << bits) - 1)], 1u);
+    }
+    // start[digit]: the place of the wave's next element of that digit.  The lanes of equal digits are found for N elements of the batch side by
+    // side (one ballot per bit and element), only the counters are a chain: with 500k elements and digits of 8 bits 10.0 -> 8.3 us a launch
+    // against one element after the other.
+    template <int N>
+    __device__ __forceinline__ void hand_out(int64_t i, int64_t b, int shift, int bits, uint32_t* start, SortPair* to) const {
+        const uint32_t mask = (1u << bits) - 1;
+        uint32_t lo[N], hi[N];
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const uint64_t m = ballot(i + 64 * u < b);
+            lo[u] = (uint32_t)m;
+            hi[u] = (uint32_t)(m >> 32);
+        }
+        for (int x = 0; x < bits; ++x)
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                const bool one = ((uint32_t)e[u].key >> (shift + x)) & 1;
+                const uint64_t o = ballot(one);
+                const uint32_t flip = one ? 0u : ~0u;
+                lo[u] &= (uint32_t)o ^ flip;
+                hi[u] &= (uint32_t)(o >> 32) ^ flip;
+            }
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
             if (i - lane_id() + 64 * u >= b) break;
             const bool valid = i + 64 * u < b;
-            const uint32_t digit = ((uint32_t)key[u] >> shift) & mask;
-            const uint64_t m = same_digit(digit, bits, valid);
-            const int rank = lanes_below(m);
-            const uint32_t to = start[digit] + rank;
+            const uint32_t digit = ((uint32_t)e[u].key >> shift) & mask;
+            const int rank = __builtin_amdgcn_mbcnt_hi(hi[u], __builtin_amdgcn_mbcnt_lo(lo[u], 0));
+            const uint32_t place = start[digit] + rank;
             wave_sync();
-            if (valid && rank == 0) start[digit] = to + (uint32_t)__popcll(m);
+            if (valid && rank == 0) start[digit] = place + (uint32_t)(__popc(lo[u]) + __popc(hi[u]));
             wave_sync();
-            if (valid) put(to, key[u], place[u]);
+            if (valid) to[place] = e[u];
         }
     }
 };
@@ -297,62 +301,81 @@ __device__ __forceinline__ void wg_scan(uint32_t* v, int count, uint32_t* s_wave
     __syncthreads();
 }
 
-template <typename I>
-__global__ __launch_bounds__(256) void k_embed_hand_out(SortSource<I> src, int64_t n, int stretch, int wgs, int shift, int bits,
+// A workgroup sorts 2,048 elements at a time in LDS and writes them out in that order: elements of a digit lie side by side in both places.
+template <typename Src>
+__global__ __launch_bounds__(256) void k_embed_hand_out(Src src, int64_t n, int stretch, int wgs, int shift, int bits,
                                                         const uint32_t* __restrict__ hist, const uint32_t* __restrict__ total,
-                                                        int32_t* __restrict__ keys, uint32_t* __restrict__ pos) {
+                                                        SortPair* __restrict__ out) {
     constexpr int PER = (1 << kDigitBits) / 256;             // digits of a thread
     __shared__ uint32_t s_start[kSortWaves << kDigitBits];
-    __shared__ uint32_t s_first[1 << kDigitBits];
+    __shared__ uint32_t s_first[1 << kDigitBits];            // places: of a digit in the workgroup, then from there to memory
     __shared__ uint32_t s_wave[kSortWaves];
+    __shared__ SortPair s_pair[kSortStretch];
     const int digits = 1 << bits, w = threadIdx.x >> 6;
-    // a workgroup's stretch is a multiple of 2,048 elements: each wave's a multiple of its batch
     const int64_t a0 = (int64_t)blockIdx.x * stretch, b0 = a0 + stretch < n ? a0 + stretch : n;
-    const int64_t a = a0 + (int64_t)w * (stretch / kSortWaves) < b0 ? a0 + (int64_t)w * (stretch / kSortWaves) : b0;
-    const int64_t b = a + stretch / kSortWaves < b0 ? a + stretch / kSortWaves : b0;
     // what comes from memory is asked for at once: the first batch, the digits' totals and places
-    SortBatch<I> batch;
-    if (a < b) batch.load(src, a + lane_id(), b);
-    uint32_t tot[PER], before[PER];
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-        const int i = threadIdx.x + 256 * j < digits ? threadIdx.x + 256 * j : digits - 1;
-        if (256 * j < digits) {
-            tot[j] = total[i];
-            before[j] = hist[(int64_t)i * wgs + blockIdx.x];
-        }
-    }
-    for (int i = threadIdx.x; i < kSortWaves * digits; i += 256) s_start[i] = 0;
-#pragma unroll
-    for (int j = 0; j < PER; ++j)
-        if (threadIdx.x + 256 * j < digits) s_first[threadIdx.x + 256 * j] = tot[j];
-    __syncthreads();
-    uint32_t* start = s_start + w * digits;
-    if (a < b) {
-#pragma unroll
-        for (int u = 0; u < kSortBatch; ++u)
-            if (a + lane_id() + 64 * u < b) atomicAdd(&start[((uint32_t)batch.key[u] >> shift) & (digits - 1)], 1u);
-        count_digits(src, a + 64 * kSortBatch + lane_id(), b, 64, shift, digits - 1, start);
-    }
-    wg_scan(s_first, digits, s_wave, kSortWaves);
+    SortBatch batch;
+    const int64_t mine = a0 + w * (kSortStretch / kSortWaves) + lane_id();
+    if (a0 < b0) batch.load(src, mine, b0);
+    uint32_t next[PER];                                      // where this workgroup's next element of the thread's digits goes
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
         const int i = threadIdx.x + 256 * j;
-        if (i >= digits) break;
-        uint32_t at = s_first[i] + before[j];
-        for (int v = 0; v < kSortWaves; ++v) {
-            const uint32_t c = s_start[v * digits + i];
-            s_start[v * digits + i] = at;
-            at += c;
-        }
+        next[j] = i < digits ? hist[(int64_t)i * wgs + blockIdx.x] : 0;
+        if (i < digits) s_first[i] = total[i];
     }
     __syncthreads();
-    for (int64_t i = a + lane_id(); i - lane_id() < b; i += 64 * kSortBatch) {
-        if (i - lane_id() > a) batch.load(src, i, b);
-        batch.hand_out(i, b, shift, bits, start, [&](uint32_t to, int32_t key, uint32_t place) {
-            keys[to] = key;
-            pos[to] = place;
-        });
+    wg_scan(s_first, digits, s_wave, kSortWaves);
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+        if (threadIdx.x + 256 * j < digits) next[j] += s_first[threadIdx.x + 256 * j];
+    uint32_t* start = s_start + w * digits;
+    for (int64_t a = a0; a < b0; a += kSortStretch) {
+        const int64_t i = mine + (a - a0), end = a + kSortStretch < b0 ? a + kSortStretch : b0;
+        const int64_t b = i - lane_id() + kSortStretch / kSortWaves < end ? i - lane_id() + kSortStretch / kSortWaves : end;
+        if (a > a0) batch.load(src, i, b0);
+        for (int x = threadIdx.x; x < kSortWaves * digits; x += 256) s_start[x] = 0;
+        __syncthreads();
+        batch.count(i, b, shift, bits, start);
+        __syncthreads();
+        uint32_t c[PER][kSortWaves];
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int x = threadIdx.x + 256 * j;
+            if (x >= digits) break;
+            uint32_t sum = 0;
+#pragma unroll
+            for (int v = 0; v < kSortWaves; ++v) sum += c[j][v] = s_start[v * digits + x];
+            s_first[x] = sum;
+        }
+        __syncthreads();
+        wg_scan(s_first, digits, s_wave, kSortWaves);
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int x = threadIdx.x + 256 * j;
+            if (x >= digits) break;
+            const uint32_t first = s_first[x];
+            uint32_t at = first;
+#pragma unroll
+            for (int v = 0; v < kSortWaves; ++v) {
+                s_start[v * digits + x] = at;
+                at += c[j][v];
+            }
+            s_first[x] = next[j] - first;                    // (added modulo 2^32)
+            next[j] += at - first;
+        }
+        __syncthreads();
+        batch.hand_out<kSortBatch>(i, b, shift, bits, start, s_pair);
+        __syncthreads();
+        const int count = (int)(end - a);
+#pragma unroll
+        for (int u = 0; u < kSortBatch; ++u) {
+            const int x = threadIdx.x + 256 * u;
+            if (x >= count) break;
+            const SortPair p = s_pair[x];
+            out[x + s_first[((uint32_t)p.key >> shift) & (digits - 1)]] = p;
+        }
+        __syncthreads();
     }
 }
 
@@ -365,8 +388,8 @@ __global__ __launch_bounds__(256) void k_embed_hand_out(SortSource<I> src, int64
 struct EmbedSums {
     const void* src;            // FIRST: the plane dx; else partial rows of d floats
     int64_t ld, gs;             // row and group stride
-    const int32_t* keys;        // ascending rows of the table; FIRST: vocab and above, else negative: nothing
-    const uint32_t* pos;        // FIRST: rows of dx
+    const SortPair* pairs;      // FIRST: rows of the table, ascending (vocab: nothing), and rows of dx
+    const int32_t* keys;        // else: rows of the table, ascending (negative: nothing)
     int32_t entries, chunks;
     int chunk;                  // entries per chunk, a multiple of kSumBatch
     int d;                      // columns of a row of the table
@@ -395,11 +418,12 @@ __global__ __launch_bounds__(256) void k_embed_sums(EmbedSums a) {
         const int64_t e = e0 + i;
         int32_t key = -1, pos = 0;
         if (e < a.entries) {
-            key = a.keys[e];
             if constexpr (FIRST) {
-                pos = (int32_t)a.pos[e];
-                if (key >= a.vocab) key = -1;
+                const SortPair p = a.pairs[e];
+                key = p.key < a.vocab ? p.key : -1;
+                pos = (int32_t)p.place;
             } else {
+                key = a.keys[e];
                 pos = (int32_t)e;
             }
         }
@@ -423,8 +447,8 @@ __global__ __launch_bounds__(256) void k_embed_sums(EmbedSums a) {
     const int64_t s = c * a.chunk, e = s + a.chunk;
     const int32_t first = keys[0];
     bool left = false, right = false;           // whether the first run goes on from before, the last one beyond
-    if (first >= 0 && s > 0) left = !FIRST || a.keys[s - 1] == first;
-    if (e < a.entries) right = FIRST ? keys[a.chunk - 1] >= 0 && a.keys[e] == keys[a.chunk - 1] : a.keys[e] >= 0;
+    if (first >= 0 && s > 0) left = !FIRST || a.pairs[s - 1].key == first;
+    if (e < a.entries) right = FIRST ? keys[a.chunk - 1] >= 0 && a.pairs[e].key == keys[a.chunk - 1] : a.keys[e] >= 0;
 
     float acc[V];
     int32_t cur = -1;
@@ -547,10 +571,9 @@ __global__ __launch_bounds__(256) void k_embed_join(const float* __restrict__ pa
 constexpr int kSmallSpan = 512, kSmallSubs = 64;
 
 template <typename S, int V, typename I>
-__global__ __launch_bounds__(1024) void k_embed_small(SortSource<I> ids, int n, int bits, int passes, EmbedSums a, int clear) {
+__global__ __launch_bounds__(1024) void k_embed_small(TokenSource<I> ids, int n, int bits, int passes, EmbedSums a, int clear) {
     constexpr int W = 16, U = kSumBatch / 2, FLAGS = W << kSmallBits;
-    __shared__ int32_t s_key[2][kSmallSort];
-    __shared__ uint32_t s_pos[2][kSmallSort];
+    __shared__ SortPair s_pair[2][kSmallSort];
     __shared__ uint32_t s_start[W << kSmallBits];
     __shared__ uint32_t s_first[1 << kSmallBits];
     __shared__ uint32_t s_wave[W];
@@ -561,27 +584,14 @@ __global__ __launch_bounds__(1024) void k_embed_small(SortSource<I> ids, int n, 
     const int wa = w * share < n ? w * share : n, wb = wa + share < n ? wa + share : n;
     for (int p = 0; p < passes; ++p) {
         uint32_t* start = s_start + w * digits;
-        SortBatch<int32_t> batch;                            // (at most 256 elements per wave: one batch)
+        SortBatch batch;                                     // (at most 256 elements per wave)
         if (wa < wb) {
-            if (p == 0) {
-                SortBatch<I> first;
-                first.load(ids, wa + lane_id(), wb);
-#pragma unroll
-                for (int u = 0; u < kSortBatch; ++u) {
-                    batch.key[u] = first.key[u];
-                    batch.place[u] = first.place[u];
-                }
-            } else {
-                batch.load(SortSource<int32_t>{s_key[p & 1], s_pos[p & 1], ids.vocab}, wa + lane_id(), wb);
-            }
+            if (p == 0) batch.load(ids, wa + lane_id(), wb);
+            else batch.load(PairSource{s_pair[p & 1]}, wa + lane_id(), wb);
         }
         for (int i = threadIdx.x; i < W * digits; i += 1024) s_start[i] = 0;
         __syncthreads();
-        if (wa < wb) {
-#pragma unroll
-            for (int u = 0; u < kSortBatch; ++u)
-                if (wa + lane_id() + 64 * u < wb) atomicAdd(&start[((uint32_t)batch.key[u] >> (p * bits)) & (digits - 1)], 1u);
-        }
+        if (wa < wb) batch.count(wa + lane_id(), wb, p * bits, bits, start);
         __syncthreads();
         if ((int)threadIdx.x < digits) {
             uint32_t c[W], sum = 0;
@@ -598,29 +608,26 @@ __global__ __launch_bounds__(1024) void k_embed_small(SortSource<I> ids, int n, 
         wg_scan(s_first, digits, s_wave, W);
         for (int i = threadIdx.x; i < W * digits; i += 1024) s_start[i] += s_first[i & (digits - 1)];
         __syncthreads();
-        int32_t* kto = s_key[(p + 1) & 1];
-        uint32_t* pto = s_pos[(p + 1) & 1];
-        if (wa < wb)
-            batch.hand_out(wa + lane_id(), wb, p * bits, bits, start, [&](uint32_t to, int32_t key, uint32_t place) {
-                kto[to] = key;
-                pto[to] = place;
-            });
+        if (wa < wb) {
+            if (share <= 64) batch.hand_out<1>(wa + lane_id(), wb, p * bits, bits, start, s_pair[(p + 1) & 1]);
+            else if (share <= 128) batch.hand_out<2>(wa + lane_id(), wb, p * bits, bits, start, s_pair[(p + 1) & 1]);
+            else batch.hand_out<4>(wa + lane_id(), wb, p * bits, bits, start, s_pair[(p + 1) & 1]);
+        }
         __syncthreads();
     }
-    const int32_t* keys = s_key[passes & 1];
-    const uint32_t* rows = s_pos[passes & 1];
+    const SortPair* pairs = s_pair[passes & 1];
     // s_bound[i] = the entries of tokens up to `key`: the thread at the border writes it
     auto bound = [&](int i, int32_t key) {
         for (int at = threadIdx.x; at <= n; at += 1024)
-            if ((at == 0 || keys[at - 1] <= key) && (at == n || keys[at] > key)) s_bound[i] = at;
+            if ((at == 0 || pairs[at - 1].key <= key) && (at == n || pairs[at].key > key)) s_bound[i] = at;
     };
     bound(0, a.vocab - 1);
     __syncthreads();
     const int valid = s_bound[0], b = (int)blockIdx.x * kSmallSpan, e = b + kSmallSpan < valid ? b + kSmallSpan : valid;
     int from = 0, to = 0;                                    // the runs that begin in [b, e)
     if (b < e) {                                             // (uniform)
-        if (b) bound(1, keys[b - 1]);
-        bound(2, keys[e - 1]);
+        if (b) bound(1, pairs[b - 1].key);
+        bound(2, pairs[e - 1].key);
         __syncthreads();
         from = b ? s_bound[1] : 0;
         to = from < e ? s_bound[2] : from;
@@ -651,17 +658,17 @@ __global__ __launch_bounds__(1024) void k_embed_small(SortSource<I> ids, int n, 
     if (lane == 0) s_on[sub] = -1;
     if (threadIdx.x < 8) s_on[kSmallSubs + threadIdx.x] = -1;
     if (s < t) {
-        open = s > from && keys[s - 1] == keys[s];
-        right = t < to && keys[t] == keys[t - 1];
-        if (open && lane == 0) s_on[sub] = keys[s];
+        open = s > from && pairs[s - 1].key == pairs[s].key;
+        right = t < to && pairs[t].key == pairs[t - 1].key;
+        if (open && lane == 0) s_on[sub] = pairs[s].key;
         for (int i0 = s; i0 < t; i0 += U) {
             int32_t k[U];
             Piece<S, V> p[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int at = i0 + u < t ? i0 + u : t - 1;
-                k[u] = keys[at];
-                p[u].load(src + (int64_t)rows[at] * a.ld);
+                const SortPair e = pairs[i0 + u < t ? i0 + u : t - 1];
+                k[u] = e.key;
+                p[u].load(src + (int64_t)e.place * a.ld);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -708,7 +715,7 @@ __global__ __launch_bounds__(1024) void k_embed_small(SortSource<I> ids, int n, 
         for (int i = threadIdx.x; i < count; i += 1024) has[i] = 0;
         __syncthreads();
         for (int i = threadIdx.x; i < valid; i += 1024)
-            if (keys[i] >= base && keys[i] < base + count) has[keys[i] - base] = 1;
+            if (pairs[i].key >= base && pairs[i].key < base + count) has[pairs[i].key - base] = 1;
         __syncthreads();
         const float zero[V] = {};
         for (int r = sub; r < count; r += kSmallSubs)
@@ -783,7 +790,7 @@ struct EmbedPlan {
     bool small;
     int wgs, stretch;               // workgroups of a pass and elements of each
     int chunk;
-    size_t keys[2], pos[2], hist, total;
+    size_t pairs[2], hist, total;
     struct Level { int64_t entries, chunks; size_t part, part_keys; } level[8];
     int levels;
     size_t bytes;
@@ -811,8 +818,7 @@ EmbedPlan embed_plan(int64_t n, int64_t vocab, int d) {
         return here;
     };
     for (int i = 0; i < 2; ++i) {
-        p.keys[i] = i < p.passes ? take(4 * (size_t)n) : p.keys[0];
-        p.pos[i] = i < p.passes ? take(4 * (size_t)n) : p.pos[0];
+        p.pairs[i] = i < p.passes ? take(sizeof(SortPair) * (size_t)n) : p.pairs[0];
     }
     p.hist = take(((size_t)p.wgs << p.bits) * 4);
     p.total = take(((size_t)1 << p.bits) * 4);
@@ -858,7 +864,7 @@ void launch_small(const EmbedPlan& p, const void* ids, int64_t n, EmbedSums a, h
     int64_t wgs = std::max<int64_t>(1, (n + kSmallSpan - 1) / kSmallSpan);
     if (clear) wgs = std::max(wgs, std::min<int64_t>(std::max(1, 256 / slabs), ((int64_t)a.vocab + 511) / 512));
     else hipLaunchKernelGGL(k_embed_clear, dim3(clear_wgs(a.vocab, a.d)), dim3(256), 0, st, a.out, a.ldt, (int64_t)a.vocab, a.d);
-    const SortSource<I> src{(const I*)ids, nullptr, a.vocab};
+    const TokenSource<I> src{(const I*)ids, a.vocab};
     hipLaunchKernelGGL((k_embed_small<S, V, I>), dim3((unsigned)wgs, slabs), dim3(1024), 0, st, src, (int)n, p.bits, p.passes, a, (int)clear);
 }
 template <typename I>
@@ -888,8 +894,7 @@ void launch_level(const EmbedPlan& p, int level, EmbedSums a, char* ws, hipStrea
 
 void launch_sums(const EmbedPlan& p, EmbedSums a, int32_t dtype, int last, char* ws, hipStream_t st) {
     const int d = a.d;
-    a.keys = (const int32_t*)(ws + p.keys[last]);
-    a.pos = (const uint32_t*)(ws + p.pos[last]);
+    a.pairs = (const SortPair*)(ws + p.pairs[last]);
     if (dtype == GSR_F32 && a.dg >= 4) launch_level<float, 4, true>(p, 0, a, ws, st);
     else if (dtype == GSR_F32) launch_level<float, 1, true>(p, 0, a, ws, st);
     else if (a.dg >= 8) launch_level<bf16_t, 8, true>(p, 0, a, ws, st);
@@ -914,27 +919,28 @@ void launch_sums(const EmbedPlan& p, EmbedSums a, int32_t dtype, int last, char*
 
 template <typename I>
 int launch_sort(const EmbedPlan& p, const void* ids, int64_t n, int64_t vocab, float* out, int64_t ldt, int d, char* ws, hipStream_t st) {
-    const SortSource<I> src{(const I*)ids, nullptr, (int32_t)vocab};
+    const TokenSource<I> src{(const I*)ids, (int32_t)vocab};
     const unsigned clear = clear_wgs(vocab, d);
     auto at = [&](size_t o) { return ws + o; };
     uint32_t *hist = (uint32_t*)at(p.hist), *total = (uint32_t*)at(p.total);
     const int digits = 1 << p.bits;
     for (int i = 0; i < p.passes; ++i) {
         const int to = i & 1;
-        int32_t* keys = (int32_t*)at(p.keys[to]);
-        uint32_t* pos = (uint32_t*)at(p.pos[to]);
-        const SortSource<int32_t> again{(const int32_t*)at(p.keys[to ^ 1]), (const uint32_t*)at(p.pos[to ^ 1]), (int32_t)vocab};
+        SortPair* out_pairs = (SortPair*)at(p.pairs[to]);
+        const PairSource again{(const SortPair*)at(p.pairs[to ^ 1])};
         if (i == 0)
-            hipLaunchKernelGGL((k_embed_count<I>), dim3(p.wgs + clear), dim3(256), 0, st, src, n, p.stretch, p.wgs, 0, p.bits, hist, out, ldt, d);
+            hipLaunchKernelGGL((k_embed_count<TokenSource<I>>), dim3(p.wgs + clear), dim3(256), 0, st, src, n, p.stretch, p.wgs, 0, p.bits, hist, out,
+                               ldt, vocab, d);
         else
-            hipLaunchKernelGGL((k_embed_count<int32_t>), dim3(p.wgs), dim3(256), 0, st, again, n, p.stretch, p.wgs, i * p.bits, p.bits, hist,
-                               (float*)nullptr, ldt, d);
+            hipLaunchKernelGGL((k_embed_count<PairSource>), dim3(p.wgs), dim3(256), 0, st, again, n, p.stretch, p.wgs, i * p.bits, p.bits, hist,
+                               (float*)nullptr, ldt, vocab, d);
         hipLaunchKernelGGL(k_embed_places, dim3((digits + 3) / 4), dim3(256), 0, st, hist, p.wgs, digits, total);
         if (i == 0)
-            hipLaunchKernelGGL((k_embed_hand_out<I>), dim3(p.wgs), dim3(256), 0, st, src, n, p.stretch, p.wgs, 0, p.bits, hist, total, keys, pos);
+            hipLaunchKernelGGL((k_embed_hand_out<TokenSource<I>>), dim3(p.wgs), dim3(256), 0, st, src, n, p.stretch, p.wgs, 0, p.bits, hist, total,
+                               out_pairs);
         else
-            hipLaunchKernelGGL((k_embed_hand_out<int32_t>), dim3(p.wgs), dim3(256), 0, st, again, n, p.stretch, p.wgs, i * p.bits, p.bits, hist,
-                               total, keys, pos);
+            hipLaunchKernelGGL((k_embed_hand_out<PairSource>), dim3(p.wgs), dim3(256), 0, st, again, n, p.stretch, p.wgs, i * p.bits, p.bits, hist,
+                               total, out_pairs);
     }
     return (p.passes - 1) & 1;
 }
