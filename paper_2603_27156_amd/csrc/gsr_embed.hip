@@ -141,7 +141,7 @@ constexpr int kSortWaves = 4;
 constexpr int kSortBatch = 8;        // elements that a lane has in flight
 constexpr int kSortStretch = 256 * kSortBatch;   // elements of a workgroup, or a multiple of them beyond kSortWgs workgroups
 constexpr int kSortWgs = 1024;
-constexpr int kSmallSort = 4096;     // elements that one workgroup sorts in LDS, at most
+constexpr int kSmallSort = 4096;     // elements that one workgroup sorts in LDS
 constexpr int kSmallBits = 8;
 static_assert(kSmallSort <= 16 * 64 * 4, "a wave of the small sort takes four elements a lane");
 
@@ -692,17 +692,20 @@ __global__ __launch_bounds__(1024) void k_embed_small(TokenSource<I> ids, int n,
     __syncthreads();
     if (cur >= 0 && !open) {                                 // the last run began here: what follows of it is in the next places
         for (int j = sub + 1; right && j < kSmallSubs; j += 8) {
-            float v[8][V];
+            float v[8][V];                                   // all asked for before the first is looked at
+            int32_t on[8];
 #pragma unroll
             for (int x = 0; x < 8; ++x) {
-                right = right && s_on[j + x] == cur;
+                on[x] = s_on[j + x];
 #pragma unroll
-                for (int i = 0; i < V; ++i) v[x][i] = right ? s_part[j + x < kSmallSubs ? j + x : j][lane * V + i] : 0.0f;
+                for (int i = 0; i < V; ++i) v[x][i] = s_part[j + x < kSmallSubs ? j + x : j][lane * V + i];
             }
 #pragma unroll
-            for (int x = 0; x < 8; ++x)
+            for (int x = 0; x < 8; ++x) {
+                right = right && on[x] == cur;
 #pragma unroll
-                for (int i = 0; i < V; ++i) acc[i] += v[x][i];
+                for (int i = 0; i < V; ++i) acc[i] += right ? v[x][i] : 0.0f;
+            }
         }
         store();
     }
@@ -799,9 +802,9 @@ EmbedPlan embed_plan(int64_t n, int64_t vocab, int d) {
     EmbedPlan p{};
     int bits = 1;
     while (((int64_t)1 << bits) <= vocab) ++bits;           // keys are 0 .. vocab
-    // one launch against five: 2,000 rows of 64 floats, 40 tokens 15 us / 20; 4,096 rows 24 / 20, but against eight launches, with a second pass
-    // of the sort, 24 / 36 (a call from Python: 24 / 37)
-    p.small = n <= kSmallSort / 2 || (n <= kSmallSort && bits > kDigitBits);
+    // one launch against five or more, a call from Python: 4,096 rows of 64 floats, 40 tokens 14 us / 22, one token 23 / 22, of 256 floats,
+    // 1,000 tokens 18 / 25 (2,000 rows of 64, 40 tokens: 11 us)
+    p.small = n <= kSmallSort;
     const int most = p.small ? kSmallBits : kDigitBits;
     p.passes = (bits + most - 1) / most;
     p.bits = (bits + p.passes - 1) / p.passes;

@@ -42,7 +42,7 @@ def test_grad_refuses(change, status):
 
 def test_grad_workspace_is_monotonic_and_refuses_the_same_sizes():
     size = gsr.gsr_embed_grad_workspace
-    assert size(0, 1, 1) == size(2048, 100, 64) == 0 < size(4097, 1, 1) <= size(100_000, 1, 1) <= size(100_000, 5_000, 1) <= size(100_000, 5_000, 256)
+    assert size(0, 1, 1) == size(4096, 100, 64) == 0 < size(4097, 1, 1) <= size(100_000, 1, 1) <= size(100_000, 5_000, 1) <= size(100_000, 5_000, 256)
     assert size(1_000_000, 5_000, 256) < 1_000_000 * (20 + 256 // 8 + 2)
     for bad in ((-1, 1, 1), (2 ** 31, 1, 1), (1, 0, 1), (1, 2 ** 31 - 1, 1), (1, 1, 0), (1, 1, 131_073)):
         assert size(*bad) == 0

@@ -125,7 +125,7 @@ def test_lookup_keeps_infinities_and_nan_to_their_tokens(dtype):
     assert bool((x[[3, 5]] == 0).all())
 
 
-# sizes around what one workgroup sorts (2,048, large vocabularies 4,096) and one stretch of the sort holds (2,048), chunks of 16 to 256 rows, one, two and three passes
+# sizes around what one workgroup sorts (4,096) and one stretch of the sort holds (2,048), chunks of 16 to 256 rows, one, two and three passes
 # of the sort (vocabularies below 256 and 65,536; 2,048 and 2^22), rows narrower than, as wide as and wider than a piece and a wave
 GRADS = [
     (1, 1, 1, 0, F32, torch.int32, "one", 0, 0),
@@ -298,6 +298,6 @@ def test_binding_refuses_what_does_not_fit():
         with pytest.raises((AssertionError, TypeError)):
             bad()
     small = torch.empty(8, dtype=torch.uint8, device=dev())
-    gsr.gsr_embed_grad(ids, x, table, workspace=small)       # up to 2,048 rows need none
+    gsr.gsr_embed_grad(ids, x, table, workspace=small)       # up to 4,096 rows need none
     with pytest.raises(gsr.GsrError):
         gsr.gsr_embed_grad(ids.repeat(1025), x.repeat(1025, 1), table, workspace=small)
