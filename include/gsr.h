@@ -323,7 +323,8 @@ gsr_status_t gsr_adam_update(float* w, const float* dw, float* m, float* v, int6
  * Planes (x, dx; device, n x d of `dtype`): ROW_MAJOR with row stride ldx elements, d at least; GROUP_PLANAR in c groups of d/c columns,
  * row stride ldx, d/c at least, group stride n * ldx (ldx = d/c: what gsr_step takes).  Elements between rows are left as they are.
  * 1 <= d <= 131072, c divides d, n < 2^31, 1 <= vocab < 2^31 - 1; pointers aligned to their elements.
- * All tensors on the current device.  Calls only launch kernels and may be captured.
+ * All tensors on the current device; what a call writes overlaps nothing that it reads.  Calls only launch kernels and may be captured; calls with
+ * workspaces of their own may run side by side.
  *
  * gsr_embed_lookup: x[i, :] = scale * E[ids[i], :], rounded once to `dtype`; table and plane of either type. */
 gsr_status_t gsr_embed_lookup(const void* table, int64_t vocab, int64_t ldt, int32_t table_dtype, const void* ids, int32_t ids_i64,
@@ -333,7 +334,7 @@ gsr_status_t gsr_embed_lookup(const void* table, int64_t vocab, int64_t ldt, int
 /* gsr_embed_grad: dE[t, :] = scale * sum of dx[i, :] over the rows i with ids[i] = t.  dtable_out: device, vocab rows of d floats,
  * row stride ldt; every row is written, zeros where a token does not occur.  The positions are sorted by token and the sums taken in
  * float32 in an order that the tokens alone fix: equal calls give equal bits.  workspace: device, 16-byte aligned, at least
- * gsr_embed_grad_workspace() bytes (the same for all types and layouts, at most n (20 + d / 2) and some; 0 for up to 4,096 rows, which need none,
+ * gsr_embed_grad_workspace() bytes (the same for all types and layouts, at most n (20 + d / 2) and some; 0 for up to 4,096 rows of 2^24 values in all, which need none,
  * and for sizes that are refused); it holds nothing between calls. */
 size_t gsr_embed_grad_workspace(int64_t n, int64_t vocab, int32_t d);
 gsr_status_t gsr_embed_grad(const void* ids, int32_t ids_i64, int64_t n, const void* dx, int64_t ldx, int32_t d, int32_t c, int32_t layout,

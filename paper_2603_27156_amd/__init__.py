@@ -365,6 +365,7 @@ def gsr_embed_lookup(table, ids, x_out, scale: float = 1.0) -> None:
 
 
 def gsr_embed_grad_workspace(n: int, vocab: int, d: int) -> int:
+    """Bytes of workspace that gsr_embed_grad needs for n rows of d columns."""
     return lib().gsr_embed_grad_workspace(n, vocab, d)
 
 
@@ -377,6 +378,7 @@ def gsr_embed_grad(ids, dx, dtable_out, scale: float = 1.0, workspace=None) -> N
     assert dt == d and dtable_out.dim() == 2 and dtable_out.dtype == torch.float32
     if workspace is None:
         workspace = torch.empty(gsr_embed_grad_workspace(n, vocab, d), dtype=torch.uint8, device=dx.device)
+    assert workspace.get_device() == _current_device() and workspace.is_contiguous()
     _check(lib().gsr_embed_grad(ids.data_ptr(), _tokens(ids, n), n, dx.data_ptr(), ldx, d, c, layout, _dtype_of(dx), scale, vocab,
                                 dtable_out.data_ptr(), ldt, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
 
@@ -420,10 +422,12 @@ def _norm_workspace(counts, workspace):
     import torch
     if workspace is None:
         workspace = torch.empty(lib().gsr_grad_norm_workspace(_at(counts), len(counts)), dtype=torch.uint8, device="cuda")
+    assert workspace.get_device() == _current_device() and workspace.is_contiguous()
     return workspace, workspace.numel() * workspace.element_size()
 
 
 def gsr_grad_norm_workspace(grads) -> int:
+    """Bytes of workspace that gsr_grad_norm and gsr_grad_clip need for this list."""
     counts = array("q", [t.numel() for t in grads])
     return lib().gsr_grad_norm_workspace(_at(counts), len(counts))
 

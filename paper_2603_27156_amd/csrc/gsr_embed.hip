@@ -803,8 +803,9 @@ EmbedPlan embed_plan(int64_t n, int64_t vocab, int d) {
     int bits = 1;
     while (((int64_t)1 << bits) <= vocab) ++bits;           // keys are 0 .. vocab
     // one launch against five or more, a call from Python: 4,096 rows of 64 floats, 40 tokens 14 us / 22, one token 23 / 22, of 256 floats,
-    // 1,000 tokens 18 / 25 (2,000 rows of 64, 40 tokens: 11 us)
-    p.small = n <= kSmallSort;
+    // 1,000 tokens 18 / 25 (2,000 rows of 64, 40 tokens: 11 us).  Every 64 columns of 512 rows sort again: with 1,000 tokens 4,096 x 4,096 43 / 47,
+    // 4,096 x 8,192 84 / 70.
+    p.small = n <= kSmallSort && n * d <= (int64_t)1 << 24;
     const int most = p.small ? kSmallBits : kDigitBits;
     p.passes = (bits + most - 1) / most;
     p.bits = (bits + p.passes - 1) / p.passes;

@@ -163,6 +163,9 @@ GRADS = [
     (300_001, 1, 128, 0, F32, torch.int32, "one", 0, 0),
     (150_001, 60, 384, 2, F32, torch.int32, "mixed", 0, 0),
     (600_001, 7, 256, 4, BF16, torch.int32, "common", 0, 0),
+    (4096, 6, 8200, 0, BF16, torch.int32, "mixed", 0, 0),
+    (4096, 100, 4096, 2, F32, torch.int64, "common", 0, 0),
+    (513, 2, 12, 4, F32, torch.int32, "one", 0, 0),
 ]
 
 
@@ -284,6 +287,26 @@ def test_other_stream_and_captured_calls_that_share_a_workspace():
             torch.cuda.synchronize()
             assert torch.equal(t["x"], want[0]) and torch.equal(t["out"], want[1])
             assert torch.equal(t["x"], lookup_ref(t["table"], t["ids"], 3.0, F32))
+
+
+def test_calls_side_by_side_on_two_streams():
+    """Two threads' worth of work: calls on two streams with workspaces of their own, many in flight."""
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    jobs = []
+    for i, stream in enumerate(streams):
+        n, vocab, d = (9000, 300, 64) if i else (3000, 50, 128)
+        rng = np.random.default_rng(i)
+        ids = torch.from_numpy(make_ids("common", n, vocab, rng)).to(dev())
+        dx = torch.from_numpy(rng.integers(-8, 9, (n, d))).to(dev()).float()
+        jobs.append((stream, ids, dx, [torch.full((vocab, d), GUARD, device=dev()) for _ in range(8)], grad_ref(dx, ids, vocab, 1.0)[0]))
+    torch.cuda.synchronize()
+    for k in range(8):
+        for stream, ids, dx, outs, _ in jobs:
+            with torch.cuda.stream(stream):
+                gsr.gsr_embed_grad(ids, dx, outs[k])
+    torch.cuda.synchronize()
+    for _, _, _, outs, want in jobs:
+        assert all(torch.equal(o.double().cpu(), want) for o in outs)
 
 
 def test_binding_refuses_what_does_not_fit():
