@@ -132,11 +132,13 @@ __global__ __launch_bounds__(256) void k_embed_lookup(const TT* __restrict__ tab
 }
 
 // ---- positions sorted by token ----------------------------------------------------------------------------
-// A stable counting sort, so that the sums are taken in an order that the tokens alone fix.  Digits of up to 11 bits: tokens of a
-// vocabulary below 2,048 take one pass, below 4M two.  A pass is three launches: every workgroup counts the digits of its
-// stretch; a wave per digit turns the counts into places; every workgroup hands its elements out.  Within a workgroup each
-// wave owns a stretch and takes it 64 elements at a time; lanes of equal digits find their order from one ballot per bit.
-constexpr int kDigitBits = 11;
+// A stable counting sort, so that the sums are taken in an order that the tokens alone fix.  A pass is three launches: every workgroup counts
+// the digits of its stretch; a wave per digit turns the counts into places; every workgroup hands its elements out.  Within a workgroup each
+// wave owns a stretch; lanes of equal digits find their order from one ballot per bit.  Bound by its launches and the round trips in them: 500k
+// elements and digits of 8 bits take 5 + 5 + 8 us a pass, for 12 MB.
+// Digits of up to 10 bits (vocabularies below 1,024: one pass, below 2^20: two).  Whole gradient of 32 columns, at most 8 / 9 / 10 / 11 bits: 1M rows,
+// 900 tokens 78 / 78 / 69 / 70 us, 2,000 tokens 79 / 80 / 80 / 80; 4M rows, 300 tokens 185 / 155 / 155 / 163, 200k tokens 236 / 218 / 219 / 231.
+constexpr int kDigitBits = 10;
 constexpr int kSortWaves = 4;
 constexpr int kSortBatch = 8;        // elements that a lane has in flight
 constexpr int kSortStretch = 256 * kSortBatch;   // elements of a workgroup, or a multiple of them beyond kSortWgs workgroups
@@ -400,8 +402,13 @@ __global__ __launch_bounds__(256) void k_embed_hand_out(Src src, int64_t n, int 
 // The sorted list is cut into chunks of equal length, one per sub-wave of as many lanes as a row has pieces (up to 64), so that a
 // token of a million rows and a million tokens of one row cost the same.  A run of equal tokens that lies in one chunk is stored as it
 // is; of a run that goes on beyond its chunk the sum is left in one of the chunk's two places of a list of partial rows (0: the run goes
-// on from the chunk before, 1: it begins here), whose tokens are ascending again.  The same kernel shortens that list 32-fold at a time, and
+// on from the chunk before, 1: it begins here), whose tokens are ascending again.  The same kernel shortens that list 16-fold at a time, and
 // where few chunks are left, k_embed_join adds up each run that began in one of them.
+//
+// Bound by the reads of dx.  Those are streamed past the caches (1M rows of 256 floats, chunks of 64: 235 -> 212 us for the whole gradient), and
+// chunks are long, so that about 4,096 waves read ascending rows each: 64 / 128 / 256 rows a chunk 212 / 200 / 190 us.  With 97 tokens the sums of
+// those rows take 158 us (6.5 TB/s, what a read loop reaches here), with 50k tokens 200 (the table's 51 MB are written twice: cleared, then
+// stored); 500k rows of 256 16-bit values with 50k tokens 63 us for 290 MB.
 struct EmbedSums {
     const void* src;            // FIRST: the plane dx; else partial rows of d floats
     int64_t ld, gs;             // row and group stride
@@ -421,7 +428,7 @@ struct EmbedSums {
 };
 constexpr int kSumBatch = 16, kSumLanesMin = 3;                        // (lanes per chunk as a logarithm)
 constexpr int kSumEntries = 2048;                                      // of a workgroup, at most
-constexpr int kPartChunk = 32;                                         // partial rows per chunk
+constexpr int kPartChunk = 32;                                         // partial rows per chunk (64: 12.6 us a level, 32: 5.7)
 constexpr int kJoinChunks = 1024;                                      // chunks from which k_embed_join takes over
 
 template <typename S, int V, bool FIRST>
@@ -534,7 +541,8 @@ __global__ __launch_bounds__(256) void k_embed_sums(EmbedSums a) {
 }
 
 // Partial rows of `chunks` chunks: workgroup (i, j) adds up the run that began in chunk i, if one did, in columns 16 V j to 16 V (j + 1): the place
-// where it begins and the first places of the chunks after it that carry on its token.  Sixteen lanes take a row, sixteen rows side by side.
+// where it begins and the first places of the chunks after it that carry on its token.  Sixteen lanes take a row, sixteen rows side by side, eight of
+// each in flight: 4.7 us for 245 chunks of 1M rows, and two levels of k_embed_sums (20 us) less.
 template <int V>
 __global__ __launch_bounds__(256) void k_embed_join(const float* __restrict__ part, const int32_t* __restrict__ keys, int chunks, int d,
                                                     float scale, float* __restrict__ out, int64_t ldt) {

@@ -126,7 +126,7 @@ def test_lookup_keeps_infinities_and_nan_to_their_tokens(dtype):
 
 
 # sizes around what one workgroup sorts (4,096) and one stretch of the sort holds (2,048), chunks of 16 to 256 rows, one, two and three passes
-# of the sort (vocabularies below 256 and 65,536; 2,048 and 2^22), rows narrower than, as wide as and wider than a piece and a wave
+# of the sort (vocabularies below 256 and 65,536; 1,024 and 2^20), rows narrower than, as wide as and wider than a piece and a wave
 GRADS = [
     (1, 1, 1, 0, F32, torch.int32, "one", 0, 0),
     (1, 3, 64, 2, BF16, torch.int64, "mixed", 0, 0),
@@ -144,7 +144,10 @@ GRADS = [
     (4095, 65_535, 20, 0, BF16, torch.int64, "distinct", 4, 2),
     (4096, 70_000, 33, 0, BF16, torch.int32, "mixed", 1, 1),
     (4096, 17_000_000, 2, 0, F32, torch.int32, "mixed", 0, 0),
-    (4097, 2047, 256, 8, BF16, torch.int32, "common", 0, 0),
+    (4097, 1023, 256, 8, BF16, torch.int32, "common", 0, 0),
+    (5000, 1024, 40, 0, F32, torch.int32, "distinct", 0, 0),
+    (70_001, 1_048_576, 8, 0, F32, torch.int32, "common", 0, 0),
+    (66_000, 511, 24, 0, F32, torch.int32, "mixed", 0, 0),
     (4097, 1, 1, 0, BF16, torch.int32, "one", 0, 0),
     (20_011, 2048, 128, 2, F32, torch.int64, "mixed", 0, 0),
     (65_536, 97, 64, 0, BF16, torch.int32, "common", 0, 0),
