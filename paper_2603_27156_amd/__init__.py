@@ -330,15 +330,16 @@ def gsr_adam_update(w, dw, m, v, t: int, lr: float, beta1: float = 0.9, beta2: f
                                  C.c_float(beta1), C.c_float(beta2), C.c_float(eps), C.c_float(weight_decay), _stream()))
 
 
-def _plane(x):
-    """(rows, D, groups, layout, row stride) of a plane [n, D] (rows may be strided) or [C, n, D/C]."""
-    assert x.is_cuda and x.device.index == _current_device() and x.dim() in (2, 3) and (x.stride(-1) == 1 or x.shape[-1] == 1)
-    if x.dim() == 2:
-        n, d = x.shape
-        return n, d, 1, GSR_LAYOUT_ROW_MAJOR, x.stride(0) if n > 1 else d
-    c, n, dg = x.shape
-    ld = x.stride(1) if n > 1 else x.stride(0) if n and c > 1 else dg
-    assert c == 1 or n == 0 or x.stride(0) == n * ld, "the groups of a plane follow each other"
+def _plane(x, dev: int):
+    """(rows, D, groups, layout, row stride) of a plane [n, D] (rows may be strided) or [C, n, D/C] on GPU `dev`."""
+    shape, strides = x.shape, x.stride()
+    assert x.get_device() == dev and (strides[-1] == 1 or shape[-1] == 1)
+    if len(shape) == 2:
+        n, d = shape
+        return n, d, 1, GSR_LAYOUT_ROW_MAJOR, strides[0] if n > 1 else d
+    c, n, dg = shape
+    ld = strides[1] if n > 1 else strides[0] if n and c > 1 else dg
+    assert c == 1 or n == 0 or strides[0] == n * ld, "the groups of a plane follow each other"
     return n, c * dg, c, GSR_LAYOUT_GROUP_PLANAR, ld
 
 
@@ -347,20 +348,22 @@ def _current_device() -> int:
     return torch.cuda.current_device()
 
 
-def _tokens(ids, n: int) -> int:
+def _tokens(ids, n: int, dev: int) -> int:
     import torch
-    assert ids.device.index == _current_device() and ids.is_cuda and ids.is_contiguous() and ids.dim() == 1 and len(ids) == n
-    assert ids.dtype in (torch.int32, torch.int64)
-    return 1 if ids.dtype == torch.int64 else 0
+    assert ids.get_device() == dev and ids.shape == (n,) and ids.is_contiguous()
+    dtype = ids.dtype
+    assert dtype == torch.int32 or dtype == torch.int64
+    return 1 if dtype == torch.int64 else 0
 
 
 def gsr_embed_lookup(table, ids, x_out, scale: float = 1.0) -> None:
     """x_out[i] = scale * table[ids[i]], zeros where a token lies outside the table.  table: [vocab, D], rows may be strided; x_out: a
     plane [n, D] or [C, n, D/C]; either of both float32 or bfloat16.  ids: [n] int32 or int64."""
-    n, d, c, layout, ldx = _plane(x_out)
-    vocab, dt, _, _, ldt = _plane(table)
-    assert dt == d and table.dim() == 2
-    _check(lib().gsr_embed_lookup(table.data_ptr(), vocab, ldt, _dtype_of(table), ids.data_ptr(), _tokens(ids, n), n, d, c, layout,
+    dev = _current_device()
+    n, d, c, layout, ldx = _plane(x_out, dev)
+    vocab, dt, _, rows, ldt = _plane(table, dev)
+    assert dt == d and rows == GSR_LAYOUT_ROW_MAJOR
+    _check(lib().gsr_embed_lookup(table.data_ptr(), vocab, ldt, _dtype_of(table), ids.data_ptr(), _tokens(ids, n, dev), n, d, c, layout,
                                   _dtype_of(x_out), scale, x_out.data_ptr(), ldx, _stream()))
 
 
@@ -373,13 +376,14 @@ def gsr_embed_grad(ids, dx, dtable_out, scale: float = 1.0, workspace=None) -> N
     """dtable_out[t] = scale * sum of dx[i] over ids[i] == t (float32 [vocab, D], rows may be strided; written whole).  dx: a plane as
     gsr_embed_lookup's x_out; workspace: device tensor of gsr_embed_grad_workspace(n, vocab, D) bytes, or None."""
     import torch
-    n, d, c, layout, ldx = _plane(dx)
-    vocab, dt, _, _, ldt = _plane(dtable_out)
-    assert dt == d and dtable_out.dim() == 2 and dtable_out.dtype == torch.float32
+    dev = _current_device()
+    n, d, c, layout, ldx = _plane(dx, dev)
+    vocab, dt, _, rows, ldt = _plane(dtable_out, dev)
+    assert dt == d and rows == GSR_LAYOUT_ROW_MAJOR and dtable_out.dtype == torch.float32
     if workspace is None:
         workspace = torch.empty(gsr_embed_grad_workspace(n, vocab, d), dtype=torch.uint8, device=dx.device)
-    assert workspace.get_device() == _current_device() and workspace.is_contiguous()
-    _check(lib().gsr_embed_grad(ids.data_ptr(), _tokens(ids, n), n, dx.data_ptr(), ldx, d, c, layout, _dtype_of(dx), scale, vocab,
+    assert workspace.get_device() == dev and workspace.is_contiguous()
+    _check(lib().gsr_embed_grad(ids.data_ptr(), _tokens(ids, n, dev), n, dx.data_ptr(), ldx, d, c, layout, _dtype_of(dx), scale, vocab,
                                 dtable_out.data_ptr(), ldt, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
 
 
