@@ -18,9 +18,10 @@ namespace gsr {
 
 constexpr int kArgBytes = 4096 - 256;           // tensor table of a launch (kernel arguments: 4 KB)
 // Elements that a workgroup takes at a time.  Every kernel here is bound by memory, reads and writes past the caches, and was timed with 2,048 to
-// 16,384: norm of 400M 16-bit values (up to 16,384 workgroups, several chunks each) 152 us at 16,384, 139 at 8,192, 130 at 4,096 (6.2 TB/s),
+// 16,384: norm of 400M 16-bit values (up to 16,384 workgroups, several chunks each) 152 us at 16,384, 139 at 8,192, 130 at 4,096,
 // 175 at 2,048; clipping 201M floats (one chunk per workgroup) 472, 426, 412, 402 us at 2,048; clipped Adam on 120M weights with 16-bit
-// gradients 706, 662, 617, 593 us (5.3 TB/s, the norm before it included).  With cached accesses at 8,192: 161, 488 and 726 us.
+// gradients 706, 662, 617, 593 us.  With cached accesses at 8,192: 161, 488 and 726 us.  A tensor found in one round trip (tensor_of):
+// 126 (6.4 TB/s, the rate of a read loop), 397 (two passes over the gradients: 6.1 TB/s) and 586 us (5.7, the norm before it included).
 constexpr int kNormChunk = 4096, kUpdateChunk = 2048;
 constexpr int kMaxPartials = 16384;             // workgroups, hence partial sums, of one launch of the norm
 constexpr double kClipEps = 1e-6;
@@ -41,16 +42,20 @@ struct TensorTable {
     int32_t first[kMax];                        // chunks of the tensors before
 };
 
-// the tensor that chunk c belongs to
+// The tensor that chunk c (the same for a wave) belongs to: the last that begins at or before it, counted by the wave's lanes in one round trip to the
+// table (a search takes eight, one after the other).
 template <int P>
 __device__ __forceinline__ int tensor_of(const TensorTable<P>& t, int c) {
-    int lo = 0, hi = t.count;                   // first[lo] <= c < first[hi]
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (t.first[mid] <= c) lo = mid;
-        else hi = mid;
+    constexpr int ROUNDS = (TensorTable<P>::kMax + 63) / 64;
+    int first[ROUNDS], before = 0;
+#pragma unroll
+    for (int u = 0; u < ROUNDS; ++u) {
+        const int i = lane_id() + 64 * u;
+        first[u] = t.first[i < TensorTable<P>::kMax ? i : 0];
     }
-    return lo;
+#pragma unroll
+    for (int u = 0; u < ROUNDS; ++u) before += __popcll(ballot(lane_id() + 64 * u < t.count && first[u] <= c));
+    return __builtin_amdgcn_readfirstlane(before - 1);
 }
 
 // ---- V elements at a time, past the caches, aligned to their elements only -------------------------------------
@@ -157,13 +162,14 @@ __global__ __launch_bounds__(1024) void k_norm_small(TensorTable<1> t, double* _
 }
 __global__ __launch_bounds__(1024) void k_norm_final(const double* __restrict__ partial, int count, double* __restrict__ norm,
                                                      float* __restrict__ norm_out) {
+    constexpr int U = 4;                        // (16: 3.4 us instead of 2.2 for 800 partial sums, no less for 30,000)
     double sum = 0.0;
-    for (int i = threadIdx.x; i < count; i += 4 * 1024) {
-        double p[4];
+    for (int i = threadIdx.x; i < count; i += U * 1024) {
+        double p[U];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) p[u] = partial[i + 1024 * u < count ? i + 1024 * u : i];
+        for (int u = 0; u < U; ++u) p[u] = partial[i + 1024 * u < count ? i + 1024 * u : i];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) sum += i + 1024 * u < count ? p[u] : 0.0;
+        for (int u = 0; u < U; ++u) sum += i + 1024 * u < count ? p[u] : 0.0;
     }
     sum = wg_sum<16>(sum);
     if (threadIdx.x == 0) {
