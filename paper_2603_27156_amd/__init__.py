@@ -392,8 +392,8 @@ _REFUSED = ("", "a list or tuple of tensors", "a tensor", "a tensor on the curre
             "contiguous", "of the size that the other lists have there")
 
 
-def _addresses(tensors, dtype: int, counts=None):
-    """(addresses, sizes) of a list of contiguous tensors of one type on the current device; `counts`: the sizes that they must have."""
+def _marshal_list():
+    """The helper that reads lists of tensors.  Raises if it has not been built."""
     global _marshal
     if _marshal is None:
         import torch  # noqa: F401  (the helper uses its libraries)
@@ -403,12 +403,17 @@ def _addresses(tensors, dtype: int, counts=None):
         f.restype = C.c_int
         f.argtypes = [C.py_object, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]
         _marshal = f
+    return _marshal
+
+
+def _addresses(tensors, dtype: int, dev: int, counts=None):
+    """(addresses, sizes) of a list of contiguous tensors of one type on GPU `dev`; `counts`: the sizes that they must have."""
     n = len(tensors)
     if counts is not None and len(counts) != n:
         raise TypeError("lists of different lengths")
     at, which = array("Q", bytes(8 * n)), array("q", (0,))
     sizes = array("q", bytes(8 * n)) if counts is None else counts
-    why = _marshal(tensors, n, _current_device(), dtype, counts is not None, _at(at), _at(sizes), _at(which))
+    why = _marshal_list()(tensors, n, dev, dtype, counts is not None, _at(at), _at(sizes), _at(which))
     if why:
         raise TypeError(f"tensor {which[0]} of the list is not {_REFUSED[why]}")
     return at, sizes
@@ -422,11 +427,12 @@ def _list_type(tensors) -> int:
     return _dtype_of(tensors[0]) if len(tensors) else GSR_F32
 
 
-def _norm_workspace(counts, workspace):
-    import torch
+def _norm_workspace(counts, workspace, dev: int):
     if workspace is None:
-        workspace = torch.empty(lib().gsr_grad_norm_workspace(_at(counts), len(counts)), dtype=torch.uint8, device="cuda")
-    assert workspace.get_device() == _current_device() and workspace.is_contiguous()
+        import torch
+        nbytes = lib().gsr_grad_norm_workspace(_at(counts), len(counts))
+        return torch.empty(nbytes, dtype=torch.uint8, device="cuda"), nbytes
+    assert workspace.get_device() == dev and workspace.is_contiguous()
     return workspace, workspace.numel() * workspace.element_size()
 
 
@@ -436,33 +442,33 @@ def gsr_grad_norm_workspace(grads) -> int:
     return lib().gsr_grad_norm_workspace(_at(counts), len(counts))
 
 
-def _scalar(t) -> int:
+def _scalar(t, dev: int) -> int:
     import torch
     if t is None:
         return 0
-    assert t.get_device() == _current_device() and t.dtype == torch.float32 and t.numel() == 1
+    assert t.get_device() == dev and t.dtype == torch.float32 and t.numel() == 1
     return t.data_ptr()
 
 
 def gsr_grad_norm(grads, norm_out, workspace=None) -> None:
     """norm_out (float32, one element) = the 2-norm over all elements of a list of tensors (float32, or all bfloat16)."""
-    dtype = _list_type(grads)
-    at, counts = _addresses(grads, dtype)
-    ws, nb = _norm_workspace(counts, workspace)
-    _check(lib().gsr_grad_norm(_at(at), _at(counts), len(counts), dtype, _scalar(norm_out), ws.data_ptr(), nb, _stream()))
+    dev, dtype = _current_device(), _list_type(grads)
+    at, counts = _addresses(grads, dtype, dev)
+    ws, nb = _norm_workspace(counts, workspace, dev)
+    _check(lib().gsr_grad_norm(_at(at), _at(counts), len(counts), dtype, _scalar(norm_out, dev), ws.data_ptr(), nb, _stream()))
 
 
 def gsr_grad_clip(grads, max_norm: float, norm_out=None, out=None, workspace=None) -> None:
     """Multiplies the tensors of a list by min(1, max_norm / (norm + 1e-6)), in place or into the tensors of `out` (of the same sizes, of
     one type); norm_out (float32, one element): the norm before clipping."""
-    dtype = _list_type(grads)
-    at, counts = _addresses(grads, dtype)
+    dev, dtype = _current_device(), _list_type(grads)
+    at, counts = _addresses(grads, dtype, dev)
     to, out_dtype = None, dtype
     if out is not None:
         out_dtype = _list_type(out)
-        to, _ = _addresses(out, out_dtype, counts)
-    ws, nb = _norm_workspace(counts, workspace)
-    _check(lib().gsr_grad_clip(_at(at), _at(counts), len(counts), dtype, max_norm, _scalar(norm_out), None if to is None else _at(to),
+        to, _ = _addresses(out, out_dtype, dev, counts)
+    ws, nb = _norm_workspace(counts, workspace, dev)
+    _check(lib().gsr_grad_clip(_at(at), _at(counts), len(counts), dtype, max_norm, _scalar(norm_out, dev), None if to is None else _at(to),
                                out_dtype, ws.data_ptr(), nb, _stream()))
 
 
@@ -470,10 +476,10 @@ def gsr_adam_update_list(w, dw, m, v, t: int, lr: float, beta1: float = 0.9, bet
                          weight_decay: float = 0.0, norm=None, max_norm: float = 0.0) -> None:
     """gsr_adam_update on every tensor of four lists, dw (float32, or all bfloat16) multiplied by min(1, max_norm / (norm + 1e-6)) where
     norm, as gsr_grad_norm leaves it on the device, is given."""
-    dtype = _list_type(dw)
-    aw, counts = _addresses(w, GSR_F32)
-    ag, am, av = (_addresses(x, k, counts)[0] for x, k in ((dw, dtype), (m, GSR_F32), (v, GSR_F32)))
-    _check(lib().gsr_adam_update_list(_at(aw), _at(ag), _at(am), _at(av), _at(counts), len(counts), dtype, _scalar(norm), max_norm, t, lr,
+    dev, dtype = _current_device(), _list_type(dw)
+    aw, counts = _addresses(w, GSR_F32, dev)
+    ag, am, av = (_addresses(x, k, dev, counts)[0] for x, k in ((dw, dtype), (m, GSR_F32), (v, GSR_F32)))
+    _check(lib().gsr_adam_update_list(_at(aw), _at(ag), _at(am), _at(av), _at(counts), len(counts), dtype, _scalar(norm, dev), max_norm, t, lr,
                                       beta1, beta2, eps, weight_decay, _stream()))
 
 
