@@ -185,8 +185,9 @@ __device__ __forceinline__ void clear_rows(float* out, int64_t ldt, int64_t voca
         const u32x4a z = {0, 0, 0, 0};
         for (int64_t i = first; i < quads; i += step) *reinterpret_cast<u32x4a*>(out + 4 * i) = z;
         for (int64_t i = 4 * quads + first; i < total; i += step) out[i] = 0.0f;
-    } else {
-        for (int64_t i = first; i < vocab * d; i += step) out[i / d * ldt + i % d] = 0.0f;
+    } else {                                    // a wave per row
+        for (int64_t row = first >> 6; row < vocab; row += step >> 6)
+            for (int col = lane_id(); col < d; col += 64) out[row * ldt + col] = 0.0f;
     }
 }
 
