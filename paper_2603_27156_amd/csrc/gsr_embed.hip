@@ -92,7 +92,8 @@ __device__ __forceinline__ int32_t token_row(I id, int32_t vocab) { return id >=
 // number by the pieces per row (ceil(2^32 / pg), 0 for one piece; exact below 2^16).  Bound by the writes (the table comes from the caches
 // unless it is larger than the plane).  They are streamed past the caches: 1M rows of 256 floats 217 -> 181 us, and with two pieces a thread
 // instead of four 143 us (7.2 TB/s; a fill by itself reaches 6.8).  gsr_step on the plane right after it, lookup included: 4,990 us cached,
-// 4,908 and 4,899 streamed; planes of 4 to 128 MB are as fast or faster streamed too.
+// 4,908 and 4,899 streamed; planes of 4 to 128 MB are as fast or faster streamed too.  Rows that start anywhere (odd widths): 4.0 to 4.4 TB/s, 1M rows of
+// 77 floats 73 us; cached 70, and going on at the next multiple of 16 bytes after a row's first piece 71.5.
 constexpr int kLookupPieces = 2;                // of a thread
 template <typename TT, typename T, typename I, int V>
 __global__ __launch_bounds__(256) void k_embed_lookup(const TT* __restrict__ table, int64_t ldt, int32_t vocab,
