@@ -178,28 +178,39 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
     return v;
 }
 
-// The table's gradient is cleared by workgroups of the sort's first launch, beside it: sums are stored later, over the zeros.
-__device__ __forceinline__ void clear_rows(float* out, int64_t ldt, int64_t vocab, int d, int64_t wg, int64_t wgs) {
-    const int64_t first = wg * blockDim.x + threadIdx.x, step = wgs * blockDim.x;
-    if (ldt == d) {
-        const int64_t total = vocab * d, quads = total / 4;
-        const u32x4a z = {0, 0, 0, 0};
-        for (int64_t i = first; i < quads; i += step) *reinterpret_cast<u32x4a*>(out + 4 * i) = z;
-        for (int64_t i = 4 * quads + first; i < total; i += step) out[i] = 0.0f;
+// The table's gradient is cleared by workgroups behind those of the sort's launches, a share in each: the sort waits for its round trips and leaves
+// the memory to them.  Sums are stored later, over the zeros.  Streamed past the caches, 8 KB a workgroup.  8,192 rows of 1,024 floats, 128k tokens
+// (525 MB; a fill takes 77 us): 149 us with all of it in the first launch, cached, 103 so; 65,536 rows of 512: 119 and 103.
+struct ClearSpan {
+    float* out;
+    int64_t ldt, rows;
+    int d, wgs;                 // the last workgroups of the launch
+};
+constexpr int kClearFloats = 2048;              // of a workgroup at a time
+__device__ __forceinline__ void clear_rows(const ClearSpan& s, int64_t wg) {
+    if (s.ldt == s.d) {
+        const int64_t total = s.rows * s.d;
+        for (int64_t base = wg * kClearFloats; base < total; base += (int64_t)s.wgs * kClearFloats) {
+#pragma unroll
+            for (int u = 0; u < kClearFloats / 1024; ++u) {
+                const int64_t i = base + 1024 * u + 4 * threadIdx.x;
+                const u32x4a z = {0, 0, 0, 0};
+                if (i + 4 <= total) __builtin_nontemporal_store(z, reinterpret_cast<u32x4a*>(s.out + i));
+                else
+                    for (int64_t j = i; j < total; ++j) s.out[j] = 0.0f;
+            }
+        }
     } else {                                    // a wave per row
-        for (int64_t row = first >> 6; row < vocab; row += step >> 6)
-            for (int col = lane_id(); col < d; col += 64) out[row * ldt + col] = 0.0f;
+        for (int64_t row = 4 * wg + (threadIdx.x >> 6); row < s.rows; row += 4 * (int64_t)s.wgs)
+            for (int col = lane_id(); col < s.d; col += 64) s.out[row * s.ldt + col] = 0.0f;
     }
 }
 
 template <typename Src>
 __global__ __launch_bounds__(256) void k_embed_count(Src src, int64_t n, int stretch, int wgs, int shift, int bits, uint32_t* __restrict__ hist,
-                                                     float* out, int64_t ldt, int64_t vocab, int d) {
+                                                     ClearSpan clear) {
     __shared__ uint32_t s_count[1 << kDigitBits];
-    if ((int)blockIdx.x >= wgs) {
-        clear_rows(out, ldt, vocab, d, blockIdx.x - wgs, gridDim.x - wgs);
-        return;
-    }
+    if ((int)blockIdx.x >= wgs) return clear_rows(clear, (int)blockIdx.x - wgs);
     const int digits = 1 << bits;
     for (int i = threadIdx.x; i < digits; i += 256) s_count[i] = 0;
     __syncthreads();
@@ -217,7 +228,9 @@ __global__ __launch_bounds__(256) void k_embed_count(Src src, int64_t n, int str
 }
 
 // counts of a digit -> elements of that digit in the workgroups before; total[digit].  A wave per digit.
-__global__ __launch_bounds__(256) void k_embed_places(uint32_t* __restrict__ hist, int wgs, int digits, uint32_t* __restrict__ total) {
+__global__ __launch_bounds__(256) void k_embed_places(uint32_t* __restrict__ hist, int wgs, int digits, uint32_t* __restrict__ total,
+                                                      ClearSpan clear) {
+    if ((int)blockIdx.x >= (digits + 3) / 4) return clear_rows(clear, (int)blockIdx.x - (digits + 3) / 4);
     const int digit = blockIdx.x * 4 + (threadIdx.x >> 6), lane = lane_id();
     if (digit >= digits) return;
     uint32_t* h = hist + (int64_t)digit * wgs;
@@ -312,7 +325,8 @@ __device__ __forceinline__ void wg_scan(uint32_t* v, int count, uint32_t* s_wave
 template <typename Src>
 __global__ __launch_bounds__(256) void k_embed_hand_out(Src src, int64_t n, int stretch, int wgs, int shift, int bits,
                                                         const uint32_t* __restrict__ hist, const uint32_t* __restrict__ total,
-                                                        SortPair* __restrict__ out) {
+                                                        SortPair* __restrict__ out, ClearSpan clear) {
+    if ((int)blockIdx.x >= wgs) return clear_rows(clear, (int)blockIdx.x - wgs);
     constexpr int PER = (1 << kDigitBits) / 256;             // digits of a thread
     __shared__ uint32_t s_start[kSortWaves << kDigitBits];
     __shared__ uint32_t s_first[1 << kDigitBits];            // places: of a digit in the workgroup, then from there to memory
@@ -749,20 +763,19 @@ __global__ __launch_bounds__(1024) void k_embed_small(TokenSource<I> ids, int n,
         __syncthreads();
         const float zero[V] = {};
         for (int r = sub; r < count; r += kSmallSubs)
-            if (!has[r] && mine) store_piece<V>(out + (base + r) * a.ldt, zero);
+            if (!has[r] && mine) store_piece<V, true>(out + (base + r) * a.ldt, zero);
         __syncthreads();
     }
 }
-__global__ __launch_bounds__(256) void k_embed_clear(float* out, int64_t ldt, int64_t vocab, int d) {
-    clear_rows(out, ldt, vocab, d, blockIdx.x, gridDim.x);
-}
+__global__ __launch_bounds__(256) void k_embed_clear(ClearSpan clear) { clear_rows(clear, blockIdx.x); }
 
 // ---- host side ----------------------------------------------------------------------------------------------
 namespace {
 
 constexpr int kMaxWidth = 1 << 17;
-// Elements of the table that k_embed_small clears beside its sums; a launch of its own before it costs 2.5 us (1,000 rows, 64 columns, calls of
-// 0.3 / 4 / 15 MB: 13.6 / 14.7 / 16.5 us beside the sums, 15.7 / 16.2 / 16.9 before) but has the whole chip.
+// Elements of the table that k_embed_small clears beside its sums; a launch of its own costs a call but has the whole chip: 10 rows of 64 columns,
+// tables of 0.3 / 4 / 15 MB 9.0 / 9.4 / 10.5 us beside the sums, 12.2 / 12.6 / 12.4 before them, 1,000 rows 12.1 / 12.9 / 14.3 and 12.7 / 13.3 / 15.1;
+// 2,048 rows and 525 MB 114 and 106.
 constexpr int64_t kSmallClear = 1 << 22;
 
 struct EmbedShape {             // a plane as the kernels take it: one group, or one per plane
@@ -871,8 +884,12 @@ EmbedPlan embed_plan(int64_t n, int64_t vocab, int d) {
     return p;
 }
 
-// workgroups of 256 that clear the gradient: up to 4,096, 16 KB or more each
-unsigned clear_wgs(int64_t vocab, int d) { return (unsigned)std::min<int64_t>(4096, (vocab * d + 4095) / 4096); }
+// share k of n of the rows of a gradient
+ClearSpan clear_share(float* out, int64_t ldt, int64_t vocab, int d, int k, int n) {
+    const int64_t a = vocab * k / n, rows = vocab * (k + 1) / n - a;
+    const int64_t wgs = ldt == d ? (rows * d + kClearFloats - 1) / kClearFloats : (rows + 3) / 4;
+    return {out + a * ldt, ldt, rows, d, (int)std::min<int64_t>(wgs, 1 << 20)};
+}
 
 EmbedSums sums_of(const EmbedShape& s, const void* dx, int d, float scale, int64_t vocab, float* out, int64_t ldt) {
     EmbedSums a{};
@@ -896,7 +913,10 @@ void launch_small(const EmbedPlan& p, const void* ids, int64_t n, EmbedSums a, h
     const bool clear = (int64_t)a.vocab * a.d <= kSmallClear;
     int64_t wgs = std::max<int64_t>(1, (n + kSmallSpan - 1) / kSmallSpan);
     if (clear) wgs = std::max(wgs, std::min<int64_t>(std::max(1, 256 / slabs), ((int64_t)a.vocab + 511) / 512));
-    else hipLaunchKernelGGL(k_embed_clear, dim3(clear_wgs(a.vocab, a.d)), dim3(256), 0, st, a.out, a.ldt, (int64_t)a.vocab, a.d);
+    if (!clear) {
+        const ClearSpan all = clear_share(a.out, a.ldt, a.vocab, a.d, 0, 1);
+        hipLaunchKernelGGL(k_embed_clear, dim3(all.wgs), dim3(256), 0, st, all);
+    }
     const TokenSource<I> src{(const I*)ids, a.vocab};
     hipLaunchKernelGGL((k_embed_small<S, V, I>), dim3((unsigned)wgs, slabs), dim3(1024), 0, st, src, (int)n, p.bits, p.passes, a, (int)clear);
 }
@@ -953,28 +973,35 @@ void launch_sums(const EmbedPlan& p, EmbedSums a, int32_t dtype, int last, char*
 template <typename I>
 int launch_sort(const EmbedPlan& p, const void* ids, int64_t n, int64_t vocab, float* out, int64_t ldt, int d, char* ws, hipStream_t st) {
     const TokenSource<I> src{(const I*)ids, (int32_t)vocab};
-    const unsigned clear = clear_wgs(vocab, d);
     auto at = [&](size_t o) { return ws + o; };
     uint32_t *hist = (uint32_t*)at(p.hist), *total = (uint32_t*)at(p.total);
     const int digits = 1 << p.bits;
     if (p.wgs <= kFewWgs && digits <= kFewDigits) total = nullptr;
+    const int launches = p.passes * (total ? 3 : 2);
+    int launch = 0;
+    auto share = [&] { return clear_share(out, ldt, vocab, d, launch++, launches); };
     for (int i = 0; i < p.passes; ++i) {
         const int to = i & 1;
         SortPair* out_pairs = (SortPair*)at(p.pairs[to]);
         const PairSource again{(const SortPair*)at(p.pairs[to ^ 1])};
+        ClearSpan clear = share();
         if (i == 0)
-            hipLaunchKernelGGL((k_embed_count<TokenSource<I>>), dim3(p.wgs + clear), dim3(256), 0, st, src, n, p.stretch, p.wgs, 0, p.bits, hist, out,
-                               ldt, vocab, d);
+            hipLaunchKernelGGL((k_embed_count<TokenSource<I>>), dim3(p.wgs + clear.wgs), dim3(256), 0, st, src, n, p.stretch, p.wgs, 0, p.bits, hist,
+                               clear);
         else
-            hipLaunchKernelGGL((k_embed_count<PairSource>), dim3(p.wgs), dim3(256), 0, st, again, n, p.stretch, p.wgs, i * p.bits, p.bits, hist,
-                               (float*)nullptr, ldt, vocab, d);
-        if (total) hipLaunchKernelGGL(k_embed_places, dim3((digits + 3) / 4), dim3(256), 0, st, hist, p.wgs, digits, total);
+            hipLaunchKernelGGL((k_embed_count<PairSource>), dim3(p.wgs + clear.wgs), dim3(256), 0, st, again, n, p.stretch, p.wgs, i * p.bits, p.bits,
+                               hist, clear);
+        if (total) {
+            clear = share();
+            hipLaunchKernelGGL(k_embed_places, dim3((digits + 3) / 4 + clear.wgs), dim3(256), 0, st, hist, p.wgs, digits, total, clear);
+        }
+        clear = share();
         if (i == 0)
-            hipLaunchKernelGGL((k_embed_hand_out<TokenSource<I>>), dim3(p.wgs), dim3(256), 0, st, src, n, p.stretch, p.wgs, 0, p.bits, hist, total,
-                               out_pairs);
+            hipLaunchKernelGGL((k_embed_hand_out<TokenSource<I>>), dim3(p.wgs + clear.wgs), dim3(256), 0, st, src, n, p.stretch, p.wgs, 0, p.bits,
+                               hist, total, out_pairs, clear);
         else
-            hipLaunchKernelGGL((k_embed_hand_out<PairSource>), dim3(p.wgs), dim3(256), 0, st, again, n, p.stretch, p.wgs, i * p.bits, p.bits, hist,
-                               total, out_pairs);
+            hipLaunchKernelGGL((k_embed_hand_out<PairSource>), dim3(p.wgs + clear.wgs), dim3(256), 0, st, again, n, p.stretch, p.wgs, i * p.bits,
+                               p.bits, hist, total, out_pairs, clear);
     }
     return (p.passes - 1) & 1;
 }
