@@ -90,6 +90,21 @@ def grad_ref(dx, ids, vocab, scale):
     (64, 9, 6, 6, F32, F32, torch.int32, "mixed", 0, 0),
     (70, 9, 14, 2, BF16, BF16, torch.int32, "mixed", 0, 0),
     (300, 9, 8, 0, F32, F32, torch.int32, "unknown", 0, 0),
+    # odd widths without gaps, in rows and in planes that begin anywhere
+    (1, 5, 5, 0, F32, F32, torch.int32, "one", 0, 0),
+    (1, 5, 9, 0, BF16, BF16, torch.int32, "one", 0, 0),
+    (2, 5, 6, 0, F32, F32, torch.int64, "mixed", 0, 0),
+    (1003, 40, 77, 0, F32, F32, torch.int32, "mixed", 0, 0),
+    (1003, 40, 77, 0, BF16, F32, torch.int64, "mixed", 0, 0),
+    (1003, 40, 301, 0, BF16, BF16, torch.int32, "mixed", 0, 0),
+    (1003, 40, 301, 0, F32, BF16, torch.int64, "mixed", 0, 0),
+    (20_000, 300, 9, 0, F32, BF16, torch.int32, "common", 0, 0),
+    (1000, 40, 231, 3, F32, F32, torch.int32, "mixed", 0, 0),
+    (1001, 40, 231, 3, F32, F32, torch.int32, "mixed", 0, 0),
+    (1016, 40, 231, 3, BF16, BF16, torch.int32, "mixed", 0, 0),
+    (50, 40, 4095, 0, F32, F32, torch.int32, "mixed", 0, 0),
+    (50, 40, 4097, 0, F32, F32, torch.int32, "mixed", 0, 0),
+    (70, 40, 4095, 0, F32, BF16, torch.int32, "mixed", 0, 0),
 ])
 def test_lookup(n, vocab, d, c, table_type, dtype, ids_type, kind, pad, offset):
     rng = np.random.default_rng(n + d)
