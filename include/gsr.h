@@ -344,10 +344,11 @@ gsr_status_t gsr_embed_grad(const void* ids, int32_t ids_i64, int64_t n, const v
 /* ---- all tensors of a step at once: gradient norm, clipping, parameter update ----
  *
  * A list is `tensors` device addresses and `counts` sizes in elements, both host arrays that are read during the call; every tensor is a
- * contiguous array on the current device, aligned to its elements, and may be empty.  At most 2^40 elements.  What a call writes may not
- * overlap anything else in its lists (GSR_ERR_INVALID_ARG; a tensor named twice is such a case).  workspace: device, 8-byte aligned, at
- * least gsr_grad_norm_workspace(counts, tensors) bytes; it holds nothing between calls.  Calls only launch kernels and may be captured;
- * addresses, sizes and scalars are then those of the capture.
+ * contiguous array on the current device, aligned to its elements, and may be empty.  At most 2^40 elements.  What a call writes, norm_out
+ * and the workspace among it, may not overlap anything else that it is given (GSR_ERR_INVALID_ARG; a tensor named twice is such a case, and so
+ * is the norm that an update reads in a tensor that it writes).  workspace: device, 8-byte aligned, at least
+ * gsr_grad_norm_workspace(counts, tensors) bytes; it holds nothing between calls.  Calls only launch kernels and may be captured; addresses,
+ * sizes and scalars are then those of the capture.
  *
  * gsr_grad_norm: norm_out (device, 1 float) = sqrt(sum g^2) over all elements of all tensors; squares and sums in float64.
  *

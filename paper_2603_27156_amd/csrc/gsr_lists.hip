@@ -370,6 +370,19 @@ gsr_status_t check_list(void* const* const (&lists)[P], const size_t (&width)[P]
     return GSR_OK;
 }
 
+// Whether `bytes` at p overlap a tensor of the arrays of pointers whose bits of `which` are set.  Addresses and sizes have passed check_list.
+template <int P>
+bool over_tensor(const void* p, size_t bytes, void* const* const (&lists)[P], const size_t (&width)[P], unsigned which, const int64_t* counts,
+                 int32_t tensors) {
+    const uintptr_t from = (uintptr_t)p, to = from + bytes;
+    for (int k = 0; k < P; ++k)
+        for (int32_t i = 0; ((which >> k) & 1) && i < tensors; ++i) {
+            const uintptr_t at = (uintptr_t)lists[k][i];
+            if (counts[i] && at < to && from < at + (uintptr_t)counts[i] * width[k]) return true;
+        }
+    return false;
+}
+
 gsr_status_t list_dtype(int32_t dtype) {
     if (dtype != GSR_F32 && dtype != GSR_BF16) return fail(GSR_ERR_UNSUPPORTED, "dtype %d", dtype);
     return GSR_OK;
@@ -415,6 +428,20 @@ gsr_status_t check_norm_workspace(int64_t tensors, int64_t elements, const void*
     return GSR_OK;
 }
 
+// norm_out and the workspace lie apart from the tensors and from each other: the first workgroup of k_clip writes norm_out while others still read
+// gradients and partial sums.
+template <int P>
+gsr_status_t check_apart(const float* norm_out, const void* workspace, void* const* const (&lists)[P], const size_t (&width)[P],
+                         const int64_t* counts, int32_t tensors, int64_t elements) {
+    const size_t bytes = norm_workspace(tensors, elements);
+    const unsigned all = (1u << P) - 1;
+    if (norm_out && over_tensor<P>(norm_out, 4, lists, width, all, counts, tensors)) return fail(GSR_ERR_INVALID_ARG, "norm_out overlaps a tensor");
+    if (over_tensor<P>(workspace, bytes, lists, width, all, counts, tensors)) return fail(GSR_ERR_INVALID_ARG, "the workspace overlaps a tensor");
+    if (norm_out && (uintptr_t)norm_out + 4 > (uintptr_t)workspace && (uintptr_t)norm_out < (uintptr_t)workspace + bytes)
+        return fail(GSR_ERR_INVALID_ARG, "norm_out lies in the workspace");
+    return GSR_OK;
+}
+
 }  // namespace
 }  // namespace gsr
 
@@ -439,6 +466,7 @@ gsr_status_t gsr_grad_norm(const void* const* grads, const int64_t* counts, int3
     GSR_TRY(check_list<1>({g}, {dtype_size(dtype)}, 0, counts, tensors, &elements));
     if (!norm_out || ((uintptr_t)norm_out & 3)) return fail(GSR_ERR_INVALID_ARG, "norm_out is null or not aligned");
     GSR_TRY(check_norm_workspace(tensors, elements, workspace, workspace_bytes));
+    GSR_TRY(check_apart<1>(norm_out, workspace, {g}, {dtype_size(dtype)}, counts, tensors, elements));
     launch_norm(g, counts, tensors, dtype, norm_out, false, workspace, (hipStream_t)stream);
     GSR_HIP_CHECK(hipGetLastError());
     return GSR_OK;
@@ -456,6 +484,7 @@ gsr_status_t gsr_grad_clip(void* const* grads, const int64_t* counts, int32_t te
     else GSR_TRY(check_list<1>({grads}, {w}, 1u, counts, tensors, &elements));
     if ((uintptr_t)norm_out & 3) return fail(GSR_ERR_INVALID_ARG, "norm_out is not aligned");
     GSR_TRY(check_norm_workspace(tensors, elements, workspace, workspace_bytes));
+    GSR_TRY(check_apart<2>(norm_out, workspace, {grads, out ? out : grads}, {w, wo}, counts, tensors, elements));
     hipStream_t s = (hipStream_t)stream;
     ClipNorm n = launch_norm(grads, counts, tensors, dtype, norm_out, true, workspace, s);
     n.max_norm = (double)max_norm;
@@ -486,6 +515,7 @@ gsr_status_t gsr_adam_update_list(float* const* w, const void* const* dw, float*
     const size_t width[4] = {4, dtype_size(dw_dtype), 4, 4};
     GSR_TRY(check_list<4>(lists, width, 13u, counts, tensors, &elements));
     if (elements == 0) return GSR_OK;
+    if (norm && over_tensor<4>(norm, 4, lists, width, 13u, counts, tensors)) return fail(GSR_ERR_INVALID_ARG, "norm lies in a tensor that is written");
     const double c1 = 1.0 - std::pow(beta1, (double)t), c2 = 1.0 - std::pow(beta2, (double)t);
     const AdamParams p{(float)lr, (float)beta1, (float)beta2, (float)(1.0 - beta1), (float)(1.0 - beta2), (float)eps, (float)weight_decay,
                        (float)(1.0 / c1), (float)(1.0 / c2)};

@@ -110,6 +110,18 @@ def test_adam_refuses(change, status):
     assert adam(**change) == status and gsr.gsr_last_error()
 
 
+# the norm and the workspace are written while tensors are read (P + 12: the last float of four at P), the norm of an update is read meanwhile
+@pytest.mark.parametrize("call", [
+    lambda: norm(out=P + 12, ws=16 * P), lambda: norm(out=2 * P, ws=16 * P), lambda: norm(out=16 * P, ws=2 * P), lambda: norm(out=16 * P, ws=P + 8),
+    lambda: norm(out=16 * P, ws=2 * P - 256), lambda: norm(out=16 * P, ws=16 * P), lambda: norm(out=16 * P + 264, ws=16 * P),
+    lambda: norm(dtype=1, out=P + 4, ws=16 * P), lambda: clip(norm_out=P, ws=16 * P), lambda: clip(norm_out=2 * P + 12, ws=16 * P), lambda: clip(ws=P),
+    lambda: clip(out=(3 * P, 4 * P), norm_out=4 * P + 4, ws=16 * P), lambda: clip(out=(3 * P, 4 * P), ws=3 * P),
+    lambda: clip(out=(3 * P, 4 * P), out_dtype=1, norm_out=3 * P + 4, ws=16 * P), lambda: clip(norm_out=16 * P + 8, ws=16 * P),
+    lambda: adam(norm=P), lambda: adam(norm=2 * P + 12), lambda: adam(norm=5 * P + 4), lambda: adam(norm=8 * P)])
+def test_a_norm_or_workspace_over_a_tensor_is_refused(call):
+    assert call() == BAD and gsr.gsr_last_error()
+
+
 def test_empty_lists_and_tensors():
     assert adam(tensors=0) == OK and adam(counts=(0, 0), w=(0, 0), dw=(0, 0), m=(0, 0), v=(0, 0)) == OK
     lib = gsr.lib()
