@@ -334,8 +334,9 @@ gsr_status_t gsr_embed_lookup(const void* table, int64_t vocab, int64_t ldt, int
 /* gsr_embed_grad: dE[t, :] = scale * sum of dx[i, :] over the rows i with ids[i] = t.  dtable_out: device, vocab rows of d floats,
  * row stride ldt; every row is written, zeros where a token does not occur.  The positions are sorted by token and the sums taken in
  * float32 in an order that the tokens alone fix: equal calls give equal bits.  workspace: device, 16-byte aligned, at least
- * gsr_embed_grad_workspace() bytes (the same for all types and layouts, at most n (20 + d / 2) and some; 0 for up to 4,096 rows of 2^24 values in all, which need none,
- * and for sizes that are refused); it holds nothing between calls. */
+ * gsr_embed_grad_workspace() bytes; it holds nothing between calls.  They are the same for all types and layouts, never fewer for more rows (of
+ * the same vocab and d), so that a workspace for n rows serves any fewer, and at most n (18 + 0.55 d) + 64 d + 2^23; 0 for up to 4,096 rows of
+ * 2^24 values in all, which need none, and for sizes that are refused. */
 size_t gsr_embed_grad_workspace(int64_t n, int64_t vocab, int32_t d);
 gsr_status_t gsr_embed_grad(const void* ids, int32_t ids_i64, int64_t n, const void* dx, int64_t ldx, int32_t d, int32_t c, int32_t layout,
                             int32_t dtype, float scale, int64_t vocab, float* dtable_out, int64_t ldt, void* workspace,

@@ -866,7 +866,7 @@ EmbedPlan embed_plan(int64_t n, int64_t vocab, int d) {
     for (int i = 0; i < 2; ++i) {
         p.pairs[i] = i < p.passes ? take(sizeof(SortPair) * (size_t)n) : p.pairs[0];
     }
-    p.hist = take(((size_t)p.wgs << p.bits) * 4);
+    p.hist = take(((size_t)std::min<int64_t>(stretches, kSortWgs) << p.bits) * 4);      // (p.wgs at most, and not falling as n grows)
     p.total = take(((size_t)1 << p.bits) * 4);
     int64_t entries = n;
     int chunk = p.chunk;
@@ -882,6 +882,17 @@ EmbedPlan embed_plan(int64_t n, int64_t vocab, int d) {
     } while (entries > 2 * kJoinChunks);
     p.bytes = at;
     return p;
+}
+
+// Workspace for n rows and for any fewer of them.  That of one size falls behind the last size of a chunk length, so those sizes count too.
+size_t embed_workspace(int64_t n, int64_t vocab, int d) {
+    size_t bytes = embed_plan(n, vocab, d).bytes;
+    auto last_size = [&](int64_t m) {
+        if (m < n) bytes = std::max(bytes, embed_plan(m, vocab, d).bytes);
+    };
+    last_size(16 * kJoinChunks);
+    for (int64_t chunk = 16; chunk < 256; chunk *= 2) last_size((((chunk + 1) << 20) - 1) / d);
+    return bytes;
 }
 
 // share k of n of the rows of a gradient
@@ -1036,7 +1047,7 @@ gsr_status_t gsr_embed_lookup(const void* table, int64_t vocab, int64_t ldt, int
 
 size_t gsr_embed_grad_workspace(int64_t n, int64_t vocab, int32_t d) {
     if (n < 0 || n >= ((int64_t)1 << 31) || vocab < 1 || vocab >= ((int64_t)1 << 31) - 1 || d < 1 || d > kMaxWidth) return 0;
-    return embed_plan(n, vocab, d).bytes;
+    return embed_workspace(n, vocab, d);
 }
 
 gsr_status_t gsr_embed_grad(const void* ids, int32_t ids_i64, int64_t n, const void* dx, int64_t ldx, int32_t d, int32_t c, int32_t layout,

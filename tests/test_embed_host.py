@@ -50,6 +50,27 @@ def test_grad_workspace_is_monotonic_and_refuses_the_same_sizes():
     assert grad(nbytes=need - 1) == SMALL
 
 
+@pytest.mark.parametrize("vocab", [97, 1_500, 50_021, 2 ** 22])
+@pytest.mark.parametrize("d", [1, 3, 17, 32, 33, 64, 77, 256, 530, 1024, 4100, 131_072])
+def test_grad_workspace_for_n_rows_serves_fewer(vocab, d):
+    """Over sizes of every scale, and one by one around those where the sort takes longer stretches or the sums longer chunks."""
+    size, most = gsr.gsr_embed_grad_workspace, 2 ** 31 - 1
+    edges = {4096, 16_384, 32_768} | {(k << 20) // d for k in (16, 17, 32, 33, 64, 65, 128, 129, 256, 257)} | {k << 21 for k in (1, 2, 3, 8, 64)}
+    ns = {int(1.03 ** i) for i in range(726)} | {e + i for e in edges for i in range(-2, 3)}
+    before = 0
+    for n in sorted(n for n in ns if 0 <= n <= most):
+        now = size(n, vocab, d)
+        assert before <= now <= n * (18 + 0.55 * d) + 64 * d + 2 ** 23, (n, before, now)
+        before = now
+
+
+def test_grad_takes_the_workspace_of_a_larger_graph():
+    """What a call asks for is never more than what a call of more rows does: 69,631 rows of 256 take chunks of 16 rows, 69,632 of 32."""
+    size = gsr.gsr_embed_grad_workspace
+    assert size(69_632, 97, 256) >= size(69_631, 97, 256) > 8 * 69_631
+    assert grad(n=69_631, d=256, ldx=256, ldt=256, vocab=97, nbytes=5_328_640) == SMALL        # enough for the chunks of 32 alone
+
+
 class Lists:
     """Host arrays of addresses and sizes, one list per keyword; they live as long as this does."""
 

@@ -307,6 +307,19 @@ def test_other_stream_and_captured_calls_that_share_a_workspace():
             assert torch.equal(t["x"], lookup_ref(t["table"], t["ids"], 3.0, F32))
 
 
+def test_workspace_of_the_largest_graph_serves_smaller_ones():
+    """69,631 rows of 256 are cut into chunks of 16 rows, 69,632 into chunks of 32: the smaller call needs more, and finds it."""
+    vocab, d, most = 97, 256, 69_632
+    ws = torch.empty(gsr.gsr_embed_grad_workspace(most, vocab, d), dtype=torch.uint8, device=dev())
+    rng = np.random.default_rng(5)
+    for n in (most, most - 1, 16_384, 16_385, 4097, 5):
+        ids = torch.from_numpy(make_ids("mixed", n, vocab, rng)).to(dev())
+        dx = torch.from_numpy(rng.integers(-8, 9, (n, d)).astype(np.float32)).to(dev())
+        out = torch.full((vocab, d), GUARD, device=dev())
+        gsr.gsr_embed_grad(ids, dx, out, workspace=ws)
+        assert torch.equal(out.double().cpu(), grad_ref(dx, ids, vocab, 1.0)[0]), n
+
+
 def test_calls_side_by_side_on_two_streams():
     """Two threads' worth of work: calls on two streams with workspaces of their own, many in flight."""
     streams = [torch.cuda.Stream() for _ in range(2)]
