@@ -36,7 +36,9 @@ def _hipcc() -> str:
 
 
 def build_marshal(verbose: bool = True) -> str:
-    """Compile gsr_marshal.cpp against the installed torch."""
+    """Compile gsr_marshal.cpp against the installed torch.  What an earlier build left goes first: it may fit another torch."""
+    if os.path.exists(MARSHAL):
+        os.remove(MARSHAL)
     import torch
     from torch.utils import cpp_extension
     includes = [*cpp_extension.include_paths(), sysconfig.get_paths()["include"]]
@@ -51,7 +53,9 @@ def build_marshal(verbose: bool = True) -> str:
 
 
 def build_library(verbose: bool = True) -> str:
-    """Compile every HIP source for gfx950 and link libgsr.so.  Always recompiles."""
+    """Compile every HIP source for gfx950 and link libgsr.so, and build the binding's helper.  Always recompiles.  libgsr.so needs no torch: where
+    the helper cannot be built (no torch, none of its headers, no host compiler) it is left out with a word on stderr, and the binding's
+    calls on lists of tensors raise."""
     objdir = os.path.join(HERE, "_build")
     os.makedirs(objdir, exist_ok=True)
     hipcc = _hipcc()
@@ -67,11 +71,14 @@ def build_library(verbose: bool = True) -> str:
     with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
         marshal = ex.submit(build_marshal, verbose)
         objs = list(ex.map(compile_one, SOURCES))
-        marshal.result()
     cmd = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.check_call(cmd)
+    try:
+        marshal.result()
+    except (ImportError, OSError, subprocess.CalledProcessError) as e:
+        print(f"{MARSHAL} was not built ({e}): calls on lists of tensors will raise", file=sys.stderr, flush=True)
     return LIB
 
 
