@@ -96,9 +96,11 @@ def _check(st: int):
 
 
 def _stream() -> C.c_void_p:
-    # the handle of torch.cuda.current_stream(), without the 3 us that making a Stream object of it takes
+    # The handle of torch.cuda.current_stream(), without the 3 us that making a Stream object of it takes, where torch has a function for it: that
+    # one is not part of its documented interface.
     import torch
-    return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return C.c_void_p(torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device()))
 
 
 def _dp(t) -> C.c_void_p:

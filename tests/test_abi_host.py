@@ -72,3 +72,12 @@ def test_options_are_validated():
     gsr.gsr_set_option("hub_threshold", 0)        # 0: chosen per graph
     gsr.gsr_set_option("hub_chunk", 0)
     gsr.gsr_set_option("max_workgroups", 0)
+
+
+def test_stream_where_torch_has_no_raw_accessor(monkeypatch):
+    torch = pytest.importorskip("torch")
+    from types import SimpleNamespace
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *_: SimpleNamespace(cuda_stream=4096))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    assert gsr._stream().value == 4096

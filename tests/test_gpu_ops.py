@@ -233,3 +233,10 @@ def test_tile_operators_with_heavy_tiles_dealt_first(workgroups, heavy_share):
             assert_close("A scatter(V,I)", got.cpu().numpy(), oracle.aggregate(og, V, I, dg))
     finally:
         gsr.gsr_set_option("max_workgroups", 0)
+
+
+def test_calls_go_to_the_current_stream():
+    streams = [torch.cuda.default_stream(), torch.cuda.Stream(), torch.cuda.Stream()]
+    for stream in streams:
+        with torch.cuda.stream(stream):
+            assert (gsr._stream().value or 0) == torch.cuda.current_stream().cuda_stream == stream.cuda_stream
