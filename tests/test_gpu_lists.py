@@ -240,6 +240,70 @@ def test_binding_refuses_what_does_not_fit():
     gsr.gsr_grad_norm((torch.nn.Parameter(a), b.view(2, 4)), one)
 
 
+# ---- long lists ------------------------------------------------------------------------------------------------------
+# The norm takes chunks of 4,096 elements, one partial sum per workgroup, 16,384 workgroups a launch at most.  Clipping adds up to 1,024 partial sums
+# by itself; above that, and for the norm always, a launch of 1,024 threads does, each four at a time, again and again above 4,096.  A chunk that
+# was left out would be one of 33,000 equal shares of the sum of squares at least, more than 2^-17 of the norm, where 2^-23 is asked for.
+CHUNK = 4096
+LONG = {
+    "1023 chunks": [1023 * CHUNK], "1024 chunks": [1000 * CHUNK, 24 * CHUNK], "1025 chunks": [1024 * CHUNK + 1], "1024 and a launch": [1] * 1024,
+    "1025 in six launches": [1] * 1025, "1800 in four launches": [2 * CHUNK + 77] * 600, "4099 chunks": [5, 4096 * CHUNK, CHUNK + 3],
+    "9000 chunks": [9000 * CHUNK - 7], "16390 chunks of one launch": [3 * CHUNK, 16_384 * CHUNK + 17, 2 * CHUNK],
+    "33000 chunks in two launches": [9] * 190 + [16_500 * CHUNK, 16_310 * CHUNK],
+}
+long_lists = pytest.mark.parametrize("sizes", LONG.values(), ids=LONG)
+
+
+def long_list(sizes, dtype):
+    """(buffer, tensors, the same values in float64 in one piece)"""
+    buffer, g = make(sizes, dtype, randn(sum(sizes)) * 3)
+    return buffer, g, torch.cat(g).double()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@long_lists
+def test_norm_of_long_lists(sizes, dtype):
+    _, g, exact = long_list(sizes, dtype)
+    want = float(exact.square().sum().sqrt())
+    assert abs(norm_of(g) - want) <= 2.0 ** -23 * want
+
+
+@pytest.mark.parametrize("dtype,out_dtype", [(F32, None), (BF16, None), (F32, BF16), (BF16, F32)])
+@long_lists
+def test_clip_of_long_lists(sizes, dtype, out_dtype):
+    buffer, g, exact = long_list(sizes, dtype)
+    before, size, norm = buffer.clone(), float(exact.square().sum().sqrt()), torch.zeros(1, device=dev())
+    out_buffer, out, to = buffer, g, None
+    if out_dtype is not None:
+        out_buffer, out = make(sizes, out_dtype, torch.zeros(sum(sizes), device=dev()), gap=3, offset=2)
+        to = out
+    for max_norm in (2.0 * size, 0.75):
+        gsr.gsr_grad_clip(g, max_norm, norm, out=to)
+        assert abs(float(norm) - size) <= 2.0 ** -23 * size
+        assert clip_close(torch.cat(out).double(), exact * min(1.0, 0.75 / (size + 1e-6) if max_norm < size else 1.0), out[0].dtype)
+        if to is not None or max_norm > size:
+            assert torch.equal(buffer, before)
+    assert gaps_untouched(out_buffer, sizes, *((1, 1) if to is None else (3, 2)))
+
+
+@pytest.mark.parametrize("dw_dtype", [F32, BF16])
+@long_lists
+def test_clipped_adam_of_long_lists(sizes, dw_dtype):
+    (wb, w), (gb, g), (mb, m), (vb, v) = adam_lists(sizes, dw_dtype)
+    w0, g0, m0, v0 = (torch.cat(x).double() for x in (w, g, m, v))
+    size, norm = float(g0.square().sum().sqrt()), torch.zeros(1, device=dev())
+    gsr.gsr_grad_norm(g, norm)
+    gsr.gsr_adam_update_list(w, g, m, v, norm=norm, max_norm=0.5, **ADAM)
+    gk = g0 * (0.5 / (size + 1e-6)) + ADAM["weight_decay"] * w0
+    m1 = ADAM["beta1"] * m0 + (1 - ADAM["beta1"]) * gk
+    v1 = ADAM["beta2"] * v0 + (1 - ADAM["beta2"]) * gk * gk
+    step = (m1 / (1 - ADAM["beta1"] ** ADAM["t"])) / ((v1 / (1 - ADAM["beta2"] ** ADAM["t"])).sqrt() + ADAM["eps"])
+    for name, got, want in (("w", w, w0 - ADAM["lr"] * step), ("m", m, m1), ("v", v, v1)):
+        low = 1e-5 * min(1.0, float(want.square().mean().sqrt()))
+        assert bool(((torch.cat(got).double() - want).abs() <= low + 1e-4 * want.abs()).all()), name
+    assert gaps_untouched(wb, sizes) and gaps_untouched(mb, sizes, 2) and gaps_untouched(vb, sizes, 1, 3)
+
+
 # ---- a training step with all of them, as a program makes it ---------------------------------------------------------
 class Training:
     """Nodes with tokens of a small vocabulary: lookup, gsr_step, gradient of the table, norm, clipped Adam."""
