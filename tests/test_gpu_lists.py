@@ -375,6 +375,22 @@ def test_training_step_against_the_oracle(layout):
         assert_close("w", p.cpu().numpy(), w)
 
 
+@pytest.mark.parametrize("layout", [gsr.GSR_LAYOUT_ROW_MAJOR, gsr.GSR_LAYOUT_GROUP_PLANAR])
+def test_every_gradient_of_a_training_step_against_the_oracle(layout):
+    """Tensor by tensor: the weights of every block against its largest entry (sums of 1,201 products that partly cancel, as the audits of whole
+    layers take them), the head element by element, the bias as a number."""
+    s = Training(layout=layout)
+    s.gradients()
+    ref, dtable = s.reference(s.table_host)
+    got = [x.double().cpu().numpy() for x in s.grads]
+    assert_close("dtable", got[0], dtable)
+    dW = np.asarray(ref["dW"], dtype=np.float64)
+    worst = np.abs(got[1] - dW).max(axis=(2, 3)) / np.abs(dW).max(axis=(2, 3))
+    assert worst.shape == dW.shape[:2] and (worst <= 1e-4).all(), worst
+    assert_close("dw", got[2], ref["dwout"])
+    assert np.isclose(got[3][0], ref["dbout"], rtol=1e-4, atol=1e-7)
+
+
 def test_table_gradient_against_differences():
     """All columns kept, no RMS scale: the loss is a quadratic function of the table, of which a central difference in the oracle's double
     arithmetic gives the derivative but for the rounding of the plane to float32 (2^-24 of entries that move by 2^-6 of their size)."""
