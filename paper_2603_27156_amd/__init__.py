@@ -475,13 +475,15 @@ def gsr_grad_clip(grads, max_norm: float, norm_out=None, out=None, workspace=Non
 
 
 def gsr_adam_update_list(w, dw, m, v, t: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
-                         weight_decay: float = 0.0, norm=None, max_norm: float = 0.0) -> None:
+                         weight_decay: float = 0.0, norm=None, max_norm: Optional[float] = None) -> None:
     """gsr_adam_update on every tensor of four lists, dw (float32, or all bfloat16) multiplied by min(1, max_norm / (norm + 1e-6)) where
-    norm, as gsr_grad_norm leaves it on the device, is given."""
+    norm, as gsr_grad_norm leaves it on the device, is given; max_norm has to be given with it."""
+    if norm is not None and max_norm is None:
+        raise TypeError("a norm without max_norm")
     dev, dtype = _current_device(), _list_type(dw)
     aw, counts = _addresses(w, GSR_F32, dev)
     ag, am, av = (_addresses(x, k, dev, counts)[0] for x, k in ((dw, dtype), (m, GSR_F32), (v, GSR_F32)))
-    _check(lib().gsr_adam_update_list(_at(aw), _at(ag), _at(am), _at(av), _at(counts), len(counts), dtype, _scalar(norm, dev), max_norm, t, lr,
+    _check(lib().gsr_adam_update_list(_at(aw), _at(ag), _at(am), _at(av), _at(counts), len(counts), dtype, _scalar(norm, dev), max_norm or 0.0, t, lr,
                                       beta1, beta2, eps, weight_decay, _stream()))
 
 

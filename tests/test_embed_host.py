@@ -151,6 +151,13 @@ def test_empty_lists_and_tensors():
     assert lib.gsr_grad_norm_workspace(a.sizes, 2) == 0
 
 
+def test_an_update_with_a_norm_has_to_say_what_it_clips_to():
+    torch = pytest.importorskip("torch")
+    x = [torch.zeros(4)]
+    with pytest.raises(TypeError, match="max_norm"):
+        gsr.gsr_adam_update_list(x, x, x, x, 1, 1e-3, norm=torch.ones(1))
+
+
 def test_lists_of_tensors_are_read_as_they_are():
     """The binding's helper on host tensors: what it refuses, and that it does so before an address is used."""
     torch = pytest.importorskip("torch")
