@@ -439,7 +439,7 @@ struct EmbedSums {
     float scale;
     float* out;
     int64_t ldt;
-    float* part;                // [2 chunks][d], nullptr if there is one chunk
+    float* part;                // [2 chunks][d]
     int32_t* part_keys;         // [2 chunks], negative: nothing
 };
 constexpr int kSumBatch = 16, kSumLanesMin = 3;                        // (lanes per chunk as a logarithm)
@@ -550,7 +550,7 @@ __global__ __launch_bounds__(256) void k_embed_sums(EmbedSums a) {
         }
     }
     if (cur >= 0) store(open || right, open ? 2 * c : 2 * c + 1);
-    if (a.part_keys && piece == 0) {
+    if (piece == 0) {
         a.part_keys[2 * c] = left ? first : -1;
         a.part_keys[2 * c + 1] = right && !open ? cur : -1;
     }
@@ -873,8 +873,7 @@ EmbedPlan embed_plan(int64_t n, int64_t vocab, int d) {
     do {
         EmbedPlan::Level& l = p.level[p.levels++];
         l.entries = entries;
-        l.chunks = (entries + chunk - 1) / chunk;
-        if (l.chunks <= 1) break;
+        l.chunks = (entries + chunk - 1) / chunk;           // several: more than 4,096 rows, or 129 and chunks of under n / 4; then more than 2,048 entries
         l.part_keys = take((size_t)l.chunks * 2 * 4);
         l.part = take((size_t)l.chunks * 2 * d * 4);
         entries = 2 * l.chunks;
@@ -944,8 +943,8 @@ void launch_level(const EmbedPlan& p, int level, EmbedSums a, char* ws, hipStrea
     const EmbedPlan::Level& v = p.level[level];
     a.entries = (int32_t)v.entries;
     a.chunks = (int32_t)v.chunks;
-    a.part = v.chunks > 1 ? (float*)(ws + v.part) : nullptr;
-    a.part_keys = v.chunks > 1 ? (int32_t*)(ws + v.part_keys) : nullptr;
+    a.part = (float*)(ws + v.part);
+    a.part_keys = (int32_t*)(ws + v.part_keys);
     a.chunk = FIRST ? p.chunk : kPartChunk;
     a.pg = (a.dg + V - 1) / V;
     a.pieces = a.pg * (a.d / a.dg);
@@ -972,7 +971,6 @@ void launch_sums(const EmbedPlan& p, EmbedSums a, int32_t dtype, int last, char*
         else launch_level<float, 1, false>(p, l, a, ws, st);
     }
     const EmbedPlan::Level& v = p.level[p.levels - 1];
-    if (v.chunks <= 1) return;
     const float* part = (const float*)(ws + v.part);
     const int32_t* keys = (const int32_t*)(ws + v.part_keys);
     if (d >= 4)
