@@ -37,6 +37,9 @@ __device__ __forceinline__ bf16_t from_float<bf16_t>(float v) {
     return r;
 }
 
+// rounded to the nearest 16-bit value, for what need not be finite: NaN stays NaN
+__device__ __forceinline__ uint32_t bf16_bits(float v) { return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v)); }
+
 // value as it will read back after a store of type T
 template <typename T>
 __device__ __forceinline__ float stored(float v) { return to_float(from_float<T>(v)); }
@@ -369,6 +372,8 @@ using f32x4 = __attribute__((__vector_size__(4 * sizeof(float)))) float;
 typedef uint32_t u32x2a __attribute__((ext_vector_type(2), aligned(4)));
 typedef uint32_t u32x3a __attribute__((ext_vector_type(3), aligned(4)));
 typedef uint32_t u32x4a __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2h __attribute__((ext_vector_type(2), aligned(2)));    // four and eight 16-bit values, aligned to one
+typedef uint32_t u32x4h __attribute__((ext_vector_type(4), aligned(2)));
 
 template <int NW>
 __device__ __forceinline__ void load_words(const void* p, uint32_t (&w)[NW]) {

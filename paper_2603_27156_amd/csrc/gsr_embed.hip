@@ -16,9 +16,6 @@ namespace gsr {
 // is no multiple of V starts V elements before the row's end and overlaps the one before it: both lanes load, sum and store the
 // same numbers, so nothing is predicated.  Rows narrower than a piece are taken element by element (V = 1).  Pieces are aligned
 // to their elements only.
-typedef uint32_t u32x2h __attribute__((ext_vector_type(2), aligned(2)));
-typedef uint32_t u32x4h __attribute__((ext_vector_type(4), aligned(2)));
-
 template <typename T, int V>
 struct Piece {                       // V elements as they lie in memory
     static constexpr int NW = (V * (int)sizeof(T) + 3) / 4;
@@ -50,9 +47,6 @@ struct Piece {                       // V elements as they lie in memory
         else return __uint_as_float((i & 1) ? (w[i >> 1] & 0xFFFF0000u) : (w[i >> 1] << 16));
     }
 };
-
-// rounded to the nearest 16-bit value, NaN stays NaN
-__device__ __forceinline__ uint32_t bf16_bits(float v) { return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v)); }
 
 template <int V, bool STREAM = false, typename T>
 __device__ __forceinline__ void store_piece(T* p, const float (&v)[V]) {

@@ -59,11 +59,6 @@ __device__ __forceinline__ int tensor_of(const TensorTable<P>& t, int c) {
 }
 
 // ---- V elements at a time, past the caches, aligned to their elements only -------------------------------------
-typedef uint32_t u32x2h __attribute__((ext_vector_type(2), aligned(2)));
-typedef uint32_t u32x4h __attribute__((ext_vector_type(4), aligned(2)));
-
-__device__ __forceinline__ uint32_t to_bits16(float v) { return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v)); }   // NaN stays NaN
-
 __device__ __forceinline__ void load_v(const float* p, float (&v)[4]) {
     const u32x4a* q = reinterpret_cast<const u32x4a*>(p);
     const u32x4a t = __builtin_nontemporal_load(q);
@@ -93,11 +88,11 @@ __device__ __forceinline__ void store_v(bf16_t* p, const float (&v)[V]) {
     typedef uint32_t words __attribute__((ext_vector_type(V / 2), aligned(2)));
     words t;
 #pragma unroll
-    for (int i = 0; i < V / 2; ++i) t[i] = to_bits16(v[2 * i]) | (to_bits16(v[2 * i + 1]) << 16);
+    for (int i = 0; i < V / 2; ++i) t[i] = bf16_bits(v[2 * i]) | (bf16_bits(v[2 * i + 1]) << 16);
     __builtin_nontemporal_store(t, reinterpret_cast<words*>(p));
 }
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store1(bf16_t* p, float v) { p->bits = (uint16_t)to_bits16(v); }
+__device__ __forceinline__ void store1(bf16_t* p, float v) { p->bits = (uint16_t)bf16_bits(v); }
 
 // ---- norm -------------------------------------------------------------------------------------------------
 __device__ __forceinline__ double wave_sum(double v) {
