@@ -319,14 +319,15 @@ gsr_status_t gsr_adam_update(float* w, const float* dw, float* m, float* v, int6
  *
  * E: a table of `vocab` rows of d values, row stride ldt elements.  ids: device, n tokens (the cell type of every node, or any other
  * number), int32, or int64 with ids_i64 = 1.  A token outside [0, vocab), such as -1, has no embedding: its row of x is zero and
- * its row of dx has no part in the gradient (nor is it read).
+ * the values in its row of dx, whatever they are, have no part in the gradient (some of these rows are loaded all the same).
  * Planes (x, dx; device, n x d of `dtype`): ROW_MAJOR with row stride ldx elements, d at least; GROUP_PLANAR in c groups of d/c columns,
  * row stride ldx, d/c at least, group stride n * ldx (ldx = d/c: what gsr_step takes).  Elements between rows are left as they are.
  * 1 <= d <= 131072, c divides d, n < 2^31, 1 <= vocab < 2^31 - 1; pointers aligned to their elements.
  * All tensors on the current device; what a call writes overlaps nothing that it reads.  Calls only launch kernels and may be captured; calls with
  * workspaces of their own may run side by side.
  *
- * gsr_embed_lookup: x[i, :] = scale * E[ids[i], :], rounded once to `dtype`; table and plane of either type. */
+ * gsr_embed_lookup: x[i, :] = scale * E[ids[i], :], the product rounded to float32 and, for a 16-bit plane, once more to that; table and
+ * plane of either type. */
 gsr_status_t gsr_embed_lookup(const void* table, int64_t vocab, int64_t ldt, int32_t table_dtype, const void* ids, int32_t ids_i64,
                               int64_t n, int32_t d, int32_t c, int32_t layout, int32_t dtype, float scale, void* x_out, int64_t ldx,
                               void* stream);

@@ -3,7 +3,8 @@
 //   gsr_embed_lookup   x[n, :] = scale * E[id_n, :]
 //   gsr_embed_grad     dE[v, :] = scale * sum over the rows n with id_n = v of dx[n, :]
 //
-// A token outside [0, vocab) has no embedding: its row of x is zero, its row of dx is not read.
+// A token outside [0, vocab) has no embedding: its row of x is zero, its row of dx has no part in the sums (where such rows stand next to others in
+// the sorted list they are loaded with them, and dropped).  The product is rounded to float32, which a 16-bit plane rounds once more.
 #include "gsr_internal.h"
 #include "gsr_device.h"
 

@@ -140,6 +140,17 @@ def test_lookup_keeps_infinities_and_nan_to_their_tokens(dtype):
     assert bool((x[[3, 5]] == 0).all())
 
 
+def test_lookup_rounds_the_product_to_float32_and_then_to_the_plane():
+    """(1 + 2^-23) (1 + (2^15 - 1) 2^-23) lies 2^-31 above 1 + 2^-8, to which it rounds in float32: half way between the 16-bit values 1 and
+    1 + 2^-7, of which 1 is the even one."""
+    table = torch.full((1, 8), 1 + 2.0 ** -23, device=dev())
+    ids = torch.zeros(1, dtype=torch.int32, device=dev())
+    for dtype, want in ((F32, 1 + 2.0 ** -8), (BF16, 1.0)):
+        x = torch.empty((1, 8), dtype=dtype, device=dev())
+        gsr.gsr_embed_lookup(table, ids, x, 1 + (2 ** 15 - 1) * 2.0 ** -23)
+        assert bool((x.double() == want).all())
+
+
 # sizes around what one workgroup sorts (4,096) and one stretch of the sort holds (2,048), chunks of 16 to 256 rows, one, two and three passes
 # of the sort (vocabularies below 256 and 65,536; 1,024 and 2^20), rows narrower than, as wide as and wider than a piece and a wave
 GRADS = [
