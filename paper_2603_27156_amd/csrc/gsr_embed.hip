@@ -417,9 +417,9 @@ __global__ __launch_bounds__(256) void k_embed_hand_out(Src src, int64_t n, int 
 // where few chunks are left, k_embed_join adds up each run that began in one of them.
 //
 // Bound by the reads of dx.  Those are streamed past the caches (1M rows of 256 floats, chunks of 64: 235 -> 212 us for the whole gradient), and
-// chunks are long, so that about 4,096 waves read ascending rows each: 64 / 128 / 256 rows a chunk 212 / 200 / 190 us.  With 97 tokens the sums of
-// those rows take 158 us (6.5 TB/s, what a read loop reaches here), with 50k tokens 200 (the table's 51 MB are written twice: cleared, then
-// stored); 500k rows of 256 16-bit values with 50k tokens 63 us for 290 MB.
+// chunks are long, so that about 4,096 waves read ascending rows each (16-bit rows, in pieces of eight: half as many): float32 with 64 / 128 / 256
+// rows a chunk 212 / 200 / 190 us.  With 97 tokens the sums of those rows take 159 us (6.5 TB/s; a loop that only reads past the caches 7.1), with 50k
+// tokens 200 (the table's 51 MB are written twice: cleared, then stored); 500k rows of 256 16-bit values with 50k tokens 66 us for 279 MB (1,956 waves).
 struct EmbedSums {
     const void* src;            // FIRST: the plane dx; else partial rows of d floats
     int64_t ld, gs;             // row and group stride
@@ -437,7 +437,11 @@ struct EmbedSums {
     float* part;                // [2 chunks][d]
     int32_t* part_keys;         // [2 chunks], negative: nothing
 };
-constexpr int kSumBatch = 16, kSumLanesMin = 3;                        // (lanes per chunk as a logarithm)
+constexpr int kSumLanesMin = 3;                                        // (lanes per chunk as a logarithm)
+// Partial rows in flight, of a chunk; rows of dx half as many.  Whole gradient with 4 / 8 / 16 rows of dx: 1M rows of 256 floats, 97 tokens 185.1 / 186.4 /
+// 186.4 us, 50,021 tokens 269 / 255 / 244; 500k rows of 256 16-bit values 69.4 / 69.3 / 69.8 and 133 / 125 / 119; 20,000 rows of 64 floats, 40 tokens
+// 20.1 / 19.3 / 19.7; 1M rows of 77 floats 95.8 / 97.1 / 96.5.
+constexpr int kSumBatch = 16;
 constexpr int kSumEntries = 2048;                                      // of a workgroup, at most
 constexpr int kPartChunk = 32;                                         // partial rows per chunk (64: 12.6 us a level, 32: 5.7)
 constexpr int kJoinChunks = 1024;                                      // chunks from which k_embed_join takes over
@@ -851,7 +855,7 @@ EmbedPlan embed_plan(int64_t n, int64_t vocab, int d) {
     p.chunk = 16;
     // so few chunks that they are joined at once: 20,000 rows of 64 floats 26.0 -> 22.6 us; with chunks of 64 60,000 rows take longer, not less
     if (n > 16 * kJoinChunks && n <= 32 * kJoinChunks) p.chunk = 32;
-    while (p.chunk < 256 && p.chunk < (n * d) >> 20 && p.chunk < d) p.chunk *= 2;       // about 4,096 waves, kSumEntries
+    while (p.chunk < 256 && p.chunk < (n * d) >> 20 && p.chunk < d) p.chunk *= 2;       // about 4,096 waves of float32 rows, kSumEntries
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;

@@ -21,15 +21,16 @@ constexpr int kArgBytes = 4096 - 256;           // tensor table of a launch (ker
 // 16,384: norm of 400M 16-bit values (up to 16,384 workgroups, several chunks each) 152 us at 16,384, 139 at 8,192, 130 at 4,096,
 // 175 at 2,048; clipping 201M floats (one chunk per workgroup) 472, 426, 412, 402 us at 2,048; clipped Adam on 120M weights with 16-bit
 // gradients 706, 662, 617, 593 us.  With cached accesses at 8,192: 161, 488 and 726 us.  A tensor found in one round trip (tensor_of):
-// 126 (6.4 TB/s, the rate of a read loop), 397 (two passes over the gradients: 6.1 TB/s) and 586 us (5.7, the norm before it included).
+// 126 (6.4 TB/s; a loop that does nothing else reads 7.1), 397 (two passes over the gradients: 6.1 TB/s) and 586 us (5.7, the norm before it included).
 constexpr int kNormChunk = 4096, kUpdateChunk = 2048;
 constexpr int kMaxPartials = 16384;             // workgroups, hence partial sums, of one launch of the norm
 constexpr double kClipEps = 1e-6;
 // Chunks of which one workgroup takes the norm in one launch. In a captured graph, 4 chunks 4.0 us against 5.0 with two launches, 8: 4.8 / 5.5,
 // 16: 7.1 / 5.6 (with the tensor of a chunk found in one round trip 8: 4.2); a call from Python 9.5 / 12.5.
 constexpr int kSmallNorm = 8;
-// Partial sums that every workgroup of the clipping adds up by itself instead of waiting for a launch that does: 115 tensors of 25,000 (805 partial
-// sums, 1,495 workgroups) 11.7 us against 12.9 in a captured graph, 18 / 21 from Python.
+// Partial sums that every workgroup of the clipping adds up by itself instead of waiting for a launch that does.  In a captured graph, tensors of 28,372
+// floats into others, 14 / 252 / 497 / 798 / 1,015 partial sums 7.4 / 8.7 / 10.9 / 13.3 / 17.9 us against 8.7 / 9.9 / 11.4 / 14.2 / 18.2 with the launch;
+// built for 2,048 of them 1,498 take as long either way (25.3), 2,037 33.8 against 32.9, and 498 11.3.
 constexpr int kClipPartials = 1024;
 
 // The tensors of one launch: P addresses each (gradient; gradient and output; w, dw, m, v).
