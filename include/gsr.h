@@ -364,9 +364,10 @@ gsr_status_t gsr_grad_clip(void* const* grads, const int64_t* counts, int32_t te
                            void* const* out, int32_t out_dtype, void* workspace, size_t workspace_bytes, void* stream);
 
 /* gsr_adam_update on every tensor of a list: w, m, v float32, dw of dw_dtype.  norm (device, 1 float, as gsr_grad_norm leaves it, or NULL):
- * the gradients count multiplied by c as above, without being changed (a norm beyond float32 is infinite here, so c is zero); max_norm is read only with it.  The scalars are doubles and 1 - beta1,
- * 1 - beta2 are rounded to float32 once; gsr_adam_update rounds the betas first, which leaves 1 - 0.999 off by 1.3e-5 of itself.  Where both
- * come to the same numbers (betas such as 0.875) and nothing is clipped, so do the results, bit for bit. */
+ * the gradients count multiplied by c as above, without being changed (a norm beyond float32 is infinite here, so c is zero); max_norm is
+ * read only with it.  The scalars are doubles and 1 - beta1, 1 - beta2 are rounded to float32 once; gsr_adam_update rounds the betas first,
+ * which leaves 1 - 0.999 off by 1.3e-5 of itself.  Where both come to the same numbers (betas such as 0.875) and nothing is clipped, so do
+ * the results, bit for bit. */
 gsr_status_t gsr_adam_update_list(float* const* w, const void* const* dw, float* const* m, float* const* v, const int64_t* counts,
                                   int32_t tensors, int32_t dw_dtype, const float* norm, float max_norm, int64_t t, double lr, double beta1,
                                   double beta2, double eps, double weight_decay, void* stream);
