@@ -372,6 +372,52 @@ gsr_status_t gsr_adam_update_list(float* const* w, const void* const* dw, float*
                                   int32_t tensors, int32_t dw_dtype, const float* norm, float max_norm, int64_t t, double lr, double beta1,
                                   double beta2, double eps, double weight_decay, void* stream);
 
+/* ---- group norm with an activation, channels last, over a batch of graphs ----
+ *
+ * Planes (device, n x d of `dtype`): ROW_MAJOR with row stride ld elements, d at least; GROUP_PLANAR in c groups of d/c columns, row stride ld,
+ * d/c at least, group stride n * ld.  The rows of a graph follow each other: graph s has the rows graph_ptr[s] .. graph_ptr[s+1] - 1.  graph_ptr:
+ * device, graphs + 1 ascending offsets, int32, or int64 with ptr_i64 = 1; NULL with graphs = 1: all rows are one graph.  Graphs may be
+ * empty (mean 0, rstd 1 / sqrt(eps)).  Rows before the first and behind the last graph are not touched in any output and have no part in any sum
+ * (they may be loaded); offsets outside [0, n] count as the border next to them.  `groups` divides d: each has d / groups columns, and may lie
+ * across the C groups of a plane.
+ *
+ * Over the rows of a graph and the columns of a group: m = mean x, r = 1 / sqrt(mean (x - m)^2 + eps); then
+ *   gsr_group_norm:       y = act(gamma_c (x - m) r + beta_c);  gamma, beta: device, d floats, or NULL for 1 and 0;  mean_out, rstd_out: device,
+ *                         graphs x groups floats, m and r.  codes_out, scales_out: NULL, or the checkpoint of x (below), written in the same pass.
+ *   gsr_group_norm_grad:  with xh = (x - m) r, dz = dy act'(gamma xh + beta), h = gamma dz:  dx = r (h - mean h - xh mean(h xh)),
+ *                         dgamma_out = sum dz xh, dbeta_out = sum dz over all graphs (device, d floats, overwritten; either may be NULL).
+ *                         m, r: as gsr_group_norm left them.  x, or with x = NULL its checkpoint, whose values then take the place of x.
+ * RELU has the derivative 0 at 0.  SILU(z) = z / (1 + exp(-z)).  Sums over rows are taken in float64, those of a gradient over up to 1,024 rows in
+ * float32 first, in an order that the sizes and the offsets alone fix.  A mean further than 2^20 standard deviations from zero loses the variance.
+ * y_out may be x and dx_out may be dy, with the same stride; apart from that what a call writes overlaps nothing that it reads.
+ * eps > 0; 1 <= d <= 131072; n < 2^31; pointers aligned to their elements.  workspace: device, 16-byte aligned, at least
+ * gsr_group_norm_workspace() bytes (0: sizes that are refused); it holds nothing between calls.  Calls only launch kernels and may be captured;
+ * calls with workspaces of their own may run side by side. */
+typedef enum gsr_act { GSR_ACT_NONE = 0, GSR_ACT_RELU = 1, GSR_ACT_SILU = 2 } gsr_act_t;
+size_t gsr_group_norm_workspace(int64_t n, int64_t graphs, int32_t d, int32_t c, int32_t layout, int32_t dtype, int32_t groups);
+gsr_status_t gsr_group_norm(const void* x, int64_t ldx, int64_t n, int32_t d, int32_t c, int32_t layout, int32_t dtype, const void* graph_ptr,
+                            int32_t ptr_i64, int64_t graphs, int32_t groups, const float* gamma, const float* beta, float eps, int32_t act,
+                            void* y_out, int64_t ldy, float* mean_out, float* rstd_out, int8_t* codes_out, float* scales_out, void* workspace,
+                            size_t workspace_bytes, void* stream);
+gsr_status_t gsr_group_norm_grad(const void* dy, int64_t lddy, const void* x, int64_t ldx, const int8_t* codes, const float* scales, int64_t n,
+                                 int32_t d, int32_t c, int32_t layout, int32_t dtype, const void* graph_ptr, int32_t ptr_i64, int64_t graphs,
+                                 int32_t groups, const float* mean, const float* rstd, const float* gamma, const float* beta, int32_t act,
+                                 void* dx_out, int64_t lddx, float* dgamma_out, float* dbeta_out, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+
+/* ---- activation checkpoints in 8 bits ----
+ *
+ * What a backward pass needs of a plane, in 1.06 bytes a value.  Every row's columns are cut into blocks of 64 from the start of each of the c groups
+ * of a GROUP_PLANAR plane (of the row, of a ROW_MAJOR one), the last block of a group with what is left.  With A = max(max |x|, 127 * 2^-126) over a
+ * block: codes = 127 x / A to the nearest whole number, ties to even, exactly; scales = A / 127 (at most the float of which 127 times is finite).  codes: device, n x d, one byte each, the columns
+ * in their order whatever the layout; scales: device, n x (c or 1) * ceil(columns of a group / 64) floats; both contiguous and 4-byte aligned.  A value
+ * comes back as code * scale (off by at most A / 254 and two roundings).  A block with an infinity or NaN comes back as NaN.
+ * Planes and limits as above; calls only launch kernels and may be captured. */
+gsr_status_t gsr_checkpoint_save(const void* x, int64_t ldx, int64_t n, int32_t d, int32_t c, int32_t layout, int32_t dtype, int8_t* codes_out,
+                                 float* scales_out, void* stream);
+gsr_status_t gsr_checkpoint_load(const int8_t* codes, const float* scales, int64_t n, int32_t d, int32_t c, int32_t layout, int32_t dtype,
+                                 void* x_out, int64_t ldx, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

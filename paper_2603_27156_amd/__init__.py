@@ -27,6 +27,8 @@ GSR_NORM_NONE, GSR_NORM_RMS = 0, 1
 GSR_LAYOUT_ROW_MAJOR, GSR_LAYOUT_GROUP_PLANAR = 0, 1
 GSR_GRAPH_SYMMETRISE, GSR_GRAPH_ADD_SELF_LOOPS, GSR_GRAPH_GCN_NORM, GSR_GRAPH_ROWPTR_I64 = 1, 2, 4, 8
 GSR_ADJ_UNIT, GSR_ADJ_GCN_SYM = 0, 1
+GSR_ACT_NONE, GSR_ACT_RELU, GSR_ACT_SILU = 0, 1, 2
+GSR_CHECKPOINT_BLOCK = 64
 
 EXPORTED = [
     "gsr_last_error", "gsr_version", "gsr_set_option", "gsr_profile_read", "gsr_profile_reset",
@@ -38,6 +40,7 @@ EXPORTED = [
     "gsr_sgd_update", "gsr_adam_update",
     "gsr_embed_lookup", "gsr_embed_grad_workspace", "gsr_embed_grad",
     "gsr_grad_norm_workspace", "gsr_grad_norm", "gsr_grad_clip", "gsr_adam_update_list",
+    "gsr_group_norm_workspace", "gsr_group_norm", "gsr_group_norm_grad", "gsr_checkpoint_save", "gsr_checkpoint_load",
 ]
 
 
@@ -86,6 +89,12 @@ def lib():
         l.gsr_grad_norm.argtypes = [p, p, i32, i32, p, p, size, p]
         l.gsr_grad_clip.argtypes = [p, p, i32, i32, f32, p, p, i32, p, size, p]
         l.gsr_adam_update_list.argtypes = [p, p, p, p, p, i32, i32, p, f32, i64, *[C.c_double] * 5, p]
+        l.gsr_group_norm_workspace.restype = size
+        l.gsr_group_norm_workspace.argtypes = [i64, i64, i32, i32, i32, i32, i32]
+        l.gsr_group_norm.argtypes = [p, i64, i64, i32, i32, i32, i32, p, i32, i64, i32, p, p, f32, i32, p, i64, p, p, p, p, p, size, p]
+        l.gsr_group_norm_grad.argtypes = [p, i64, p, i64, p, p, i64, i32, i32, i32, i32, p, i32, i64, i32, p, p, p, p, i32, p, i64, p, p, p, size, p]
+        l.gsr_checkpoint_save.argtypes = [p, i64, i64, i32, i32, i32, i32, p, p, p]
+        l.gsr_checkpoint_load.argtypes = [p, p, i64, i32, i32, i32, i32, p, i64, p]
         _lib = l
     return _lib
 
@@ -485,6 +494,117 @@ def gsr_adam_update_list(w, dw, m, v, t: int, lr: float, beta1: float = 0.9, bet
     ag, am, av = (_addresses(x, k, dev, counts)[0] for x, k in ((dw, dtype), (m, GSR_F32), (v, GSR_F32)))
     _check(lib().gsr_adam_update_list(_at(aw), _at(ag), _at(am), _at(av), _at(counts), len(counts), dtype, _scalar(norm, dev), max_norm or 0.0, t, lr,
                                       beta1, beta2, eps, weight_decay, _stream()))
+
+
+def _like_plane(x, dev: int, n: int, d: int, c: int, layout: int, dtype) -> int:
+    """Row stride of a plane that has to be of the same rows, columns, layout and type as another."""
+    assert x.dtype == dtype
+    n2, d2, c2, layout2, ld = _plane(x, dev)
+    assert (n2, d2, c2, layout2) == (n, d, c, layout)
+    return ld
+
+
+def _floats(t, dev: int, shape) -> int:
+    """Address of a contiguous float32 tensor of this shape, or 0 for None."""
+    if t is None:
+        return 0
+    import torch
+    assert t.get_device() == dev and t.dtype == torch.float32 and t.shape == shape and t.is_contiguous()
+    return t.data_ptr()
+
+
+def _checkpoint(codes, scales, dev: int, n: int, d: int, c: int):
+    """Addresses of a checkpoint of n rows of d columns in c groups, (0, 0) for none."""
+    if codes is None and scales is None:
+        return 0, 0
+    import torch
+    assert codes is not None and scales is not None and codes.get_device() == dev and codes.dtype == torch.int8
+    assert codes.shape == (n, d) and codes.is_contiguous()
+    return codes.data_ptr(), _floats(scales, dev, (n, gsr_checkpoint_blocks(d, c)))
+
+
+def _graph_ptr(graph_ptr, dev: int):
+    """(address, whether of 64 bits, graphs)."""
+    if graph_ptr is None:
+        return 0, 0, 1
+    assert graph_ptr.dim() == 1 and len(graph_ptr) >= 1
+    return graph_ptr.data_ptr(), _tokens(graph_ptr, len(graph_ptr), dev), len(graph_ptr) - 1
+
+
+def gsr_group_norm_workspace(x, groups: int, graph_ptr=None) -> int:
+    """Bytes of workspace that gsr_group_norm and gsr_group_norm_grad need for a plane like x."""
+    n, d, c, layout, _ = _plane(x, x.get_device())
+    return lib().gsr_group_norm_workspace(n, 1 if graph_ptr is None else len(graph_ptr) - 1, d, c, layout, _dtype_of(x), groups)
+
+
+def _norm_scratch(workspace, n: int, graphs: int, d: int, c: int, layout: int, dtype: int, groups: int, dev: int):
+    if workspace is None:
+        import torch
+        workspace = torch.empty(lib().gsr_group_norm_workspace(n, graphs, d, c, layout, dtype, groups), dtype=torch.uint8, device="cuda")
+    assert workspace.get_device() == dev and workspace.is_contiguous()
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def gsr_group_norm(x, y_out, mean_out, rstd_out, gamma=None, beta=None, eps: float = 1e-5, act: int = GSR_ACT_NONE, graph_ptr=None,
+                   codes_out=None, scales_out=None, workspace=None) -> None:
+    """y_out = act(gamma * (x - mean) * rstd + beta), mean and 1 / sqrt(variance + eps) over the rows of a graph and the columns of a group.
+
+    x, y_out: planes [n, D] (rows may be strided) or [C, n, D/C], both float32 or both bfloat16; y_out may be x.  mean_out, rstd_out: float32
+    [graphs, groups].  gamma, beta: float32 [D].  graph_ptr: [graphs + 1] int32 or int64, first rows of the graphs; None: one graph of all rows.
+    Rows of no graph are left as they are.  codes_out, scales_out: also the checkpoint of x, as gsr_checkpoint_save leaves it."""
+    dev = _current_device()
+    n, d, c, layout, ldx = _plane(x, dev)
+    dtype = _dtype_of(x)
+    ldy = _like_plane(y_out, dev, n, d, c, layout, x.dtype)
+    at, i64, graphs = _graph_ptr(graph_ptr, dev)
+    groups = mean_out.shape[-1]
+    codes, scales = _checkpoint(codes_out, scales_out, dev, n, d, c)
+    ws, nb = _norm_scratch(workspace, n, graphs, d, c, layout, dtype, groups, dev)
+    _check(lib().gsr_group_norm(x.data_ptr(), ldx, n, d, c, layout, dtype, at, i64, graphs, groups, _floats(gamma, dev, (d,)), _floats(beta, dev, (d,)),
+                                eps, act, y_out.data_ptr(), ldy, _floats(mean_out, dev, (graphs, groups)), _floats(rstd_out, dev, (graphs, groups)),
+                                codes, scales, ws.data_ptr(), nb, _stream()))
+
+
+def gsr_group_norm_grad(dy, mean, rstd, dx_out, x=None, codes=None, scales=None, gamma=None, beta=None, act: int = GSR_ACT_NONE, graph_ptr=None,
+                        dgamma_out=None, dbeta_out=None, workspace=None) -> None:
+    """The gradients of gsr_group_norm: dx_out (a plane as dy, may be dy), dgamma_out and dbeta_out (float32 [D], or None), from mean and rstd as
+    it left them and x, or x's checkpoint (codes, scales) in its place."""
+    dev = _current_device()
+    n, d, c, layout, lddy = _plane(dy, dev)
+    dtype = _dtype_of(dy)
+    lddx = _like_plane(dx_out, dev, n, d, c, layout, dy.dtype)
+    assert (x is None) != (codes is None), "x or its checkpoint"
+    ldx = 0 if x is None else _like_plane(x, dev, n, d, c, layout, dy.dtype)
+    at, i64, graphs = _graph_ptr(graph_ptr, dev)
+    groups = mean.shape[-1]
+    k, s = _checkpoint(codes, scales, dev, n, d, c)
+    ws, nb = _norm_scratch(workspace, n, graphs, d, c, layout, dtype, groups, dev)
+    _check(lib().gsr_group_norm_grad(dy.data_ptr(), lddy, 0 if x is None else x.data_ptr(), ldx, k, s, n, d, c, layout, dtype, at, i64, graphs, groups,
+                                     _floats(mean, dev, (graphs, groups)), _floats(rstd, dev, (graphs, groups)), _floats(gamma, dev, (d,)),
+                                     _floats(beta, dev, (d,)), act, dx_out.data_ptr(), lddx, _floats(dgamma_out, dev, (d,)), _floats(dbeta_out, dev, (d,)),
+                                     ws.data_ptr(), nb, _stream()))
+
+
+def gsr_checkpoint_blocks(d: int, c: int = 1) -> int:
+    """Scales of a row in a checkpoint of planes [n, d] (c = 1) or [c, n, d / c]."""
+    return c * -(-(d // c) // GSR_CHECKPOINT_BLOCK)
+
+
+def gsr_checkpoint_save(x, codes_out, scales_out) -> None:
+    """A plane ([n, D], rows may be strided, or [C, n, D/C]; float32 or bfloat16) in 8 bits: codes_out int8 [n, D], scales_out float32
+    [n, gsr_checkpoint_blocks(D, C)]."""
+    dev = _current_device()
+    n, d, c, layout, ldx = _plane(x, dev)
+    codes, scales = _checkpoint(codes_out, scales_out, dev, n, d, c)
+    _check(lib().gsr_checkpoint_save(x.data_ptr(), ldx, n, d, c, layout, _dtype_of(x), codes, scales, _stream()))
+
+
+def gsr_checkpoint_load(codes, scales, x_out) -> None:
+    """The plane that gsr_checkpoint_save put away, every value as code * scale."""
+    dev = _current_device()
+    n, d, c, layout, ldx = _plane(x_out, dev)
+    k, s = _checkpoint(codes, scales, dev, n, d, c)
+    _check(lib().gsr_checkpoint_load(k, s, n, d, c, layout, _dtype_of(x_out), x_out.data_ptr(), ldx, _stream()))
 
 
 def gsr_spmm_compressed(g: Graph, vals, idx, dg: int):

@@ -1,0 +1,892 @@
+// Group norm with an activation over a batch of graphs, channels last, its gradient, and activation checkpoints in 8 bits.
+//
+// Rows of a plane belong to graphs, one behind the other; the d columns are cut into `groups` groups of cg.  Over the rows of a graph and
+// the columns of a group
+//   m = mean x,  r = 1 / sqrt(mean (x - m)^2 + eps),  xh = (x - m) r,  y = act(gamma xh + beta)
+//   dz = dy act'(gamma xh + beta),  h = gamma dz,  dx = r (h - mean h - xh mean(h xh)),  dgamma = sum dz xh,  dbeta = sum dz.
+// A checkpoint holds a row's columns in blocks of up to 64: with A = max |x| (at least 127 * 2^-126) the codes are 127 x / A rounded to the
+// nearest whole number, ties to even, and the block's scale is A / 127.
+//
+// Both directions are two passes over the rows, sums first: a wave takes `rows` consecutive rows of one slab of columns, keeps the sums of
+// its columns in registers, and leaves one pair of sums for every (graph, group) that it met.  Those pairs ("pieces") are joined by a launch
+// between the passes, in an order that the sizes and the graphs alone fix.
+#include "gsr_internal.h"
+#include "gsr_pieces.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace gsr {
+
+constexpr int kBlock = 64;                      // columns that share the scale of a checkpoint
+constexpr float kSmallestTop = 127.0f * 0x1p-126f;
+constexpr float kLargestScale = 0x1.020406p+121f;       // the largest float of which 127 times is one
+
+// First rows of the graphs, ascending, int32 or int64; NULL: one graph of all rows.  What lies outside the plane counts as its border, so that
+// no offsets lead out of it.
+struct GraphRows {
+    const void* ptr;
+    int32_t i64;
+    int64_t graphs, n;
+    __device__ __forceinline__ int64_t at(int64_t s) const {
+        if (!ptr) return s ? n : 0;
+        const int64_t v = i64 ? static_cast<const int64_t*>(ptr)[s] : static_cast<const int32_t*>(ptr)[s];
+        return v < 0 ? 0 : v > n ? n : v;
+    }
+};
+
+// How rows and columns are dealt out.  Columns go to lanes in pieces of V; 2^lanes_log2 lanes hold a slab of a row and the wave 64 >> lanes_log2
+// rows at a time.  A slab never crosses the border of a plane of a GROUP_PLANAR tensor.
+struct NormShape {
+    int64_t n, chunks;              // chunks of `rows` rows, one per wave
+    int32_t d, dg, cg, groups;
+    int32_t lanes_log2, group_slabs, slabs;     // slabs of one plane, and of all
+    int32_t rows;
+    __host__ __device__ int64_t stride() const { return slabs + groups; }       // pieces of one graph in one chunk
+};
+struct RowPlane {
+    int64_t ld, gs;                 // elements between rows, between planes
+};
+
+// What a lane holds of its slab.
+struct LaneColumns {
+    int sub, subs;                  // its row of the wave's, and how many there are
+    int plane, col;                 // plane and first column of it
+    int column;                     // the same in the whole row of d
+    int group;                      // the group of all its columns; -1 for a lane without columns
+    bool on, head;                  // head: the first lane of its group in the slab
+    uint32_t joins;                 // bit k: the lane 2^k further holds columns of the same group
+};
+template <int V>
+__device__ __forceinline__ LaneColumns lane_columns(const NormShape& s, int slab) {
+    LaneColumns c;
+    const int lanes = 1 << s.lanes_log2, lane = lane_id(), li = lane & (lanes - 1);
+    c.sub = lane >> s.lanes_log2;
+    c.subs = 64 >> s.lanes_log2;
+    c.plane = slab / s.group_slabs;
+    const int first = (slab - c.plane * s.group_slabs) * lanes * V;
+    auto group = [&](int l) {
+        const int col = first + l * V;
+        return l >= 0 && l < lanes && col < s.dg ? (c.plane * s.dg + col) / s.cg : -1;
+    };
+    c.col = first + li * V;
+    c.on = c.col < s.dg;
+    if (!c.on) c.col = 0;
+    c.column = c.plane * s.dg + c.col;
+    c.group = group(li);
+    c.head = c.on && group(li - 1) != c.group;
+    c.joins = 0;
+    for (int k = 0; k < s.lanes_log2; ++k) c.joins |= (uint32_t)(c.on && group(li + (1 << k)) == c.group) << k;
+    return c;
+}
+
+// The first graph that ends behind `row` (g.graphs if none does): the wave's lanes probe 64 borders at a time.
+__device__ __forceinline__ int64_t graph_of(const GraphRows& g, int64_t row) {
+    int64_t lo = 0, len = g.graphs;             // it is one of [lo, lo + len], and lo + len if none of [lo, lo + len) does
+    while (len > 0) {
+        const int64_t step = (len + 63) >> 6, begin = lane_id() * step, end = begin + step < len ? begin + step : len;
+        const uint64_t behind = ballot(begin < len && g.at(lo + (begin < len ? end : len)) > row);      // by the last of each lane's graphs
+        if (!behind) break;
+        const int64_t skip = __builtin_ctzll(behind) * step;
+        lo += skip;
+        len = (step < len - skip ? step : len - skip) - 1;
+    }
+    return lo + len;
+}
+
+// body(graph, a, b) for the rows [a, b) of every graph that has some in chunk w
+template <typename Body>
+__device__ __forceinline__ void over_graphs(const NormShape& s, const GraphRows& g, int64_t w, Body body) {
+    const int64_t r0 = w * s.rows, r1 = r0 + s.rows < s.n ? r0 + s.rows : s.n;
+    for (int64_t i = g.ptr ? graph_of(g, r0) : 0; i < g.graphs; ++i) {
+        const int64_t first = g.at(i), last = g.at(i + 1);
+        if (first >= r1) break;
+        const int64_t a = first > r0 ? first : r0, b = last < r1 ? last : r1;
+        if (a < b) body(i, a, b);
+    }
+}
+
+// The sums over a group's columns in the slab and over the wave's rows, in the group's first lane.
+__device__ __forceinline__ void join_lanes(const NormShape& s, const LaneColumns& c, double& u, double& v) {
+    for (int o = 1 << s.lanes_log2; o < 64; o <<= 1) {
+        u += __shfl_xor(u, o);
+        v += __shfl_xor(v, o);
+    }
+    for (int k = 0; k < s.lanes_log2; ++k) {
+        const double a = __shfl_down(u, 1 << k), b = __shfl_down(v, 1 << k);
+        if (c.joins >> k & 1) {
+            u += a;
+            v += b;
+        }
+    }
+}
+__device__ __forceinline__ void leave_piece(const NormShape& s, const LaneColumns& c, int slab, int64_t w, int64_t graph, double u, double v,
+                                            double2* __restrict__ pieces) {
+    join_lanes(s, c, u, v);
+    // chunks and graphs both go up along the rows, slabs and groups along the columns: the sums of two indices name a piece
+    if (c.head && c.sub == 0) pieces[(w + graph) * s.stride() + slab + c.group] = make_double2(u, v);
+}
+
+// Pieces of (graph, group) added up by `threads` threads, of which this is `thread`.
+__device__ __forceinline__ void add_pieces(const NormShape& s, const GraphRows& g, int V, int64_t graph, int group, int thread, int threads,
+                                           const double2* __restrict__ pieces, double& u, double& v, int64_t& rows) {
+    const int64_t first = g.at(graph), last = g.at(graph + 1);
+    u = v = 0.0;
+    rows = last > first ? last - first : 0;
+    if (!rows) return;
+    const int width = V << s.lanes_log2;
+    auto slab_of = [&](int column) { return column / s.dg * s.group_slabs + column % s.dg / width; };
+    const int s0 = slab_of(group * s.cg), count = slab_of(group * s.cg + s.cg - 1) - s0 + 1;
+    const int64_t w0 = first / s.rows, all = ((last - 1) / s.rows - w0 + 1) * count;
+    constexpr int U = 4;
+    for (int64_t i = thread; i < all; i += U * threads) {
+        double2 p[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int64_t j = i + (int64_t)k * threads < all ? i + (int64_t)k * threads : i;
+            p[k] = pieces[(w0 + j / count + graph) * s.stride() + s0 + j % count + group];
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const bool in = i + (int64_t)k * threads < all;
+            u += in ? p[k].x : 0.0;
+            v += in ? p[k].y : 0.0;
+        }
+    }
+}
+__device__ __forceinline__ double wave_total(double v) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+// (graph, group) of this wave (WIDE: of this workgroup of 256) and the sums of its pieces, in every lane of (the first) wave; false: no task
+template <bool WIDE>
+__device__ __forceinline__ bool joined(const NormShape& s, const GraphRows& g, int V, int64_t block, const double2* __restrict__ pieces,
+                                       int64_t& task, double& u, double& v, int64_t& rows) {
+    task = WIDE ? block : block * 4 + (threadIdx.x >> 6);
+    if (task >= g.graphs * s.groups) return false;      // (WIDE: the whole workgroup or none)
+    add_pieces(s, g, V, task / s.groups, (int)(task % s.groups), WIDE ? threadIdx.x : lane_id(), WIDE ? 256 : 64, pieces, u, v, rows);
+    u = wave_total(u);
+    v = wave_total(v);
+    if constexpr (WIDE) {
+        __shared__ double s_sum[4][2];
+        if (lane_id() == 0) {
+            s_sum[threadIdx.x >> 6][0] = u;
+            s_sum[threadIdx.x >> 6][1] = v;
+        }
+        __syncthreads();
+        if (threadIdx.x >= 64) return false;
+        u = (s_sum[0][0] + s_sum[1][0]) + (s_sum[2][0] + s_sum[3][0]);
+        v = (s_sum[0][1] + s_sum[1][1]) + (s_sum[2][1] + s_sum[3][1]);
+    }
+    return true;
+}
+
+// ---- 8 bits ----------------------------------------------------------------------------------------------
+// The largest over the 2^k >= 4 neighbouring lanes that share a block.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_umax(uint32_t v) {
+    const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true);
+    return v > o ? v : o;
+}
+__device__ __forceinline__ uint32_t lanes_umax(uint32_t v, int lanes) {
+    v = dpp_umax<0xB1>(v);          // quad_perm [1,0,3,2]
+    v = dpp_umax<0x4E>(v);          // quad_perm [2,3,0,1]
+    if (lanes > 4) v = dpp_umax<0x141>(v);              // row_half_mirror
+    if (lanes > 8) v = dpp_umax<0x140>(v);              // row_mirror
+    if (lanes > 16) {
+        const uint32_t o = __shfl_xor(v, 16);
+        v = v > o ? v : o;
+    }
+    if (lanes > 32) {
+        const uint32_t o = __shfl_xor(v, 32);
+        v = v > o ? v : o;
+    }
+    return v;
+}
+// 127 x / top to the nearest whole number, ties to even, exactly: x * (127 / top) in 32 bits is off by less than 127 * 2^-22, and where it
+// lies that near to a border the exact products decide (16-bit values are half of the largest, a tie, all the time).
+__device__ __forceinline__ int code_of(float x, float top, float inv) {
+    const float t = x * inv;
+    float q = __builtin_rintf(t);
+    const float f = t - q;
+    if (fabsf(f) >= 0.5f - 0x1p-14f) {
+        const float side = copysignf(1.0f, f);
+        const double over = (double)side * fma(127.0, (double)x, -(double)(q + 0.5f * side) * (double)top);      // (the second product is exact)
+        if (over > 0.0 || (over == 0.0 && ((int)q & 1))) q += side;
+    }
+    return (int)q;
+}
+template <int V>
+__device__ __forceinline__ void store_codes(int8_t* p, const int (&q)[V]) {
+    if constexpr (V == 1) {
+        *p = (int8_t)q[0];
+    } else {
+        typedef uint32_t words __attribute__((ext_vector_type(V / 4), aligned(4)));
+        words t;
+#pragma unroll
+        for (int i = 0; i < V / 4; ++i)
+            t[i] = (q[4 * i] & 0xFF) | (q[4 * i + 1] & 0xFF) << 8 | (q[4 * i + 2] & 0xFF) << 16 | (uint32_t)q[4 * i + 3] << 24;
+        __builtin_nontemporal_store(t, reinterpret_cast<words*>(p));
+    }
+}
+struct Checkpoint {
+    int8_t* codes;                  // [n][d]
+    float* scales;                  // [n][blocks]
+    int32_t blocks, plane_blocks;   // of a row, of a plane's part of it
+};
+// The codes of a lane's V values; every lane of the wave takes part.
+template <int V>
+__device__ __forceinline__ void save_piece(const Checkpoint& k, const NormShape& s, const LaneColumns& c, int64_t row, bool in, const float (&x)[V]) {
+    uint32_t bits = 0;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const uint32_t b = __float_as_uint(x[j]) & 0x7FFFFFFFu;         // an infinity is above every number, NaN above that
+        bits = bits > b ? bits : b;
+    }
+    if (!c.on) bits = 0;
+    const int lanes = 1 << s.lanes_log2;
+    bits = lanes_umax(bits, lanes < kBlock / V ? lanes : kBlock / V);
+    const bool finite = bits < 0x7F800000u;
+    const float top = fmaxf(__uint_as_float(finite ? bits : 0u), kSmallestTop), inv = 127.0f / top;
+    if (!in || !c.on) return;
+    int q[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) q[j] = finite ? code_of(x[j], top, inv) : 0;
+    store_codes<V>(k.codes + row * s.d + c.column, q);
+    if (c.col % kBlock == 0)
+        k.scales[row * k.blocks + c.plane * k.plane_blocks + c.col / kBlock] = finite ? fminf(top / 127.0f, kLargestScale) : __builtin_nanf("");
+}
+
+// Where the values of a plane come from: the plane, or its checkpoint.
+template <typename T, int V, bool STREAM>
+struct PlaneSource {
+    const T* x;
+    RowPlane p;
+    Piece<T, V> w;
+    __device__ __forceinline__ void load(const NormShape&, const LaneColumns& c, int64_t row) {
+        w.template load<STREAM>(x + c.plane * p.gs + row * p.ld + c.col);
+    }
+    __device__ __forceinline__ float at(int j) const { return w.at(j); }
+};
+template <int V>
+struct CodeSource {
+    Checkpoint k;
+    uint32_t w[V == 1 ? 1 : V / 4];
+    float scale;
+    __device__ __forceinline__ void load(const NormShape& s, const LaneColumns& c, int64_t row) {
+        const int8_t* p = k.codes + row * s.d + c.column;
+        if constexpr (V == 1) {
+            w[0] = (uint8_t)*p;
+        } else {
+            typedef uint32_t words __attribute__((ext_vector_type(V / 4), aligned(4)));
+            const words t = *reinterpret_cast<const words*>(p);
+#pragma unroll
+            for (int i = 0; i < V / 4; ++i) w[i] = t[i];
+        }
+        scale = k.scales[row * k.blocks + c.plane * k.plane_blocks + c.col / kBlock];
+    }
+    __device__ __forceinline__ float at(int j) const { return (float)(int8_t)(w[j >> 2] >> 8 * (j & 3)) * scale; }
+};
+
+// ---- forward ---------------------------------------------------------------------------------------------
+// Sums of x and x^2 in 64 bits: squares are exact there, and the difference mean x^2 - m^2 keeps the variance as long as the mean is within some
+// 2^20 standard deviations of zero.
+template <typename T, int V>
+__global__ __launch_bounds__(256) void k_norm_sums(NormShape s, GraphRows g, const T* __restrict__ x, RowPlane p, double2* __restrict__ pieces) {
+    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (w >= s.chunks) return;
+    const int slab = blockIdx.y;
+    const LaneColumns c = lane_columns<V>(s, slab);
+    over_graphs(s, g, w, [&](int64_t graph, int64_t a, int64_t b) {
+        constexpr int U = 4;
+        double u = 0.0, v = 0.0;
+        for (int64_t r = a; r < b; r += U * c.subs) {
+            PlaneSource<T, V, false> q[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int64_t row = r + k * c.subs + c.sub;
+                q[k].x = x;
+                q[k].p = p;
+                q[k].load(s, c, row < b ? row : a);
+            }
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const bool in = r + k * c.subs + c.sub < b;
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const double t = in ? (double)q[k].at(j) : 0.0;
+                    u += t;
+                    v = fma(t, t, v);
+                }
+            }
+        }
+        leave_piece(s, c, slab, w, graph, u, v, pieces);
+    });
+}
+template <bool WIDE>
+__global__ __launch_bounds__(256) void k_norm_join(NormShape s, GraphRows g, int V, const double2* __restrict__ pieces, double eps,
+                                                   float* __restrict__ mean, float* __restrict__ rstd) {
+    int64_t task, rows;
+    double u, v;
+    if (!joined<WIDE>(s, g, V, blockIdx.x, pieces, task, u, v, rows)) return;
+    if (lane_id()) return;
+    const double count = (double)rows * s.cg, m = rows ? u / count : 0.0, var = rows ? v / count - m * m : 0.0;
+    mean[task] = (float)m;
+    rstd[task] = (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + eps));     // (NaN stays NaN)
+}
+
+__device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
+template <int ACT>
+__device__ __forceinline__ float activation(float z) {
+    if constexpr (ACT == GSR_ACT_RELU) return z < 0.0f ? 0.0f : z;
+    else if constexpr (ACT == GSR_ACT_SILU) return z * logistic(z);
+    else return z;
+}
+template <int V>
+__device__ __forceinline__ void load_affine(const float* __restrict__ p, const LaneColumns& c, float other, float (&v)[V]) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = p ? p[c.column + j] : other;
+}
+struct Affine {
+    const float *gamma, *beta, *mean, *rstd;
+};
+
+template <typename T, int V, int ACT, bool SAVE>
+__global__ __launch_bounds__(256) void k_norm_apply(NormShape s, GraphRows g, const T* x, RowPlane p, Affine f, T* y, RowPlane py, Checkpoint ck) {
+    const int64_t w = s.chunks - 1 - ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6));        // backwards: what was read last may still be cached
+    if (w < 0) return;
+    const LaneColumns c = lane_columns<V>(s, blockIdx.y);
+    float gamma[V], beta[V];
+    load_affine<V>(f.gamma, c, 1.0f, gamma);
+    load_affine<V>(f.beta, c, 0.0f, beta);
+    over_graphs(s, g, w, [&](int64_t graph, int64_t a, int64_t b) {
+        constexpr int U = 4;
+        const int64_t at = graph * s.groups + (c.on ? c.group : 0);
+        const float m = f.mean[at], rs = f.rstd[at];
+        for (int64_t r = a; r < b; r += U * c.subs) {
+            PlaneSource<T, V, true> q[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int64_t row = r + k * c.subs + c.sub;
+                q[k].x = x;
+                q[k].p = p;
+                q[k].load(s, c, row < b ? row : a);
+            }
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int64_t row = r + k * c.subs + c.sub;
+                float v[V];
+                if constexpr (SAVE) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) v[j] = q[k].at(j);
+                    save_piece<V>(ck, s, c, row, row < b, v);
+                }
+#pragma unroll
+                for (int j = 0; j < V; ++j) v[j] = activation<ACT>((q[k].at(j) - m) * rs * gamma[j] + beta[j]);
+                if (row < b && c.on) store_piece<V, true>(y + c.plane * py.gs + row * py.ld + c.col, v);
+            }
+        }
+    });
+}
+
+// ---- backward --------------------------------------------------------------------------------------------
+// dz = dy act'(z).  Which side of zero z lies on is decided in 64 bits: in 32 one value in ten million falls on the other one.
+template <int ACT>
+__device__ __forceinline__ float before_activation(float dy, float x, float xh, float m, float rs, float gamma, float beta) {
+    if constexpr (ACT == GSR_ACT_RELU) {
+        const double z = fma(((double)x - (double)m) * (double)rs, (double)gamma, (double)beta);
+        return z > 0.0 ? dy : z <= 0.0 ? 0.0f : (float)z;               // (NaN stays NaN)
+    } else if constexpr (ACT == GSR_ACT_SILU) {
+        const float z = xh * gamma + beta, l = logistic(z);
+        return dy * (l * (1.0f + z * (1.0f - l)));
+    } else {
+        return dy;
+    }
+}
+
+// Sums of a chunk in 32 bits (`rows` of a column at most), joined in 64.  columns: [workgroups][2][d], sums of dz xh and of dz.
+template <typename T, int V, int ACT, typename Source>
+__global__ __launch_bounds__(256) void k_norm_grad_sums(NormShape s, GraphRows g, const T* __restrict__ dy, RowPlane pd, Source source, Affine f,
+                                                        double2* __restrict__ pieces, float* __restrict__ columns) {
+    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int slab = blockIdx.y;
+    const LaneColumns c = lane_columns<V>(s, slab);
+    float all_x[V], all_z[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) all_x[j] = all_z[j] = 0.0f;
+    if (w < s.chunks) {
+        float gamma[V], beta[V];
+        load_affine<V>(f.gamma, c, 1.0f, gamma);
+        load_affine<V>(f.beta, c, 0.0f, beta);
+        over_graphs(s, g, w, [&](int64_t graph, int64_t a, int64_t b) {
+            constexpr int U = 2;
+            const int64_t at = graph * s.groups + (c.on ? c.group : 0);
+            const float m = f.mean[at], rs = f.rstd[at];
+            float sum_x[V], sum_z[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum_x[j] = sum_z[j] = 0.0f;
+            for (int64_t r = a; r < b; r += U * c.subs) {
+                PlaneSource<T, V, false> e[U];
+                Source q[U];
+#pragma unroll
+                for (int k = 0; k < U; ++k) {
+                    const int64_t row = r + k * c.subs + c.sub, have = row < b ? row : a;
+                    e[k].x = dy;
+                    e[k].p = pd;
+                    e[k].load(s, c, have);
+                    q[k] = source;
+                    q[k].load(s, c, have);
+                }
+#pragma unroll
+                for (int k = 0; k < U; ++k) {
+                    const bool in = r + k * c.subs + c.sub < b;
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        const float x = q[k].at(j), xh = (x - m) * rs;
+                        const float dz = before_activation<ACT>(e[k].at(j), x, xh, m, rs, gamma[j], beta[j]);
+                        sum_z[j] += in ? dz : 0.0f;
+                        sum_x[j] += in ? dz * xh : 0.0f;
+                    }
+                }
+            }
+            double u = 0.0, v = 0.0;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                u = fma((double)gamma[j], (double)sum_z[j], u);
+                v = fma((double)gamma[j], (double)sum_x[j], v);
+                all_z[j] += sum_z[j];
+                all_x[j] += sum_x[j];
+            }
+            leave_piece(s, c, slab, w, graph, u, v, pieces);
+        });
+    }
+    __shared__ float s_col[4][2][64 * V];
+    const int lanes = 1 << s.lanes_log2, li = lane_id() & (lanes - 1);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        for (int o = lanes; o < 64; o <<= 1) {
+            all_x[j] += __shfl_xor(all_x[j], o);
+            all_z[j] += __shfl_xor(all_z[j], o);
+        }
+        if (c.sub == 0) {
+            s_col[threadIdx.x >> 6][0][li * V + j] = all_x[j];
+            s_col[threadIdx.x >> 6][1][li * V + j] = all_z[j];
+        }
+    }
+    __syncthreads();
+    const int first = (slab % s.group_slabs) * lanes * V, plane = slab / s.group_slabs;
+    for (int i = threadIdx.x; i < 2 * lanes * V; i += 256) {
+        const int which = i >= lanes * V, k = which ? i - lanes * V : i;
+        if (first + k >= s.dg) continue;
+        columns[((int64_t)blockIdx.x * 2 + which) * s.d + plane * s.dg + first + k] =
+            (s_col[0][which][k] + s_col[1][which][k]) + (s_col[2][which][k] + s_col[3][which][k]);
+    }
+}
+
+// The first `task_blocks` workgroups join the pieces: means of h and of h xh of every (graph, group).  The others add up 16 columns of
+// dgamma and dbeta each, with 16 threads a column.
+template <bool WIDE>
+__global__ __launch_bounds__(256) void k_norm_grad_join(NormShape s, GraphRows g, int V, const double2* __restrict__ pieces, int64_t task_blocks,
+                                                        float2* __restrict__ means, const float* __restrict__ columns, int64_t parts,
+                                                        float* __restrict__ dgamma, float* __restrict__ dbeta) {
+    if ((int64_t)blockIdx.x < task_blocks) {
+        int64_t task, rows;
+        double u, v;
+        if (!joined<WIDE>(s, g, V, blockIdx.x, pieces, task, u, v, rows) || lane_id()) return;
+        const double count = (double)rows * s.cg;
+        means[task] = rows ? make_float2((float)(u / count), (float)(v / count)) : make_float2(0.0f, 0.0f);
+        return;
+    }
+    __shared__ double s_part[16][16];
+    const int64_t block = blockIdx.x - task_blocks;
+    const int col = (int)(block * 16 + (threadIdx.x & 15)), k = threadIdx.x >> 4;       // of 2 d: dgamma's columns, then dbeta's
+    double sum = 0.0;
+    if (col < 2 * s.d) {
+        constexpr int U = 8;
+        const float* from = columns + col;
+        const int64_t stride = 2 * (int64_t)s.d;
+        for (int64_t i = k; i < parts; i += 16 * U) {
+            float t[U];
+#pragma unroll
+            for (int q = 0; q < U; ++q) t[q] = from[(i + 16 * q < parts ? i + 16 * q : i) * stride];
+#pragma unroll
+            for (int q = 0; q < U; ++q) sum += i + 16 * q < parts ? (double)t[q] : 0.0;
+        }
+    }
+    s_part[k][threadIdx.x & 15] = sum;
+    __syncthreads();
+    if (threadIdx.x >= 16 || col >= 2 * s.d) return;
+    sum = 0.0;
+    for (int i = 0; i < 16; ++i) sum += s_part[i][threadIdx.x];
+    float* out = col < s.d ? dgamma : dbeta;
+    if (out) out[col < s.d ? col : col - s.d] = (float)sum;
+}
+
+template <typename T, int V, int ACT, typename Source>
+__global__ __launch_bounds__(256) void k_norm_grad_apply(NormShape s, GraphRows g, const T* dy, RowPlane pd, Source source, Affine f,
+                                                         const float2* __restrict__ means, T* dx, RowPlane px) {
+    const int64_t w = s.chunks - 1 - ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6));        // backwards, as k_norm_apply
+    if (w < 0) return;
+    const LaneColumns c = lane_columns<V>(s, blockIdx.y);
+    float gamma[V], beta[V];
+    load_affine<V>(f.gamma, c, 1.0f, gamma);
+    load_affine<V>(f.beta, c, 0.0f, beta);
+    over_graphs(s, g, w, [&](int64_t graph, int64_t a, int64_t b) {
+        constexpr int U = 2;
+        const int64_t at = graph * s.groups + (c.on ? c.group : 0);
+        const float m = f.mean[at], rs = f.rstd[at];
+        const float2 mm = means[at];
+        for (int64_t r = a; r < b; r += U * c.subs) {
+            PlaneSource<T, V, true> e[U];
+            Source q[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int64_t row = r + k * c.subs + c.sub, have = row < b ? row : a;
+                e[k].x = dy;
+                e[k].p = pd;
+                e[k].load(s, c, have);
+                q[k] = source;
+                q[k].load(s, c, have);
+            }
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int64_t row = r + k * c.subs + c.sub;
+                float v[V];
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float x = q[k].at(j), xh = (x - m) * rs;
+                    const float dz = before_activation<ACT>(e[k].at(j), x, xh, m, rs, gamma[j], beta[j]);
+                    v[j] = rs * (gamma[j] * dz - mm.x - xh * mm.y);
+                }
+                if (row < b && c.on) store_piece<V, true>(dx + c.plane * px.gs + row * px.ld + c.col, v);
+            }
+        }
+    });
+}
+
+// ---- checkpoints by themselves -----------------------------------------------------------------------------
+template <typename T, int V>
+__global__ __launch_bounds__(256) void k_checkpoint_save(NormShape s, const T* __restrict__ x, RowPlane p, Checkpoint ck) {
+    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (w >= s.chunks) return;
+    const LaneColumns c = lane_columns<V>(s, blockIdx.y);
+    const int64_t a = w * s.rows, b = a + s.rows < s.n ? a + s.rows : s.n;
+    constexpr int U = 4;
+    for (int64_t r = a; r < b; r += U * c.subs) {
+        PlaneSource<T, V, true> q[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int64_t row = r + k * c.subs + c.sub;
+            q[k].x = x;
+            q[k].p = p;
+            q[k].load(s, c, row < b ? row : a);
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int64_t row = r + k * c.subs + c.sub;
+            float v[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] = q[k].at(j);
+            save_piece<V>(ck, s, c, row, row < b, v);
+        }
+    }
+}
+template <typename T, int V>
+__global__ __launch_bounds__(256) void k_checkpoint_load(NormShape s, Checkpoint ck, T* __restrict__ x, RowPlane p) {
+    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (w >= s.chunks) return;
+    const LaneColumns c = lane_columns<V>(s, blockIdx.y);
+    const int64_t a = w * s.rows, b = a + s.rows < s.n ? a + s.rows : s.n;
+    constexpr int U = 4;
+    for (int64_t r = a; r < b; r += U * c.subs) {
+        CodeSource<V> q[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int64_t row = r + k * c.subs + c.sub;
+            q[k].k = ck;
+            q[k].load(s, c, row < b ? row : a);
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int64_t row = r + k * c.subs + c.sub;
+            float v[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] = q[k].at(j);
+            if (row < b && c.on) store_piece<V, true>(x + c.plane * p.gs + row * p.ld + c.col, v);
+        }
+    }
+}
+
+// ---- host side ---------------------------------------------------------------------------------------------
+namespace {
+
+constexpr int kMaxWidth = 131072;
+constexpr int64_t kMaxPieces = (int64_t)1 << 31;
+
+bool aligned_to(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+
+// Vectors where every lane's columns lie in one group; else single columns.
+int piece_of(int32_t dg, int32_t cg, int32_t dtype) {
+    const int v = dtype == GSR_BF16 ? 8 : 4;
+    return dg % v == 0 && cg % v == 0 ? v : 1;
+}
+NormShape norm_shape(int64_t n, int32_t d, int32_t planes, int32_t groups, int V) {
+    NormShape s{};
+    s.n = n;
+    s.d = d;
+    s.dg = d / planes;
+    s.groups = groups;
+    s.cg = d / groups;
+    const int pieces = (s.dg + V - 1) / V;
+    int best = 1 << 30;
+    for (int k = 6; k >= 3; --k) {              // as few idle lanes as can be, then as long rows; a block of a checkpoint in one slab
+        const int lanes = 1 << k, all = (pieces + lanes - 1) / lanes * lanes;
+        if (all >= best || (lanes * V % kBlock && lanes * V < s.dg)) continue;
+        best = all;
+        s.lanes_log2 = k;
+        s.group_slabs = all / lanes;
+    }
+    s.slabs = s.group_slabs * planes;
+    const int64_t least = 8 * (64 >> s.lanes_log2);
+    s.rows = (int32_t)std::min<int64_t>(1024, std::max<int64_t>(least, (n * s.slabs + 8191) / 8192));
+    s.chunks = (n + s.rows - 1) / s.rows;
+    return s;
+}
+int planes_of(int32_t c, int32_t layout) { return layout == GSR_LAYOUT_GROUP_PLANAR ? c : 1; }
+
+gsr_status_t plane_shape(int64_t n, int32_t d, int32_t c, int32_t layout, int32_t dtype) {
+    if (n < 0) return fail(GSR_ERR_INVALID_ARG, "negative n");
+    if (n >= ((int64_t)1 << 31)) return fail(GSR_ERR_UNSUPPORTED, "n=%lld at or above 2^31", (long long)n);
+    if (d < 1 || d > kMaxWidth) return fail(GSR_ERR_UNSUPPORTED, "d=%d outside [1, %d]", d, kMaxWidth);
+    if (c < 1 || d % c) return fail(GSR_ERR_UNSUPPORTED, "c=%d does not divide d=%d", c, d);
+    if (layout != GSR_LAYOUT_ROW_MAJOR && layout != GSR_LAYOUT_GROUP_PLANAR) return fail(GSR_ERR_INVALID_ARG, "layout %d", layout);
+    if (dtype != GSR_F32 && dtype != GSR_BF16) return fail(GSR_ERR_UNSUPPORTED, "dtype %d", dtype);
+    if (planes_of(c, layout) > 4096) return fail(GSR_ERR_UNSUPPORTED, "c=%d above 4096", c);
+    return GSR_OK;
+}
+gsr_status_t row_plane(const char* name, const void* at, int64_t n, int32_t dg, int64_t ld, int32_t dtype, RowPlane* p) {
+    if (ld < dg || ld >= ((int64_t)1 << 31)) return fail(GSR_ERR_INVALID_ARG, "row stride %lld of %s outside [%d, 2^31)", (long long)ld, name, dg);
+    if (n > 0 && !at) return fail(GSR_ERR_INVALID_ARG, "%s is null", name);
+    if (!aligned_to(at, dtype_size(dtype))) return fail(GSR_ERR_INVALID_ARG, "%s is not aligned to its elements", name);
+    p->ld = ld;
+    p->gs = n * ld;
+    return GSR_OK;
+}
+gsr_status_t checkpoint_of(int64_t n, int32_t dg, int32_t planes, const int8_t* codes, const float* scales, Checkpoint* k) {
+    if (n > 0 && (!codes || !scales)) return fail(GSR_ERR_INVALID_ARG, "null codes or scales");
+    if (!aligned_to(codes, 4) || !aligned_to(scales, 4)) return fail(GSR_ERR_INVALID_ARG, "codes or scales not aligned to 4 bytes");
+    k->codes = const_cast<int8_t*>(codes);
+    k->scales = const_cast<float*>(scales);
+    k->plane_blocks = (dg + kBlock - 1) / kBlock;
+    k->blocks = k->plane_blocks * planes;
+    return GSR_OK;
+}
+gsr_status_t graph_rows(const void* graph_ptr, int32_t ptr_i64, int64_t graphs, int64_t n, GraphRows* g) {
+    if (graphs < 0) return fail(GSR_ERR_INVALID_ARG, "negative number of graphs");
+    if (graphs >= ((int64_t)1 << 31)) return fail(GSR_ERR_UNSUPPORTED, "%lld graphs", (long long)graphs);
+    if (!graph_ptr && graphs != 1) return fail(GSR_ERR_INVALID_ARG, "%lld graphs without their first rows", (long long)graphs);
+    if (!aligned_to(graph_ptr, ptr_i64 ? 8 : 4)) return fail(GSR_ERR_INVALID_ARG, "graph_ptr is not aligned to its elements");
+    *g = GraphRows{graph_ptr, ptr_i64, graphs, n};
+    return GSR_OK;
+}
+gsr_status_t norm_args(int32_t d, int32_t groups, int32_t act, const float* gamma, const float* beta, const float* mean, const float* rstd,
+                       int64_t graphs) {
+    if (groups < 1 || groups > d || d % groups) return fail(GSR_ERR_UNSUPPORTED, "%d groups do not divide d=%d", groups, d);
+    if (act != GSR_ACT_NONE && act != GSR_ACT_RELU && act != GSR_ACT_SILU) return fail(GSR_ERR_UNSUPPORTED, "activation %d", act);
+    if (graphs > 0 && (!mean || !rstd)) return fail(GSR_ERR_INVALID_ARG, "null mean or rstd");
+    if (!aligned_to(gamma, 4) || !aligned_to(beta, 4) || !aligned_to(mean, 4) || !aligned_to(rstd, 4))
+        return fail(GSR_ERR_INVALID_ARG, "gamma, beta, mean or rstd is not aligned to its elements");
+    return GSR_OK;
+}
+
+// The workspace of both directions: pieces, the means of the gradient, the columns' partial sums.
+struct NormWs {
+    size_t pieces, means, columns, total;
+    bool wide;
+    int64_t task_blocks;
+};
+NormWs carve_norm(const NormShape& s, int64_t graphs) {
+    NormWs w{};
+    w.pieces = 0;
+    w.means = align_up((size_t)(s.chunks + graphs) * s.stride() * sizeof(double2));
+    w.columns = w.means + align_up((size_t)graphs * s.groups * sizeof(float2));
+    w.total = w.columns + align_up((size_t)((s.chunks + 3) / 4) * 2 * s.d * 4);
+    w.wide = s.chunks > 64 * graphs;
+    const int64_t tasks = graphs * s.groups;
+    w.task_blocks = w.wide ? tasks : (tasks + 3) / 4;
+    return w;
+}
+gsr_status_t workspace_of(const NormWs& w, const NormShape& s, int64_t graphs, void* workspace, size_t bytes) {
+    if ((s.chunks + graphs) * s.stride() >= kMaxPieces || graphs * s.groups >= kMaxPieces)
+        return fail(GSR_ERR_UNSUPPORTED, "%lld graphs of %d groups", (long long)graphs, s.groups);
+    if (bytes < w.total) return fail(GSR_ERR_WORKSPACE_TOO_SMALL, "workspace of %zu bytes, %zu needed", bytes, w.total);
+    if ((w.total && !workspace) || !aligned_to(workspace, 16)) return fail(GSR_ERR_INVALID_ARG, "workspace null or not aligned to 16 bytes");
+    return GSR_OK;
+}
+
+dim3 rows_grid(const NormShape& s) { return dim3((unsigned)((s.chunks + 3) / 4), (unsigned)s.slabs); }
+
+// call(T{}, integral_constant<V>) for the storage type and piece
+template <typename Call>
+void by_piece(int32_t dtype, int V, Call call) {
+    if (dtype == GSR_F32 && V == 4) call(float{}, std::integral_constant<int, 4>{});
+    else if (dtype == GSR_F32) call(float{}, std::integral_constant<int, 1>{});
+    else if (V == 8) call(bf16_t{}, std::integral_constant<int, 8>{});
+    else call(bf16_t{}, std::integral_constant<int, 1>{});
+}
+template <typename Call>
+void by_activation(int32_t act, Call call) {
+    if (act == GSR_ACT_RELU) call(std::integral_constant<int, GSR_ACT_RELU>{});
+    else if (act == GSR_ACT_SILU) call(std::integral_constant<int, GSR_ACT_SILU>{});
+    else call(std::integral_constant<int, GSR_ACT_NONE>{});
+}
+
+}  // namespace
+}  // namespace gsr
+
+using namespace gsr;
+
+extern "C" {
+
+size_t gsr_group_norm_workspace(int64_t n, int64_t graphs, int32_t d, int32_t c, int32_t layout, int32_t dtype, int32_t groups) {
+    if (plane_shape(n, d, c, layout, dtype) != GSR_OK || graphs < 0 || graphs >= ((int64_t)1 << 31) || groups < 1 || groups > d || d % groups) return 0;
+    const int planes = planes_of(c, layout);
+    return carve_norm(norm_shape(n, d, planes, groups, piece_of(d / planes, d / groups, dtype)), graphs).total;
+}
+
+gsr_status_t gsr_group_norm(const void* x, int64_t ldx, int64_t n, int32_t d, int32_t c, int32_t layout, int32_t dtype, const void* graph_ptr,
+                            int32_t ptr_i64, int64_t graphs, int32_t groups, const float* gamma, const float* beta, float eps, int32_t act,
+                            void* y_out, int64_t ldy, float* mean_out, float* rstd_out, int8_t* codes_out, float* scales_out, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+    GSR_TRY(plane_shape(n, d, c, layout, dtype));
+    const int planes = planes_of(c, layout), dg = d / planes;
+    RowPlane px, py;
+    GraphRows g;
+    Checkpoint ck{};
+    GSR_TRY(row_plane("x", x, n, dg, ldx, dtype, &px));
+    GSR_TRY(row_plane("y_out", y_out, n, dg, ldy, dtype, &py));
+    GSR_TRY(graph_rows(graph_ptr, ptr_i64, graphs, n, &g));
+    GSR_TRY(norm_args(d, groups, act, gamma, beta, mean_out, rstd_out, graphs));
+    if (!(eps > 0.0f) || std::isinf(eps)) return fail(GSR_ERR_INVALID_ARG, "eps=%g is not a positive number", (double)eps);
+    if (x == y_out && ldx != ldy) return fail(GSR_ERR_INVALID_ARG, "in place, but with row strides of %lld and %lld", (long long)ldx, (long long)ldy);
+    const bool save = codes_out || scales_out;
+    if (save) GSR_TRY(checkpoint_of(n, dg, planes, codes_out, scales_out, &ck));
+    const int V = piece_of(dg, d / groups, dtype);
+    const NormShape s = norm_shape(n, d, planes, groups, V);
+    const NormWs ws = carve_norm(s, graphs);
+    GSR_TRY(workspace_of(ws, s, graphs, workspace, workspace_bytes));
+    if (graphs == 0) return GSR_OK;
+    hipStream_t st = (hipStream_t)stream;
+    double2* pieces = (double2*)((char*)workspace + ws.pieces);
+    by_piece(dtype, V, [&](auto t, auto v) {
+        using T = decltype(t);
+        constexpr int P = v.value;
+        if (n) hipLaunchKernelGGL((k_norm_sums<T, P>), rows_grid(s), dim3(256), 0, st, s, g, (const T*)x, px, pieces);
+        if (ws.wide) hipLaunchKernelGGL((k_norm_join<true>), dim3((unsigned)ws.task_blocks), dim3(256), 0, st, s, g, V, pieces, (double)eps, mean_out, rstd_out);
+        else hipLaunchKernelGGL((k_norm_join<false>), dim3((unsigned)ws.task_blocks), dim3(256), 0, st, s, g, V, pieces, (double)eps, mean_out, rstd_out);
+        if (!n) return;
+        const Affine f{gamma, beta, mean_out, rstd_out};
+        by_activation(act, [&](auto a) {
+            if (save) hipLaunchKernelGGL((k_norm_apply<T, P, a.value, true>), rows_grid(s), dim3(256), 0, st, s, g, (const T*)x, px, f, (T*)y_out, py, ck);
+            else hipLaunchKernelGGL((k_norm_apply<T, P, a.value, false>), rows_grid(s), dim3(256), 0, st, s, g, (const T*)x, px, f, (T*)y_out, py, ck);
+        });
+    });
+    GSR_HIP_CHECK(hipGetLastError());
+    return GSR_OK;
+}
+
+gsr_status_t gsr_group_norm_grad(const void* dy, int64_t lddy, const void* x, int64_t ldx, const int8_t* codes, const float* scales, int64_t n,
+                                 int32_t d, int32_t c, int32_t layout, int32_t dtype, const void* graph_ptr, int32_t ptr_i64, int64_t graphs,
+                                 int32_t groups, const float* mean, const float* rstd, const float* gamma, const float* beta, int32_t act,
+                                 void* dx_out, int64_t lddx, float* dgamma_out, float* dbeta_out, void* workspace, size_t workspace_bytes,
+                                 void* stream) {
+    GSR_TRY(plane_shape(n, d, c, layout, dtype));
+    const int planes = planes_of(c, layout), dg = d / planes;
+    RowPlane pd, px{}, po;
+    GraphRows g;
+    Checkpoint ck{};
+    const bool coded = codes || scales;
+    if (coded && x) return fail(GSR_ERR_INVALID_ARG, "x and its checkpoint");
+    GSR_TRY(row_plane("dy", dy, n, dg, lddy, dtype, &pd));
+    if (coded) GSR_TRY(checkpoint_of(n, dg, planes, codes, scales, &ck));
+    else GSR_TRY(row_plane("x", x, n, dg, ldx, dtype, &px));
+    GSR_TRY(row_plane("dx_out", dx_out, n, dg, lddx, dtype, &po));
+    GSR_TRY(graph_rows(graph_ptr, ptr_i64, graphs, n, &g));
+    GSR_TRY(norm_args(d, groups, act, gamma, beta, mean, rstd, graphs));
+    if (!aligned_to(dgamma_out, 4) || !aligned_to(dbeta_out, 4)) return fail(GSR_ERR_INVALID_ARG, "dgamma_out or dbeta_out is not aligned to its elements");
+    if (dy == dx_out && lddy != lddx) return fail(GSR_ERR_INVALID_ARG, "in place, but with row strides of %lld and %lld", (long long)lddy, (long long)lddx);
+    const int V = piece_of(dg, d / groups, dtype);
+    const NormShape s = norm_shape(n, d, planes, groups, V);
+    const NormWs ws = carve_norm(s, graphs);
+    GSR_TRY(workspace_of(ws, s, graphs, workspace, workspace_bytes));
+    hipStream_t st = (hipStream_t)stream;
+    double2* pieces = (double2*)((char*)workspace + ws.pieces);
+    float2* means = (float2*)((char*)workspace + ws.means);
+    float* columns = (float*)((char*)workspace + ws.columns);
+    const Affine f{gamma, beta, mean, rstd};
+    auto both = [&](auto t, auto v, auto a, auto source) {
+        using T = decltype(t);
+        using Source = decltype(source);
+        constexpr int P = v.value, ACT = a.value;
+        if (n) hipLaunchKernelGGL((k_norm_grad_sums<T, P, ACT, Source>), rows_grid(s), dim3(256), 0, st, s, g, (const T*)dy, pd, source, f, pieces, columns);
+        const int64_t column_blocks = dgamma_out || dbeta_out ? (2 * (int64_t)d + 15) / 16 : 0;
+        const dim3 grid((unsigned)(ws.task_blocks + column_blocks));
+        const int64_t parts = (s.chunks + 3) / 4;
+        if (grid.x && ws.wide)
+            hipLaunchKernelGGL((k_norm_grad_join<true>), grid, dim3(256), 0, st, s, g, V, pieces, ws.task_blocks, means, columns, parts, dgamma_out, dbeta_out);
+        else if (grid.x)
+            hipLaunchKernelGGL((k_norm_grad_join<false>), grid, dim3(256), 0, st, s, g, V, pieces, ws.task_blocks, means, columns, parts, dgamma_out, dbeta_out);
+        if (n && graphs) hipLaunchKernelGGL((k_norm_grad_apply<T, P, ACT, Source>), rows_grid(s), dim3(256), 0, st, s, g, (const T*)dy, pd, source, f, means, (T*)dx_out, po);
+    };
+    by_piece(dtype, V, [&](auto t, auto v) {
+        using T = decltype(t);
+        constexpr int P = v.value;
+        by_activation(act, [&](auto a) {
+            if (coded) both(t, v, a, CodeSource<P>{ck, {}, 0.0f});
+            else both(t, v, a, PlaneSource<T, P, false>{(const T*)x, px, {}});
+        });
+    });
+    GSR_HIP_CHECK(hipGetLastError());
+    return GSR_OK;
+}
+
+gsr_status_t gsr_checkpoint_save(const void* x, int64_t ldx, int64_t n, int32_t d, int32_t c, int32_t layout, int32_t dtype, int8_t* codes_out,
+                                 float* scales_out, void* stream) {
+    GSR_TRY(plane_shape(n, d, c, layout, dtype));
+    const int planes = planes_of(c, layout), dg = d / planes;
+    RowPlane p;
+    Checkpoint ck;
+    GSR_TRY(row_plane("x", x, n, dg, ldx, dtype, &p));
+    GSR_TRY(checkpoint_of(n, dg, planes, codes_out, scales_out, &ck));
+    if (n == 0) return GSR_OK;
+    const int V = piece_of(dg, dg, dtype);
+    const NormShape s = norm_shape(n, d, planes, 1, V);
+    by_piece(dtype, V, [&](auto t, auto v) {
+        using T = decltype(t);
+        hipLaunchKernelGGL((k_checkpoint_save<T, v.value>), rows_grid(s), dim3(256), 0, (hipStream_t)stream, s, (const T*)x, p, ck);
+    });
+    GSR_HIP_CHECK(hipGetLastError());
+    return GSR_OK;
+}
+
+gsr_status_t gsr_checkpoint_load(const int8_t* codes, const float* scales, int64_t n, int32_t d, int32_t c, int32_t layout, int32_t dtype,
+                                 void* x_out, int64_t ldx, void* stream) {
+    GSR_TRY(plane_shape(n, d, c, layout, dtype));
+    const int planes = planes_of(c, layout), dg = d / planes;
+    RowPlane p;
+    Checkpoint ck;
+    GSR_TRY(row_plane("x_out", x_out, n, dg, ldx, dtype, &p));
+    GSR_TRY(checkpoint_of(n, dg, planes, codes, scales, &ck));
+    if (n == 0) return GSR_OK;
+    const int V = piece_of(dg, dg, dtype);
+    const NormShape s = norm_shape(n, d, planes, 1, V);
+    by_piece(dtype, V, [&](auto t, auto v) {
+        using T = decltype(t);
+        hipLaunchKernelGGL((k_checkpoint_load<T, v.value>), rows_grid(s), dim3(256), 0, (hipStream_t)stream, s, ck, (T*)x_out, p);
+    });
+    GSR_HIP_CHECK(hipGetLastError());
+    return GSR_OK;
+}
+
+}  // extern "C"
