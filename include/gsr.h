@@ -418,6 +418,37 @@ gsr_status_t gsr_checkpoint_save(const void* x, int64_t ldx, int64_t n, int32_t 
 gsr_status_t gsr_checkpoint_load(const int8_t* codes, const float* scales, int64_t n, int32_t d, int32_t c, int32_t layout, int32_t dtype,
                                  void* x_out, int64_t ldx, void* stream);
 
+/* ---- softmax cross entropy over many classes, without the logits ----
+ *
+ * A head on the output of a stack for tasks whose targets are classes (the type of a masked cell, say, with the table of the node embeddings):
+ *   z_ij = x_i . E_j + b_j,  lse_i = log sum_j exp z_ij,  loss = mean over the rows with a class of lse_i - z_i,t_i  (0 if there are none).
+ * x: a plane (device, n x d of `dtype`; ROW_MAJOR with row stride ldx, d at least; GROUP_PLANAR in c groups of d/c columns, row stride ldx, d/c at
+ * least, group stride n * ldx).  E: `classes` rows of d values of the same dtype, row stride ldt.  bias: device, `classes` floats (-inf takes a class
+ * out), or NULL.  ids: device, n classes, int32, or int64 with ids_i64 = 1; a row whose id lies outside [0, classes), such as -1, has no class: no part
+ * in the loss or in any gradient, whatever its values, and a dx of 0.  z is never stored: neither call needs memory of the order n * classes.
+ *
+ * gsr_class_loss: loss_out (device, 1 float), lse_out (device, n floats, every row's).
+ *
+ * gsr_class_grad: the gradients of scale * loss, with lse as gsr_class_loss left it and dz_ij = (exp(z_ij - lse_i) - [j = t_i]) scale / rows with a
+ * class:  dx_out = dz E (a plane as x, row stride lddx), dtable_out = dz^T x (classes rows of d values of `dtype`, row stride lddt), dbias_out_j =
+ * sum_i dz_ij (`classes` floats); any but not all of them may be NULL.  Every element is written.
+ *
+ * float32 values enter the products exactly, and sums are taken in float32 (the loss and dbias: in float64 across tiles).  With 16-bit planes
+ * dz is rounded to 16 bits before the products with E and x.  Equal calls give equal bits.  Values must be finite: a row with infinities or NaN gets a
+ * loss that is none, which then is the mean's.  1 <= d <= 512, c divides d, n and classes below 2^31 - 256; pointers aligned to their elements.
+ * workspace: device, 16-byte aligned, at least gsr_class_loss_workspace() / gsr_class_grad_workspace() bytes (0: sizes that are refused), some
+ * copies of x and E; it holds nothing between calls.  What a call writes overlaps nothing that it reads.  Calls only launch kernels and may be captured;
+ * calls with workspaces of their own may run side by side. */
+size_t gsr_class_loss_workspace(int64_t n, int64_t classes, int32_t d, int32_t dtype);
+size_t gsr_class_grad_workspace(int64_t n, int64_t classes, int32_t d, int32_t dtype);
+gsr_status_t gsr_class_loss(const void* x, int64_t ldx, int64_t n, int32_t d, int32_t c, int32_t layout, int32_t dtype, const void* table,
+                            int64_t classes, int64_t ldt, const float* bias, const void* ids, int32_t ids_i64, float* loss_out, float* lse_out,
+                            void* workspace, size_t workspace_bytes, void* stream);
+gsr_status_t gsr_class_grad(const void* x, int64_t ldx, int64_t n, int32_t d, int32_t c, int32_t layout, int32_t dtype, const void* table,
+                            int64_t classes, int64_t ldt, const float* bias, const void* ids, int32_t ids_i64, const float* lse, float scale,
+                            void* dx_out, int64_t lddx, void* dtable_out, int64_t lddt, float* dbias_out, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
 #ifdef __cplusplus
 }
 #endif

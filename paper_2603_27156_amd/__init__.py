@@ -41,6 +41,7 @@ EXPORTED = [
     "gsr_embed_lookup", "gsr_embed_grad_workspace", "gsr_embed_grad",
     "gsr_grad_norm_workspace", "gsr_grad_norm", "gsr_grad_clip", "gsr_adam_update_list",
     "gsr_group_norm_workspace", "gsr_group_norm", "gsr_group_norm_grad", "gsr_checkpoint_save", "gsr_checkpoint_load",
+    "gsr_class_loss_workspace", "gsr_class_grad_workspace", "gsr_class_loss", "gsr_class_grad",
 ]
 
 
@@ -95,6 +96,11 @@ def lib():
         l.gsr_group_norm_grad.argtypes = [p, i64, p, i64, p, p, i64, i32, i32, i32, i32, p, i32, i64, i32, p, p, p, p, i32, p, i64, p, p, p, size, p]
         l.gsr_checkpoint_save.argtypes = [p, i64, i64, i32, i32, i32, i32, p, p, p]
         l.gsr_checkpoint_load.argtypes = [p, p, i64, i32, i32, i32, i32, p, i64, p]
+        for f in (l.gsr_class_loss_workspace, l.gsr_class_grad_workspace):
+            f.restype = size
+            f.argtypes = [i64, i64, i32, i32]
+        l.gsr_class_loss.argtypes = [p, i64, i64, i32, i32, i32, i32, p, i64, i64, p, p, i32, p, p, p, size, p]
+        l.gsr_class_grad.argtypes = [p, i64, i64, i32, i32, i32, i32, p, i64, i64, p, p, i32, p, f32, p, i64, p, i64, p, p, size, p]
         _lib = l
     return _lib
 
@@ -605,6 +611,63 @@ def gsr_checkpoint_load(codes, scales, x_out) -> None:
     n, d, c, layout, ldx = _plane(x_out, dev)
     k, s = _checkpoint(codes, scales, dev, n, d, c)
     _check(lib().gsr_checkpoint_load(k, s, n, d, c, layout, _dtype_of(x_out), x_out.data_ptr(), ldx, _stream()))
+
+
+def gsr_class_loss_workspace(x, classes: int) -> int:
+    """Bytes of workspace that gsr_class_loss needs for a plane like x."""
+    n, d, *_ = _plane(x, x.get_device())
+    return lib().gsr_class_loss_workspace(n, classes, d, _dtype_of(x))
+
+
+def gsr_class_grad_workspace(x, classes: int) -> int:
+    """Bytes of workspace that gsr_class_grad needs for a plane like x."""
+    n, d, *_ = _plane(x, x.get_device())
+    return lib().gsr_class_grad_workspace(n, classes, d, _dtype_of(x))
+
+
+def _class_table(t, d: int, dtype, dev: int):
+    """(address, rows, row stride) of a table [classes, d] of a type; rows may be strided."""
+    assert t.dtype == dtype
+    classes, dt, _, layout, ld = _plane(t, dev)
+    assert dt == d and layout == GSR_LAYOUT_ROW_MAJOR
+    return t.data_ptr(), classes, ld
+
+
+def _class_scratch(workspace, size, n: int, classes: int, d: int, dtype: int, dev: int):
+    if workspace is None:
+        import torch
+        workspace = torch.empty(size(n, classes, d, dtype), dtype=torch.uint8, device="cuda")
+    assert workspace.get_device() == dev and workspace.is_contiguous()
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def gsr_class_loss(x, table, targets, loss_out, lse_out, bias=None, workspace=None) -> None:
+    """loss_out (float32, one element) = mean over the rows with a class of lse - logit of the class, where the logits x @ table.T + bias are
+    never stored; lse_out (float32 [n]): log sum exp of every row's.  x: a plane [n, D] (rows may be strided) or [C, n, D/C]; table: [classes, D]
+    of x's type, rows may be strided; targets: [n] int32 or int64, no class where outside [0, classes); bias: float32 [classes] or None."""
+    dev = _current_device()
+    n, d, c, layout, ldx = _plane(x, dev)
+    dtype = _dtype_of(x)
+    at, classes, ldt = _class_table(table, d, x.dtype, dev)
+    ws, nb = _class_scratch(workspace, lib().gsr_class_loss_workspace, n, classes, d, dtype, dev)
+    _check(lib().gsr_class_loss(x.data_ptr(), ldx, n, d, c, layout, dtype, at, classes, ldt, _floats(bias, dev, (classes,)), targets.data_ptr(),
+                                _tokens(targets, n, dev), _scalar(loss_out, dev), _floats(lse_out, dev, (n,)), ws.data_ptr(), nb, _stream()))
+
+
+def gsr_class_grad(x, table, targets, lse, dx_out=None, dtable_out=None, bias=None, dbias_out=None, scale: float = 1.0, workspace=None) -> None:
+    """The gradients of scale * gsr_class_loss, lse as it left it: dx_out (a plane as x), dtable_out (as table), dbias_out (float32
+    [classes]); at least one of them."""
+    dev = _current_device()
+    n, d, c, layout, ldx = _plane(x, dev)
+    dtype = _dtype_of(x)
+    at, classes, ldt = _class_table(table, d, x.dtype, dev)
+    lddx = 0 if dx_out is None else _like_plane(dx_out, dev, n, d, c, layout, x.dtype)
+    dt, rows, lddt = (0, classes, 0) if dtable_out is None else _class_table(dtable_out, d, x.dtype, dev)
+    assert rows == classes
+    ws, nb = _class_scratch(workspace, lib().gsr_class_grad_workspace, n, classes, d, dtype, dev)
+    _check(lib().gsr_class_grad(x.data_ptr(), ldx, n, d, c, layout, dtype, at, classes, ldt, _floats(bias, dev, (classes,)), targets.data_ptr(),
+                                _tokens(targets, n, dev), _floats(lse, dev, (n,)), scale, 0 if dx_out is None else dx_out.data_ptr(), lddx, dt, lddt,
+                                _floats(dbias_out, dev, (classes,)), ws.data_ptr(), nb, _stream()))
 
 
 def gsr_spmm_compressed(g: Graph, vals, idx, dg: int):

@@ -15,7 +15,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libgsr.so")
 MARSHAL = os.path.join(HERE, "libgsr_marshal.so")
 SOURCES = ["gsr_graph.hip", "gsr_ops.hip", "gsr_layer.hip", "gsr_literal.hip", "gsr_optim.hip", "gsr_embed.hip",
-           "gsr_lists.hip", "gsr_norm.hip"]
+           "gsr_lists.hip", "gsr_norm.hip", "gsr_classes.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",

@@ -1,0 +1,784 @@
+// Softmax cross entropy of a linear head over many classes, without its logits, and its gradient.
+//
+//   z_ij = x_i . E_j + b_j        lse_i = log sum_j exp z_ij        loss = mean over the rows with a class of lse_i - z_i,t_i
+//   dz_ij = (exp(z_ij - lse_i) - [j = t_i]) scale / rows with a class;    dx = dz E,   dE = dz^T x,   db_j = sum_i dz_ij
+//
+// The n x classes logits exist only as 32-row tiles in the registers of the matrix cores.  A workgroup keeps a block of rows of one side
+// (x or E) in registers, the other side streams through LDS in tiles of 32 rows, and of every tile the wave takes the products Z^T with its own
+// rows, then exp, and, in the backward, a second product that adds dz times the streamed tile to its rows' gradients.  The accumulators of the first
+// product hold a lane's row and four neighbouring streamed rows, which is how the second one wants its operand (the K index is permuted
+// alike on both sides), so dz never leaves the registers.  dx and dE are the same kernel with the sides exchanged; each computes the logits anew.
+//
+// Operands are laid out once per call as the matrix instructions take them: rows in blocks of 16, columns in steps of 32, and of every (block, step)
+// 64 pieces of 16 bytes in lane order, zeros behind the last row and column.  So tiles are copied to LDS as they lie, from any layout, stride and
+// width.  16-bit planes go in as they are; floats as three 16-bit pieces whose sum they are, and a product of floats as the six products of pieces
+// that matter at 2^-24 of it (hh, hm, mh, mm, hl, lh; each exact, added up in float32).
+#include "gsr_internal.h"
+#include "gsr_pieces.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace gsr {
+
+constexpr int kMaxClassWidth = 512;
+constexpr int kTileRows = 32;                   // streamed rows of a tile
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kNoMax = -3.0e38f;              // a running maximum that no logit has reached
+
+// ---- operands ------------------------------------------------------------------------------------------
+struct RowSource {              // rows of a plane, or of a table
+    const void* at;
+    int64_t rows, ld, gs;
+    int32_t d, dg;
+};
+struct ClassTokens {
+    const void* ids;
+    int32_t i64, classes;
+    __device__ __forceinline__ int32_t at(int64_t i) const {        // -1: none
+        const int64_t t = i64 ? static_cast<const int64_t*>(ids)[i] : static_cast<const int32_t*>(ids)[i];
+        return t >= 0 && t < classes ? (int32_t)t : -1;
+    }
+};
+// What a launch lays out.  Blocks of 256 threads: x, then E, then 1,024 rows' classes and lse each, then 1,024 biases each.
+struct ClassSetup {
+    RowSource x, e;
+    ClassTokens ids;
+    uint4 *xf, *ef;                 // in pieces
+    const float *lse, *bias;        // lse: NULL in the forward
+    float *lse_out, *bias_out;      // of all rows that the kernels read, padded ones too
+    int32_t *target, *counts;       // class of every row; rows with a class of every block
+    int64_t x_pad, e_pad;           // rows laid out
+    int32_t ks;
+    unsigned x_blocks, e_blocks, row_blocks, bias_blocks;
+};
+template <typename T, int NP>
+__device__ __forceinline__ void lay_out(const RowSource& s, uint4* __restrict__ out, int64_t pad, int ks, int64_t wave, const ClassTokens* known) {
+    if (wave >= pad / 16 * ks) return;
+    const int lane = lane_id(), step = (int)(wave % ks);
+    const int64_t row = wave / ks * 16 + (lane & 15);
+    const int col = step * 32 + (lane >> 4) * 8;
+    float v[8];
+    const bool in = row < s.rows && (!known || known->at(row) >= 0);
+    if (in && s.dg % 8 == 0) {
+        const int plane = col / s.dg;
+        if (col < s.d) {
+            Piece<T, 8> p;
+            p.load(static_cast<const T*>(s.at) + plane * s.gs + row * s.ld + (col - plane * s.dg));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = p.at(j);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int c = col + j, plane = c / s.dg;
+            v[j] = in && c < s.d ? to_float(static_cast<const T*>(s.at)[plane * s.gs + row * s.ld + (c - plane * s.dg)]) : 0.0f;
+        }
+    }
+    uint32_t h[NP][8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        h[0][j] = __float_as_uint(v[j]);
+        if constexpr (NP == 3) {
+            const float r1 = v[j] - __uint_as_float(h[0][j] & 0xFFFF0000u);
+            h[1][j] = __float_as_uint(r1);
+            h[2][j] = __float_as_uint(r1 - __uint_as_float(h[1][j] & 0xFFFF0000u));
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < NP; ++k) {
+        uint4 w;
+        w.x = __builtin_amdgcn_perm(h[k][1], h[k][0], 0x07060302u);
+        w.y = __builtin_amdgcn_perm(h[k][3], h[k][2], 0x07060302u);
+        w.z = __builtin_amdgcn_perm(h[k][5], h[k][4], 0x07060302u);
+        w.w = __builtin_amdgcn_perm(h[k][7], h[k][6], 0x07060302u);
+        out[(wave * NP + k) * 64 + lane] = w;
+    }
+}
+template <typename T, int NP>
+__global__ __launch_bounds__(256) void k_class_setup(ClassSetup s) {
+    unsigned b = blockIdx.x;
+    const int wave = threadIdx.x >> 6;
+    if (b < s.x_blocks) {
+        lay_out<T, NP>(s.x, s.xf, s.x_pad, s.ks, (int64_t)b * 4 + wave, s.lse ? &s.ids : nullptr);
+        return;
+    }
+    b -= s.x_blocks;
+    if (b < s.e_blocks) {
+        lay_out<T, NP>(s.e, s.ef, s.e_pad, s.ks, (int64_t)b * 4 + wave, nullptr);
+        return;
+    }
+    b -= s.e_blocks;
+    if (b < s.row_blocks) {
+        int count = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t i = (int64_t)b * 1024 + k * 256 + threadIdx.x;
+            if (i >= s.x_pad) continue;
+            const int32_t t = i < s.x.rows ? s.ids.at(i) : -1;
+            s.target[i] = t;
+            if (s.lse) s.lse_out[i] = t >= 0 ? s.lse[i] : INFINITY;         // exp(z - inf): no part in any gradient
+            count += t >= 0;
+        }
+        __shared__ int s_count[4];
+        for (int o = 32; o; o >>= 1) count += __shfl_xor(count, o);
+        if (lane_id() == 0) s_count[wave] = count;
+        __syncthreads();
+        if (threadIdx.x == 0) s.counts[b] = s_count[0] + s_count[1] + s_count[2] + s_count[3];
+        return;
+    }
+    b -= s.row_blocks;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int64_t j = (int64_t)b * 1024 + k * 256 + threadIdx.x;
+        if (j < s.e_pad) s.bias_out[j] = j < s.e.rows ? (s.bias ? s.bias[j] : 0.0f) : -INFINITY;          // exp(-inf): no class
+    }
+}
+
+// A tile of N pieces of 1 KB into LDS; arrives once this wave has waited for its loads and all waves have met.
+template <int N>
+__device__ __forceinline__ void fetch_tile(const uint4* __restrict__ from, uint4* to, int wave, int lane) {
+#pragma unroll
+    for (int c = 0; c < (N + 3) / 4; ++c) {
+        const int piece = c * 4 + wave;
+        if (N % 4 == 0 || piece < N)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(from + piece * 64 + lane),
+                                             (__attribute__((address_space(3))) uint32_t*)(to + piece * 64), 16, 0, 0);
+    }
+}
+// whether two tiles fit into LDS
+constexpr bool two_tiles(int kilobytes) { return 2 * kilobytes <= 160; }
+__device__ __forceinline__ void tile_arrived() {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+__device__ __forceinline__ bf16x8 piece_of_lds(const uint4* p) { return __builtin_bit_cast(bf16x8, *p); }
+
+// The products of pieces, small ones first.
+template <int NP>
+__device__ __forceinline__ f32x4 mfma_pieces(const bf16x8 (&a)[NP], const bf16x8 (&b)[NP], f32x4 c) {
+    if constexpr (NP == 3) {
+        c = mfma_k32(a[2], b[0], c);
+        c = mfma_k32(a[0], b[2], c);
+        c = mfma_k32(a[1], b[1], c);
+        c = mfma_k32(a[1], b[0], c);
+        c = mfma_k32(a[0], b[1], c);
+    }
+    return mfma_k32(a[0], b[0], c);
+}
+
+// z[blk][r]: logits of the streamed rows 16 blk + 4 (lane / 16) + reg with this wave's row 16 r + lane % 16
+template <int KS, int NP, int RB>
+__device__ __forceinline__ void tile_logits(const uint4* tile, const bf16x8 (&own)[RB][KS][NP], int lane, f32x4 (&z)[2][RB]) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk) {
+            bf16x8 a[NP];
+#pragma unroll
+            for (int p = 0; p < NP; ++p) a[p] = piece_of_lds(tile + ((blk * KS + k) * NP + p) * 64 + lane);
+#pragma unroll
+            for (int r = 0; r < RB; ++r) z[blk][r] = mfma_pieces<NP>(a, own[r][k], z[blk][r]);
+        }
+    }
+}
+template <int KS, int NP, int RB>
+__device__ __forceinline__ void load_own(const uint4* __restrict__ from, int64_t block0, int lane, bf16x8 (&own)[RB][KS][NP]) {
+#pragma unroll
+    for (int r = 0; r < RB; ++r)
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int p = 0; p < NP; ++p) own[r][k][p] = __builtin_bit_cast(bf16x8, from[(((block0 + r) * KS + k) * NP + p) * 64 + lane]);
+}
+
+// ---- forward ---------------------------------------------------------------------------------------------
+struct ClassLossArgs {
+    const uint4 *xf, *ef;
+    const float* bias;
+    const int32_t* target;
+    float2* part;                   // [splits][x_pad]: running maximum, sum of exp(z - maximum)
+    float* at_target;               // [x_pad]
+    int64_t x_pad;
+    int32_t tiles, splits;
+};
+template <int KS, int NP, int RB>
+__global__ __launch_bounds__(256, 2) void k_class_loss(ClassLossArgs g) {
+    constexpr int N = 2 * KS * NP;
+    constexpr bool TWO = two_tiles(N);
+    __shared__ uint4 s_tile[TWO ? 2 : 1][N * 64];
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4;
+    const int64_t block0 = ((int64_t)blockIdx.x * 4 + wave) * RB;
+    const int t0 = (int)((int64_t)g.tiles * blockIdx.y / g.splits), t1 = (int)((int64_t)g.tiles * (blockIdx.y + 1) / g.splits);
+    fetch_tile<N>(g.ef + (int64_t)t0 * N * 64, s_tile[0], wave, lane);          // (no part is empty)
+    bf16x8 own[RB][KS][NP];
+    load_own<KS, NP, RB>(g.xf, block0, lane, own);
+    int target[RB];
+    float top[RB], sum[RB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        target[r] = g.target[(block0 + r) * 16 + (lane & 15)];
+        top[r] = kNoMax;
+        sum[r] = 0.0f;
+    }
+    tile_arrived();
+    for (int t = t0; t < t1; ++t) {
+        const uint4* tile = s_tile[TWO ? (t - t0) & 1 : 0];
+        if (TWO && t + 1 < t1) fetch_tile<N>(g.ef + (int64_t)(t + 1) * N * 64, s_tile[TWO ? (t - t0 + 1) & 1 : 0], wave, lane);
+        f32x4 z[2][RB];
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk) {
+            const f32x4 b = *reinterpret_cast<const f32x4*>(g.bias + t * kTileRows + blk * 16 + grp * 4);
+#pragma unroll
+            for (int r = 0; r < RB; ++r) z[blk][r] = b;
+        }
+        tile_logits<KS, NP, RB>(tile, own, lane, z);
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            if (ballot((unsigned)(target[r] - t * kTileRows) < (unsigned)kTileRows)) {
+#pragma unroll
+                for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (target[r] == t * kTileRows + blk * 16 + grp * 4 + i) g.at_target[(block0 + r) * 16 + (lane & 15)] = z[blk][r][i];
+            }
+            float m = top[r];
+#pragma unroll
+            for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) m = fmaxf(m, z[blk][r][i]);
+            float s = sum[r] * __builtin_amdgcn_exp2f((top[r] - m) * kLog2e);
+#pragma unroll
+            for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s += __builtin_amdgcn_exp2f((z[blk][r][i] - m) * kLog2e);
+            top[r] = m;
+            sum[r] = s;
+        }
+        if constexpr (!TWO) {
+            __syncthreads();
+            if (t + 1 < t1) fetch_tile<N>(g.ef + (int64_t)(t + 1) * N * 64, s_tile[0], wave, lane);
+        }
+        tile_arrived();
+    }
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        float m = fmaxf(top[r], __shfl_xor(top[r], 16));
+        m = fmaxf(m, __shfl_xor(m, 32));
+        float s = sum[r] * __builtin_amdgcn_exp2f((top[r] - m) * kLog2e);
+        s += __shfl_xor(s, 16);
+        s += __shfl_xor(s, 32);
+        if (grp == 0) g.part[blockIdx.y * g.x_pad + (block0 + r) * 16 + lane] = make_float2(m, s);
+    }
+}
+// lse of 1,024 rows and their part of the loss; a single workgroup writes the loss itself
+struct LossPart {
+    double sum;
+    int64_t count;
+};
+__device__ __forceinline__ void add_up(double& sum, int64_t& count) {          // over 1,024 threads, in the first
+    __shared__ double s_sum[16];
+    __shared__ int64_t s_count[16];
+    for (int o = 32; o; o >>= 1) {
+        sum += __shfl_xor(sum, o);
+        count += __shfl_xor(count, o);
+    }
+    if (lane_id() == 0) {
+        s_sum[threadIdx.x >> 6] = sum;
+        s_count[threadIdx.x >> 6] = count;
+    }
+    __syncthreads();
+    if (threadIdx.x) return;
+    sum = 0.0;
+    count = 0;
+    for (int i = 0; i < 16; ++i) {
+        sum += s_sum[i];
+        count += s_count[i];
+    }
+}
+__global__ __launch_bounds__(1024) void k_class_lse(const float2* __restrict__ part, const float* __restrict__ at_target,
+                                                    const int32_t* __restrict__ target, int64_t n, int64_t x_pad, int splits,
+                                                    float* __restrict__ lse_out, LossPart* __restrict__ parts, float* __restrict__ loss) {
+    const int64_t i = (int64_t)blockIdx.x * 1024 + threadIdx.x;
+    double sum = 0.0;
+    int64_t count = 0;
+    if (i < n) {
+        float m = kNoMax;
+        for (int s = 0; s < splits; ++s) m = fmaxf(m, part[s * x_pad + i].x);
+        double l = 0.0;
+        for (int s = 0; s < splits; ++s) l += (double)part[s * x_pad + i].y * exp((double)part[s * x_pad + i].x - (double)m);
+        const double lse = (double)m + log(l);
+        lse_out[i] = (float)lse;
+        if (target[i] >= 0) {
+            sum = lse - (double)at_target[i];
+            count = 1;
+        }
+    }
+    add_up(sum, count);
+    if (threadIdx.x) return;
+    if (gridDim.x == 1) *loss = count ? (float)(sum / (double)count) : 0.0f;
+    else parts[blockIdx.x] = LossPart{sum, count};
+}
+__global__ __launch_bounds__(1024) void k_class_loss_sum(const LossPart* __restrict__ parts, int blocks, float* __restrict__ loss) {
+    double sum = 0.0;
+    int64_t count = 0;
+    for (int i = threadIdx.x; i < blocks; i += 1024) {
+        sum += parts[i].sum;
+        count += parts[i].count;
+    }
+    add_up(sum, count);
+    if (threadIdx.x == 0) *loss = count ? (float)(sum / (double)count) : 0.0f;
+}
+
+// ---- backward --------------------------------------------------------------------------------------------
+struct ClassGradArgs {
+    const uint4 *own, *stream;      // in pieces: the rows that a workgroup keeps, and the tiles
+    const float *lse, *bias;
+    const int32_t *target, *counts;
+    void* out;                      // rows x d of T: a plane, or a table
+    int64_t rows, ld, gs;
+    float* part;                    // [splits][own_pad][KS * 32], where there are several
+    double* bias_part;              // BY_CLASS: [splits][own_pad]
+    int64_t own_pad;
+    int32_t d, dg, tiles, splits, count_blocks;
+    float scale;
+};
+__device__ __forceinline__ float gradient_scale(const int32_t* __restrict__ counts, int blocks, float scale) {
+    int count = 0;
+    for (int i = lane_id(); i < blocks; i += 64) count += counts[i];
+    for (int o = 32; o; o >>= 1) count += __shfl_xor(count, o);
+    return count ? scale / (float)count : 0.0f;
+}
+__device__ __forceinline__ void store_as(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store_as(bf16_t* p, float v) { p->bits = (uint16_t)bf16_bits(v); }
+
+// eight dz as the operand of the second product: as they are rounded to 16 bits (a relative 2^-9 of each, like the gradients that they are
+// summed to), or in three pieces
+template <int NP>
+__device__ __forceinline__ void operand_of(const f32x4& a, const f32x4& b, bf16x8 (&o)[NP]) {
+    if constexpr (NP == 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            o[0][i] = static_cast<__bf16>(a[i]);
+            o[0][4 + i] = static_cast<__bf16>(b[i]);
+        }
+    } else {
+        const float pa[4] = {a[0], a[1], a[2], a[3]}, pb[4] = {b[0], b[1], b[2], b[3]};
+        bf16x4 ha, ma, la, hb, mb, lb;
+        split_p4(pa, ha, ma, la);
+        split_p4(pb, hb, mb, lb);
+        o[0] = join8(ha, hb);
+        o[1] = join8(ma, mb);
+        o[2] = join8(la, lb);
+    }
+}
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+// the streamed rows 4 (lane / 16) .. + 3 of block blk at column 16 cb + lane % 16: 16 lanes together read four rows of 16 columns
+template <int KS, int NP>
+__device__ __forceinline__ bf16x4 column_of_lds(const uint4* tile, int blk, int cb, int p, int lane) {
+    const int grp = lane >> 4, i = lane & 15;
+    const char* at = reinterpret_cast<const char*>(tile + ((blk * KS + (cb >> 1)) * NP + p) * 64) +
+                     (((cb & 1) * 2 + ((i & 3) >> 1)) * 16 + 4 * grp + (i >> 2)) * 16 + (i & 1) * 8;
+    return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at));
+}
+
+template <int KS, int NP, int RB, bool BY_CLASS, typename T>
+__global__ __launch_bounds__(256, RB * KS * (4 * NP + 8) > 192 ? 1 : 2) void k_class_grad(ClassGradArgs g) {
+    constexpr int N = 2 * KS * NP;
+    constexpr bool TWO = two_tiles(N);
+    __shared__ uint4 s_tile[TWO ? 2 : 1][N * 64];
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4;
+    const int64_t block0 = ((int64_t)blockIdx.x * 4 + wave) * RB;
+    const int t0 = (int)((int64_t)g.tiles * blockIdx.y / g.splits), t1 = (int)((int64_t)g.tiles * (blockIdx.y + 1) / g.splits);
+    if (t0 < t1) fetch_tile<N>(g.stream + (int64_t)t0 * N * 64, s_tile[0], wave, lane);
+    bf16x8 own[RB][KS][NP];
+    load_own<KS, NP, RB>(g.own, block0, lane, own);
+    // of this wave's rows: lse and class (BY_CLASS: bias and class number); the same of streamed rows comes with the tile
+    float own_f[RB];
+    int own_c[RB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        const int64_t i = (block0 + r) * 16 + (lane & 15);
+        own_f[r] = BY_CLASS ? g.bias[i] : g.lse[i];
+        own_c[r] = BY_CLASS ? (int)i : g.target[i];
+    }
+    f32x4 acc[RB][2 * KS];
+    double bias_sum[RB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        bias_sum[r] = 0.0;
+#pragma unroll
+        for (int c = 0; c < 2 * KS; ++c) acc[r][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    tile_arrived();
+    for (int t = t0; t < t1; ++t) {
+        const uint4* tile = s_tile[TWO ? (t - t0) & 1 : 0];
+        if (TWO && t + 1 < t1) fetch_tile<N>(g.stream + (int64_t)(t + 1) * N * 64, s_tile[TWO ? (t - t0 + 1) & 1 : 0], wave, lane);
+        f32x4 z[2][RB], row_f[2];
+        int row_c[2][4];
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk) {
+            const int64_t i = (int64_t)t * kTileRows + blk * 16 + grp * 4;
+            row_f[blk] = *reinterpret_cast<const f32x4*>((BY_CLASS ? g.lse : g.bias) + i);
+            int4 c = make_int4((int)i, (int)i + 1, (int)i + 2, (int)i + 3);
+            if constexpr (BY_CLASS) c = *reinterpret_cast<const int4*>(g.target + i);
+            row_c[blk][0] = c.x; row_c[blk][1] = c.y; row_c[blk][2] = c.z; row_c[blk][3] = c.w;
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+                z[blk][r] = BY_CLASS ? f32x4{own_f[r], own_f[r], own_f[r], own_f[r]} : row_f[blk];
+        }
+        tile_logits<KS, NP, RB>(tile, own, lane, z);
+        bf16x8 dz[RB][NP];
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+#pragma unroll
+            for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float l = BY_CLASS ? row_f[blk][i] : own_f[r];
+                    const float p = __builtin_amdgcn_exp2f((z[blk][r][i] - l) * kLog2e);
+                    z[blk][r][i] = row_c[blk][i] == own_c[r] ? p - 1.0f : p;
+                }
+            if constexpr (BY_CLASS) {
+                const f32x4 s = z[0][r] + z[1][r];
+                bias_sum[r] += (double)((s[0] + s[1]) + (s[2] + s[3]));
+            }
+            operand_of<NP>(z[0][r], z[1][r], dz[r]);
+        }
+#pragma unroll
+        for (int c = 0; c < 2 * KS; ++c) {
+            bf16x8 b[NP];
+#pragma unroll
+            for (int p = 0; p < NP; ++p) b[p] = join8(column_of_lds<KS, NP>(tile, 0, c, p, lane), column_of_lds<KS, NP>(tile, 1, c, p, lane));
+#pragma unroll
+            for (int r = 0; r < RB; ++r) acc[r][c] = mfma_pieces<NP>(dz[r], b, acc[r][c]);
+        }
+        if constexpr (!TWO) {
+            __syncthreads();
+            if (t + 1 < t1) fetch_tile<N>(g.stream + (int64_t)(t + 1) * N * 64, s_tile[0], wave, lane);
+        }
+        tile_arrived();
+    }
+    const float scale = gradient_scale(g.counts, g.count_blocks, g.scale);
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        const int64_t row0 = (block0 + r) * 16 + grp * 4;
+        if constexpr (BY_CLASS) {
+            bias_sum[r] += __shfl_xor(bias_sum[r], 16);
+            bias_sum[r] += __shfl_xor(bias_sum[r], 32);
+            if (grp == 0) g.bias_part[blockIdx.y * g.own_pad + (block0 + r) * 16 + lane] = bias_sum[r];
+        }
+#pragma unroll
+        for (int c = 0; c < 2 * KS; ++c) {
+            if (!g.out) break;                  // only the bias is asked for
+            const int col = c * 16 + (lane & 15);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (g.splits > 1) {
+                    g.part[((int64_t)blockIdx.y * g.own_pad + row0 + i) * (KS * 32) + col] = acc[r][c][i];
+                } else if (row0 + i < g.rows && col < g.d) {
+                    const int plane = col / g.dg;
+                    store_as(static_cast<T*>(g.out) + plane * g.gs + (row0 + i) * g.ld + (col - plane * g.dg), acc[r][c][i] * scale);
+                }
+            }
+        }
+    }
+}
+// the splits' sums joined: a thread per value
+template <typename T>
+__global__ __launch_bounds__(256) void k_class_grad_join(ClassGradArgs g, int width) {
+    const float scale = gradient_scale(g.counts, g.count_blocks, g.scale);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < g.rows * g.d; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / g.d;
+        const int col = (int)(i - row * g.d), plane = col / g.dg;
+        float v = 0.0f;
+        for (int s = 0; s < g.splits; ++s) v += g.part[((int64_t)s * g.own_pad + row) * width + col];
+        store_as(static_cast<T*>(g.out) + plane * g.gs + row * g.ld + (col - plane * g.dg), v * scale);
+    }
+}
+__global__ __launch_bounds__(256) void k_class_bias_join(const double* __restrict__ part, int64_t own_pad, int splits, const int32_t* __restrict__ counts,
+                                                         int count_blocks, float scale, int64_t classes, float* __restrict__ dbias) {
+    const float k = gradient_scale(counts, count_blocks, scale);
+    const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (j >= classes) return;
+    double v = 0.0;
+    for (int s = 0; s < splits; ++s) v += part[s * own_pad + j];
+    dbias[j] = (float)(v * (double)k);
+}
+
+// ---- host side ---------------------------------------------------------------------------------------------
+namespace {
+
+constexpr int kPadRows = 256;                   // operands are laid out to a multiple of what a workgroup keeps at most
+constexpr int kMaxSplits = 64;
+
+bool aligned_to(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+
+int steps_of(int d) {
+    for (int ks : {1, 2, 4, 6, 8, 12}) if (d <= 32 * ks) return ks;
+    return 16;
+}
+// 16-row blocks that a wave keeps: as many as leave two waves of a SIMD their registers, one at least
+constexpr int loss_blocks(int ks, int np) { return ks * np * 16 <= 128 ? 4 : ks * np * 8 <= 128 ? 2 : 1; }
+constexpr int grad_blocks(int ks, int np) { return ks * (4 * np + 8) * 4 <= 128 ? 4 : ks * (4 * np + 8) * 2 <= 192 ? 2 : 1; }
+
+// Parts that the streamed side is cut into, so that `blocks` workgroups of it fill the card: the shortest schedule over 512 places, a tile of
+// extra work for every part.
+int splits_of(int64_t blocks, int64_t tiles) {
+    constexpr int64_t places = 512;
+    int best = 1;
+    double least = 1e300;
+    for (int s = 1; s <= kMaxSplits && s <= tiles; ++s) {
+        const double time = (double)((blocks * s + places - 1) / places) * ((double)((tiles + s - 1) / s) + 1.0);
+        if (time < 0.97 * least) {
+            least = time;
+            best = s;
+        }
+    }
+    return best;
+}
+struct ClassPlan {
+    int ks, np, loss_rb, grad_rb;
+    int64_t x_pad, e_pad;
+    int loss_splits, x_splits, e_splits;
+    size_t xf, ef, lse, bias, target, counts, loss_bytes;       // the first of these are shared
+    size_t part, at_target, parts;                              // forward
+    size_t x_part, e_part, bias_part, grad_bytes;               // backward
+};
+ClassPlan class_plan(int64_t n, int64_t classes, int32_t d, int32_t dtype) {
+    ClassPlan p{};
+    p.ks = steps_of(d);
+    p.np = dtype == GSR_F32 ? 3 : 1;
+    p.loss_rb = loss_blocks(p.ks, p.np);
+    p.grad_rb = grad_blocks(p.ks, p.np);
+    p.x_pad = (n + kPadRows - 1) / kPadRows * kPadRows;
+    p.e_pad = (classes + kPadRows - 1) / kPadRows * kPadRows;
+    const int64_t x_tiles = (n + kTileRows - 1) / kTileRows, e_tiles = (classes + kTileRows - 1) / kTileRows;
+    auto blocks = [](int64_t rows, int rb) { return (rows + 64 * rb - 1) / (64 * rb); };
+    p.loss_splits = splits_of(blocks(n, p.loss_rb), e_tiles);
+    p.x_splits = splits_of(blocks(n, p.grad_rb), e_tiles);
+    p.e_splits = splits_of(blocks(classes, p.grad_rb), x_tiles);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += align_up(bytes);
+        return here;
+    };
+    p.xf = take((size_t)p.x_pad * p.ks * 64 * p.np);
+    p.ef = take((size_t)p.e_pad * p.ks * 64 * p.np);
+    p.lse = take((size_t)p.x_pad * 4);
+    p.bias = take((size_t)p.e_pad * 4);
+    p.target = take((size_t)p.x_pad * 4);
+    p.counts = take((size_t)((p.x_pad + 1023) / 1024) * 4);
+    const size_t shared = at;
+    p.part = take((size_t)p.loss_splits * p.x_pad * sizeof(float2));
+    p.at_target = take((size_t)p.x_pad * 4);
+    p.parts = take((size_t)((n + 1023) / 1024) * sizeof(LossPart));
+    p.loss_bytes = at;
+    at = shared;
+    p.bias_part = take((size_t)p.e_splits * p.e_pad * sizeof(double));
+    // one after the other in the same place
+    p.x_part = p.e_part = at;
+    const size_t xp = p.x_splits > 1 ? (size_t)p.x_splits * p.x_pad * p.ks * 128 : 0, ep = p.e_splits > 1 ? (size_t)p.e_splits * p.e_pad * p.ks * 128 : 0;
+    p.grad_bytes = at + align_up(std::max(xp, ep));
+    return p;
+}
+
+template <typename Call>
+void by_steps(int ks, Call call) {
+    switch (ks) {
+        case 1: return call(std::integral_constant<int, 1>{});
+        case 2: return call(std::integral_constant<int, 2>{});
+        case 4: return call(std::integral_constant<int, 4>{});
+        case 6: return call(std::integral_constant<int, 6>{});
+        case 8: return call(std::integral_constant<int, 8>{});
+        case 12: return call(std::integral_constant<int, 12>{});
+        default: return call(std::integral_constant<int, 16>{});
+    }
+}
+
+struct ClassShape {
+    RowSource x, e;
+    ClassTokens ids;
+};
+gsr_status_t class_shape(const void* x, int64_t ldx, int64_t n, int32_t d, int32_t c, int32_t layout, int32_t dtype, const void* table, int64_t classes,
+                         int64_t ldt, const float* bias, const void* ids, int32_t ids_i64, ClassShape* s) {
+    if (n < 0) return fail(GSR_ERR_INVALID_ARG, "negative n");
+    if (n >= ((int64_t)1 << 31) - kPadRows) return fail(GSR_ERR_UNSUPPORTED, "n=%lld too large", (long long)n);
+    if (classes < 1) return fail(GSR_ERR_INVALID_ARG, "%lld classes", (long long)classes);
+    if (classes >= ((int64_t)1 << 31) - kPadRows) return fail(GSR_ERR_UNSUPPORTED, "%lld classes", (long long)classes);
+    if (d < 1 || d > kMaxClassWidth) return fail(GSR_ERR_UNSUPPORTED, "d=%d outside [1, %d]", d, kMaxClassWidth);
+    if (c < 1 || d % c) return fail(GSR_ERR_UNSUPPORTED, "c=%d does not divide d=%d", c, d);
+    if (layout != GSR_LAYOUT_ROW_MAJOR && layout != GSR_LAYOUT_GROUP_PLANAR) return fail(GSR_ERR_INVALID_ARG, "layout %d", layout);
+    if (dtype != GSR_F32 && dtype != GSR_BF16) return fail(GSR_ERR_UNSUPPORTED, "dtype %d", dtype);
+    const int dg = layout == GSR_LAYOUT_GROUP_PLANAR ? d / c : d;
+    if (ldx < dg || ldx >= ((int64_t)1 << 31)) return fail(GSR_ERR_INVALID_ARG, "row stride %lld outside [%d, 2^31)", (long long)ldx, dg);
+    if (ldt < d || ldt >= ((int64_t)1 << 31)) return fail(GSR_ERR_INVALID_ARG, "row stride %lld of the table outside [%d, 2^31)", (long long)ldt, d);
+    if (!table || (n > 0 && (!x || !ids))) return fail(GSR_ERR_INVALID_ARG, "null pointer");
+    if (!aligned_to(x, dtype_size(dtype)) || !aligned_to(table, dtype_size(dtype)) || !aligned_to(bias, 4) || !aligned_to(ids, ids_i64 ? 8 : 4))
+        return fail(GSR_ERR_INVALID_ARG, "a pointer is not aligned to its elements");
+    s->x = RowSource{x, n, ldx, n * ldx, d, dg};
+    s->e = RowSource{table, classes, ldt, 0, d, d};
+    s->ids = ClassTokens{ids, ids_i64, (int32_t)classes};
+    return GSR_OK;
+}
+gsr_status_t class_workspace(size_t need, const void* workspace, size_t bytes) {
+    if (bytes < need) return fail(GSR_ERR_WORKSPACE_TOO_SMALL, "workspace of %zu bytes, %zu needed", bytes, need);
+    if (!workspace || !aligned_to(workspace, 16)) return fail(GSR_ERR_INVALID_ARG, "workspace null or not aligned to 16 bytes");
+    return GSR_OK;
+}
+ClassSetup launch_setup(const ClassShape& s, const ClassPlan& p, const float* bias, const float* lse, char* ws, int32_t dtype, hipStream_t st) {
+    ClassSetup a{};
+    a.x = s.x;
+    a.e = s.e;
+    a.ids = s.ids;
+    a.xf = (uint4*)(ws + p.xf);
+    a.ef = (uint4*)(ws + p.ef);
+    a.lse = lse;
+    a.bias = bias;
+    a.lse_out = (float*)(ws + p.lse);
+    a.bias_out = (float*)(ws + p.bias);
+    a.target = (int32_t*)(ws + p.target);
+    a.counts = (int32_t*)(ws + p.counts);
+    a.x_pad = p.x_pad;
+    a.e_pad = p.e_pad;
+    a.ks = p.ks;
+    a.x_blocks = (unsigned)((p.x_pad / 16 * p.ks + 3) / 4);
+    a.e_blocks = (unsigned)((p.e_pad / 16 * p.ks + 3) / 4);
+    a.row_blocks = (unsigned)((p.x_pad + 1023) / 1024);
+    a.bias_blocks = (unsigned)((p.e_pad + 1023) / 1024);
+    const dim3 grid(a.x_blocks + a.e_blocks + a.row_blocks + a.bias_blocks);
+    if (dtype == GSR_F32) hipLaunchKernelGGL((k_class_setup<float, 3>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_class_setup<bf16_t, 1>), grid, dim3(256), 0, st, a);
+    return a;
+}
+
+template <int KS, typename T, bool BY_CLASS>
+void launch_grad(const ClassGradArgs& g, hipStream_t st) {
+    constexpr int NP = sizeof(T) == 4 ? 3 : 1, RB = grad_blocks(KS, NP);
+    const dim3 grid((unsigned)((g.rows + 64 * RB - 1) / (64 * RB)), (unsigned)g.splits);
+    hipLaunchKernelGGL((k_class_grad<KS, NP, RB, BY_CLASS, T>), grid, dim3(256), 0, st, g);
+    if (g.splits > 1 && g.out) {
+        const unsigned wgs = (unsigned)std::min<int64_t>((g.rows * g.d + 255) / 256, 1 << 20);
+        hipLaunchKernelGGL((k_class_grad_join<T>), dim3(wgs), dim3(256), 0, st, g, KS * 32);
+    }
+}
+
+}  // namespace
+}  // namespace gsr
+
+using namespace gsr;
+
+extern "C" {
+
+size_t gsr_class_loss_workspace(int64_t n, int64_t classes, int32_t d, int32_t dtype) {
+    if (n < 0 || n >= ((int64_t)1 << 31) - kPadRows || classes < 1 || classes >= ((int64_t)1 << 31) - kPadRows || d < 1 || d > kMaxClassWidth ||
+        (dtype != GSR_F32 && dtype != GSR_BF16))
+        return 0;
+    return class_plan(n, classes, d, dtype).loss_bytes;
+}
+size_t gsr_class_grad_workspace(int64_t n, int64_t classes, int32_t d, int32_t dtype) {
+    return gsr_class_loss_workspace(n, classes, d, dtype) ? class_plan(n, classes, d, dtype).grad_bytes : 0;
+}
+
+gsr_status_t gsr_class_loss(const void* x, int64_t ldx, int64_t n, int32_t d, int32_t c, int32_t layout, int32_t dtype, const void* table,
+                            int64_t classes, int64_t ldt, const float* bias, const void* ids, int32_t ids_i64, float* loss_out, float* lse_out,
+                            void* workspace, size_t workspace_bytes, void* stream) {
+    ClassShape s;
+    GSR_TRY(class_shape(x, ldx, n, d, c, layout, dtype, table, classes, ldt, bias, ids, ids_i64, &s));
+    if (!loss_out || (n > 0 && !lse_out)) return fail(GSR_ERR_INVALID_ARG, "null loss_out or lse_out");
+    if (!aligned_to(loss_out, 4) || !aligned_to(lse_out, 4)) return fail(GSR_ERR_INVALID_ARG, "loss_out or lse_out is not aligned to its elements");
+    const ClassPlan p = class_plan(n, classes, d, dtype);
+    GSR_TRY(class_workspace(p.loss_bytes, workspace, workspace_bytes));
+    hipStream_t st = (hipStream_t)stream;
+    char* ws = (char*)workspace;
+    const int blocks = (int)((n + 1023) / 1024);
+    LossPart* parts = (LossPart*)(ws + p.parts);
+    if (n) {
+        const ClassSetup a = launch_setup(s, p, bias, nullptr, ws, dtype, st);
+        const ClassLossArgs g{a.xf, a.ef, a.bias_out, a.target, (float2*)(ws + p.part), (float*)(ws + p.at_target), p.x_pad,
+                              (int32_t)((classes + kTileRows - 1) / kTileRows), p.loss_splits};
+        by_steps(p.ks, [&](auto k) {
+            constexpr int KS = k.value, R1 = loss_blocks(KS, 1), R3 = loss_blocks(KS, 3);
+            const dim3 grid((unsigned)((n + 64 * p.loss_rb - 1) / (64 * p.loss_rb)), (unsigned)p.loss_splits);
+            if (dtype == GSR_F32) hipLaunchKernelGGL((k_class_loss<KS, 3, R3>), grid, dim3(256), 0, st, g);
+            else hipLaunchKernelGGL((k_class_loss<KS, 1, R1>), grid, dim3(256), 0, st, g);
+        });
+        hipLaunchKernelGGL(k_class_lse, dim3(blocks), dim3(1024), 0, st, g.part, g.at_target, a.target, n, p.x_pad, p.loss_splits, lse_out, parts, loss_out);
+    }
+    if (blocks != 1) hipLaunchKernelGGL(k_class_loss_sum, dim3(1), dim3(1024), 0, st, parts, blocks, loss_out);
+    GSR_HIP_CHECK(hipGetLastError());
+    return GSR_OK;
+}
+
+gsr_status_t gsr_class_grad(const void* x, int64_t ldx, int64_t n, int32_t d, int32_t c, int32_t layout, int32_t dtype, const void* table,
+                            int64_t classes, int64_t ldt, const float* bias, const void* ids, int32_t ids_i64, const float* lse, float scale,
+                            void* dx_out, int64_t lddx, void* dtable_out, int64_t lddt, float* dbias_out, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+    ClassShape s;
+    GSR_TRY(class_shape(x, ldx, n, d, c, layout, dtype, table, classes, ldt, bias, ids, ids_i64, &s));
+    if (n > 0 && !lse) return fail(GSR_ERR_INVALID_ARG, "null lse");
+    if (!dx_out && !dtable_out && !dbias_out) return fail(GSR_ERR_INVALID_ARG, "no gradient asked for");
+    if (dx_out && (lddx < s.x.dg || lddx >= ((int64_t)1 << 31))) return fail(GSR_ERR_INVALID_ARG, "row stride %lld of dx_out outside [%d, 2^31)", (long long)lddx, s.x.dg);
+    if (dtable_out && (lddt < d || lddt >= ((int64_t)1 << 31))) return fail(GSR_ERR_INVALID_ARG, "row stride %lld of dtable_out outside [%d, 2^31)", (long long)lddt, d);
+    if (!aligned_to(lse, 4) || !aligned_to(dbias_out, 4) || !aligned_to(dx_out, dtype_size(dtype)) || !aligned_to(dtable_out, dtype_size(dtype)))
+        return fail(GSR_ERR_INVALID_ARG, "a pointer is not aligned to its elements");
+    const ClassPlan p = class_plan(n, classes, d, dtype);
+    GSR_TRY(class_workspace(p.grad_bytes, workspace, workspace_bytes));
+    hipStream_t st = (hipStream_t)stream;
+    char* ws = (char*)workspace;
+    ClassSetup a{};
+    a = launch_setup(s, p, bias, lse, ws, dtype, st);
+    ClassGradArgs g{};
+    g.lse = a.lse_out;
+    g.bias = a.bias_out;
+    g.target = a.target;
+    g.counts = a.counts;
+    g.count_blocks = (int32_t)a.row_blocks;
+    g.bias_part = (double*)(ws + p.bias_part);
+    g.scale = scale;
+    g.d = d;
+    by_steps(p.ks, [&](auto k) {
+        constexpr int KS = k.value;
+        if (dx_out && n) {
+            g.own = a.xf;
+            g.stream = a.ef;
+            g.out = dx_out;
+            g.rows = n;
+            g.ld = lddx;
+            g.gs = n * lddx;
+            g.dg = s.x.dg;
+            g.own_pad = p.x_pad;
+            g.part = (float*)(ws + p.x_part);
+            g.tiles = (int32_t)((classes + kTileRows - 1) / kTileRows);
+            g.splits = p.x_splits;
+            if (dtype == GSR_F32) launch_grad<KS, float, false>(g, st);
+            else launch_grad<KS, bf16_t, false>(g, st);
+        }
+        if (dtable_out || dbias_out) {
+            g.own = a.ef;
+            g.stream = a.xf;
+            g.out = dtable_out;
+            g.rows = classes;
+            g.ld = lddt;
+            g.gs = 0;
+            g.dg = d;
+            g.own_pad = p.e_pad;
+            g.part = (float*)(ws + p.e_part);
+            g.tiles = (int32_t)((n + kTileRows - 1) / kTileRows);
+            g.splits = p.e_splits;
+            if (dtype == GSR_F32) launch_grad<KS, float, true>(g, st);
+            else launch_grad<KS, bf16_t, true>(g, st);
+            if (dbias_out)
+                hipLaunchKernelGGL(k_class_bias_join, dim3((unsigned)((classes + 255) / 256)), dim3(256), 0, st, g.bias_part, p.e_pad, p.e_splits, g.counts,
+                                   g.count_blocks, scale, classes, dbias_out);
+        }
+    });
+    GSR_HIP_CHECK(hipGetLastError());
+    return GSR_OK;
+}
+
+}  // extern "C"
