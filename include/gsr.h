@@ -391,8 +391,8 @@ gsr_status_t gsr_adam_update_list(float* const* w, const void* const* dw, float*
  * float32 first, in an order that the sizes and the offsets alone fix.  A mean further than 2^20 standard deviations from zero loses the variance.
  * y_out may be x and dx_out may be dy, with the same stride; apart from that what a call writes overlaps nothing that it reads.
  * eps > 0; 1 <= d <= 131072; n < 2^31; pointers aligned to their elements.  workspace: device, 16-byte aligned, at least
- * gsr_group_norm_workspace() bytes (0: sizes that are refused); it holds nothing between calls.  Calls only launch kernels and may be captured;
- * calls with workspaces of their own may run side by side. */
+ * gsr_group_norm_workspace() bytes (0: sizes that are refused; never fewer for more rows or graphs, so that one serves any fewer); it holds nothing between
+ * calls.  Calls only launch kernels and may be captured; calls with workspaces of their own may run side by side. */
 typedef enum gsr_act { GSR_ACT_NONE = 0, GSR_ACT_RELU = 1, GSR_ACT_SILU = 2 } gsr_act_t;
 size_t gsr_group_norm_workspace(int64_t n, int64_t graphs, int32_t d, int32_t c, int32_t layout, int32_t dtype, int32_t groups);
 gsr_status_t gsr_group_norm(const void* x, int64_t ldx, int64_t n, int32_t d, int32_t c, int32_t layout, int32_t dtype, const void* graph_ptr,
@@ -436,8 +436,8 @@ gsr_status_t gsr_checkpoint_load(const int8_t* codes, const float* scales, int64
  * float32 values enter the products exactly, and sums are taken in float32 (the loss and dbias: in float64 across tiles).  With 16-bit planes
  * dz is rounded to 16 bits before the products with E and x.  Equal calls give equal bits.  Values must be finite: a row with infinities or NaN gets a
  * loss that is none, which then is the mean's.  1 <= d <= 512, c divides d, n and classes below 2^31 - 256; pointers aligned to their elements.
- * workspace: device, 16-byte aligned, at least gsr_class_loss_workspace() / gsr_class_grad_workspace() bytes (0: sizes that are refused), some
- * copies of x and E; it holds nothing between calls.  What a call writes overlaps nothing that it reads.  Calls only launch kernels and may be captured;
+ * workspace: device, 16-byte aligned, at least gsr_class_loss_workspace() / gsr_class_grad_workspace() bytes (0: sizes that are refused; never
+ * fewer for more rows or classes, so that one serves any fewer), some copies of x and E; it holds nothing between calls.  What a call writes overlaps nothing that it reads.  Calls only launch kernels and may be captured;
  * calls with workspaces of their own may run side by side. */
 size_t gsr_class_loss_workspace(int64_t n, int64_t classes, int32_t d, int32_t dtype);
 size_t gsr_class_grad_workspace(int64_t n, int64_t classes, int32_t d, int32_t dtype);

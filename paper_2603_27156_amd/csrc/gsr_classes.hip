@@ -514,6 +514,7 @@ namespace {
 
 constexpr int kPadRows = 256;                   // operands are laid out to a multiple of what a workgroup keeps at most
 constexpr int kMaxSplits = 64;
+constexpr int64_t kMaxPartRows = 1 << 17;       // rows of partial sums, of all parts together
 
 bool aligned_to(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 
@@ -527,11 +528,11 @@ constexpr int grad_blocks(int ks, int np) { return ks * (4 * np + 8) * 4 <= 128 
 
 // Parts that the streamed side is cut into, so that `blocks` workgroups of it fill the card: the shortest schedule over 512 places, a tile of
 // extra work for every part.
-int splits_of(int64_t blocks, int64_t tiles) {
+int splits_of(int64_t blocks, int64_t tiles, int64_t pad) {
     constexpr int64_t places = 512;
     int best = 1;
     double least = 1e300;
-    for (int s = 1; s <= kMaxSplits && s <= tiles; ++s) {
+    for (int s = 1; s <= kMaxSplits && s <= tiles && (s == 1 || s * pad <= kMaxPartRows); ++s) {
         const double time = (double)((blocks * s + places - 1) / places) * ((double)((tiles + s - 1) / s) + 1.0);
         if (time < 0.97 * least) {
             least = time;
@@ -540,6 +541,8 @@ int splits_of(int64_t blocks, int64_t tiles) {
     }
     return best;
 }
+// Rows of partial sums that a workspace has room for: what any split of as many rows or fewer can need, so that a workspace serves them all.
+int64_t part_rows(int64_t tiles, int64_t pad) { return std::min(kMaxPartRows, std::min<int64_t>(kMaxSplits, tiles) * pad); }
 struct ClassPlan {
     int ks, np, loss_rb, grad_rb;
     int64_t x_pad, e_pad;
@@ -558,9 +561,9 @@ ClassPlan class_plan(int64_t n, int64_t classes, int32_t d, int32_t dtype) {
     p.e_pad = (classes + kPadRows - 1) / kPadRows * kPadRows;
     const int64_t x_tiles = (n + kTileRows - 1) / kTileRows, e_tiles = (classes + kTileRows - 1) / kTileRows;
     auto blocks = [](int64_t rows, int rb) { return (rows + 64 * rb - 1) / (64 * rb); };
-    p.loss_splits = splits_of(blocks(n, p.loss_rb), e_tiles);
-    p.x_splits = splits_of(blocks(n, p.grad_rb), e_tiles);
-    p.e_splits = splits_of(blocks(classes, p.grad_rb), x_tiles);
+    p.loss_splits = splits_of(blocks(n, p.loss_rb), e_tiles, p.x_pad);
+    p.x_splits = splits_of(blocks(n, p.grad_rb), e_tiles, p.x_pad);
+    p.e_splits = splits_of(blocks(classes, p.grad_rb), x_tiles, p.e_pad);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -574,16 +577,15 @@ ClassPlan class_plan(int64_t n, int64_t classes, int32_t d, int32_t dtype) {
     p.target = take((size_t)p.x_pad * 4);
     p.counts = take((size_t)((p.x_pad + 1023) / 1024) * 4);
     const size_t shared = at;
-    p.part = take((size_t)p.loss_splits * p.x_pad * sizeof(float2));
+    const int64_t x_parts = part_rows(e_tiles, p.x_pad), e_parts = part_rows(x_tiles, p.e_pad);
+    p.part = take((size_t)std::max(p.x_pad, x_parts) * sizeof(float2));
     p.at_target = take((size_t)p.x_pad * 4);
     p.parts = take((size_t)((n + 1023) / 1024) * sizeof(LossPart));
     p.loss_bytes = at;
     at = shared;
-    p.bias_part = take((size_t)p.e_splits * p.e_pad * sizeof(double));
-    // one after the other in the same place
-    p.x_part = p.e_part = at;
-    const size_t xp = p.x_splits > 1 ? (size_t)p.x_splits * p.x_pad * p.ks * 128 : 0, ep = p.e_splits > 1 ? (size_t)p.e_splits * p.e_pad * p.ks * 128 : 0;
-    p.grad_bytes = at + align_up(std::max(xp, ep));
+    p.bias_part = take((size_t)std::max(p.e_pad, e_parts) * sizeof(double));
+    p.x_part = p.e_part = at;                                   // one after the other in the same place
+    p.grad_bytes = at + align_up((size_t)std::max(x_parts, e_parts) * p.ks * 128);
     return p;
 }
 

@@ -36,7 +36,8 @@ struct GraphRows {
 };
 
 // How rows and columns are dealt out.  Columns go to lanes in pieces of V; 2^lanes_log2 lanes hold a slab of a row and the wave 64 >> lanes_log2
-// rows at a time.  A slab never crosses the border of a plane of a GROUP_PLANAR tensor.
+// rows at a time.  A slab never crosses the border of a plane of a GROUP_PLANAR tensor.  Where V does not divide a plane's columns (TAIL) the last
+// piece of a row begins before its own columns, in those of the lane before, which count there alone.
 struct NormShape {
     int64_t n, chunks;              // chunks of `rows` rows, one per wave
     int32_t d, dg, cg, groups;
@@ -51,8 +52,10 @@ struct RowPlane {
 // What a lane holds of its slab.
 struct LaneColumns {
     int sub, subs;                  // its row of the wave's, and how many there are
-    int plane, col;                 // plane and first column of it
+    int plane, col;                 // plane and first column of it that is loaded
     int column;                     // the same in the whole row of d
+    int own;                        // first column of its own: col + skip
+    int skip;                       // TAIL: columns that are the lane's before
     int group;                      // the group of all its columns; -1 for a lane without columns
     bool on, head;                  // head: the first lane of its group in the slab
     uint32_t joins;                 // bit k: the lane 2^k further holds columns of the same group
@@ -69,9 +72,11 @@ __device__ __forceinline__ LaneColumns lane_columns(const NormShape& s, int slab
         const int col = first + l * V;
         return l >= 0 && l < lanes && col < s.dg ? (c.plane * s.dg + col) / s.cg : -1;
     };
-    c.col = first + li * V;
-    c.on = c.col < s.dg;
-    if (!c.on) c.col = 0;
+    c.own = first + li * V;
+    c.on = c.own < s.dg;
+    if (!c.on) c.own = 0;
+    c.col = c.own + V <= s.dg ? c.own : s.dg - V;
+    c.skip = c.own - c.col;
     c.column = c.plane * s.dg + c.col;
     c.group = group(li);
     c.head = c.on && group(li - 1) != c.group;
@@ -159,25 +164,29 @@ __device__ __forceinline__ double wave_total(double v) {
     for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
     return v;
 }
-// (graph, group) of this wave (WIDE: of this workgroup of 256) and the sums of its pieces, in every lane of (the first) wave; false: no task
+// (graph, group) of this wave (WIDE: of this workgroup of 1,024) and the sums of its pieces, in every lane of (the first) wave; false: no task
 template <bool WIDE>
 __device__ __forceinline__ bool joined(const NormShape& s, const GraphRows& g, int V, int64_t block, const double2* __restrict__ pieces,
                                        int64_t& task, double& u, double& v, int64_t& rows) {
-    task = WIDE ? block : block * 4 + (threadIdx.x >> 6);
+    task = WIDE ? block : block * 16 + (threadIdx.x >> 6);
     if (task >= g.graphs * s.groups) return false;      // (WIDE: the whole workgroup or none)
-    add_pieces(s, g, V, task / s.groups, (int)(task % s.groups), WIDE ? threadIdx.x : lane_id(), WIDE ? 256 : 64, pieces, u, v, rows);
+    add_pieces(s, g, V, task / s.groups, (int)(task % s.groups), WIDE ? threadIdx.x : lane_id(), WIDE ? 1024 : 64, pieces, u, v, rows);
     u = wave_total(u);
     v = wave_total(v);
     if constexpr (WIDE) {
-        __shared__ double s_sum[4][2];
+        __shared__ double s_sum[16][2];
         if (lane_id() == 0) {
             s_sum[threadIdx.x >> 6][0] = u;
             s_sum[threadIdx.x >> 6][1] = v;
         }
         __syncthreads();
         if (threadIdx.x >= 64) return false;
-        u = (s_sum[0][0] + s_sum[1][0]) + (s_sum[2][0] + s_sum[3][0]);
-        v = (s_sum[0][1] + s_sum[1][1]) + (s_sum[2][1] + s_sum[3][1]);
+        u = v = 0.0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            u += s_sum[i][0];
+            v += s_sum[i][1];
+        }
     }
     return true;
 }
@@ -217,17 +226,39 @@ __device__ __forceinline__ int code_of(float x, float top, float inv) {
     }
     return (int)q;
 }
-template <int V>
-__device__ __forceinline__ void store_codes(int8_t* p, const int (&q)[V]) {
+typedef uint32_t u32_b __attribute__((aligned(1)));
+typedef uint16_t u16_b __attribute__((aligned(1)));
+// V codes, or with a tail the last V - skip of them
+template <int V, bool TAIL>
+__device__ __forceinline__ void store_codes(int8_t* p, const int (&q)[V], int skip) {
     if constexpr (V == 1) {
         *p = (int8_t)q[0];
     } else {
-        typedef uint32_t words __attribute__((ext_vector_type(V / 4), aligned(4)));
+        typedef uint32_t words __attribute__((ext_vector_type(V / 4), aligned(TAIL ? 1 : 4)));
         words t;
 #pragma unroll
         for (int i = 0; i < V / 4; ++i)
             t[i] = (q[4 * i] & 0xFF) | (q[4 * i + 1] & 0xFF) << 8 | (q[4 * i + 2] & 0xFF) << 16 | (uint32_t)q[4 * i + 3] << 24;
-        __builtin_nontemporal_store(t, reinterpret_cast<words*>(p));
+        if (TAIL && skip) {
+            uint64_t w = t[0];
+            if constexpr (V == 8) w |= (uint64_t)t[1] << 32;
+            w >>= 8 * skip;
+            p += skip;
+            const int own = V - skip;
+            if (own & 4) {
+                *reinterpret_cast<u32_b*>(p) = (uint32_t)w;
+                w >>= 32;
+                p += 4;
+            }
+            if (own & 2) {
+                *reinterpret_cast<u16_b*>(p) = (uint16_t)w;
+                w >>= 16;
+                p += 2;
+            }
+            if (own & 1) *p = (int8_t)w;
+        } else {
+            __builtin_nontemporal_store(t, reinterpret_cast<words*>(p));
+        }
     }
 }
 struct Checkpoint {
@@ -236,13 +267,13 @@ struct Checkpoint {
     int32_t blocks, plane_blocks;   // of a row, of a plane's part of it
 };
 // The codes of a lane's V values; every lane of the wave takes part.
-template <int V>
+template <int V, bool TAIL>
 __device__ __forceinline__ void save_piece(const Checkpoint& k, const NormShape& s, const LaneColumns& c, int64_t row, bool in, const float (&x)[V]) {
     uint32_t bits = 0;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         const uint32_t b = __float_as_uint(x[j]) & 0x7FFFFFFFu;         // an infinity is above every number, NaN above that
-        bits = bits > b ? bits : b;
+        bits = bits > b || (TAIL && j < c.skip) ? bits : b;
     }
     if (!c.on) bits = 0;
     const int lanes = 1 << s.lanes_log2;
@@ -253,9 +284,9 @@ __device__ __forceinline__ void save_piece(const Checkpoint& k, const NormShape&
     int q[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) q[j] = finite ? code_of(x[j], top, inv) : 0;
-    store_codes<V>(k.codes + row * s.d + c.column, q);
-    if (c.col % kBlock == 0)
-        k.scales[row * k.blocks + c.plane * k.plane_blocks + c.col / kBlock] = finite ? fminf(top / 127.0f, kLargestScale) : __builtin_nanf("");
+    store_codes<V, TAIL>(k.codes + row * s.d + c.column, q, c.skip);
+    if (c.own % kBlock == 0)
+        k.scales[row * k.blocks + c.plane * k.plane_blocks + c.own / kBlock] = finite ? fminf(top / 127.0f, kLargestScale) : __builtin_nanf("");
 }
 
 // Where the values of a plane come from: the plane, or its checkpoint.
@@ -269,30 +300,38 @@ struct PlaneSource {
     }
     __device__ __forceinline__ float at(int j) const { return w.at(j); }
 };
-template <int V>
+template <int V, bool TAIL>
 struct CodeSource {
     Checkpoint k;
     uint32_t w[V == 1 ? 1 : V / 4];
-    float scale;
+    float scale, scale_before;      // scale_before: of the columns before a block's border, in a tail
+    int before;
     __device__ __forceinline__ void load(const NormShape& s, const LaneColumns& c, int64_t row) {
         const int8_t* p = k.codes + row * s.d + c.column;
         if constexpr (V == 1) {
             w[0] = (uint8_t)*p;
         } else {
-            typedef uint32_t words __attribute__((ext_vector_type(V / 4), aligned(4)));
+            typedef uint32_t words __attribute__((ext_vector_type(V / 4), aligned(TAIL ? 1 : 4)));
             const words t = *reinterpret_cast<const words*>(p);
 #pragma unroll
             for (int i = 0; i < V / 4; ++i) w[i] = t[i];
         }
-        scale = k.scales[row * k.blocks + c.plane * k.plane_blocks + c.col / kBlock];
+        const float* scales = k.scales + row * k.blocks + c.plane * k.plane_blocks;
+        scale = scales[(c.col + V - 1) / kBlock];
+        if constexpr (TAIL) {
+            scale_before = scales[c.col / kBlock];
+            before = (c.col + V - 1) / kBlock * kBlock - c.col;
+        }
     }
-    __device__ __forceinline__ float at(int j) const { return (float)(int8_t)(w[j >> 2] >> 8 * (j & 3)) * scale; }
+    __device__ __forceinline__ float at(int j) const {
+        return (float)(int8_t)(w[j >> 2] >> 8 * (j & 3)) * (TAIL && j < before ? scale_before : scale);
+    }
 };
 
 // ---- forward ---------------------------------------------------------------------------------------------
 // Sums of x and x^2 in 64 bits: squares are exact there, and the difference mean x^2 - m^2 keeps the variance as long as the mean is within some
 // 2^20 standard deviations of zero.
-template <typename T, int V>
+template <typename T, int V, bool TAIL>
 __global__ __launch_bounds__(256) void k_norm_sums(NormShape s, GraphRows g, const T* __restrict__ x, RowPlane p, double2* __restrict__ pieces) {
     const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (w >= s.chunks) return;
@@ -315,7 +354,7 @@ __global__ __launch_bounds__(256) void k_norm_sums(NormShape s, GraphRows g, con
                 const bool in = r + k * c.subs + c.sub < b;
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const double t = in ? (double)q[k].at(j) : 0.0;
+                    const double t = in && !(TAIL && j < c.skip) ? (double)q[k].at(j) : 0.0;
                     u += t;
                     v = fma(t, t, v);
                 }
@@ -325,7 +364,7 @@ __global__ __launch_bounds__(256) void k_norm_sums(NormShape s, GraphRows g, con
     });
 }
 template <bool WIDE>
-__global__ __launch_bounds__(256) void k_norm_join(NormShape s, GraphRows g, int V, const double2* __restrict__ pieces, double eps,
+__global__ __launch_bounds__(1024) void k_norm_join(NormShape s, GraphRows g, int V, const double2* __restrict__ pieces, double eps,
                                                    float* __restrict__ mean, float* __restrict__ rstd) {
     int64_t task, rows;
     double u, v;
@@ -352,7 +391,7 @@ struct Affine {
     const float *gamma, *beta, *mean, *rstd;
 };
 
-template <typename T, int V, int ACT, bool SAVE>
+template <typename T, int V, bool TAIL, int ACT, bool SAVE>
 __global__ __launch_bounds__(256) void k_norm_apply(NormShape s, GraphRows g, const T* x, RowPlane p, Affine f, T* y, RowPlane py, Checkpoint ck) {
     const int64_t w = s.chunks - 1 - ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6));        // backwards: what was read last may still be cached
     if (w < 0) return;
@@ -380,7 +419,7 @@ __global__ __launch_bounds__(256) void k_norm_apply(NormShape s, GraphRows g, co
                 if constexpr (SAVE) {
 #pragma unroll
                     for (int j = 0; j < V; ++j) v[j] = q[k].at(j);
-                    save_piece<V>(ck, s, c, row, row < b, v);
+                    save_piece<V, TAIL>(ck, s, c, row, row < b, v);
                 }
 #pragma unroll
                 for (int j = 0; j < V; ++j) v[j] = activation<ACT>((q[k].at(j) - m) * rs * gamma[j] + beta[j]);
@@ -391,22 +430,35 @@ __global__ __launch_bounds__(256) void k_norm_apply(NormShape s, GraphRows g, co
 }
 
 // ---- backward --------------------------------------------------------------------------------------------
-// dz = dy act'(z).  Which side of zero z lies on is decided in 64 bits: in 32 one value in ten million falls on the other one.
-template <int ACT>
-__device__ __forceinline__ float before_activation(float dy, float x, float xh, float m, float rs, float gamma, float beta) {
-    if constexpr (ACT == GSR_ACT_RELU) {
-        const double z = fma(((double)x - (double)m) * (double)rs, (double)gamma, (double)beta);
-        return z > 0.0 ? dy : z <= 0.0 ? 0.0f : (float)z;               // (NaN stays NaN)
-    } else if constexpr (ACT == GSR_ACT_SILU) {
-        const float z = xh * gamma + beta, l = logistic(z);
-        return dy * (l * (1.0f + z * (1.0f - l)));
-    } else {
-        return dy;
+// dz = dy act'(z) for a lane's columns in a graph.  Which side of zero z lies on is decided in 64 bits (z = a x + b; 500k x 256 16-bit values: 113 -> 105 us for
+// the sums, 94 without an activation): in 32 one value in ten million falls on the other one.
+template <int V, int ACT>
+struct BeforeActivation {
+    double a[ACT == GSR_ACT_RELU ? V : 1], b[ACT == GSR_ACT_RELU ? V : 1];
+    __device__ __forceinline__ BeforeActivation(float m, float rs, const float (&gamma)[V], const float (&beta)[V]) {
+        if constexpr (ACT == GSR_ACT_RELU) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                a[j] = (double)rs * (double)gamma[j];
+                b[j] = fma(-(double)m, a[j], (double)beta[j]);
+            }
+        }
     }
-}
+    __device__ __forceinline__ float operator()(int j, float dy, float x, float xh, const float (&gamma)[V], const float (&beta)[V]) const {
+        if constexpr (ACT == GSR_ACT_RELU) {
+            const double z = fma((double)x, a[j], b[j]);
+            return z > 0.0 ? dy : z <= 0.0 ? 0.0f : (float)z;               // (NaN stays NaN)
+        } else if constexpr (ACT == GSR_ACT_SILU) {
+            const float z = xh * gamma[j] + beta[j], l = logistic(z);
+            return dy * (l * (1.0f + z * (1.0f - l)));
+        } else {
+            return dy;
+        }
+    }
+};
 
 // Sums of a chunk in 32 bits (`rows` of a column at most), joined in 64.  columns: [workgroups][2][d], sums of dz xh and of dz.
-template <typename T, int V, int ACT, typename Source>
+template <typename T, int V, bool TAIL, int ACT, typename Source>
 __global__ __launch_bounds__(256) void k_norm_grad_sums(NormShape s, GraphRows g, const T* __restrict__ dy, RowPlane pd, Source source, Affine f,
                                                         double2* __restrict__ pieces, float* __restrict__ columns) {
     const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -423,6 +475,7 @@ __global__ __launch_bounds__(256) void k_norm_grad_sums(NormShape s, GraphRows g
             constexpr int U = 2;
             const int64_t at = graph * s.groups + (c.on ? c.group : 0);
             const float m = f.mean[at], rs = f.rstd[at];
+            const BeforeActivation<V, ACT> before(m, rs, gamma, beta);
             float sum_x[V], sum_z[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) sum_x[j] = sum_z[j] = 0.0f;
@@ -444,9 +497,10 @@ __global__ __launch_bounds__(256) void k_norm_grad_sums(NormShape s, GraphRows g
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
                         const float x = q[k].at(j), xh = (x - m) * rs;
-                        const float dz = before_activation<ACT>(e[k].at(j), x, xh, m, rs, gamma[j], beta[j]);
-                        sum_z[j] += in ? dz : 0.0f;
-                        sum_x[j] += in ? dz * xh : 0.0f;
+                        const float dz = before(j, e[k].at(j), x, xh, gamma, beta);
+                        const bool counts = in && !(TAIL && j < c.skip);
+                        sum_z[j] += counts ? dz : 0.0f;
+                        sum_x[j] += counts ? dz * xh : 0.0f;
                     }
                 }
             }
@@ -469,9 +523,9 @@ __global__ __launch_bounds__(256) void k_norm_grad_sums(NormShape s, GraphRows g
             all_x[j] += __shfl_xor(all_x[j], o);
             all_z[j] += __shfl_xor(all_z[j], o);
         }
-        if (c.sub == 0) {
-            s_col[threadIdx.x >> 6][0][li * V + j] = all_x[j];
-            s_col[threadIdx.x >> 6][1][li * V + j] = all_z[j];
+        if (c.sub == 0 && !(TAIL && j < c.skip)) {
+            s_col[threadIdx.x >> 6][0][li * V + j - c.skip] = all_x[j];
+            s_col[threadIdx.x >> 6][1][li * V + j - c.skip] = all_z[j];
         }
     }
     __syncthreads();
@@ -485,9 +539,9 @@ __global__ __launch_bounds__(256) void k_norm_grad_sums(NormShape s, GraphRows g
 }
 
 // The first `task_blocks` workgroups join the pieces: means of h and of h xh of every (graph, group).  The others add up 16 columns of
-// dgamma and dbeta each, with 16 threads a column.
+// dgamma and dbeta each, with 64 threads a column.
 template <bool WIDE>
-__global__ __launch_bounds__(256) void k_norm_grad_join(NormShape s, GraphRows g, int V, const double2* __restrict__ pieces, int64_t task_blocks,
+__global__ __launch_bounds__(1024) void k_norm_grad_join(NormShape s, GraphRows g, int V, const double2* __restrict__ pieces, int64_t task_blocks,
                                                         float2* __restrict__ means, const float* __restrict__ columns, int64_t parts,
                                                         float* __restrict__ dgamma, float* __restrict__ dbeta) {
     if ((int64_t)blockIdx.x < task_blocks) {
@@ -498,7 +552,7 @@ __global__ __launch_bounds__(256) void k_norm_grad_join(NormShape s, GraphRows g
         means[task] = rows ? make_float2((float)(u / count), (float)(v / count)) : make_float2(0.0f, 0.0f);
         return;
     }
-    __shared__ double s_part[16][16];
+    __shared__ double s_part[64][16];
     const int64_t block = blockIdx.x - task_blocks;
     const int col = (int)(block * 16 + (threadIdx.x & 15)), k = threadIdx.x >> 4;       // of 2 d: dgamma's columns, then dbeta's
     double sum = 0.0;
@@ -506,24 +560,25 @@ __global__ __launch_bounds__(256) void k_norm_grad_join(NormShape s, GraphRows g
         constexpr int U = 8;
         const float* from = columns + col;
         const int64_t stride = 2 * (int64_t)s.d;
-        for (int64_t i = k; i < parts; i += 16 * U) {
+        for (int64_t i = k; i < parts; i += 64 * U) {
             float t[U];
 #pragma unroll
-            for (int q = 0; q < U; ++q) t[q] = from[(i + 16 * q < parts ? i + 16 * q : i) * stride];
+            for (int q = 0; q < U; ++q) t[q] = from[(i + 64 * q < parts ? i + 64 * q : i) * stride];
 #pragma unroll
-            for (int q = 0; q < U; ++q) sum += i + 16 * q < parts ? (double)t[q] : 0.0;
+            for (int q = 0; q < U; ++q) sum += i + 64 * q < parts ? (double)t[q] : 0.0;
         }
     }
     s_part[k][threadIdx.x & 15] = sum;
     __syncthreads();
     if (threadIdx.x >= 16 || col >= 2 * s.d) return;
     sum = 0.0;
-    for (int i = 0; i < 16; ++i) sum += s_part[i][threadIdx.x];
+#pragma unroll
+    for (int i = 0; i < 64; ++i) sum += s_part[i][threadIdx.x];
     float* out = col < s.d ? dgamma : dbeta;
     if (out) out[col < s.d ? col : col - s.d] = (float)sum;
 }
 
-template <typename T, int V, int ACT, typename Source>
+template <typename T, int V, bool TAIL, int ACT, typename Source>
 __global__ __launch_bounds__(256) void k_norm_grad_apply(NormShape s, GraphRows g, const T* dy, RowPlane pd, Source source, Affine f,
                                                          const float2* __restrict__ means, T* dx, RowPlane px) {
     const int64_t w = s.chunks - 1 - ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6));        // backwards, as k_norm_apply
@@ -537,6 +592,7 @@ __global__ __launch_bounds__(256) void k_norm_grad_apply(NormShape s, GraphRows 
         const int64_t at = graph * s.groups + (c.on ? c.group : 0);
         const float m = f.mean[at], rs = f.rstd[at];
         const float2 mm = means[at];
+        const BeforeActivation<V, ACT> before(m, rs, gamma, beta);
         for (int64_t r = a; r < b; r += U * c.subs) {
             PlaneSource<T, V, true> e[U];
             Source q[U];
@@ -556,7 +612,7 @@ __global__ __launch_bounds__(256) void k_norm_grad_apply(NormShape s, GraphRows 
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
                     const float x = q[k].at(j), xh = (x - m) * rs;
-                    const float dz = before_activation<ACT>(e[k].at(j), x, xh, m, rs, gamma[j], beta[j]);
+                    const float dz = before(j, e[k].at(j), x, xh, gamma, beta);
                     v[j] = rs * (gamma[j] * dz - mm.x - xh * mm.y);
                 }
                 if (row < b && c.on) store_piece<V, true>(dx + c.plane * px.gs + row * px.ld + c.col, v);
@@ -566,7 +622,7 @@ __global__ __launch_bounds__(256) void k_norm_grad_apply(NormShape s, GraphRows 
 }
 
 // ---- checkpoints by themselves -----------------------------------------------------------------------------
-template <typename T, int V>
+template <typename T, int V, bool TAIL>
 __global__ __launch_bounds__(256) void k_checkpoint_save(NormShape s, const T* __restrict__ x, RowPlane p, Checkpoint ck) {
     const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (w >= s.chunks) return;
@@ -588,11 +644,11 @@ __global__ __launch_bounds__(256) void k_checkpoint_save(NormShape s, const T* _
             float v[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) v[j] = q[k].at(j);
-            save_piece<V>(ck, s, c, row, row < b, v);
+            save_piece<V, TAIL>(ck, s, c, row, row < b, v);
         }
     }
 }
-template <typename T, int V>
+template <typename T, int V, bool TAIL>
 __global__ __launch_bounds__(256) void k_checkpoint_load(NormShape s, Checkpoint ck, T* __restrict__ x, RowPlane p) {
     const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (w >= s.chunks) return;
@@ -600,7 +656,7 @@ __global__ __launch_bounds__(256) void k_checkpoint_load(NormShape s, Checkpoint
     const int64_t a = w * s.rows, b = a + s.rows < s.n ? a + s.rows : s.n;
     constexpr int U = 4;
     for (int64_t r = a; r < b; r += U * c.subs) {
-        CodeSource<V> q[U];
+        CodeSource<V, TAIL> q[U];
 #pragma unroll
         for (int k = 0; k < U; ++k) {
             const int64_t row = r + k * c.subs + c.sub;
@@ -626,10 +682,21 @@ constexpr int64_t kMaxPieces = (int64_t)1 << 31;
 
 bool aligned_to(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 
-// Vectors where every lane's columns lie in one group; else single columns.
-int piece_of(int32_t dg, int32_t cg, int32_t dtype) {
+// Rows of a wave: as many as make kChunks waves of all slabs together; eight pieces of every lane at least, and at most kMaxRows.
+constexpr int64_t kChunks = 4096, kMaxRows = 1024;
+int64_t least_rows(const NormShape& s) { return 8 * (64 >> s.lanes_log2); }
+
+// Pieces of 16 bytes of the plane's type where every lane's columns lie in one group; else single columns.  With a tail the last piece overlaps the one
+// before it, whose lane may have stored already where a pass works in place.
+struct PieceRule {
+    int v;
+    bool tail;
+};
+PieceRule piece_of(int32_t dg, int32_t groups, int32_t cg, int32_t dtype, bool in_place) {
     const int v = dtype == GSR_BF16 ? 8 : 4;
-    return dg % v == 0 && cg % v == 0 ? v : 1;
+    if (dg % v == 0 && cg % v == 0) return {v, false};
+    if (groups == 1 && dg > v && !in_place) return {v, dg % v != 0};
+    return {1, false};
 }
 NormShape norm_shape(int64_t n, int32_t d, int32_t planes, int32_t groups, int V) {
     NormShape s{};
@@ -639,17 +706,15 @@ NormShape norm_shape(int64_t n, int32_t d, int32_t planes, int32_t groups, int V
     s.groups = groups;
     s.cg = d / groups;
     const int pieces = (s.dg + V - 1) / V;
-    int best = 1 << 30;
-    for (int k = 6; k >= 3; --k) {              // as few idle lanes as can be, then as long rows; a block of a checkpoint in one slab
-        const int lanes = 1 << k, all = (pieces + lanes - 1) / lanes * lanes;
-        if (all >= best || (lanes * V % kBlock && lanes * V < s.dg)) continue;
-        best = all;
-        s.lanes_log2 = k;
-        s.group_slabs = all / lanes;
-    }
+    // as few idle lanes as can be, or up to a quarter more for longer rows; a block of a checkpoint in one slab
+    auto lanes_for = [&](int k) { return ((pieces - 1) >> k) + 1 << k; };
+    auto fits = [&](int k) { return (V << k) % kBlock == 0 || (V << k) >= s.dg; };
+    int least = 1 << 30;
+    for (int k = 3; k <= 6; ++k) if (fits(k)) least = std::min(least, lanes_for(k));
+    for (int k = 3; k <= 6; ++k) if (fits(k) && lanes_for(k) <= least + least / 4) s.lanes_log2 = k;
+    s.group_slabs = lanes_for(s.lanes_log2) >> s.lanes_log2;
     s.slabs = s.group_slabs * planes;
-    const int64_t least = 8 * (64 >> s.lanes_log2);
-    s.rows = (int32_t)std::min<int64_t>(1024, std::max<int64_t>(least, (n * s.slabs + 8191) / 8192));
+    s.rows = (int32_t)std::min(kMaxRows, std::max(least_rows(s), (n * s.slabs + kChunks - 1) / kChunks));
     s.chunks = (n + s.rows - 1) / s.rows;
     return s;
 }
@@ -709,12 +774,14 @@ struct NormWs {
 NormWs carve_norm(const NormShape& s, int64_t graphs) {
     NormWs w{};
     w.pieces = 0;
-    w.means = align_up((size_t)(s.chunks + graphs) * s.stride() * sizeof(double2));
+    // at least as many chunks as any number of rows up to n has, so that a workspace serves them all
+    const int64_t chunks = std::max((s.n + kMaxRows - 1) / kMaxRows, std::min((s.n + least_rows(s) - 1) / least_rows(s), kChunks / s.slabs + 1));
+    w.means = align_up((size_t)(chunks + graphs) * s.stride() * sizeof(double2));
     w.columns = w.means + align_up((size_t)graphs * s.groups * sizeof(float2));
-    w.total = w.columns + align_up((size_t)((s.chunks + 3) / 4) * 2 * s.d * 4);
+    w.total = w.columns + align_up((size_t)((chunks + 3) / 4) * 2 * s.d * 4);
     w.wide = s.chunks > 64 * graphs;
     const int64_t tasks = graphs * s.groups;
-    w.task_blocks = w.wide ? tasks : (tasks + 3) / 4;
+    w.task_blocks = w.wide ? tasks : (tasks + 15) / 16;
     return w;
 }
 gsr_status_t workspace_of(const NormWs& w, const NormShape& s, int64_t graphs, void* workspace, size_t bytes) {
@@ -725,15 +792,27 @@ gsr_status_t workspace_of(const NormWs& w, const NormShape& s, int64_t graphs, v
     return GSR_OK;
 }
 
+// A pass that leaves no sums takes eight pieces of every lane a wave, so that the waves at work lie close together in memory, and with offsets to
+// look up 16.  1M x 256 floats with 2,048 waves of a plane / 8 / 16 pieces: forward with a checkpoint 517 / 391 / 403 us, gradient from it 527 / 399 / 419,
+// save 336 / 297 / 313; 500k x 256 16-bit values in 301 graphs, gradient: 143 / 154 / 144.
+NormShape apply_shape(NormShape s, const void* graph_ptr) {
+    s.rows = (graph_ptr ? 16 : 8) * (64 >> s.lanes_log2);
+    s.chunks = (s.n + s.rows - 1) / s.rows;
+    return s;
+}
 dim3 rows_grid(const NormShape& s) { return dim3((unsigned)((s.chunks + 3) / 4), (unsigned)s.slabs); }
 
-// call(T{}, integral_constant<V>) for the storage type and piece
+// call(T{}, integral_constant<V>, bool_constant<TAIL>) for the storage type and piece
+template <typename T, int W, typename Call>
+void by_tail(const PieceRule& r, Call call) {
+    if (r.tail) call(T{}, std::integral_constant<int, W>{}, std::true_type{});
+    else if (r.v == W) call(T{}, std::integral_constant<int, W>{}, std::false_type{});
+    else call(T{}, std::integral_constant<int, 1>{}, std::false_type{});
+}
 template <typename Call>
-void by_piece(int32_t dtype, int V, Call call) {
-    if (dtype == GSR_F32 && V == 4) call(float{}, std::integral_constant<int, 4>{});
-    else if (dtype == GSR_F32) call(float{}, std::integral_constant<int, 1>{});
-    else if (V == 8) call(bf16_t{}, std::integral_constant<int, 8>{});
-    else call(bf16_t{}, std::integral_constant<int, 1>{});
+void by_piece(int32_t dtype, const PieceRule& r, Call call) {
+    if (dtype == GSR_F32) by_tail<float, 4>(r, call);
+    else by_tail<bf16_t, 8>(r, call);
 }
 template <typename Call>
 void by_activation(int32_t act, Call call) {
@@ -752,7 +831,11 @@ extern "C" {
 size_t gsr_group_norm_workspace(int64_t n, int64_t graphs, int32_t d, int32_t c, int32_t layout, int32_t dtype, int32_t groups) {
     if (plane_shape(n, d, c, layout, dtype) != GSR_OK || graphs < 0 || graphs >= ((int64_t)1 << 31) || groups < 1 || groups > d || d % groups) return 0;
     const int planes = planes_of(c, layout);
-    return carve_norm(norm_shape(n, d, planes, groups, piece_of(d / planes, d / groups, dtype)), graphs).total;
+    // in place, single columns may take the place of pieces
+    size_t bytes = 0;
+    for (bool in_place : {false, true})
+        bytes = std::max(bytes, carve_norm(norm_shape(n, d, planes, groups, piece_of(d / planes, groups, d / groups, dtype, in_place).v), graphs).total);
+    return bytes;
 }
 
 gsr_status_t gsr_group_norm(const void* x, int64_t ldx, int64_t n, int32_t d, int32_t c, int32_t layout, int32_t dtype, const void* graph_ptr,
@@ -772,24 +855,26 @@ gsr_status_t gsr_group_norm(const void* x, int64_t ldx, int64_t n, int32_t d, in
     if (x == y_out && ldx != ldy) return fail(GSR_ERR_INVALID_ARG, "in place, but with row strides of %lld and %lld", (long long)ldx, (long long)ldy);
     const bool save = codes_out || scales_out;
     if (save) GSR_TRY(checkpoint_of(n, dg, planes, codes_out, scales_out, &ck));
-    const int V = piece_of(dg, d / groups, dtype);
+    const PieceRule rule = piece_of(dg, groups, d / groups, dtype, x == y_out);
+    const int V = rule.v;
     const NormShape s = norm_shape(n, d, planes, groups, V);
     const NormWs ws = carve_norm(s, graphs);
     GSR_TRY(workspace_of(ws, s, graphs, workspace, workspace_bytes));
     if (graphs == 0) return GSR_OK;
     hipStream_t st = (hipStream_t)stream;
     double2* pieces = (double2*)((char*)workspace + ws.pieces);
-    by_piece(dtype, V, [&](auto t, auto v) {
+    by_piece(dtype, rule, [&](auto t, auto v, auto tail) {
         using T = decltype(t);
         constexpr int P = v.value;
-        if (n) hipLaunchKernelGGL((k_norm_sums<T, P>), rows_grid(s), dim3(256), 0, st, s, g, (const T*)x, px, pieces);
-        if (ws.wide) hipLaunchKernelGGL((k_norm_join<true>), dim3((unsigned)ws.task_blocks), dim3(256), 0, st, s, g, V, pieces, (double)eps, mean_out, rstd_out);
-        else hipLaunchKernelGGL((k_norm_join<false>), dim3((unsigned)ws.task_blocks), dim3(256), 0, st, s, g, V, pieces, (double)eps, mean_out, rstd_out);
+        if (n) hipLaunchKernelGGL((k_norm_sums<T, P, tail.value>), rows_grid(s), dim3(256), 0, st, s, g, (const T*)x, px, pieces);
+        if (ws.wide) hipLaunchKernelGGL((k_norm_join<true>), dim3((unsigned)ws.task_blocks), dim3(1024), 0, st, s, g, V, pieces, (double)eps, mean_out, rstd_out);
+        else hipLaunchKernelGGL((k_norm_join<false>), dim3((unsigned)ws.task_blocks), dim3(1024), 0, st, s, g, V, pieces, (double)eps, mean_out, rstd_out);
         if (!n) return;
         const Affine f{gamma, beta, mean_out, rstd_out};
+        const NormShape q = apply_shape(s, graph_ptr);
         by_activation(act, [&](auto a) {
-            if (save) hipLaunchKernelGGL((k_norm_apply<T, P, a.value, true>), rows_grid(s), dim3(256), 0, st, s, g, (const T*)x, px, f, (T*)y_out, py, ck);
-            else hipLaunchKernelGGL((k_norm_apply<T, P, a.value, false>), rows_grid(s), dim3(256), 0, st, s, g, (const T*)x, px, f, (T*)y_out, py, ck);
+            if (save) hipLaunchKernelGGL((k_norm_apply<T, P, tail.value, a.value, true>), rows_grid(q), dim3(256), 0, st, q, g, (const T*)x, px, f, (T*)y_out, py, ck);
+            else hipLaunchKernelGGL((k_norm_apply<T, P, tail.value, a.value, false>), rows_grid(q), dim3(256), 0, st, q, g, (const T*)x, px, f, (T*)y_out, py, ck);
         });
     });
     GSR_HIP_CHECK(hipGetLastError());
@@ -816,7 +901,8 @@ gsr_status_t gsr_group_norm_grad(const void* dy, int64_t lddy, const void* x, in
     GSR_TRY(norm_args(d, groups, act, gamma, beta, mean, rstd, graphs));
     if (!aligned_to(dgamma_out, 4) || !aligned_to(dbeta_out, 4)) return fail(GSR_ERR_INVALID_ARG, "dgamma_out or dbeta_out is not aligned to its elements");
     if (dy == dx_out && lddy != lddx) return fail(GSR_ERR_INVALID_ARG, "in place, but with row strides of %lld and %lld", (long long)lddy, (long long)lddx);
-    const int V = piece_of(dg, d / groups, dtype);
+    const PieceRule rule = piece_of(dg, groups, d / groups, dtype, dy == dx_out);
+    const int V = rule.v;
     const NormShape s = norm_shape(n, d, planes, groups, V);
     const NormWs ws = carve_norm(s, graphs);
     GSR_TRY(workspace_of(ws, s, graphs, workspace, workspace_bytes));
@@ -825,26 +911,27 @@ gsr_status_t gsr_group_norm_grad(const void* dy, int64_t lddy, const void* x, in
     float2* means = (float2*)((char*)workspace + ws.means);
     float* columns = (float*)((char*)workspace + ws.columns);
     const Affine f{gamma, beta, mean, rstd};
-    auto both = [&](auto t, auto v, auto a, auto source) {
+    const NormShape q = apply_shape(s, graph_ptr);
+    auto both = [&](auto t, auto v, auto tail, auto a, auto source) {
         using T = decltype(t);
         using Source = decltype(source);
         constexpr int P = v.value, ACT = a.value;
-        if (n) hipLaunchKernelGGL((k_norm_grad_sums<T, P, ACT, Source>), rows_grid(s), dim3(256), 0, st, s, g, (const T*)dy, pd, source, f, pieces, columns);
+        if (n) hipLaunchKernelGGL((k_norm_grad_sums<T, P, tail.value, ACT, Source>), rows_grid(s), dim3(256), 0, st, s, g, (const T*)dy, pd, source, f, pieces, columns);
         const int64_t column_blocks = dgamma_out || dbeta_out ? (2 * (int64_t)d + 15) / 16 : 0;
         const dim3 grid((unsigned)(ws.task_blocks + column_blocks));
         const int64_t parts = (s.chunks + 3) / 4;
         if (grid.x && ws.wide)
-            hipLaunchKernelGGL((k_norm_grad_join<true>), grid, dim3(256), 0, st, s, g, V, pieces, ws.task_blocks, means, columns, parts, dgamma_out, dbeta_out);
+            hipLaunchKernelGGL((k_norm_grad_join<true>), grid, dim3(1024), 0, st, s, g, V, pieces, ws.task_blocks, means, columns, parts, dgamma_out, dbeta_out);
         else if (grid.x)
-            hipLaunchKernelGGL((k_norm_grad_join<false>), grid, dim3(256), 0, st, s, g, V, pieces, ws.task_blocks, means, columns, parts, dgamma_out, dbeta_out);
-        if (n && graphs) hipLaunchKernelGGL((k_norm_grad_apply<T, P, ACT, Source>), rows_grid(s), dim3(256), 0, st, s, g, (const T*)dy, pd, source, f, means, (T*)dx_out, po);
+            hipLaunchKernelGGL((k_norm_grad_join<false>), grid, dim3(1024), 0, st, s, g, V, pieces, ws.task_blocks, means, columns, parts, dgamma_out, dbeta_out);
+        if (n && graphs) hipLaunchKernelGGL((k_norm_grad_apply<T, P, tail.value, ACT, Source>), rows_grid(q), dim3(256), 0, st, q, g, (const T*)dy, pd, source, f, means, (T*)dx_out, po);
     };
-    by_piece(dtype, V, [&](auto t, auto v) {
+    by_piece(dtype, rule, [&](auto t, auto v, auto tail) {
         using T = decltype(t);
         constexpr int P = v.value;
         by_activation(act, [&](auto a) {
-            if (coded) both(t, v, a, CodeSource<P>{ck, {}, 0.0f});
-            else both(t, v, a, PlaneSource<T, P, false>{(const T*)x, px, {}});
+            if (coded) both(t, v, tail, a, CodeSource<P, tail.value>{ck});
+            else both(t, v, tail, a, PlaneSource<T, P, false>{(const T*)x, px, {}});
         });
     });
     GSR_HIP_CHECK(hipGetLastError());
@@ -860,11 +947,11 @@ gsr_status_t gsr_checkpoint_save(const void* x, int64_t ldx, int64_t n, int32_t 
     GSR_TRY(row_plane("x", x, n, dg, ldx, dtype, &p));
     GSR_TRY(checkpoint_of(n, dg, planes, codes_out, scales_out, &ck));
     if (n == 0) return GSR_OK;
-    const int V = piece_of(dg, dg, dtype);
-    const NormShape s = norm_shape(n, d, planes, 1, V);
-    by_piece(dtype, V, [&](auto t, auto v) {
+    const PieceRule rule = piece_of(dg, 1, dg, dtype, false);
+    const NormShape s = apply_shape(norm_shape(n, d, planes, 1, rule.v), nullptr);
+    by_piece(dtype, rule, [&](auto t, auto v, auto tail) {
         using T = decltype(t);
-        hipLaunchKernelGGL((k_checkpoint_save<T, v.value>), rows_grid(s), dim3(256), 0, (hipStream_t)stream, s, (const T*)x, p, ck);
+        hipLaunchKernelGGL((k_checkpoint_save<T, v.value, tail.value>), rows_grid(s), dim3(256), 0, (hipStream_t)stream, s, (const T*)x, p, ck);
     });
     GSR_HIP_CHECK(hipGetLastError());
     return GSR_OK;
@@ -879,11 +966,11 @@ gsr_status_t gsr_checkpoint_load(const int8_t* codes, const float* scales, int64
     GSR_TRY(row_plane("x_out", x_out, n, dg, ldx, dtype, &p));
     GSR_TRY(checkpoint_of(n, dg, planes, codes, scales, &ck));
     if (n == 0) return GSR_OK;
-    const int V = piece_of(dg, dg, dtype);
-    const NormShape s = norm_shape(n, d, planes, 1, V);
-    by_piece(dtype, V, [&](auto t, auto v) {
+    const PieceRule rule = piece_of(dg, 1, dg, dtype, false);
+    const NormShape s = apply_shape(norm_shape(n, d, planes, 1, rule.v), nullptr);
+    by_piece(dtype, rule, [&](auto t, auto v, auto tail) {
         using T = decltype(t);
-        hipLaunchKernelGGL((k_checkpoint_load<T, v.value>), rows_grid(s), dim3(256), 0, (hipStream_t)stream, s, ck, (T*)x_out, p);
+        hipLaunchKernelGGL((k_checkpoint_load<T, v.value, tail.value>), rows_grid(s), dim3(256), 0, (hipStream_t)stream, s, ck, (T*)x_out, p);
     });
     GSR_HIP_CHECK(hipGetLastError());
     return GSR_OK;

@@ -44,3 +44,13 @@ def test_workspaces():
         for bad in ((-1, 1, 1, 0), (2 ** 31 - 256, 1, 1, 0), (1, 0, 1, 0), (1, 2 ** 31 - 256, 1, 0), (1, 1, 0, 0), (1, 1, 513, 0), (1, 1, 1, 2)):
             assert size(*bad) == 0
     assert loss(nbytes=lib.gsr_class_loss_workspace(4, 10, 8, 0) - 1) == SMALL and grad(nbytes=lib.gsr_class_grad_workspace(4, 10, 8, 0) - 1) == SMALL
+
+
+@pytest.mark.parametrize("d,dtype", [(1, 0), (64, 0), (256, 1), (384, 0), (512, 1)])
+def test_a_workspace_serves_fewer_rows_and_classes(d, dtype):
+    sizes = sorted({int(1.13 ** i) for i in range(140)} | {255, 256, 257, 32_768, 65_536, 131_072, 131_073})
+    for size in (gsr.lib().gsr_class_loss_workspace, gsr.lib().gsr_class_grad_workspace):
+        for other in (1, 33, 4_099, 50_021, 1_000_000):
+            rows = [size(n, other, d, dtype) for n in sizes]
+            classes = [size(other, n, d, dtype) for n in sizes]
+            assert rows == sorted(rows) and classes == sorted(classes)

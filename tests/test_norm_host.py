@@ -75,3 +75,15 @@ def test_workspace():
                 (4, 1, 64, 1, 0, 0, 0), (4, 1, 64, 1, 0, 0, 3), (4, 1, 64, 1, 0, 0, 128)):
         assert size(*bad) == 0
     assert norm(n=2 ** 31 - 1, d=64, ldx=64, ldy=64, graphs=2 ** 31 - 1, groups=64) == UNSUPPORTED         # more sums than can be named
+
+
+@pytest.mark.parametrize("d,c,layout,dtype,groups", [(1, 1, 0, 0, 1), (64, 2, 1, 0, 2), (256, 1, 0, 1, 32), (77, 1, 0, 0, 7), (384, 2, 1, 1, 6), (131_072, 1, 0, 0, 8)])
+def test_a_workspace_serves_fewer_rows_and_graphs(d, c, layout, dtype, groups):
+    size = gsr.lib().gsr_group_norm_workspace
+    slabs = -(-d // 256)
+    sizes = sorted({int(1.07 ** i) for i in range(300)} | {8192 * k // slabs + i for k in (1, 8, 32, 64, 1024) for i in range(-2, 3)})
+    sizes = [n for n in sizes if 0 <= n < 2 ** 31]
+    for other in (1, 300):
+        rows = [size(n, other, d, c, layout, dtype, groups) for n in sizes]
+        graphs = [size(other, n, d, c, layout, dtype, groups) for n in sizes]
+        assert rows == sorted(rows) and graphs == sorted(graphs)
