@@ -7,7 +7,7 @@
 // A checkpoint holds a row's columns in blocks of up to 64: with A = max |x| (at least 127 * 2^-126) the codes are 127 x / A rounded to the
 // nearest whole number, ties to even, and the block's scale is A / 127.
 //
-// Both directions are two passes over the rows, sums first: a wave takes `rows` consecutive rows of one slab of columns, keeps the sums of
+// Both directions are two passes over the rows (a small graph's in one launch), sums first: a wave takes `rows` consecutive rows of one slab of columns, keeps the sums of
 // its columns in registers, and leaves one pair of sums for every (graph, group) that it met.  Those pairs ("pieces") are joined by a launch
 // between the passes, in an order that the sizes and the graphs alone fix.
 #include "gsr_internal.h"
@@ -213,8 +213,9 @@ __device__ __forceinline__ uint32_t lanes_umax(uint32_t v, int lanes) {
     }
     return v;
 }
-// 127 x / top to the nearest whole number, ties to even, exactly: x * (127 / top) in 32 bits is off by less than 127 * 2^-22, and where it
-// lies that near to a border the exact products decide (16-bit values are half of the largest, a tie, all the time).
+// 127 x / top to the nearest whole number, ties to even, exactly: x * (127 / top) in 32 bits, three roundings and a reciprocal good to one unit, is off by
+// less than 127 * 5 * 2^-24 < 2^-14, and where it lies that near to a border the exact products decide (16-bit values are half of the largest, a tie,
+// all the time).
 __device__ __forceinline__ int code_of(float x, float top, float inv) {
     const float t = x * inv;
     float q = __builtin_rintf(t);
@@ -225,6 +226,11 @@ __device__ __forceinline__ int code_of(float x, float top, float inv) {
         if (over > 0.0 || (over == 0.0 && ((int)q & 1))) q += side;
     }
     return (int)q;
+}
+// top / 127, correctly rounded: a quotient within one unit, corrected by its exact remainder times the rounded 1 / 127 (Markstein)
+__device__ __forceinline__ float by_127(float top) {
+    const float q = top * (1.0f / 127.0f);
+    return fmaf(fmaf(-127.0f, q, top), 1.0f / 127.0f, q);
 }
 typedef uint32_t u32_b __attribute__((aligned(1)));
 typedef uint16_t u16_b __attribute__((aligned(1)));
@@ -279,14 +285,14 @@ __device__ __forceinline__ void save_piece(const Checkpoint& k, const NormShape&
     const int lanes = 1 << s.lanes_log2;
     bits = lanes_umax(bits, lanes < kBlock / V ? lanes : kBlock / V);
     const bool finite = bits < 0x7F800000u;
-    const float top = fmaxf(__uint_as_float(finite ? bits : 0u), kSmallestTop), inv = 127.0f / top;
+    const float top = fmaxf(__uint_as_float(finite ? bits : 0u), kSmallestTop), inv = __builtin_amdgcn_rcpf(fmaxf(top * (1.0f / 127.0f), 0x1p-126f));
     if (!in || !c.on) return;
     int q[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) q[j] = finite ? code_of(x[j], top, inv) : 0;
     store_codes<V, TAIL>(k.codes + row * s.d + c.column, q, c.skip);
     if (c.own % kBlock == 0)
-        k.scales[row * k.blocks + c.plane * k.plane_blocks + c.own / kBlock] = finite ? fminf(top / 127.0f, kLargestScale) : __builtin_nanf("");
+        k.scales[row * k.blocks + c.plane * k.plane_blocks + c.own / kBlock] = finite ? fminf(by_127(top), kLargestScale) : __builtin_nanf("");
 }
 
 // Where the values of a plane come from: the plane, or its checkpoint.
@@ -363,6 +369,11 @@ __global__ __launch_bounds__(256) void k_norm_sums(NormShape s, GraphRows g, con
         leave_piece(s, c, slab, w, graph, u, v, pieces);
     });
 }
+__device__ __forceinline__ void statistics(double u, double v, double count, double eps, float& mean, float& rstd) {
+    const double m = count ? u / count : 0.0, var = count ? v / count - m * m : 0.0;
+    mean = (float)m;
+    rstd = (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + eps));          // (NaN stays NaN)
+}
 template <bool WIDE>
 __global__ __launch_bounds__(1024) void k_norm_join(NormShape s, GraphRows g, int V, const double2* __restrict__ pieces, double eps,
                                                    float* __restrict__ mean, float* __restrict__ rstd) {
@@ -370,9 +381,10 @@ __global__ __launch_bounds__(1024) void k_norm_join(NormShape s, GraphRows g, in
     double u, v;
     if (!joined<WIDE>(s, g, V, blockIdx.x, pieces, task, u, v, rows)) return;
     if (lane_id()) return;
-    const double count = (double)rows * s.cg, m = rows ? u / count : 0.0, var = rows ? v / count - m * m : 0.0;
-    mean[task] = (float)m;
-    rstd[task] = (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + eps));     // (NaN stays NaN)
+    float m, r;
+    statistics(u, v, (double)rows * s.cg, eps, m, r);
+    mean[task] = m;
+    rstd[task] = r;
 }
 
 __device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
@@ -427,6 +439,78 @@ __global__ __launch_bounds__(256) void k_norm_apply(NormShape s, GraphRows g, co
             }
         }
     });
+}
+
+// One launch for a single graph whose slabs are small and hold whole groups: every workgroup takes the sums of all rows of its slab by itself, and then
+// writes its share of the rows.
+__device__ __forceinline__ double2 small_total(const NormShape& s, const LaneColumns& c, double u, double v) {          // over the lane's group
+    __shared__ double2 s_sum[16][64];
+    join_lanes(s, c, u, v);
+    const int first = __builtin_amdgcn_readfirstlane(c.group), mine = c.on ? c.group - first : 0;
+    if (c.head && c.sub == 0) s_sum[threadIdx.x >> 6][mine] = make_double2(u, v);
+    __syncthreads();
+    double2 t = make_double2(0.0, 0.0);
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+        t.x += s_sum[w][mine].x;
+        t.y += s_sum[w][mine].y;
+    }
+    return t;
+}
+template <typename T, int V, int ACT, bool SAVE>
+__global__ __launch_bounds__(1024) void k_norm_small(NormShape s, GraphRows g, const T* x, RowPlane p, const float* __restrict__ gamma_in,
+                                                     const float* __restrict__ beta_in, double eps, float* __restrict__ mean, float* __restrict__ rstd,
+                                                     T* y, RowPlane py, Checkpoint ck) {
+    const LaneColumns c = lane_columns<V>(s, blockIdx.y);
+    const int wave = threadIdx.x >> 6;
+    const int64_t a = g.at(0), b = g.at(1) > a ? g.at(1) : a;
+    constexpr int U = 4;
+    double u = 0.0, v = 0.0;
+    for (int64_t r = a + (int64_t)wave * U * c.subs; r < b; r += 16 * U * c.subs) {
+        PlaneSource<T, V, false> q[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int64_t row = r + k * c.subs + c.sub;
+            q[k].x = x;
+            q[k].p = p;
+            q[k].load(s, c, row < b ? row : a);
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const bool in = r + k * c.subs + c.sub < b;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const double t = in ? (double)q[k].at(j) : 0.0;
+                u += t;
+                v = fma(t, t, v);
+            }
+        }
+    }
+    float gamma[V], beta[V], m, rs;
+    load_affine<V>(gamma_in, c, 1.0f, gamma);
+    load_affine<V>(beta_in, c, 0.0f, beta);
+    const double2 t = small_total(s, c, u, v);
+    statistics(t.x, t.y, (double)(b - a) * s.cg, eps, m, rs);
+    if (blockIdx.x == 0 && wave == 0 && c.head && c.sub == 0) {
+        mean[c.group] = m;
+        rstd[c.group] = rs;
+    }
+    for (int64_t r = a + ((int64_t)blockIdx.x * 16 + wave) * c.subs; r < b; r += (int64_t)gridDim.x * 16 * c.subs) {
+        const int64_t row = r + c.sub, have = row < b ? row : a;
+        PlaneSource<T, V, false> q;
+        q.x = x;
+        q.p = p;
+        q.load(s, c, have);
+        float z[V];
+        if constexpr (SAVE) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) z[j] = q.at(j);
+            save_piece<V, false>(ck, s, c, row, row < b, z);
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) z[j] = activation<ACT>((q.at(j) - m) * rs * gamma[j] + beta[j]);
+        if (row < b && c.on) store_piece<V>(y + c.plane * py.gs + row * py.ld + c.col, z);
+    }
 }
 
 // ---- backward --------------------------------------------------------------------------------------------
@@ -621,6 +705,99 @@ __global__ __launch_bounds__(256) void k_norm_grad_apply(NormShape s, GraphRows 
     });
 }
 
+// k_norm_small's counterpart.  One workgroup of a slab also writes the gradients of gamma and beta.
+template <typename T, int V, int ACT, typename Source>
+__global__ __launch_bounds__(1024) void k_norm_grad_small(NormShape s, GraphRows g, const T* dy, RowPlane pd, Source source, Affine f, T* dx, RowPlane px,
+                                                          float* __restrict__ dgamma, float* __restrict__ dbeta) {
+    const int slab = blockIdx.y, wave = threadIdx.x >> 6;
+    const LaneColumns c = lane_columns<V>(s, slab);
+    const int64_t a = g.at(0), b = g.at(1) > a ? g.at(1) : a;
+    float gamma[V], beta[V];
+    load_affine<V>(f.gamma, c, 1.0f, gamma);
+    load_affine<V>(f.beta, c, 0.0f, beta);
+    const int group = c.on ? c.group : 0;
+    const float m = f.mean[group], rs = f.rstd[group];
+    const BeforeActivation<V, ACT> before(m, rs, gamma, beta);
+    float sum_x[V], sum_z[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum_x[j] = sum_z[j] = 0.0f;
+    constexpr int U = 2;
+    for (int64_t r = a + (int64_t)wave * U * c.subs; r < b; r += 16 * U * c.subs) {
+        PlaneSource<T, V, false> e[U];
+        Source q[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int64_t row = r + k * c.subs + c.sub, have = row < b ? row : a;
+            e[k].x = dy;
+            e[k].p = pd;
+            e[k].load(s, c, have);
+            q[k] = source;
+            q[k].load(s, c, have);
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const bool in = r + k * c.subs + c.sub < b;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float x = q[k].at(j), xh = (x - m) * rs, dz = before(j, e[k].at(j), x, xh, gamma, beta);
+                sum_z[j] += in ? dz : 0.0f;
+                sum_x[j] += in ? dz * xh : 0.0f;
+            }
+        }
+    }
+    double u = 0.0, v = 0.0;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        u = fma((double)gamma[j], (double)sum_z[j], u);
+        v = fma((double)gamma[j], (double)sum_x[j], v);
+    }
+    __shared__ float s_col[16][2][64 * V];
+    const int lanes = 1 << s.lanes_log2, li = lane_id() & (lanes - 1);
+    if (blockIdx.x == 0) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            for (int o = lanes; o < 64; o <<= 1) {
+                sum_x[j] += __shfl_xor(sum_x[j], o);
+                sum_z[j] += __shfl_xor(sum_z[j], o);
+            }
+            if (c.sub == 0) {
+                s_col[wave][0][li * V + j] = sum_x[j];
+                s_col[wave][1][li * V + j] = sum_z[j];
+            }
+        }
+    }
+    const double2 t = small_total(s, c, u, v);              // (meets the other waves)
+    if (blockIdx.x == 0) {
+        const int first = (slab % s.group_slabs) * lanes * V, plane = slab / s.group_slabs;
+        for (int i = threadIdx.x; i < 2 * lanes * V; i += 1024) {
+            const int which = i >= lanes * V, k = which ? i - lanes * V : i;
+            float* out = which ? dbeta : dgamma;
+            if (first + k >= s.dg || !out) continue;
+            double sum = 0.0;
+            for (int w = 0; w < 16; ++w) sum += (double)s_col[w][which][k];
+            out[plane * s.dg + first + k] = (float)sum;
+        }
+    }
+    const double count = (double)(b - a) * s.cg;
+    const float m1 = (float)(t.x / count), m2 = (float)(t.y / count);           // (an empty graph has no rows to use them)
+    for (int64_t r = a + ((int64_t)blockIdx.x * 16 + wave) * c.subs; r < b; r += (int64_t)gridDim.x * 16 * c.subs) {
+        const int64_t row = r + c.sub, have = row < b ? row : a;
+        PlaneSource<T, V, false> e;
+        e.x = dy;
+        e.p = pd;
+        e.load(s, c, have);
+        Source q = source;
+        q.load(s, c, have);
+        float w[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float x = q.at(j), xh = (x - m) * rs, dz = before(j, e.at(j), x, xh, gamma, beta);
+            w[j] = rs * (gamma[j] * dz - m1 - xh * m2);
+        }
+        if (row < b && c.on) store_piece<V>(dx + c.plane * px.gs + row * px.ld + c.col, w);
+    }
+}
+
 // ---- checkpoints by themselves -----------------------------------------------------------------------------
 template <typename T, int V, bool TAIL>
 __global__ __launch_bounds__(256) void k_checkpoint_save(NormShape s, const T* __restrict__ x, RowPlane p, Checkpoint ck) {
@@ -707,7 +884,7 @@ NormShape norm_shape(int64_t n, int32_t d, int32_t planes, int32_t groups, int V
     s.cg = d / groups;
     const int pieces = (s.dg + V - 1) / V;
     // as few idle lanes as can be, or up to a quarter more for longer rows; a block of a checkpoint in one slab
-    auto lanes_for = [&](int k) { return ((pieces - 1) >> k) + 1 << k; };
+    auto lanes_for = [&](int k) { return (((pieces - 1) >> k) + 1) << k; };
     auto fits = [&](int k) { return (V << k) % kBlock == 0 || (V << k) >= s.dg; };
     int least = 1 << 30;
     for (int k = 3; k <= 6; ++k) if (fits(k)) least = std::min(least, lanes_for(k));
@@ -800,6 +977,19 @@ NormShape apply_shape(NormShape s, const void* graph_ptr) {
     s.chunks = (s.n + s.rows - 1) / s.rows;
     return s;
 }
+// Workgroups for a slab of a graph that takes one launch, or 0.  One launch against three, floats, groups of 32 columns, in a captured graph: 200 rows 5.6 us /
+// 10.5, gradient 7.6 / 13.7; 2,000 rows (256 KB) 9.1 / 10.7 and 13.6 / 14.0; 4,000 rows 12.9 / 10.7 and 20.4 / 14.7.  Called from Python, where launches
+// wait for the host: 2,000 rows 12.2 / 16.4 and 13.7 / 18.2, 4,000 rows 12.8 / 16.4 and 20.2 / 18.2.
+constexpr int kSmallShares = 32;
+constexpr int64_t kSmallBytes = 256 << 10;
+unsigned small_shares(const NormShape& s, const PieceRule& rule, int64_t graphs, int32_t dtype, bool in_place) {
+    const int width = rule.v << s.lanes_log2;
+    const bool whole = s.dg % s.cg == 0 && (s.group_slabs == 1 || width % s.cg == 0);
+    if (graphs != 1 || rule.tail || !whole || s.n < 1 || s.n * std::min(width, s.dg) * (int64_t)dtype_size(dtype) > kSmallBytes) return 0;
+    if (in_place) return 1;                     // others would read what it has written
+    const int rows = 16 * (64 >> s.lanes_log2);
+    return (unsigned)std::min<int64_t>(kSmallShares, (s.n + rows - 1) / rows);
+}
 dim3 rows_grid(const NormShape& s) { return dim3((unsigned)((s.chunks + 3) / 4), (unsigned)s.slabs); }
 
 // call(T{}, integral_constant<V>, bool_constant<TAIL>) for the storage type and piece
@@ -866,6 +1056,18 @@ gsr_status_t gsr_group_norm(const void* x, int64_t ldx, int64_t n, int32_t d, in
     by_piece(dtype, rule, [&](auto t, auto v, auto tail) {
         using T = decltype(t);
         constexpr int P = v.value;
+        if (const unsigned shares = small_shares(s, rule, graphs, dtype, x == y_out)) {
+            const dim3 grid(shares, (unsigned)s.slabs);
+            by_activation(act, [&](auto a) {
+                if (save)
+                    hipLaunchKernelGGL((k_norm_small<T, P, a.value, true>), grid, dim3(1024), 0, st, s, g, (const T*)x, px, gamma, beta, (double)eps, mean_out,
+                                       rstd_out, (T*)y_out, py, ck);
+                else
+                    hipLaunchKernelGGL((k_norm_small<T, P, a.value, false>), grid, dim3(1024), 0, st, s, g, (const T*)x, px, gamma, beta, (double)eps, mean_out,
+                                       rstd_out, (T*)y_out, py, ck);
+            });
+            return;
+        }
         if (n) hipLaunchKernelGGL((k_norm_sums<T, P, tail.value>), rows_grid(s), dim3(256), 0, st, s, g, (const T*)x, px, pieces);
         if (ws.wide) hipLaunchKernelGGL((k_norm_join<true>), dim3((unsigned)ws.task_blocks), dim3(1024), 0, st, s, g, V, pieces, (double)eps, mean_out, rstd_out);
         else hipLaunchKernelGGL((k_norm_join<false>), dim3((unsigned)ws.task_blocks), dim3(1024), 0, st, s, g, V, pieces, (double)eps, mean_out, rstd_out);
@@ -916,6 +1118,12 @@ gsr_status_t gsr_group_norm_grad(const void* dy, int64_t lddy, const void* x, in
         using T = decltype(t);
         using Source = decltype(source);
         constexpr int P = v.value, ACT = a.value;
+        if (const unsigned shares = small_shares(s, rule, graphs, dtype, dy == dx_out)) {
+            if constexpr (!tail.value)
+                hipLaunchKernelGGL((k_norm_grad_small<T, P, ACT, Source>), dim3(shares, (unsigned)s.slabs), dim3(1024), 0, st, s, g, (const T*)dy, pd, source, f,
+                                   (T*)dx_out, po, dgamma_out, dbeta_out);
+            return;
+        }
         if (n) hipLaunchKernelGGL((k_norm_grad_sums<T, P, tail.value, ACT, Source>), rows_grid(s), dim3(256), 0, st, s, g, (const T*)dy, pd, source, f, pieces, columns);
         const int64_t column_blocks = dgamma_out || dbeta_out ? (2 * (int64_t)d + 15) / 16 : 0;
         const dim3 grid((unsigned)(ws.task_blocks + column_blocks));
