@@ -388,7 +388,8 @@ gsr_status_t gsr_adam_update_list(float* const* w, const void* const* dw, float*
  *                         dgamma_out = sum dz xh, dbeta_out = sum dz over all graphs (device, d floats, overwritten; either may be NULL).
  *                         m, r: as gsr_group_norm left them.  x, or with x = NULL its checkpoint, whose values then take the place of x.
  * RELU has the derivative 0 at 0.  SILU(z) = z / (1 + exp(-z)).  Sums over rows are taken in float64, those of a gradient over up to 1,024 rows in
- * float32 first, in an order that the sizes and the offsets alone fix.  A mean further than 2^20 standard deviations from zero loses the variance.
+ * float32 first, in an order that the sizes and the offsets alone fix.  Values are summed from the first value of their group
+ * in the first graph on: a graph whose mean lies 2^20 standard deviations from it loses the variance.
  * y_out may be x and dx_out may be dy, with the same stride; apart from that what a call writes overlaps nothing that it reads.
  * eps > 0; 1 <= d <= 131072; n < 2^31; pointers aligned to their elements.  workspace: device, 16-byte aligned, at least
  * gsr_group_norm_workspace() bytes (0: sizes that are refused; never fewer for more rows or graphs, so that one serves any fewer); it holds nothing between
@@ -433,7 +434,8 @@ gsr_status_t gsr_checkpoint_load(const int8_t* codes, const float* scales, int64
  * class:  dx_out = dz E (a plane as x, row stride lddx), dtable_out = dz^T x (classes rows of d values of `dtype`, row stride lddt), dbias_out_j =
  * sum_i dz_ij (`classes` floats); any but not all of them may be NULL.  Every element is written.
  *
- * float32 values enter the products exactly, and sums are taken in float32 (the loss and dbias: in float64 across tiles).  With 16-bit planes
+ * float32 values, |v| < 2^64, enter the products as multiples of 2^-22 of themselves or 2^-39 of the largest of 32 rows (aligned ones), dz as those of
+ * 2^-22 of itself or 2^-36 of the largest in its sum; sums are taken in float32 (the loss and dbias: in float64 across tiles).  With 16-bit planes
  * dz is rounded to 16 bits before the products with E and x.  Equal calls give equal bits.  Values must be finite: a row with infinities or NaN gets a
  * loss that is none, which then is the mean's.  1 <= d <= 512, c divides d, n and classes below 2^31 - 256; pointers aligned to their elements.
  * workspace: device, 16-byte aligned, at least gsr_class_loss_workspace() / gsr_class_grad_workspace() bytes (0: sizes that are refused; never

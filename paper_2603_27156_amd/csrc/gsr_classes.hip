@@ -11,8 +11,10 @@
 //
 // Operands are laid out once per call as the matrix instructions take them: rows in blocks of 16, columns in steps of 32, and of every (block, step)
 // 64 pieces of 16 bytes in lane order, zeros behind the last row and column.  So tiles are copied to LDS as they lie, from any layout, stride and
-// width.  16-bit planes go in as they are; floats as three 16-bit pieces whose sum they are, and a product of floats as the six products of pieces
-// that matter at 2^-24 of it (hh, hm, mh, mm, hl, lh; each exact, added up in float32).
+// width.  bf16 planes go in as they are.  Floats go in as two fp16 pieces h + l of 11 bits each: 32 rows at a time are first multiplied by the power of two that
+// brings their largest value to 2^14 .. 2^15, which keeps both pieces in fp16's range (what is left out is below 2^-22 of a value, or 2^-39 of the
+// largest), and a product of floats is hh + hl + lh (l l is below 2^-24 of it), added up in float32.  Exact products of three bf16 pieces, which need no powers of two, are six:
+// 8,191 x 4,099 at D = 384, gradients 708 us instead of 372.
 #include "gsr_internal.h"
 #include "gsr_pieces.h"
 
@@ -27,6 +29,14 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kNoMax = -3.0e38f;              // a running maximum that no logit has reached
 
 // ---- operands ------------------------------------------------------------------------------------------
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short frag8 __attribute__((ext_vector_type(8)));        // a lane's eight values of a step: bf16, or a piece in fp16
+template <int NP>
+__device__ __forceinline__ f32x4 mfma_frag(frag8 a, frag8 b, f32x4 c) {
+    if constexpr (NP == 1) return mfma_k32(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
 struct RowSource {              // rows of a plane, or of a table
     const void* at;
     int64_t rows, ld, gs;
@@ -45,6 +55,7 @@ struct ClassSetup {
     RowSource x, e;
     ClassTokens ids;
     uint4 *xf, *ef;                 // in pieces
+    float *x_exp, *e_exp;           // floats: exponents of the powers of two that the 32 rows of a tile have to be multiplied by
     const float *lse, *bias;        // lse: NULL in the forward
     float *lse_out, *bias_out;      // of all rows that the kernels read, padded ones too
     int32_t *target, *counts;       // class of every row; rows with a class of every block
@@ -52,17 +63,12 @@ struct ClassSetup {
     int32_t ks;
     unsigned x_blocks, e_blocks, row_blocks, bias_blocks;
 };
-template <typename T, int NP>
-__device__ __forceinline__ void lay_out(const RowSource& s, uint4* __restrict__ out, int64_t pad, int ks, int64_t wave, const ClassTokens* known) {
-    if (wave >= pad / 16 * ks) return;
-    const int lane = lane_id(), step = (int)(wave % ks);
-    const int64_t row = wave / ks * 16 + (lane & 15);
-    const int col = step * 32 + (lane >> 4) * 8;
-    float v[8];
-    const bool in = row < s.rows && (!known || known->at(row) >= 0);
-    if (in && s.dg % 8 == 0) {
-        const int plane = col / s.dg;
-        if (col < s.d) {
+// Columns col .. col + 7 of a row, zeros where there are none.
+template <typename T>
+__device__ __forceinline__ void load_eight(const RowSource& s, int64_t row, bool in, int col, float (&v)[8]) {
+    if (s.dg % 8 == 0) {
+        if (in && col < s.d) {
+            const int plane = col / s.dg;
             Piece<T, 8> p;
             p.load(static_cast<const T*>(s.at) + plane * s.gs + row * s.ld + (col - plane * s.dg));
 #pragma unroll
@@ -78,37 +84,87 @@ __device__ __forceinline__ void lay_out(const RowSource& s, uint4* __restrict__ 
             v[j] = in && c < s.d ? to_float(static_cast<const T*>(s.at)[plane * s.gs + row * s.ld + (c - plane * s.dg)]) : 0.0f;
         }
     }
-    uint32_t h[NP][8];
+}
+__device__ __forceinline__ uint32_t f16_bits(float v) { return __builtin_bit_cast(uint16_t, static_cast<_Float16>(v)); }
+// a float in two pieces
+__device__ __forceinline__ void two_pieces(float v, uint32_t& h, uint32_t& l) {
+    const _Float16 top = static_cast<_Float16>(v);
+    h = __builtin_bit_cast(uint16_t, top);
+    l = f16_bits(v - static_cast<float>(top));
+}
+// 32 rows by a wave
+template <typename T>
+__device__ __forceinline__ void lay_out(const RowSource& s, uint4* __restrict__ out, float* __restrict__ exponents, int64_t pad, int ks, int64_t tile,
+                                        const ClassTokens* known) {
+    if (tile >= pad / kTileRows) return;
+    const int lane = lane_id(), col = (lane >> 4) * 8;
+    int64_t row[2];
+    bool in[2];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        h[0][j] = __float_as_uint(v[j]);
-        if constexpr (NP == 3) {
-            const float r1 = v[j] - __uint_as_float(h[0][j] & 0xFFFF0000u);
-            h[1][j] = __float_as_uint(r1);
-            h[2][j] = __float_as_uint(r1 - __uint_as_float(h[1][j] & 0xFFFF0000u));
-        }
+    for (int b = 0; b < 2; ++b) {
+        row[b] = tile * kTileRows + b * 16 + (lane & 15);
+        in[b] = row[b] < s.rows && (!known || known->at(row[b]) >= 0);
     }
+    float v[8];
+    if constexpr (sizeof(T) == 2) {
+        for (int k = 0; k < ks; ++k) {
 #pragma unroll
-    for (int k = 0; k < NP; ++k) {
-        uint4 w;
-        w.x = __builtin_amdgcn_perm(h[k][1], h[k][0], 0x07060302u);
-        w.y = __builtin_amdgcn_perm(h[k][3], h[k][2], 0x07060302u);
-        w.z = __builtin_amdgcn_perm(h[k][5], h[k][4], 0x07060302u);
-        w.w = __builtin_amdgcn_perm(h[k][7], h[k][6], 0x07060302u);
-        out[(wave * NP + k) * 64 + lane] = w;
+            for (int b = 0; b < 2; ++b) {
+                load_eight<T>(s, row[b], in[b], k * 32 + col, v);
+                uint4 w;
+                w.x = __builtin_amdgcn_perm(__float_as_uint(v[1]), __float_as_uint(v[0]), 0x07060302u);
+                w.y = __builtin_amdgcn_perm(__float_as_uint(v[3]), __float_as_uint(v[2]), 0x07060302u);
+                w.z = __builtin_amdgcn_perm(__float_as_uint(v[5]), __float_as_uint(v[4]), 0x07060302u);
+                w.w = __builtin_amdgcn_perm(__float_as_uint(v[7]), __float_as_uint(v[6]), 0x07060302u);
+                out[((tile * 2 + b) * ks + k) * 64 + lane] = w;
+            }
+        }
+    } else {
+        uint32_t top = 0;               // bits of the largest finite value
+        for (int k = 0; k < ks; ++k)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                load_eight<T>(s, row[b], in[b], k * 32 + col, v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t u = __float_as_uint(v[j]) & 0x7FFFFFFFu;
+                    if (u < 0x7F800000u) top = top > u ? top : u;
+                }
+            }
+        for (int o = 32; o; o >>= 1) {
+            const uint32_t u = __shfl_xor(top, o);
+            top = top > u ? top : u;
+        }
+        // rows of zeros, and rows below 2^-100, whose products are nothing beside the rounding of any logit
+        int e = (int)(top >> 23) - 127;
+        if (top == 0) e = 0;
+        if (e < -100) e = -100;
+        const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
+        if (lane == 0) exponents[tile] = (float)(e - 14);
+        for (int k = 0; k < ks; ++k)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                load_eight<T>(s, row[b], in[b], k * 32 + col, v);
+                uint32_t h[8], l[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) two_pieces(v[j] * up, h[j], l[j]);
+                uint4* to = out + ((tile * 2 + b) * ks + k) * 128 + lane;
+                to[0] = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+                to[64] = make_uint4(l[0] | l[1] << 16, l[2] | l[3] << 16, l[4] | l[5] << 16, l[6] | l[7] << 16);
+            }
     }
 }
-template <typename T, int NP>
+template <typename T>
 __global__ __launch_bounds__(256) void k_class_setup(ClassSetup s) {
     unsigned b = blockIdx.x;
     const int wave = threadIdx.x >> 6;
     if (b < s.x_blocks) {
-        lay_out<T, NP>(s.x, s.xf, s.x_pad, s.ks, (int64_t)b * 4 + wave, s.lse ? &s.ids : nullptr);
+        lay_out<T>(s.x, s.xf, s.x_exp, s.x_pad, s.ks, (int64_t)b * 4 + wave, s.lse ? &s.ids : nullptr);
         return;
     }
     b -= s.x_blocks;
     if (b < s.e_blocks) {
-        lay_out<T, NP>(s.e, s.ef, s.e_pad, s.ks, (int64_t)b * 4 + wave, nullptr);
+        lay_out<T>(s.e, s.ef, s.e_exp, s.e_pad, s.ks, (int64_t)b * 4 + wave, nullptr);
         return;
     }
     b -= s.e_blocks;
@@ -141,7 +197,7 @@ __global__ __launch_bounds__(256) void k_class_setup(ClassSetup s) {
 // A tile of N pieces of 1 KB into LDS; arrives once this wave has waited for its loads and all waves have met.
 template <int N>
 __device__ __forceinline__ void fetch_tile(const uint4* __restrict__ from, uint4* to, int wave, int lane) {
-#pragma unroll
+#pragma unroll 8
     for (int c = 0; c < (N + 3) / 4; ++c) {
         const int piece = c * 4 + wave;
         if (N % 4 == 0 || piece < N)
@@ -149,55 +205,66 @@ __device__ __forceinline__ void fetch_tile(const uint4* __restrict__ from, uint4
                                              (__attribute__((address_space(3))) uint32_t*)(to + piece * 64), 16, 0, 0);
     }
 }
-// whether two tiles fit into LDS
-constexpr bool two_tiles(int kilobytes) { return 2 * kilobytes <= 160; }
+// 16-row blocks that a wave keeps, by the registers that they take (operands: 4 NP a step; sums: 8 a step), waves of a SIMD that these and LDS leave room
+// for, and whether a workgroup has two tiles in LDS.
+constexpr int tile_kilobytes(int ks, int np) { return 2 * ks * np; }
+constexpr int loss_blocks(int ks, int np) { return ks * np * 16 <= 128 ? 4 : ks * np * 8 <= 128 ? 2 : 1; }
+constexpr int loss_waves(int ks, int np) { return 2 * tile_kilobytes(ks, np) <= 160 ? 2 : 1; }
+constexpr bool loss_two(int ks, int np) { return 2 * loss_waves(ks, np) * tile_kilobytes(ks, np) <= 160; }
+constexpr int grad_registers(int ks, int np, int rb) { return rb * ks * (4 * np + 8); }
+constexpr int grad_blocks(int ks, int np) { return grad_registers(ks, np, 4) <= 128 ? 4 : grad_registers(ks, np, 2) <= (np == 1 ? 192 : 128) ? 2 : 1; }
+// (8,191 x 4,099 floats, dx: two waves of one block each against one of two, D = 192 / 256 / 384: 96 / 117 / 170 us against 128 / 160 / 268)
+constexpr int grad_waves(int ks, int np) { return grad_registers(ks, np, grad_blocks(ks, np)) <= 192 && 2 * tile_kilobytes(ks, np) <= 160 ? 2 : 1; }
+constexpr bool grad_two(int ks, int np) { return 2 * grad_waves(ks, np) * tile_kilobytes(ks, np) <= 160; }
 __device__ __forceinline__ void tile_arrived() {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
 }
-__device__ __forceinline__ bf16x8 piece_of_lds(const uint4* p) { return __builtin_bit_cast(bf16x8, *p); }
+__device__ __forceinline__ frag8 piece_of_lds(const uint4* p) { return __builtin_bit_cast(frag8, *p); }
 
-// The products of pieces, small ones first.
+// Product i of two values' pieces: 0 .. products<NP>() - 1, small ones first.  They are added to one accumulator, so products of others stand between them.
 template <int NP>
-__device__ __forceinline__ f32x4 mfma_pieces(const bf16x8 (&a)[NP], const bf16x8 (&b)[NP], f32x4 c) {
-    if constexpr (NP == 3) {
-        c = mfma_k32(a[2], b[0], c);
-        c = mfma_k32(a[0], b[2], c);
-        c = mfma_k32(a[1], b[1], c);
-        c = mfma_k32(a[1], b[0], c);
-        c = mfma_k32(a[0], b[1], c);
-    }
-    return mfma_k32(a[0], b[0], c);
+constexpr int products() { return NP == 2 ? 3 : 1; }
+template <int NP>
+__device__ __forceinline__ f32x4 mfma_product(int i, const frag8 (&a)[NP], const frag8 (&b)[NP], f32x4 c) {
+    if constexpr (NP == 2) return i == 0 ? mfma_frag<NP>(a[1], b[0], c) : i == 1 ? mfma_frag<NP>(a[0], b[1], c) : mfma_frag<NP>(a[0], b[0], c);
+    else return mfma_frag<NP>(a[0], b[0], c);
 }
 
-// z[blk][r]: logits of the streamed rows 16 blk + 4 (lane / 16) + reg with this wave's row 16 r + lane % 16
+// z[blk][r] += products of the streamed rows 16 blk + 4 (lane / 16) + reg with this wave's row 16 r + lane % 16
 template <int KS, int NP, int RB>
-__device__ __forceinline__ void tile_logits(const uint4* tile, const bf16x8 (&own)[RB][KS][NP], int lane, f32x4 (&z)[2][RB]) {
+__device__ __forceinline__ void tile_logits(const uint4* tile, const frag8 (&own)[RB][KS][NP], int lane, f32x4 (&z)[2][RB]) {
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
+        frag8 a[2][NP];
 #pragma unroll
-        for (int blk = 0; blk < 2; ++blk) {
-            bf16x8 a[NP];
+        for (int blk = 0; blk < 2; ++blk)
 #pragma unroll
-            for (int p = 0; p < NP; ++p) a[p] = piece_of_lds(tile + ((blk * KS + k) * NP + p) * 64 + lane);
+            for (int p = 0; p < NP; ++p) a[blk][p] = piece_of_lds(tile + ((blk * KS + k) * NP + p) * 64 + lane);
 #pragma unroll
-            for (int r = 0; r < RB; ++r) z[blk][r] = mfma_pieces<NP>(a, own[r][k], z[blk][r]);
-        }
+        for (int i = 0; i < products<NP>(); ++i)
+#pragma unroll
+            for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+                for (int r = 0; r < RB; ++r) z[blk][r] = mfma_product<NP>(i, a[blk], own[r][k], z[blk][r]);
     }
 }
 template <int KS, int NP, int RB>
-__device__ __forceinline__ void load_own(const uint4* __restrict__ from, int64_t block0, int lane, bf16x8 (&own)[RB][KS][NP]) {
+__device__ __forceinline__ void load_own(const uint4* __restrict__ from, int64_t block0, int lane, frag8 (&own)[RB][KS][NP]) {
 #pragma unroll
     for (int r = 0; r < RB; ++r)
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
-            for (int p = 0; p < NP; ++p) own[r][k][p] = __builtin_bit_cast(bf16x8, from[(((block0 + r) * KS + k) * NP + p) * 64 + lane]);
+            for (int p = 0; p < NP; ++p) own[r][k][p] = __builtin_bit_cast(frag8, from[(((block0 + r) * KS + k) * NP + p) * 64 + lane]);
 }
+__device__ __forceinline__ f32x4 four(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
+__device__ __forceinline__ f32x4 all_four(float v) { return f32x4{v, v, v, v}; }
 
 // ---- forward ---------------------------------------------------------------------------------------------
 struct ClassLossArgs {
     const uint4 *xf, *ef;
+    const float *x_exp, *e_exp;             // floats only
     const float* bias;
     const int32_t* target;
     float2* part;                   // [splits][x_pad]: running maximum, sum of exp(z - maximum)
@@ -206,21 +273,22 @@ struct ClassLossArgs {
     int32_t tiles, splits;
 };
 template <int KS, int NP, int RB>
-__global__ __launch_bounds__(256, 2) void k_class_loss(ClassLossArgs g) {
+__global__ __launch_bounds__(256, loss_waves(KS, NP)) void k_class_loss(ClassLossArgs g) {
     constexpr int N = 2 * KS * NP;
-    constexpr bool TWO = two_tiles(N);
+    constexpr bool TWO = loss_two(KS, NP);
     __shared__ uint4 s_tile[TWO ? 2 : 1][N * 64];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4;
     const int64_t block0 = ((int64_t)blockIdx.x * 4 + wave) * RB;
     const int t0 = (int)((int64_t)g.tiles * blockIdx.y / g.splits), t1 = (int)((int64_t)g.tiles * (blockIdx.y + 1) / g.splits);
     fetch_tile<N>(g.ef + (int64_t)t0 * N * 64, s_tile[0], wave, lane);          // (no part is empty)
-    bf16x8 own[RB][KS][NP];
+    frag8 own[RB][KS][NP];
     load_own<KS, NP, RB>(g.xf, block0, lane, own);
     int target[RB];
-    float top[RB], sum[RB];
+    float top[RB], sum[RB], own_exp[RB];
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
         target[r] = g.target[(block0 + r) * 16 + (lane & 15)];
+        own_exp[r] = NP == 2 ? g.x_exp[(block0 + r) >> 1] : 0.0f;
         top[r] = kNoMax;
         sum[r] = 0.0f;
     }
@@ -228,14 +296,26 @@ __global__ __launch_bounds__(256, 2) void k_class_loss(ClassLossArgs g) {
     for (int t = t0; t < t1; ++t) {
         const uint4* tile = s_tile[TWO ? (t - t0) & 1 : 0];
         if (TWO && t + 1 < t1) fetch_tile<N>(g.ef + (int64_t)(t + 1) * N * 64, s_tile[TWO ? (t - t0 + 1) & 1 : 0], wave, lane);
-        f32x4 z[2][RB];
+        f32x4 z[2][RB], bias[2];
 #pragma unroll
         for (int blk = 0; blk < 2; ++blk) {
-            const f32x4 b = *reinterpret_cast<const f32x4*>(g.bias + t * kTileRows + blk * 16 + grp * 4);
+            const int64_t i = (int64_t)t * kTileRows + blk * 16 + grp * 4;
+            bias[blk] = four(g.bias + i);
 #pragma unroll
-            for (int r = 0; r < RB; ++r) z[blk][r] = b;
+            for (int r = 0; r < RB; ++r) z[blk][r] = NP == 2 ? all_four(0.0f) : bias[blk];
         }
         tile_logits<KS, NP, RB>(tile, own, lane, z);
+        if constexpr (NP == 2) {
+            const float e = g.e_exp[t];
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                const float f = __builtin_amdgcn_exp2f(own_exp[r] + e);
+#pragma unroll
+                for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) z[blk][r][i] = fmaf(z[blk][r][i], f, bias[blk][i]);
+            }
+        }
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
             if (ballot((unsigned)(target[r] - t * kTileRows) < (unsigned)kTileRows)) {
@@ -274,7 +354,7 @@ __global__ __launch_bounds__(256, 2) void k_class_loss(ClassLossArgs g) {
         if (grp == 0) g.part[blockIdx.y * g.x_pad + (block0 + r) * 16 + lane] = make_float2(m, s);
     }
 }
-// lse of 1,024 rows and their part of the loss; a single workgroup writes the loss itself
+// lse of rows and their part of the loss; a single workgroup writes the loss itself
 struct LossPart {
     double sum;
     int64_t count;
@@ -302,10 +382,9 @@ __device__ __forceinline__ void add_up(double& sum, int64_t& count) {          /
 __global__ __launch_bounds__(1024) void k_class_lse(const float2* __restrict__ part, const float* __restrict__ at_target,
                                                     const int32_t* __restrict__ target, int64_t n, int64_t x_pad, int splits,
                                                     float* __restrict__ lse_out, LossPart* __restrict__ parts, float* __restrict__ loss) {
-    const int64_t i = (int64_t)blockIdx.x * 1024 + threadIdx.x;
     double sum = 0.0;
     int64_t count = 0;
-    if (i < n) {
+    for (int64_t i = (int64_t)blockIdx.x * 1024 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 1024) {
         float m = kNoMax;
         for (int s = 0; s < splits; ++s) m = fmaxf(m, part[s * x_pad + i].x);
         double l = 0.0;
@@ -313,8 +392,8 @@ __global__ __launch_bounds__(1024) void k_class_lse(const float2* __restrict__ p
         const double lse = (double)m + log(l);
         lse_out[i] = (float)lse;
         if (target[i] >= 0) {
-            sum = lse - (double)at_target[i];
-            count = 1;
+            sum += lse - (double)at_target[i];
+            ++count;
         }
     }
     add_up(sum, count);
@@ -336,6 +415,7 @@ __global__ __launch_bounds__(1024) void k_class_loss_sum(const LossPart* __restr
 // ---- backward --------------------------------------------------------------------------------------------
 struct ClassGradArgs {
     const uint4 *own, *stream;      // in pieces: the rows that a workgroup keeps, and the tiles
+    const float *own_exp, *stream_exp;          // floats only: of their tiles
     const float *lse, *bias;
     const int32_t *target, *counts;
     void* out;                      // rows x d of T: a plane, or a table
@@ -355,63 +435,87 @@ __device__ __forceinline__ float gradient_scale(const int32_t* __restrict__ coun
 __device__ __forceinline__ void store_as(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_as(bf16_t* p, float v) { p->bits = (uint16_t)bf16_bits(v); }
 
-// eight dz as the operand of the second product: as they are rounded to 16 bits (a relative 2^-9 of each, like the gradients that they are
-// summed to), or in three pieces
+// eight dz as the operand of the second product: rounded to bf16 (a relative 2^-9 of each, like the gradients that they are summed to), or in two pieces
 template <int NP>
-__device__ __forceinline__ void operand_of(const f32x4& a, const f32x4& b, bf16x8 (&o)[NP]) {
+__device__ __forceinline__ void operand_of(const f32x4& a, const f32x4& b, frag8 (&o)[NP]) {
     if constexpr (NP == 1) {
+        bf16x8 w;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            o[0][i] = static_cast<__bf16>(a[i]);
-            o[0][4 + i] = static_cast<__bf16>(b[i]);
+            w[i] = static_cast<__bf16>(a[i]);
+            w[4 + i] = static_cast<__bf16>(b[i]);
         }
+        o[0] = __builtin_bit_cast(frag8, w);
     } else {
-        const float pa[4] = {a[0], a[1], a[2], a[3]}, pb[4] = {b[0], b[1], b[2], b[3]};
-        bf16x4 ha, ma, la, hb, mb, lb;
-        split_p4(pa, ha, ma, la);
-        split_p4(pb, hb, mb, lb);
-        o[0] = join8(ha, hb);
-        o[1] = join8(ma, mb);
-        o[2] = join8(la, lb);
+        f16x8 h, l;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float v = i < 4 ? a[i & 3] : b[i & 3];
+            h[i] = static_cast<_Float16>(v);
+            l[i] = static_cast<_Float16>(v - static_cast<float>(h[i]));
+        }
+        o[0] = __builtin_bit_cast(frag8, h);
+        o[1] = __builtin_bit_cast(frag8, l);
     }
 }
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 // the streamed rows 4 (lane / 16) .. + 3 of block blk at column 16 cb + lane % 16: 16 lanes together read four rows of 16 columns
 template <int KS, int NP>
-__device__ __forceinline__ bf16x4 column_of_lds(const uint4* tile, int blk, int cb, int p, int lane) {
+__device__ __forceinline__ s16x4 column_of_lds(const uint4* tile, int blk, int cb, int p, int lane) {
     const int grp = lane >> 4, i = lane & 15;
     const char* at = reinterpret_cast<const char*>(tile + ((blk * KS + (cb >> 1)) * NP + p) * 64) +
                      (((cb & 1) * 2 + ((i & 3) >> 1)) * 16 + 4 * grp + (i >> 2)) * 16 + (i & 1) * 8;
-    return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at));
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
+}
+
+// Two pieces of fp16 hold dz only in its range, and gradients of rare classes and of rows that are nearly learnt are far below 1.  So every own row has a power of
+// two 2^k by which its dz (times the streamed tile's power of two) and its sums are multiplied; k begins high, and whenever a value of the row would leave
+// fp16's range it goes down so far that the row may grow eightfold before it does again.  A dz is held to 2^-22 of itself or 2^-36 of the row's largest so far.
+constexpr float kFirstExponent = 60.0f, kLargestPiece = 32768.0f;
+template <int KS, int RB>
+__device__ __forceinline__ void fit_row(int r, float largest, float& k, f32x4 (&z)[2][RB], f32x4 (&acc)[RB][2 * KS], int grp) {
+    const bool over = largest >= kLargestPiece;         // (not for NaN)
+    const float down = over ? (float)(14 - 3) - (float)((int)(__float_as_uint(largest) >> 23) - 127) : 0.0f;
+    const float f = __builtin_amdgcn_exp2f(down);
+    k += down;
+#pragma unroll
+    for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[blk][r][i] *= f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float row = __shfl(f, grp * 4 + i);       // sums lie by rows, values by columns
+#pragma unroll
+        for (int c = 0; c < 2 * KS; ++c) acc[r][c][i] *= row;
+    }
 }
 
 template <int KS, int NP, int RB, bool BY_CLASS, typename T>
-__global__ __launch_bounds__(256, RB * KS * (4 * NP + 8) > 192 ? 1 : 2) void k_class_grad(ClassGradArgs g) {
+__global__ __launch_bounds__(256, grad_waves(KS, NP)) void k_class_grad(ClassGradArgs g) {
     constexpr int N = 2 * KS * NP;
-    constexpr bool TWO = two_tiles(N);
+    constexpr bool TWO = grad_two(KS, NP);
     __shared__ uint4 s_tile[TWO ? 2 : 1][N * 64];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4;
     const int64_t block0 = ((int64_t)blockIdx.x * 4 + wave) * RB;
     const int t0 = (int)((int64_t)g.tiles * blockIdx.y / g.splits), t1 = (int)((int64_t)g.tiles * (blockIdx.y + 1) / g.splits);
     if (t0 < t1) fetch_tile<N>(g.stream + (int64_t)t0 * N * 64, s_tile[0], wave, lane);
-    bf16x8 own[RB][KS][NP];
+    frag8 own[RB][KS][NP];
     load_own<KS, NP, RB>(g.own, block0, lane, own);
-    // of this wave's rows: lse and class (BY_CLASS: bias and class number); the same of streamed rows comes with the tile
-    float own_f[RB];
+    // of this wave's rows: lse and class (BY_CLASS: bias and class number), and their powers of two; the same of streamed rows comes with the tile
+    float own_f[RB], own_exp[RB], k[RB];
     int own_c[RB];
+    f32x4 acc[RB][2 * KS];
+    double bias_sum[RB];
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
         const int64_t i = (block0 + r) * 16 + (lane & 15);
         own_f[r] = BY_CLASS ? g.bias[i] : g.lse[i];
         own_c[r] = BY_CLASS ? (int)i : g.target[i];
-    }
-    f32x4 acc[RB][2 * KS];
-    double bias_sum[RB];
-#pragma unroll
-    for (int r = 0; r < RB; ++r) {
+        own_exp[r] = NP == 2 ? g.own_exp[(block0 + r) >> 1] : 0.0f;
+        k[r] = NP == 2 ? kFirstExponent : 0.0f;
         bias_sum[r] = 0.0;
 #pragma unroll
-        for (int c = 0; c < 2 * KS; ++c) acc[r][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int c = 0; c < 2 * KS; ++c) acc[r][c] = all_four(0.0f);
     }
     tile_arrived();
     for (int t = t0; t < t1; ++t) {
@@ -422,39 +526,77 @@ __global__ __launch_bounds__(256, RB * KS * (4 * NP + 8) > 192 ? 1 : 2) void k_c
 #pragma unroll
         for (int blk = 0; blk < 2; ++blk) {
             const int64_t i = (int64_t)t * kTileRows + blk * 16 + grp * 4;
-            row_f[blk] = *reinterpret_cast<const f32x4*>((BY_CLASS ? g.lse : g.bias) + i);
+            row_f[blk] = four((BY_CLASS ? g.lse : g.bias) + i);
             int4 c = make_int4((int)i, (int)i + 1, (int)i + 2, (int)i + 3);
             if constexpr (BY_CLASS) c = *reinterpret_cast<const int4*>(g.target + i);
             row_c[blk][0] = c.x; row_c[blk][1] = c.y; row_c[blk][2] = c.z; row_c[blk][3] = c.w;
 #pragma unroll
-            for (int r = 0; r < RB; ++r)
-                z[blk][r] = BY_CLASS ? f32x4{own_f[r], own_f[r], own_f[r], own_f[r]} : row_f[blk];
+            for (int r = 0; r < RB; ++r) z[blk][r] = NP == 2 ? all_four(0.0f) : BY_CLASS ? all_four(own_f[r]) : row_f[blk];
         }
         tile_logits<KS, NP, RB>(tile, own, lane, z);
-        bf16x8 dz[RB][NP];
+        frag8 dz[RB][NP];
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
+            if constexpr (NP == 1) {
 #pragma unroll
-            for (int blk = 0; blk < 2; ++blk)
+                for (int blk = 0; blk < 2; ++blk)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float l = BY_CLASS ? row_f[blk][i] : own_f[r];
-                    const float p = __builtin_amdgcn_exp2f((z[blk][r][i] - l) * kLog2e);
-                    z[blk][r][i] = row_c[blk][i] == own_c[r] ? p - 1.0f : p;
+                    for (int i = 0; i < 4; ++i) {
+                        const float p = __builtin_amdgcn_exp2f((z[blk][r][i] - (BY_CLASS ? row_f[blk][i] : own_f[r])) * kLog2e);
+                        z[blk][r][i] = row_c[blk][i] == own_c[r] ? p - 1.0f : p;
+                    }
+                if constexpr (BY_CLASS) {
+                    const f32x4 s = z[0][r] + z[1][r];
+                    bias_sum[r] += (double)((s[0] + s[1]) + (s[2] + s[3]));
                 }
-            if constexpr (BY_CLASS) {
-                const f32x4 s = z[0][r] + z[1][r];
-                bias_sum[r] += (double)((s[0] + s[1]) + (s[2] + s[3]));
+            } else {
+                const float e = g.stream_exp[t], f = __builtin_amdgcn_exp2f(own_exp[r] + e), up = e + k[r];
+#pragma unroll
+                for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float b = BY_CLASS ? own_f[r] : row_f[blk][i], l = BY_CLASS ? row_f[blk][i] : own_f[r];
+                        z[blk][r][i] = __builtin_amdgcn_exp2f(fmaf(fmaf(z[blk][r][i], f, b) - l, kLog2e, up));
+                    }
+                bool hit = false;
+#pragma unroll
+                for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) hit |= row_c[blk][i] == own_c[r];
+                if (ballot(hit)) {
+                    const float one = __builtin_amdgcn_exp2f(up);
+#pragma unroll
+                    for (int blk = 0; blk < 2; ++blk)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (row_c[blk][i] == own_c[r]) z[blk][r][i] -= one;
+                }
+                if constexpr (BY_CLASS) {
+                    const f32x4 s = z[0][r] + z[1][r];
+                    bias_sum[r] += (double)((s[0] + s[1]) + (s[2] + s[3])) * (double)__builtin_amdgcn_exp2f(-up);
+                }
+                float largest = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) largest = fmaxf(largest, fmaxf(fabsf(z[0][r][i]), fabsf(z[1][r][i])));
+                largest = quarter_fmax(largest);
+                if (ballot(largest >= kLargestPiece)) fit_row<KS, RB>(r, largest, k[r], z, acc, grp);
             }
             operand_of<NP>(z[0][r], z[1][r], dz[r]);
         }
 #pragma unroll
-        for (int c = 0; c < 2 * KS; ++c) {
-            bf16x8 b[NP];
+        for (int c = 0; c < 2 * KS; c += 2) {
+            frag8 b[2][NP];
 #pragma unroll
-            for (int p = 0; p < NP; ++p) b[p] = join8(column_of_lds<KS, NP>(tile, 0, c, p, lane), column_of_lds<KS, NP>(tile, 1, c, p, lane));
+            for (int q = 0; q < 2; ++q)
 #pragma unroll
-            for (int r = 0; r < RB; ++r) acc[r][c] = mfma_pieces<NP>(dz[r], b, acc[r][c]);
+                for (int p = 0; p < NP; ++p)
+                    b[q][p] = __builtin_shufflevector(column_of_lds<KS, NP>(tile, 0, c + q, p, lane), column_of_lds<KS, NP>(tile, 1, c + q, p, lane), 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+            for (int i = 0; i < products<NP>(); ++i)
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) acc[r][c + q] = mfma_product<NP>(i, dz[r], b[q], acc[r][c + q]);
         }
         if constexpr (!TWO) {
             __syncthreads();
@@ -471,19 +613,33 @@ __global__ __launch_bounds__(256, RB * KS * (4 * NP + 8) > 192 ? 1 : 2) void k_c
             bias_sum[r] += __shfl_xor(bias_sum[r], 32);
             if (grp == 0) g.bias_part[blockIdx.y * g.own_pad + (block0 + r) * 16 + lane] = bias_sum[r];
         }
-#pragma unroll
-        for (int c = 0; c < 2 * KS; ++c) {
-            if (!g.out) break;                  // only the bias is asked for
-            const int col = c * 16 + (lane & 15);
+        if (!g.out) continue;                   // only the bias is asked for
+        if constexpr (NP == 2) {
+            const float f = __builtin_amdgcn_exp2f(-k[r]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (g.splits > 1) {
-                    g.part[((int64_t)blockIdx.y * g.own_pad + row0 + i) * (KS * 32) + col] = acc[r][c][i];
-                } else if (row0 + i < g.rows && col < g.d) {
-                    const int plane = col / g.dg;
-                    store_as(static_cast<T*>(g.out) + plane * g.gs + (row0 + i) * g.ld + (col - plane * g.dg), acc[r][c][i] * scale);
-                }
+                const float row = __shfl(f, grp * 4 + i);
+#pragma unroll
+                for (int c = 0; c < 2 * KS; ++c) acc[r][c][i] *= row;
             }
+        }
+        if (g.splits > 1) {
+            float* to = g.part + ((int64_t)blockIdx.y * g.own_pad + row0) * (KS * 32) + (lane & 15);
+#pragma unroll
+            for (int c = 0; c < 2 * KS; ++c)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) to[i * (KS * 32) + c * 16] = acc[r][c][i];
+            continue;
+        }
+        const int64_t left = g.rows - row0;             // of the lane's four rows
+#pragma unroll
+        for (int c = 0; c < 2 * KS; ++c) {
+            const int col = c * 16 + (lane & 15), plane = col / g.dg;
+            if (col >= g.d) continue;
+            T* to = static_cast<T*>(g.out) + plane * g.gs + row0 * g.ld + (col - plane * g.dg);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < left) store_as(to + i * g.ld, acc[r][c][i] * scale);
         }
     }
 }
@@ -522,10 +678,6 @@ int steps_of(int d) {
     for (int ks : {1, 2, 4, 6, 8, 12}) if (d <= 32 * ks) return ks;
     return 16;
 }
-// 16-row blocks that a wave keeps: as many as leave two waves of a SIMD their registers, one at least
-constexpr int loss_blocks(int ks, int np) { return ks * np * 16 <= 128 ? 4 : ks * np * 8 <= 128 ? 2 : 1; }
-constexpr int grad_blocks(int ks, int np) { return ks * (4 * np + 8) * 4 <= 128 ? 4 : ks * (4 * np + 8) * 2 <= 192 ? 2 : 1; }
-
 // Parts that the streamed side is cut into, so that `blocks` workgroups of it fill the card: the shortest schedule over 512 places, a tile of
 // extra work for every part.
 int splits_of(int64_t blocks, int64_t tiles, int64_t pad) {
@@ -547,14 +699,14 @@ struct ClassPlan {
     int ks, np, loss_rb, grad_rb;
     int64_t x_pad, e_pad;
     int loss_splits, x_splits, e_splits;
-    size_t xf, ef, lse, bias, target, counts, loss_bytes;       // the first of these are shared
+    size_t xf, ef, x_exp, e_exp, lse, bias, target, counts, loss_bytes;         // the first of these are shared
     size_t part, at_target, parts;                              // forward
     size_t x_part, e_part, bias_part, grad_bytes;               // backward
 };
 ClassPlan class_plan(int64_t n, int64_t classes, int32_t d, int32_t dtype) {
     ClassPlan p{};
     p.ks = steps_of(d);
-    p.np = dtype == GSR_F32 ? 3 : 1;
+    p.np = dtype == GSR_F32 ? 2 : 1;
     p.loss_rb = loss_blocks(p.ks, p.np);
     p.grad_rb = grad_blocks(p.ks, p.np);
     p.x_pad = (n + kPadRows - 1) / kPadRows * kPadRows;
@@ -572,6 +724,8 @@ ClassPlan class_plan(int64_t n, int64_t classes, int32_t d, int32_t dtype) {
     };
     p.xf = take((size_t)p.x_pad * p.ks * 64 * p.np);
     p.ef = take((size_t)p.e_pad * p.ks * 64 * p.np);
+    p.x_exp = take((size_t)p.x_pad / kTileRows * 4);
+    p.e_exp = take((size_t)p.e_pad / kTileRows * 4);
     p.lse = take((size_t)p.x_pad * 4);
     p.bias = take((size_t)p.e_pad * 4);
     p.target = take((size_t)p.x_pad * 4);
@@ -639,6 +793,8 @@ ClassSetup launch_setup(const ClassShape& s, const ClassPlan& p, const float* bi
     a.ids = s.ids;
     a.xf = (uint4*)(ws + p.xf);
     a.ef = (uint4*)(ws + p.ef);
+    a.x_exp = (float*)(ws + p.x_exp);
+    a.e_exp = (float*)(ws + p.e_exp);
     a.lse = lse;
     a.bias = bias;
     a.lse_out = (float*)(ws + p.lse);
@@ -648,19 +804,19 @@ ClassSetup launch_setup(const ClassShape& s, const ClassPlan& p, const float* bi
     a.x_pad = p.x_pad;
     a.e_pad = p.e_pad;
     a.ks = p.ks;
-    a.x_blocks = (unsigned)((p.x_pad / 16 * p.ks + 3) / 4);
-    a.e_blocks = (unsigned)((p.e_pad / 16 * p.ks + 3) / 4);
+    a.x_blocks = (unsigned)(p.x_pad / (4 * kTileRows));
+    a.e_blocks = (unsigned)(p.e_pad / (4 * kTileRows));
     a.row_blocks = (unsigned)((p.x_pad + 1023) / 1024);
     a.bias_blocks = (unsigned)((p.e_pad + 1023) / 1024);
     const dim3 grid(a.x_blocks + a.e_blocks + a.row_blocks + a.bias_blocks);
-    if (dtype == GSR_F32) hipLaunchKernelGGL((k_class_setup<float, 3>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_class_setup<bf16_t, 1>), grid, dim3(256), 0, st, a);
+    if (dtype == GSR_F32) hipLaunchKernelGGL((k_class_setup<float>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_class_setup<bf16_t>), grid, dim3(256), 0, st, a);
     return a;
 }
 
 template <int KS, typename T, bool BY_CLASS>
 void launch_grad(const ClassGradArgs& g, hipStream_t st) {
-    constexpr int NP = sizeof(T) == 4 ? 3 : 1, RB = grad_blocks(KS, NP);
+    constexpr int NP = sizeof(T) == 4 ? 2 : 1, RB = grad_blocks(KS, NP);
     const dim3 grid((unsigned)((g.rows + 64 * RB - 1) / (64 * RB)), (unsigned)g.splits);
     hipLaunchKernelGGL((k_class_grad<KS, NP, RB, BY_CLASS, T>), grid, dim3(256), 0, st, g);
     if (g.splits > 1 && g.out) {
@@ -697,16 +853,16 @@ gsr_status_t gsr_class_loss(const void* x, int64_t ldx, int64_t n, int32_t d, in
     GSR_TRY(class_workspace(p.loss_bytes, workspace, workspace_bytes));
     hipStream_t st = (hipStream_t)stream;
     char* ws = (char*)workspace;
-    const int blocks = (int)((n + 1023) / 1024);
+    const int blocks = n <= 4096 ? (n ? 1 : 0) : (int)((n + 1023) / 1024);
     LossPart* parts = (LossPart*)(ws + p.parts);
     if (n) {
         const ClassSetup a = launch_setup(s, p, bias, nullptr, ws, dtype, st);
-        const ClassLossArgs g{a.xf, a.ef, a.bias_out, a.target, (float2*)(ws + p.part), (float*)(ws + p.at_target), p.x_pad,
+        const ClassLossArgs g{a.xf, a.ef, a.x_exp, a.e_exp, a.bias_out, a.target, (float2*)(ws + p.part), (float*)(ws + p.at_target), p.x_pad,
                               (int32_t)((classes + kTileRows - 1) / kTileRows), p.loss_splits};
         by_steps(p.ks, [&](auto k) {
-            constexpr int KS = k.value, R1 = loss_blocks(KS, 1), R3 = loss_blocks(KS, 3);
+            constexpr int KS = k.value, R1 = loss_blocks(KS, 1), R2 = loss_blocks(KS, 2);
             const dim3 grid((unsigned)((n + 64 * p.loss_rb - 1) / (64 * p.loss_rb)), (unsigned)p.loss_splits);
-            if (dtype == GSR_F32) hipLaunchKernelGGL((k_class_loss<KS, 3, R3>), grid, dim3(256), 0, st, g);
+            if (dtype == GSR_F32) hipLaunchKernelGGL((k_class_loss<KS, 2, R2>), grid, dim3(256), 0, st, g);
             else hipLaunchKernelGGL((k_class_loss<KS, 1, R1>), grid, dim3(256), 0, st, g);
         });
         hipLaunchKernelGGL(k_class_lse, dim3(blocks), dim3(1024), 0, st, g.part, g.at_target, a.target, n, p.x_pad, p.loss_splits, lse_out, parts, loss_out);
@@ -748,6 +904,8 @@ gsr_status_t gsr_class_grad(const void* x, int64_t ldx, int64_t n, int32_t d, in
         if (dx_out && n) {
             g.own = a.xf;
             g.stream = a.ef;
+            g.own_exp = a.x_exp;
+            g.stream_exp = a.e_exp;
             g.out = dx_out;
             g.rows = n;
             g.ld = lddx;
@@ -763,6 +921,8 @@ gsr_status_t gsr_class_grad(const void* x, int64_t ldx, int64_t n, int32_t d, in
         if (dtable_out || dbias_out) {
             g.own = a.ef;
             g.stream = a.xf;
+            g.own_exp = a.e_exp;
+            g.stream_exp = a.x_exp;
             g.out = dtable_out;
             g.rows = classes;
             g.ld = lddt;

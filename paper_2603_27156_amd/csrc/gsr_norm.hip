@@ -335,14 +335,24 @@ struct CodeSource {
 };
 
 // ---- forward ---------------------------------------------------------------------------------------------
-// Sums of x and x^2 in 64 bits: squares are exact there, and the difference mean x^2 - m^2 keeps the variance as long as the mean is within some
-// 2^20 standard deviations of zero.
+// Sums of x - k and (x - k)^2 in 64 bits, with the first value of the group in the first graph as k for all graphs: squares are all but exact there, and what
+// mean (x - k)^2 - (mean (x - k))^2 loses of the variance to cancellation is nothing unless a graph's mean lies some 2^20 standard deviations from k.
+template <typename T>
+__device__ __forceinline__ double group_shift(const NormShape& s, const GraphRows& g, const T* x, const RowPlane& p, int group) {
+    const int column = group * s.cg, plane = column / s.dg;
+    const int64_t first = g.at(0), row = first < s.n ? first : s.n - 1;
+    const float v = to_float(x[plane * p.gs + row * p.ld + (column - plane * s.dg)]);
+    return fabsf(v) < INFINITY ? (double)v : 0.0;
+}
 template <typename T, int V, bool TAIL>
-__global__ __launch_bounds__(256) void k_norm_sums(NormShape s, GraphRows g, const T* __restrict__ x, RowPlane p, double2* __restrict__ pieces) {
+__global__ __launch_bounds__(256) void k_norm_sums(NormShape s, GraphRows g, const T* __restrict__ x, RowPlane p, double2* __restrict__ pieces,
+                                                   double* __restrict__ shifts) {
     const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (w >= s.chunks) return;
     const int slab = blockIdx.y;
     const LaneColumns c = lane_columns<V>(s, slab);
+    const double shift = group_shift(s, g, x, p, c.on ? c.group : 0);
+    if (w == 0 && c.head && c.sub == 0 && c.plane * s.dg + c.own == c.group * s.cg) shifts[c.group] = shift;
     over_graphs(s, g, w, [&](int64_t graph, int64_t a, int64_t b) {
         constexpr int U = 4;
         double u = 0.0, v = 0.0;
@@ -360,7 +370,7 @@ __global__ __launch_bounds__(256) void k_norm_sums(NormShape s, GraphRows g, con
                 const bool in = r + k * c.subs + c.sub < b;
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const double t = in && !(TAIL && j < c.skip) ? (double)q[k].at(j) : 0.0;
+                    const double t = in && !(TAIL && j < c.skip) ? (double)q[k].at(j) - shift : 0.0;
                     u += t;
                     v = fma(t, t, v);
                 }
@@ -369,20 +379,21 @@ __global__ __launch_bounds__(256) void k_norm_sums(NormShape s, GraphRows g, con
         leave_piece(s, c, slab, w, graph, u, v, pieces);
     });
 }
-__device__ __forceinline__ void statistics(double u, double v, double count, double eps, float& mean, float& rstd) {
+__device__ __forceinline__ void statistics(double u, double v, double count, double shift, double eps, float& mean, float& rstd) {
     const double m = count ? u / count : 0.0, var = count ? v / count - m * m : 0.0;
-    mean = (float)m;
+    mean = count ? (float)(m + shift) : 0.0f;
     rstd = (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + eps));          // (NaN stays NaN)
 }
 template <bool WIDE>
-__global__ __launch_bounds__(1024) void k_norm_join(NormShape s, GraphRows g, int V, const double2* __restrict__ pieces, double eps,
+__global__ __launch_bounds__(1024) void k_norm_join(NormShape s, GraphRows g, int V, const double2* __restrict__ pieces,
+                                                    const double* __restrict__ shifts, double eps,
                                                    float* __restrict__ mean, float* __restrict__ rstd) {
     int64_t task, rows;
     double u, v;
     if (!joined<WIDE>(s, g, V, blockIdx.x, pieces, task, u, v, rows)) return;
     if (lane_id()) return;
     float m, r;
-    statistics(u, v, (double)rows * s.cg, eps, m, r);
+    statistics(u, v, (double)rows * s.cg, rows ? shifts[task % s.groups] : 0.0, eps, m, r);
     mean[task] = m;
     rstd[task] = r;
 }
@@ -465,6 +476,7 @@ __global__ __launch_bounds__(1024) void k_norm_small(NormShape s, GraphRows g, c
     const int wave = threadIdx.x >> 6;
     const int64_t a = g.at(0), b = g.at(1) > a ? g.at(1) : a;
     constexpr int U = 4;
+    const double shift = group_shift(s, g, x, p, c.on ? c.group : 0);
     double u = 0.0, v = 0.0;
     for (int64_t r = a + (int64_t)wave * U * c.subs; r < b; r += 16 * U * c.subs) {
         PlaneSource<T, V, false> q[U];
@@ -480,7 +492,7 @@ __global__ __launch_bounds__(1024) void k_norm_small(NormShape s, GraphRows g, c
             const bool in = r + k * c.subs + c.sub < b;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const double t = in ? (double)q[k].at(j) : 0.0;
+                const double t = in ? (double)q[k].at(j) - shift : 0.0;
                 u += t;
                 v = fma(t, t, v);
             }
@@ -490,7 +502,7 @@ __global__ __launch_bounds__(1024) void k_norm_small(NormShape s, GraphRows g, c
     load_affine<V>(gamma_in, c, 1.0f, gamma);
     load_affine<V>(beta_in, c, 0.0f, beta);
     const double2 t = small_total(s, c, u, v);
-    statistics(t.x, t.y, (double)(b - a) * s.cg, eps, m, rs);
+    statistics(t.x, t.y, (double)(b - a) * s.cg, shift, eps, m, rs);
     if (blockIdx.x == 0 && wave == 0 && c.head && c.sub == 0) {
         mean[c.group] = m;
         rstd[c.group] = rs;
@@ -942,9 +954,9 @@ gsr_status_t norm_args(int32_t d, int32_t groups, int32_t act, const float* gamm
     return GSR_OK;
 }
 
-// The workspace of both directions: pieces, the means of the gradient, the columns' partial sums.
+// The workspace of both directions: pieces; the groups' shifts; the means of the gradient, the columns' partial sums.
 struct NormWs {
-    size_t pieces, means, columns, total;
+    size_t pieces, shifts, means, columns, total;
     bool wide;
     int64_t task_blocks;
 };
@@ -953,7 +965,8 @@ NormWs carve_norm(const NormShape& s, int64_t graphs) {
     w.pieces = 0;
     // at least as many chunks as any number of rows up to n has, so that a workspace serves them all
     const int64_t chunks = std::max((s.n + kMaxRows - 1) / kMaxRows, std::min((s.n + least_rows(s) - 1) / least_rows(s), kChunks / s.slabs + 1));
-    w.means = align_up((size_t)(chunks + graphs) * s.stride() * sizeof(double2));
+    w.shifts = align_up((size_t)(chunks + graphs) * s.stride() * sizeof(double2));
+    w.means = w.shifts + align_up((size_t)s.groups * sizeof(double));
     w.columns = w.means + align_up((size_t)graphs * s.groups * sizeof(float2));
     w.total = w.columns + align_up((size_t)((chunks + 3) / 4) * 2 * s.d * 4);
     w.wide = s.chunks > 64 * graphs;
@@ -1053,6 +1066,7 @@ gsr_status_t gsr_group_norm(const void* x, int64_t ldx, int64_t n, int32_t d, in
     if (graphs == 0) return GSR_OK;
     hipStream_t st = (hipStream_t)stream;
     double2* pieces = (double2*)((char*)workspace + ws.pieces);
+    double* shifts = (double*)((char*)workspace + ws.shifts);
     by_piece(dtype, rule, [&](auto t, auto v, auto tail) {
         using T = decltype(t);
         constexpr int P = v.value;
@@ -1068,9 +1082,9 @@ gsr_status_t gsr_group_norm(const void* x, int64_t ldx, int64_t n, int32_t d, in
             });
             return;
         }
-        if (n) hipLaunchKernelGGL((k_norm_sums<T, P, tail.value>), rows_grid(s), dim3(256), 0, st, s, g, (const T*)x, px, pieces);
-        if (ws.wide) hipLaunchKernelGGL((k_norm_join<true>), dim3((unsigned)ws.task_blocks), dim3(1024), 0, st, s, g, V, pieces, (double)eps, mean_out, rstd_out);
-        else hipLaunchKernelGGL((k_norm_join<false>), dim3((unsigned)ws.task_blocks), dim3(1024), 0, st, s, g, V, pieces, (double)eps, mean_out, rstd_out);
+        if (n) hipLaunchKernelGGL((k_norm_sums<T, P, tail.value>), rows_grid(s), dim3(256), 0, st, s, g, (const T*)x, px, pieces, shifts);
+        if (ws.wide) hipLaunchKernelGGL((k_norm_join<true>), dim3((unsigned)ws.task_blocks), dim3(1024), 0, st, s, g, V, pieces, shifts, (double)eps, mean_out, rstd_out);
+        else hipLaunchKernelGGL((k_norm_join<false>), dim3((unsigned)ws.task_blocks), dim3(1024), 0, st, s, g, V, pieces, shifts, (double)eps, mean_out, rstd_out);
         if (!n) return;
         const Affine f{gamma, beta, mean_out, rstd_out};
         const NormShape q = apply_shape(s, graph_ptr);

@@ -1,8 +1,8 @@
 """Softmax cross entropy over many classes and its gradient against the definitions in 64 bits.
 
 u = 2^-24.  A sum of k terms on the matrix cores is off by at most 2 k u times the sum of absolute values (whether its additions round or
-truncate).  Logits: 16-bit values give d terms; floats six products of pieces each, 6 d terms, and what the products of smaller pieces leave out is below
-2^-21 = 8 u of each value.  exp(z - l) by base 2: u |z - l| for the difference, 2 u |z - l| for the product, 2 u for the function.  lse: T tiles of a lane
+truncate).  Logits: 16-bit values give d terms; floats three products of pieces each, 3 d terms (bounded here by six), and what the pieces and the product of
+the smaller ones leave out is below 2^-21 = 8 u of each value, or 2^-38 of the largest in 32 rows.  exp(z - l) by base 2: u |z - l| for the difference, 2 u |z - l| for the product, 2 u for the function.  lse: T tiles of a lane
 have 8 additions each, and the running maximum is exchanged at most T times (2 u each, and 3 u of the way it goes).  dz: one rounding, and with
 16-bit planes a relative 2^-8 more; then sums over all classes or rows, their parts joined (64 at most), and three roundings.  A 16-bit
 output adds half a step, 2^-8 of the value."""
@@ -33,6 +33,8 @@ class Reference:
         self.z = x @ e.T + b
         finite_b = np.where(np.isfinite(b), np.abs(b), 0.0)
         self.z_off = (terms(dtype, d) + 4) * U * (np.abs(x) @ np.abs(e).T + finite_b)
+        self.small_x, self.small_e = (self.smallest(v) if dtype == F32 else np.zeros((len(v), 1)) for v in (x, e))
+        self.z_off += self.small_x * np.abs(e).sum(1) + (self.small_e * np.abs(x).sum(1)).T
         top = self.z.max(1, keepdims=True) if n else np.zeros((0, 1))
         w = np.exp(self.z - top)
         self.lse = top[:, 0] + np.log(w.sum(1))
@@ -41,6 +43,14 @@ class Reference:
         low = np.where(np.isfinite(self.z), self.z, np.inf).min(1) if n else np.zeros(0)
         tiles = -(-len(e) // 32)
         self.lse_off = (p * (self.z_off + U * (3 * way + 2))).sum(1) + U * (10 * tiles + 8 + 3 * (top[:, 0] - low) + 2 * np.abs(self.lse))
+
+    @staticmethod
+    def smallest(v):
+        """2^-38 of the largest value of every 32 rows, for each of them."""
+        out = np.zeros((len(v), 1))
+        for a in range(0, len(v), 32):
+            out[a:a + 32] = 2.0 ** -38 * np.abs(v[a:a + 32]).max()
+        return out
 
     def loss(self):
         """(loss, bound)."""
@@ -63,12 +73,17 @@ class Reference:
         bias = dz.sum(0) * k, off.sum(0) * abs(k) + 8 * U * (np.abs(dz)).sum(0) * abs(k)
         rounded = off + (2.0 ** -8 * (np.abs(dz) + off) if self.dtype == BF16 else 0.0)
 
-        def product(dz, rounded, other, length):
+        def product(dz, rounded, other, small, length):
             size = np.abs(dz) @ np.abs(other)
-            return dz @ other * k, (rounded @ np.abs(other) + (terms(self.dtype, length) + 64 + 4) * U * size) * abs(k)
+            off = rounded @ np.abs(other) + (terms(self.dtype, length) + 64 + 4) * U * size
+            if self.dtype == F32 and dz.size:       # what pieces leave out: of the streamed rows, and of dz, 2^-36 of the largest product with a streamed tile
+                off += np.abs(dz) @ np.broadcast_to(small, other.shape)
+                tops = 2.0 ** 38 * small[:, 0]
+                off += 2.0 ** -34 * (np.abs(dz) * tops).max(1, keepdims=True) * len(other)
+            return dz @ other * k, off * abs(k)
 
         x = np.where(self.known[:, None], self.x, 0.0)
-        return dict(dx=product(dz, rounded, self.e, len(self.e)), dtable=product(dz.T, rounded.T, x, len(self.x)), dbias=bias)
+        return dict(dx=product(dz, rounded, self.e, self.small_e, len(self.e)), dtable=product(dz.T, rounded.T, x, self.smallest(x), len(self.x)), dbias=bias)
 
 
 def close(got, want, off, dtype=F32):
@@ -199,6 +214,39 @@ def test_large_logits_stay_finite():
         dx = torch.empty_like(x)
         gsr.gsr_class_grad(x, e, ids, lse, dx_out=dx)
         assert bool(dx.isfinite().all()) and abs(loss.item() - ref.loss()[0]) <= ref.loss()[1]
+
+
+@pytest.mark.parametrize("spread", ["classes", "rows", "columns", "learnt"])
+def test_values_of_very_different_size(spread):
+    """Classes of probabilities down to 1e-13, rows and columns of very different size, rows whose class is nearly certain.  Of the first two every row of
+    every gradient is right to 1e-4 of its own largest value (its sums are of hundreds of terms, each right to 1e-5: logits of up to 30 are off by
+    30 u and more)."""
+    n, classes, d = 200, 300, 64
+    rng = np.random.default_rng(11)
+    x, e, b = rng.standard_normal((n, d)), rng.standard_normal((classes, d)) * 0.2, np.zeros(classes)
+    if spread == "classes":
+        b = -30.0 * rng.random(classes)
+    elif spread == "rows":
+        x *= np.exp(6.0 * rng.standard_normal((n, 1)).clip(-2, 0.3))
+        e *= np.exp(4.0 * rng.standard_normal((classes, 1)).clip(-2, 0.3))
+    elif spread == "columns":
+        scale = np.exp(4.0 * rng.standard_normal(d))
+        x, e = x * scale, e / scale
+    ids = rng.integers(0, classes, n)
+    if spread == "learnt":
+        for i in range(n):
+            x[i] += 15.0 * rng.random() * e[ids[i]] / (e[ids[i]] ** 2).sum()
+    x, e, b, ids = put(x), put(e), put(b), torch.from_numpy(ids).to(dev())
+    _, lse = forward(x, e, b, ids, n)
+    ref = Reference(host(x), host(e), b.double().cpu().numpy(), ids.cpu().numpy(), F32)
+    close(lse.double().cpu().numpy(), ref.lse, ref.lse_off)
+    dx, de = torch.empty_like(x), torch.empty_like(e)
+    gsr.gsr_class_grad(x, e, ids, lse, dx_out=dx, dtable_out=de, bias=b)
+    want = ref.gradients(lse.double().cpu().numpy(), 1.0)
+    for got, (exact, off) in ((host(dx), want["dx"]), (host(de), want["dtable"])):
+        close(got, exact, off)
+        if spread in ("classes", "rows"):
+            assert (np.abs(got - exact) / np.abs(exact).max(1, keepdims=True)).max() <= 1e-4, spread
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])

@@ -277,18 +277,25 @@ def test_in_place(dtype, n, d, c, groups):
     assert torch.equal(rows_of(dy)[:ptr[0]], torch.from_numpy(given[:ptr[0]]).to(dtype).to(dev()))
 
 
-def test_a_constant_group_and_far_means():
-    """Variance 0 gives rstd = 1 / sqrt(eps) and y = beta; a mean of 10,000 standard deviations keeps rstd to 2 u."""
-    x = torch.full((300, 8), 3.25, device=dev())
-    y, (mean, rstd) = torch.empty_like(x), stats([0, 1], 2)
+@pytest.mark.parametrize("n,ptr", [(5_000, None), (60_000, None), (9_000, [0, 4_000, 4_000, 9_000])])
+def test_a_constant_group_and_far_means(n, ptr):
+    """Variance 0 gives rstd = 1 / sqrt(eps) and y = beta.  A mean of 10,000 or a million standard deviations leaves rstd right: values are summed from the first one
+    on, a few standard deviations from all, so that 64 bits lose below 2^13 additions * 2^-53 * 100 of the variance, less than half a float's step."""
+    graphs = [0, n] if ptr is None else ptr
+    dptr = None if ptr is None else torch.tensor(ptr, device=dev())
+    x = torch.full((n, 8), 3.25, device=dev())
+    y, (mean, rstd) = torch.empty_like(x), stats(graphs, 2)
     beta = torch.arange(8.0, device=dev())
-    gsr.gsr_group_norm(x, y, mean, rstd, beta=beta)
-    assert torch.equal(mean, torch.full_like(mean, 3.25)) and torch.equal(y, beta.expand(300, 8))
+    gsr.gsr_group_norm(x, y, mean, rstd, beta=beta, graph_ptr=dptr)
+    empty = torch.tensor([a == b for a, b in zip(graphs, graphs[1:])], device=dev())[:, None].expand(-1, 2)
+    assert torch.equal(mean, torch.where(empty, 0.0, 3.25).float()) and torch.equal(y, beta.expand(n, 8))
     assert torch.equal(rstd, torch.full_like(rstd, 1.0 / np.sqrt(np.float64(np.float32(1e-5)))))
-    far = (torch.randn((5000, 8), device=dev()) + 10_000.0)
-    gsr.gsr_group_norm(far, torch.empty_like(far), mean, rstd)
-    ref = Reference(far.double().cpu().numpy(), np.array([0, 5000]), 2, None, None, "none")
-    close(rstd.double().cpu().numpy(), ref.rstd, 2 * U * ref.rstd)
+    for off in (1e4, 1e6):
+        far = torch.randn((n, 8), generator=torch.Generator(device="cuda").manual_seed(1), device=dev()) + off
+        gsr.gsr_group_norm(far, torch.empty_like(far), mean, rstd, graph_ptr=dptr)
+        ref = Reference(far.double().cpu().numpy(), np.array(graphs), 2, None, None, "none")
+        close(mean.double().cpu().numpy(), ref.mean, 2 * U * np.abs(ref.mean))
+        close(rstd.double().cpu().numpy(), ref.rstd, 2 * U * ref.rstd)
 
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
