@@ -26,7 +26,7 @@ namespace gsr {
 constexpr int kMaxClassWidth = 512;
 constexpr int kTileRows = 32;                   // streamed rows of a tile
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kNoMax = -3.0e38f;              // a running maximum that no logit has reached
+constexpr float kNoMax = -1.0e38f;              // a running maximum that no logit has reached; times log2 e it is finite
 
 // ---- operands ------------------------------------------------------------------------------------------
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -92,66 +92,73 @@ __device__ __forceinline__ void two_pieces(float v, uint32_t& h, uint32_t& l) {
     h = __builtin_bit_cast(uint16_t, top);
     l = f16_bits(v - static_cast<float>(top));
 }
-// 32 rows by a wave
-template <typename T>
+// 16-bit rows: four pieces by a workgroup
+__device__ __forceinline__ void lay_out(const RowSource& s, uint4* __restrict__ out, float*, int64_t pad, int ks, int64_t block, const ClassTokens* known, bf16_t) {
+    const int64_t piece = block * 4 + (threadIdx.x >> 6);
+    if (piece >= pad / 16 * ks) return;
+    const int lane = lane_id();
+    const int64_t row = piece / ks * 16 + (lane & 15);
+    float v[8];
+    load_eight<bf16_t>(s, row, row < s.rows && (!known || known->at(row) >= 0), (int)(piece % ks) * 32 + (lane >> 4) * 8, v);
+    uint4 w;
+    w.x = __builtin_amdgcn_perm(__float_as_uint(v[1]), __float_as_uint(v[0]), 0x07060302u);
+    w.y = __builtin_amdgcn_perm(__float_as_uint(v[3]), __float_as_uint(v[2]), 0x07060302u);
+    w.z = __builtin_amdgcn_perm(__float_as_uint(v[5]), __float_as_uint(v[4]), 0x07060302u);
+    w.w = __builtin_amdgcn_perm(__float_as_uint(v[7]), __float_as_uint(v[6]), 0x07060302u);
+    out[piece * 64 + lane] = w;
+}
+// floats: 32 rows by a workgroup, all of them in its registers
 __device__ __forceinline__ void lay_out(const RowSource& s, uint4* __restrict__ out, float* __restrict__ exponents, int64_t pad, int ks, int64_t tile,
-                                        const ClassTokens* known) {
-    if (tile >= pad / kTileRows) return;
-    const int lane = lane_id(), col = (lane >> 4) * 8;
-    int64_t row[2];
+                                        const ClassTokens* known, float) {
+    constexpr int MOST = kMaxClassWidth / 32 * 2 / 4;           // of a wave
+    const int lane = lane_id(), wave = threadIdx.x >> 6;
     bool in[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-        row[b] = tile * kTileRows + b * 16 + (lane & 15);
-        in[b] = row[b] < s.rows && (!known || known->at(row[b]) >= 0);
+        const int64_t row = tile * kTileRows + b * 16 + (lane & 15);
+        in[b] = row < s.rows && (!known || known->at(row) >= 0);
     }
-    float v[8];
-    if constexpr (sizeof(T) == 2) {
-        for (int k = 0; k < ks; ++k) {
+    float v[MOST][8];
+    uint32_t top = 0;                   // bits of the largest finite value
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                load_eight<T>(s, row[b], in[b], k * 32 + col, v);
-                uint4 w;
-                w.x = __builtin_amdgcn_perm(__float_as_uint(v[1]), __float_as_uint(v[0]), 0x07060302u);
-                w.y = __builtin_amdgcn_perm(__float_as_uint(v[3]), __float_as_uint(v[2]), 0x07060302u);
-                w.z = __builtin_amdgcn_perm(__float_as_uint(v[5]), __float_as_uint(v[4]), 0x07060302u);
-                w.w = __builtin_amdgcn_perm(__float_as_uint(v[7]), __float_as_uint(v[6]), 0x07060302u);
-                out[((tile * 2 + b) * ks + k) * 64 + lane] = w;
-            }
+    for (int i = 0; i < MOST; ++i) {
+        const int piece = i * 4 + wave, b = piece >= ks, k = b ? piece - ks : piece;
+        if (piece < 2 * ks) load_eight<float>(s, tile * kTileRows + b * 16 + (lane & 15), b ? in[1] : in[0], k * 32 + (lane >> 4) * 8, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < MOST; ++i) {
+        if (i * 4 + wave >= 2 * ks) continue;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t u = __float_as_uint(v[i][j]) & 0x7FFFFFFFu;
+            if (u < 0x7F800000u) top = top > u ? top : u;
         }
-    } else {
-        uint32_t top = 0;               // bits of the largest finite value
-        for (int k = 0; k < ks; ++k)
+    }
+    for (int o = 32; o; o >>= 1) {
+        const uint32_t u = __shfl_xor(top, o);
+        top = top > u ? top : u;
+    }
+    __shared__ uint32_t s_top[4];
+    if (lane == 0) s_top[wave] = top;
+    __syncthreads();
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                load_eight<T>(s, row[b], in[b], k * 32 + col, v);
+    for (int w = 0; w < 4; ++w) top = top > s_top[w] ? top : s_top[w];
+    // rows of zeros, and rows below 2^-100, whose products are nothing beside the rounding of any logit
+    int e = (int)(top >> 23) - 127;
+    if (top == 0) e = 0;
+    if (e < -100) e = -100;
+    const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
+    if (threadIdx.x == 0) exponents[tile] = (float)(e - 14);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const uint32_t u = __float_as_uint(v[j]) & 0x7FFFFFFFu;
-                    if (u < 0x7F800000u) top = top > u ? top : u;
-                }
-            }
-        for (int o = 32; o; o >>= 1) {
-            const uint32_t u = __shfl_xor(top, o);
-            top = top > u ? top : u;
-        }
-        // rows of zeros, and rows below 2^-100, whose products are nothing beside the rounding of any logit
-        int e = (int)(top >> 23) - 127;
-        if (top == 0) e = 0;
-        if (e < -100) e = -100;
-        const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
-        if (lane == 0) exponents[tile] = (float)(e - 14);
-        for (int k = 0; k < ks; ++k)
+    for (int i = 0; i < MOST; ++i) {
+        const int piece = i * 4 + wave;
+        if (piece >= 2 * ks) continue;
+        uint32_t h[8], l[8];
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                load_eight<T>(s, row[b], in[b], k * 32 + col, v);
-                uint32_t h[8], l[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) two_pieces(v[j] * up, h[j], l[j]);
-                uint4* to = out + ((tile * 2 + b) * ks + k) * 128 + lane;
-                to[0] = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
-                to[64] = make_uint4(l[0] | l[1] << 16, l[2] | l[3] << 16, l[4] | l[5] << 16, l[6] | l[7] << 16);
-            }
+        for (int j = 0; j < 8; ++j) two_pieces(v[i][j] * up, h[j], l[j]);
+        uint4* to = out + (tile * 2 * ks + piece) * 128 + lane;
+        to[0] = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+        to[64] = make_uint4(l[0] | l[1] << 16, l[2] | l[3] << 16, l[4] | l[5] << 16, l[6] | l[7] << 16);
     }
 }
 template <typename T>
@@ -159,12 +166,12 @@ __global__ __launch_bounds__(256) void k_class_setup(ClassSetup s) {
     unsigned b = blockIdx.x;
     const int wave = threadIdx.x >> 6;
     if (b < s.x_blocks) {
-        lay_out<T>(s.x, s.xf, s.x_exp, s.x_pad, s.ks, (int64_t)b * 4 + wave, s.lse ? &s.ids : nullptr);
+        lay_out(s.x, s.xf, s.x_exp, s.x_pad, s.ks, b, s.lse ? &s.ids : nullptr, T{});
         return;
     }
     b -= s.x_blocks;
     if (b < s.e_blocks) {
-        lay_out<T>(s.e, s.ef, s.e_exp, s.e_pad, s.ks, (int64_t)b * 4 + wave, nullptr);
+        lay_out(s.e, s.ef, s.e_exp, s.e_pad, s.ks, b, nullptr, T{});
         return;
     }
     b -= s.e_blocks;
@@ -330,11 +337,12 @@ __global__ __launch_bounds__(256, loss_waves(KS, NP)) void k_class_loss(ClassLos
             for (int blk = 0; blk < 2; ++blk)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) m = fmaxf(m, z[blk][r][i]);
+            const float by = -m * kLog2e;               // rounded once for all: off by 2^-24 |m| in lse, as the logits are
             float s = sum[r] * __builtin_amdgcn_exp2f((top[r] - m) * kLog2e);
 #pragma unroll
             for (int blk = 0; blk < 2; ++blk)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s += __builtin_amdgcn_exp2f((z[blk][r][i] - m) * kLog2e);
+                for (int i = 0; i < 4; ++i) s += __builtin_amdgcn_exp2f(fmaf(z[blk][r][i], kLog2e, by));
             top[r] = m;
             sum[r] = s;
         }
@@ -379,16 +387,22 @@ __device__ __forceinline__ void add_up(double& sum, int64_t& count) {          /
         count += s_count[i];
     }
 }
+// 2^q lanes take the splits of a row
 __global__ __launch_bounds__(1024) void k_class_lse(const float2* __restrict__ part, const float* __restrict__ at_target,
-                                                    const int32_t* __restrict__ target, int64_t n, int64_t x_pad, int splits,
+                                                    const int32_t* __restrict__ target, int64_t n, int64_t x_pad, int splits, int q,
                                                     float* __restrict__ lse_out, LossPart* __restrict__ parts, float* __restrict__ loss) {
     double sum = 0.0;
     int64_t count = 0;
-    for (int64_t i = (int64_t)blockIdx.x * 1024 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 1024) {
+    const int first = threadIdx.x & ((1 << q) - 1), step = 1 << q;
+    for (int64_t r = (int64_t)blockIdx.x * (1024 >> q); r < n; r += (int64_t)gridDim.x * (1024 >> q)) {          // the same for a workgroup
+        const int64_t row = r + (threadIdx.x >> q), i = row < n ? row : n - 1;
         float m = kNoMax;
-        for (int s = 0; s < splits; ++s) m = fmaxf(m, part[s * x_pad + i].x);
+        for (int s = first; s < splits; s += step) m = fmaxf(m, part[s * x_pad + i].x);
+        for (int o = step >> 1; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
         double l = 0.0;
-        for (int s = 0; s < splits; ++s) l += (double)part[s * x_pad + i].y * exp((double)part[s * x_pad + i].x - (double)m);
+        for (int s = first; s < splits; s += step) l += (double)part[s * x_pad + i].y * exp((double)part[s * x_pad + i].x - (double)m);
+        for (int o = step >> 1; o; o >>= 1) l += __shfl_xor(l, o);
+        if (first || row >= n) continue;
         const double lse = (double)m + log(l);
         lse_out[i] = (float)lse;
         if (target[i] >= 0) {
@@ -420,10 +434,12 @@ struct ClassGradArgs {
     const int32_t *target, *counts;
     void* out;                      // rows x d of T: a plane, or a table
     int64_t rows, ld, gs;
-    float* part;                    // [splits][own_pad][KS * 32], where there are several
-    double* bias_part;              // BY_CLASS: [splits][own_pad]
+    float* part;                    // [splits][own_pad][KS * 32], where there are several; of rows and of classes each its own
+    double* bias_part;              // BY_CLASS: [splits][own_pad], where there are several
+    float* dbias;                   // BY_CLASS
     int64_t own_pad;
     int32_t d, dg, tiles, splits, count_blocks;
+    uint32_t blocks;                // workgroups of a part; 0: this side is not asked for
     float scale;
 };
 __device__ __forceinline__ float gradient_scale(const int32_t* __restrict__ counts, int blocks, float scale) {
@@ -490,14 +506,15 @@ __device__ __forceinline__ void fit_row(int r, float largest, float& k, f32x4 (&
     }
 }
 
+// Workgroup `index` of those of one side: a block of its rows and a part of the tiles.
 template <int KS, int NP, int RB, bool BY_CLASS, typename T>
-__global__ __launch_bounds__(256, grad_waves(KS, NP)) void k_class_grad(ClassGradArgs g) {
+__device__ __forceinline__ void grad_side(const ClassGradArgs& g, unsigned index, uint4 (*s_tile)[2 * KS * NP * 64]) {
     constexpr int N = 2 * KS * NP;
     constexpr bool TWO = grad_two(KS, NP);
-    __shared__ uint4 s_tile[TWO ? 2 : 1][N * 64];
+    const unsigned part = index / g.blocks;
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4;
-    const int64_t block0 = ((int64_t)blockIdx.x * 4 + wave) * RB;
-    const int t0 = (int)((int64_t)g.tiles * blockIdx.y / g.splits), t1 = (int)((int64_t)g.tiles * (blockIdx.y + 1) / g.splits);
+    const int64_t block0 = ((int64_t)(index - part * g.blocks) * 4 + wave) * RB;
+    const int t0 = (int)((int64_t)g.tiles * part / g.splits), t1 = (int)((int64_t)g.tiles * (part + 1) / g.splits);
     if (t0 < t1) fetch_tile<N>(g.stream + (int64_t)t0 * N * 64, s_tile[0], wave, lane);
     frag8 own[RB][KS][NP];
     load_own<KS, NP, RB>(g.own, block0, lane, own);
@@ -611,7 +628,9 @@ __global__ __launch_bounds__(256, grad_waves(KS, NP)) void k_class_grad(ClassGra
         if constexpr (BY_CLASS) {
             bias_sum[r] += __shfl_xor(bias_sum[r], 16);
             bias_sum[r] += __shfl_xor(bias_sum[r], 32);
-            if (grp == 0) g.bias_part[blockIdx.y * g.own_pad + (block0 + r) * 16 + lane] = bias_sum[r];
+            const int64_t j = (block0 + r) * 16 + lane;
+            if (grp == 0 && g.splits > 1) g.bias_part[part * g.own_pad + j] = bias_sum[r];
+            else if (grp == 0 && g.dbias && j < g.rows) g.dbias[j] = (float)(bias_sum[r] * (double)scale);
         }
         if (!g.out) continue;                   // only the bias is asked for
         if constexpr (NP == 2) {
@@ -624,7 +643,7 @@ __global__ __launch_bounds__(256, grad_waves(KS, NP)) void k_class_grad(ClassGra
             }
         }
         if (g.splits > 1) {
-            float* to = g.part + ((int64_t)blockIdx.y * g.own_pad + row0) * (KS * 32) + (lane & 15);
+            float* to = g.part + ((int64_t)part * g.own_pad + row0) * (KS * 32) + (lane & 15);
 #pragma unroll
             for (int c = 0; c < 2 * KS; ++c)
 #pragma unroll
@@ -643,33 +662,70 @@ __global__ __launch_bounds__(256, grad_waves(KS, NP)) void k_class_grad(ClassGra
         }
     }
 }
-// the splits' sums joined: a thread per value
-template <typename T>
-__global__ __launch_bounds__(256) void k_class_grad_join(ClassGradArgs g, int width) {
-    const float scale = gradient_scale(g.counts, g.count_blocks, g.scale);
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < g.rows * g.d; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / g.d;
-        const int col = (int)(i - row * g.d), plane = col / g.dg;
-        float v = 0.0f;
-        for (int s = 0; s < g.splits; ++s) v += g.part[((int64_t)s * g.own_pad + row) * width + col];
-        store_as(static_cast<T*>(g.out) + plane * g.gs + row * g.ld + (col - plane * g.dg), v * scale);
-    }
+// dx and dE, or one of them, in one launch: what is left of the one's last round is filled by the other, and few rows and classes wait for one launch less
+template <int KS, int NP, int RB, typename T>
+__global__ __launch_bounds__(256, grad_waves(KS, NP)) void k_class_grad(ClassGradArgs by_row, ClassGradArgs by_class) {
+    __shared__ uint4 s_tile[grad_two(KS, NP) ? 2 : 1][2 * KS * NP * 64];
+    const unsigned rows = by_row.blocks * by_row.splits;
+    if (blockIdx.x < rows) grad_side<KS, NP, RB, false, T>(by_row, blockIdx.x, s_tile);
+    else grad_side<KS, NP, RB, true, T>(by_class, blockIdx.x - rows, s_tile);
 }
-__global__ __launch_bounds__(256) void k_class_bias_join(const double* __restrict__ part, int64_t own_pad, int splits, const int32_t* __restrict__ counts,
-                                                         int count_blocks, float scale, int64_t classes, float* __restrict__ dbias) {
-    const float k = gradient_scale(counts, count_blocks, scale);
-    const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (j >= classes) return;
-    double v = 0.0;
-    for (int s = 0; s < splits; ++s) v += part[s * own_pad + j];
-    dbias[j] = (float)(v * (double)k);
+// The parts' sums joined, 2^q threads of a workgroup a value: every 2^q-th part each, then one after the other.
+template <typename V, typename Part, typename Store>
+__device__ __forceinline__ void join_parts(int64_t first, int64_t count, int splits, int q, V* s_sum, Part part, Store store) {
+    const int each = 256 >> q, mine = threadIdx.x & (each - 1), lane = threadIdx.x >> (8 - q);
+    const int64_t i = first + mine;
+    V v = 0;
+    if (i < count) {
+        constexpr int U = 4;
+        for (int s = lane; s < splits; s += U << q) {
+            V t[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) t[k] = s + (k << q) < splits ? part(s + (k << q), i) : V(0);
+#pragma unroll
+            for (int k = 0; k < U; ++k) v += t[k];
+        }
+    }
+    if (q) {
+        s_sum[threadIdx.x] = v;
+        __syncthreads();
+        if (lane) return;
+        for (int k = 1; k < 1 << q; ++k) v += s_sum[(k << (8 - q)) + mine];
+    }
+    if (i < count) store(i, v);
+}
+struct JoinShape {
+    unsigned row_blocks, class_blocks, bias_blocks;         // workgroups of each; 0: nothing to join
+    int row_q, class_q, width;
+};
+template <typename T>
+__global__ __launch_bounds__(256) void k_class_grad_join(ClassGradArgs by_row, ClassGradArgs by_class, JoinShape j) {
+    __shared__ double s_sum[256];
+    unsigned b = blockIdx.x;
+    const bool rows = b < j.row_blocks;
+    if (!rows) b -= j.row_blocks;
+    const ClassGradArgs& g = rows ? by_row : by_class;
+    const int q = rows ? j.row_q : j.class_q;
+    const float scale = gradient_scale(g.counts, g.count_blocks, g.scale);
+    if (rows || b < j.class_blocks) {
+        join_parts<float>((int64_t)b * (256 >> q), g.rows * g.d, g.splits, q, reinterpret_cast<float*>(s_sum),
+            [&](int s, int64_t i) { return g.part[((int64_t)s * g.own_pad + i / g.d) * j.width + i % g.d]; },
+            [&](int64_t i, float v) {
+                const int64_t row = i / g.d;
+                const int col = (int)(i - row * g.d), plane = col / g.dg;
+                store_as(static_cast<T*>(g.out) + plane * g.gs + row * g.ld + (col - plane * g.dg), v * scale);
+            });
+    } else {
+        join_parts<double>((int64_t)(b - j.class_blocks) * (256 >> q), g.rows, g.splits, q, s_sum,
+            [&](int s, int64_t i) { return g.bias_part[(int64_t)s * g.own_pad + i]; }, [&](int64_t i, double v) { g.dbias[i] = (float)(v * (double)scale); });
+    }
 }
 
 // ---- host side ---------------------------------------------------------------------------------------------
 namespace {
 
 constexpr int kPadRows = 256;                   // operands are laid out to a multiple of what a workgroup keeps at most
-constexpr int kMaxSplits = 64;
+constexpr int kMaxSplits = 512;
 constexpr int64_t kMaxPartRows = 1 << 17;       // rows of partial sums, of all parts together
 
 bool aligned_to(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
@@ -678,20 +734,22 @@ int steps_of(int d) {
     for (int ks : {1, 2, 4, 6, 8, 12}) if (d <= 32 * ks) return ks;
     return 16;
 }
-// Parts that the streamed side is cut into, so that `blocks` workgroups of it fill the card: the shortest schedule over 512 places, a tile of
+// Parts that the streamed side is cut into, so that `blocks` workgroups of it fill the card: of those that make whole rounds of 512 places, the shortest, a tile of
 // extra work for every part.
 int splits_of(int64_t blocks, int64_t tiles, int64_t pad) {
     constexpr int64_t places = 512;
-    int best = 1;
+    const int64_t most = std::max<int64_t>(1, std::min({(int64_t)kMaxSplits, tiles, blocks ? kMaxPartRows / pad : 1}));
+    int64_t best = 1;
     double least = 1e300;
-    for (int s = 1; s <= kMaxSplits && s <= tiles && (s == 1 || s * pad <= kMaxPartRows); ++s) {
+    for (int64_t rounds = 0; rounds <= 8; ++rounds) {
+        const int64_t s = rounds ? std::min(most, std::max<int64_t>(1, places * rounds / std::max<int64_t>(1, blocks))) : 1;
         const double time = (double)((blocks * s + places - 1) / places) * ((double)((tiles + s - 1) / s) + 1.0);
         if (time < 0.97 * least) {
             least = time;
             best = s;
         }
     }
-    return best;
+    return (int)best;
 }
 // Rows of partial sums that a workspace has room for: what any split of as many rows or fewer can need, so that a workspace serves them all.
 int64_t part_rows(int64_t tiles, int64_t pad) { return std::min(kMaxPartRows, std::min<int64_t>(kMaxSplits, tiles) * pad); }
@@ -734,12 +792,13 @@ ClassPlan class_plan(int64_t n, int64_t classes, int32_t d, int32_t dtype) {
     const int64_t x_parts = part_rows(e_tiles, p.x_pad), e_parts = part_rows(x_tiles, p.e_pad);
     p.part = take((size_t)std::max(p.x_pad, x_parts) * sizeof(float2));
     p.at_target = take((size_t)p.x_pad * 4);
-    p.parts = take((size_t)((n + 1023) / 1024) * sizeof(LossPart));
+    p.parts = take((size_t)((n + 1023) / 1024 + 64) * sizeof(LossPart));       // (65,536 threads at most where a row has several)
     p.loss_bytes = at;
     at = shared;
     p.bias_part = take((size_t)std::max(p.e_pad, e_parts) * sizeof(double));
-    p.x_part = p.e_part = at;                                   // one after the other in the same place
-    p.grad_bytes = at + align_up((size_t)std::max(x_parts, e_parts) * p.ks * 128);
+    p.x_part = take((size_t)x_parts * p.ks * 128);
+    p.e_part = take((size_t)e_parts * p.ks * 128);
+    p.grad_bytes = at;
     return p;
 }
 
@@ -804,8 +863,9 @@ ClassSetup launch_setup(const ClassShape& s, const ClassPlan& p, const float* bi
     a.x_pad = p.x_pad;
     a.e_pad = p.e_pad;
     a.ks = p.ks;
-    a.x_blocks = (unsigned)(p.x_pad / (4 * kTileRows));
-    a.e_blocks = (unsigned)(p.e_pad / (4 * kTileRows));
+    const int64_t share = dtype == GSR_F32 ? kTileRows : 64;           // (padded rows are a multiple of both)
+    a.x_blocks = (unsigned)(p.x_pad * (dtype == GSR_F32 ? 1 : p.ks) / share);
+    a.e_blocks = (unsigned)(p.e_pad * (dtype == GSR_F32 ? 1 : p.ks) / share);
     a.row_blocks = (unsigned)((p.x_pad + 1023) / 1024);
     a.bias_blocks = (unsigned)((p.e_pad + 1023) / 1024);
     const dim3 grid(a.x_blocks + a.e_blocks + a.row_blocks + a.bias_blocks);
@@ -814,15 +874,35 @@ ClassSetup launch_setup(const ClassShape& s, const ClassPlan& p, const float* bi
     return a;
 }
 
-template <int KS, typename T, bool BY_CLASS>
-void launch_grad(const ClassGradArgs& g, hipStream_t st) {
+// Threads for a value of a join: four parts each.
+int join_lanes(int splits) {
+    int q = 0;
+    while (q < 4 && splits > 4 << q) ++q;
+    return q;
+}
+template <int KS, typename T>
+void launch_grad(ClassGradArgs by_row, ClassGradArgs by_class, hipStream_t st) {
     constexpr int NP = sizeof(T) == 4 ? 2 : 1, RB = grad_blocks(KS, NP);
-    const dim3 grid((unsigned)((g.rows + 64 * RB - 1) / (64 * RB)), (unsigned)g.splits);
-    hipLaunchKernelGGL((k_class_grad<KS, NP, RB, BY_CLASS, T>), grid, dim3(256), 0, st, g);
-    if (g.splits > 1 && g.out) {
-        const unsigned wgs = (unsigned)std::min<int64_t>((g.rows * g.d + 255) / 256, 1 << 20);
-        hipLaunchKernelGGL((k_class_grad_join<T>), dim3(wgs), dim3(256), 0, st, g, KS * 32);
+    auto blocks = [](const ClassGradArgs& g) { return (unsigned)((g.rows + 64 * RB - 1) / (64 * RB)); };
+    if (by_row.splits) by_row.blocks = blocks(by_row);
+    if (by_class.splits) by_class.blocks = blocks(by_class);
+    const unsigned wgs = by_row.blocks * by_row.splits + by_class.blocks * by_class.splits;
+    if (!wgs) return;
+    hipLaunchKernelGGL((k_class_grad<KS, NP, RB, T>), dim3(wgs), dim3(256), 0, st, by_row, by_class);
+    JoinShape j{};
+    j.width = KS * 32;
+    auto values = [](int64_t count, int q) { return (unsigned)((count + (256 >> q) - 1) / (256 >> q)); };
+    if (by_row.splits > 1) {
+        j.row_q = join_lanes(by_row.splits);
+        j.row_blocks = values(by_row.rows * by_row.d, j.row_q);
     }
+    if (by_class.splits > 1) {
+        j.class_q = join_lanes(by_class.splits);
+        if (by_class.out) j.class_blocks = values(by_class.rows * by_class.d, j.class_q);
+        if (by_class.dbias) j.bias_blocks = values(by_class.rows, j.class_q);
+    }
+    const unsigned joins = j.row_blocks + j.class_blocks + j.bias_blocks;
+    if (joins) hipLaunchKernelGGL((k_class_grad_join<T>), dim3(joins), dim3(256), 0, st, by_row, by_class, j);
 }
 
 }  // namespace
@@ -853,7 +933,9 @@ gsr_status_t gsr_class_loss(const void* x, int64_t ldx, int64_t n, int32_t d, in
     GSR_TRY(class_workspace(p.loss_bytes, workspace, workspace_bytes));
     hipStream_t st = (hipStream_t)stream;
     char* ws = (char*)workspace;
-    const int blocks = n <= 4096 ? (n ? 1 : 0) : (int)((n + 1023) / 1024);
+    int q = 0;                                  // lanes of a row in the join of the splits
+    while (q < 6 && 2 << q <= p.loss_splits && n << (q + 1) <= 65536) ++q;
+    const int blocks = n << q <= 4096 ? (n ? 1 : 0) : (int)((n + (1024 >> q) - 1) / (1024 >> q));
     LossPart* parts = (LossPart*)(ws + p.parts);
     if (n) {
         const ClassSetup a = launch_setup(s, p, bias, nullptr, ws, dtype, st);
@@ -865,7 +947,7 @@ gsr_status_t gsr_class_loss(const void* x, int64_t ldx, int64_t n, int32_t d, in
             if (dtype == GSR_F32) hipLaunchKernelGGL((k_class_loss<KS, 2, R2>), grid, dim3(256), 0, st, g);
             else hipLaunchKernelGGL((k_class_loss<KS, 1, R1>), grid, dim3(256), 0, st, g);
         });
-        hipLaunchKernelGGL(k_class_lse, dim3(blocks), dim3(1024), 0, st, g.part, g.at_target, a.target, n, p.x_pad, p.loss_splits, lse_out, parts, loss_out);
+        hipLaunchKernelGGL(k_class_lse, dim3(blocks), dim3(1024), 0, st, g.part, g.at_target, a.target, n, p.x_pad, p.loss_splits, q, lse_out, parts, loss_out);
     }
     if (blocks != 1) hipLaunchKernelGGL(k_class_loss_sum, dim3(1), dim3(1024), 0, st, parts, blocks, loss_out);
     GSR_HIP_CHECK(hipGetLastError());
@@ -890,54 +972,49 @@ gsr_status_t gsr_class_grad(const void* x, int64_t ldx, int64_t n, int32_t d, in
     char* ws = (char*)workspace;
     ClassSetup a{};
     a = launch_setup(s, p, bias, lse, ws, dtype, st);
-    ClassGradArgs g{};
+    ClassGradArgs g{}, h{};                     // by row, by class
     g.lse = a.lse_out;
     g.bias = a.bias_out;
     g.target = a.target;
     g.counts = a.counts;
     g.count_blocks = (int32_t)a.row_blocks;
-    g.bias_part = (double*)(ws + p.bias_part);
     g.scale = scale;
     g.d = d;
+    h = g;
+    if (dx_out && n) {
+        g.own = a.xf;
+        g.stream = a.ef;
+        g.own_exp = a.x_exp;
+        g.stream_exp = a.e_exp;
+        g.out = dx_out;
+        g.rows = n;
+        g.ld = lddx;
+        g.gs = n * lddx;
+        g.dg = s.x.dg;
+        g.own_pad = p.x_pad;
+        g.part = (float*)(ws + p.x_part);
+        g.tiles = (int32_t)((classes + kTileRows - 1) / kTileRows);
+        g.splits = p.x_splits;
+    }
+    if (dtable_out || dbias_out) {
+        h.own = a.ef;
+        h.stream = a.xf;
+        h.own_exp = a.e_exp;
+        h.stream_exp = a.x_exp;
+        h.out = dtable_out;
+        h.dbias = dbias_out;
+        h.rows = classes;
+        h.ld = lddt;
+        h.dg = d;
+        h.own_pad = p.e_pad;
+        h.part = (float*)(ws + p.e_part);
+        h.bias_part = (double*)(ws + p.bias_part);
+        h.tiles = (int32_t)((n + kTileRows - 1) / kTileRows);
+        h.splits = p.e_splits;
+    }
     by_steps(p.ks, [&](auto k) {
-        constexpr int KS = k.value;
-        if (dx_out && n) {
-            g.own = a.xf;
-            g.stream = a.ef;
-            g.own_exp = a.x_exp;
-            g.stream_exp = a.e_exp;
-            g.out = dx_out;
-            g.rows = n;
-            g.ld = lddx;
-            g.gs = n * lddx;
-            g.dg = s.x.dg;
-            g.own_pad = p.x_pad;
-            g.part = (float*)(ws + p.x_part);
-            g.tiles = (int32_t)((classes + kTileRows - 1) / kTileRows);
-            g.splits = p.x_splits;
-            if (dtype == GSR_F32) launch_grad<KS, float, false>(g, st);
-            else launch_grad<KS, bf16_t, false>(g, st);
-        }
-        if (dtable_out || dbias_out) {
-            g.own = a.ef;
-            g.stream = a.xf;
-            g.own_exp = a.e_exp;
-            g.stream_exp = a.x_exp;
-            g.out = dtable_out;
-            g.rows = classes;
-            g.ld = lddt;
-            g.gs = 0;
-            g.dg = d;
-            g.own_pad = p.e_pad;
-            g.part = (float*)(ws + p.e_part);
-            g.tiles = (int32_t)((n + kTileRows - 1) / kTileRows);
-            g.splits = p.e_splits;
-            if (dtype == GSR_F32) launch_grad<KS, float, true>(g, st);
-            else launch_grad<KS, bf16_t, true>(g, st);
-            if (dbias_out)
-                hipLaunchKernelGGL(k_class_bias_join, dim3((unsigned)((classes + 255) / 256)), dim3(256), 0, st, g.bias_part, p.e_pad, p.e_splits, g.counts,
-                                   g.count_blocks, scale, classes, dbias_out);
-        }
+        if (dtype == GSR_F32) launch_grad<k.value, float>(g, h, st);
+        else launch_grad<k.value, bf16_t>(g, h, st);
     });
     GSR_HIP_CHECK(hipGetLastError());
     return GSR_OK;

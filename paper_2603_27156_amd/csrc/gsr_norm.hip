@@ -899,8 +899,8 @@ NormShape norm_shape(int64_t n, int32_t d, int32_t planes, int32_t groups, int V
     auto lanes_for = [&](int k) { return (((pieces - 1) >> k) + 1) << k; };
     auto fits = [&](int k) { return (V << k) % kBlock == 0 || (V << k) >= s.dg; };
     int least = 1 << 30;
-    for (int k = 3; k <= 6; ++k) if (fits(k)) least = std::min(least, lanes_for(k));
-    for (int k = 3; k <= 6; ++k) if (fits(k) && lanes_for(k) <= least + least / 4) s.lanes_log2 = k;
+    for (int k = 2; k <= 6; ++k) if (fits(k)) least = std::min(least, lanes_for(k));
+    for (int k = 2; k <= 6; ++k) if (fits(k) && lanes_for(k) <= least + least / 4) s.lanes_log2 = k;
     s.group_slabs = lanes_for(s.lanes_log2) >> s.lanes_log2;
     s.slabs = s.group_slabs * planes;
     s.rows = (int32_t)std::min(kMaxRows, std::max(least_rows(s), (n * s.slabs + kChunks - 1) / kChunks));
