@@ -410,8 +410,9 @@ gsr_status_t gsr_group_norm_grad(const void* dy, int64_t lddy, const void* x, in
  *
  * What a backward pass needs of a plane, in 1.06 bytes a value.  Every row's columns are cut into blocks of 64 from the start of each of the c groups
  * of a GROUP_PLANAR plane (of the row, of a ROW_MAJOR one), the last block of a group with what is left.  With A = max(max |x|, 127 * 2^-126) over a
- * block: codes = 127 x / A to the nearest whole number, ties to even, exactly; scales = A / 127 (at most the float of which 127 times is finite).  codes: device, n x d, one byte each, the columns
- * in their order whatever the layout; scales: device, n x (c or 1) * ceil(columns of a group / 64) floats; both contiguous and 4-byte aligned.  A value
+ * block: codes = 127 x / A to the nearest whole number, ties to even, exactly; scales = A / 127 (at most the float of which 127 times is finite).  codes: device,
+ * n * d bytes in the order of the plane without its gaps (ROW_MAJOR row by row, GROUP_PLANAR group by group); scales: device, as many floats for every row of a
+ * group as it has blocks, in the same order; both 4-byte aligned.  A value
  * comes back as code * scale (off by at most A / 254 and two roundings).  A block with an infinity or NaN comes back as NaN.
  * Planes and limits as above; calls only launch kernels and may be captured. */
 gsr_status_t gsr_checkpoint_save(const void* x, int64_t ldx, int64_t n, int32_t d, int32_t c, int32_t layout, int32_t dtype, int8_t* codes_out,

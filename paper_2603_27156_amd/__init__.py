@@ -525,8 +525,9 @@ def _checkpoint(codes, scales, dev: int, n: int, d: int, c: int):
         return 0, 0
     import torch
     assert codes is not None and scales is not None and codes.get_device() == dev and codes.dtype == torch.int8
-    assert codes.shape == (n, d) and codes.is_contiguous()
-    return codes.data_ptr(), _floats(scales, dev, (n, gsr_checkpoint_blocks(d, c)))
+    assert scales.get_device() == dev and scales.dtype == torch.float32 and codes.is_contiguous() and scales.is_contiguous()
+    assert codes.numel() == n * d and scales.numel() == n * gsr_checkpoint_blocks(d, c)
+    return codes.data_ptr(), scales.data_ptr()
 
 
 def _graph_ptr(graph_ptr, dev: int):
@@ -597,8 +598,8 @@ def gsr_checkpoint_blocks(d: int, c: int = 1) -> int:
 
 
 def gsr_checkpoint_save(x, codes_out, scales_out) -> None:
-    """A plane ([n, D], rows may be strided, or [C, n, D/C]; float32 or bfloat16) in 8 bits: codes_out int8 [n, D], scales_out float32
-    [n, gsr_checkpoint_blocks(D, C)]."""
+    """A plane ([n, D], rows may be strided, or [C, n, D/C]; float32 or bfloat16) in 8 bits: codes_out int8, n * D of them, and scales_out float32,
+    n * gsr_checkpoint_blocks(D, C), contiguous and of any shape: they hold [n, D] and [n, blocks], or [C, n, D/C] and [C, n, blocks of a group]."""
     dev = _current_device()
     n, d, c, layout, ldx = _plane(x, dev)
     codes, scales = _checkpoint(codes_out, scales_out, dev, n, d, c)

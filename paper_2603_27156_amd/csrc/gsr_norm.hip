@@ -268,9 +268,11 @@ __device__ __forceinline__ void store_codes(int8_t* p, const int (&q)[V], int sk
     }
 }
 struct Checkpoint {
-    int8_t* codes;                  // [n][d]
-    float* scales;                  // [n][blocks]
-    int32_t blocks, plane_blocks;   // of a row, of a plane's part of it
+    int8_t* codes;                  // [planes][n][dg]
+    float* scales;                  // [planes][n][blocks]
+    int32_t blocks;                 // of a row of a plane
+    __device__ __forceinline__ int8_t* codes_at(const NormShape& s, const LaneColumns& c, int64_t row) const { return codes + (c.plane * s.n + row) * s.dg + c.col; }
+    __device__ __forceinline__ float* scales_at(const NormShape& s, const LaneColumns& c, int64_t row) const { return scales + (c.plane * s.n + row) * blocks; }
 };
 // The codes of a lane's V values; every lane of the wave takes part.
 template <int V, bool TAIL>
@@ -290,9 +292,9 @@ __device__ __forceinline__ void save_piece(const Checkpoint& k, const NormShape&
     int q[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) q[j] = finite ? code_of(x[j], top, inv) : 0;
-    store_codes<V, TAIL>(k.codes + row * s.d + c.column, q, c.skip);
+    store_codes<V, TAIL>(k.codes_at(s, c, row), q, c.skip);
     if (c.own % kBlock == 0)
-        k.scales[row * k.blocks + c.plane * k.plane_blocks + c.own / kBlock] = finite ? fminf(by_127(top), kLargestScale) : __builtin_nanf("");
+        k.scales_at(s, c, row)[c.own / kBlock] = finite ? fminf(by_127(top), kLargestScale) : __builtin_nanf("");
 }
 
 // Where the values of a plane come from: the plane, or its checkpoint.
@@ -313,7 +315,7 @@ struct CodeSource {
     float scale, scale_before;      // scale_before: of the columns before a block's border, in a tail
     int before;
     __device__ __forceinline__ void load(const NormShape& s, const LaneColumns& c, int64_t row) {
-        const int8_t* p = k.codes + row * s.d + c.column;
+        const int8_t* p = k.codes_at(s, c, row);
         if constexpr (V == 1) {
             w[0] = (uint8_t)*p;
         } else {
@@ -322,7 +324,7 @@ struct CodeSource {
 #pragma unroll
             for (int i = 0; i < V / 4; ++i) w[i] = t[i];
         }
-        const float* scales = k.scales + row * k.blocks + c.plane * k.plane_blocks;
+        const float* scales = k.scales_at(s, c, row);
         scale = scales[(c.col + V - 1) / kBlock];
         if constexpr (TAIL) {
             scale_before = scales[c.col / kBlock];
@@ -927,13 +929,12 @@ gsr_status_t row_plane(const char* name, const void* at, int64_t n, int32_t dg, 
     p->gs = n * ld;
     return GSR_OK;
 }
-gsr_status_t checkpoint_of(int64_t n, int32_t dg, int32_t planes, const int8_t* codes, const float* scales, Checkpoint* k) {
+gsr_status_t checkpoint_of(int64_t n, int32_t dg, const int8_t* codes, const float* scales, Checkpoint* k) {
     if (n > 0 && (!codes || !scales)) return fail(GSR_ERR_INVALID_ARG, "null codes or scales");
     if (!aligned_to(codes, 4) || !aligned_to(scales, 4)) return fail(GSR_ERR_INVALID_ARG, "codes or scales not aligned to 4 bytes");
     k->codes = const_cast<int8_t*>(codes);
     k->scales = const_cast<float*>(scales);
-    k->plane_blocks = (dg + kBlock - 1) / kBlock;
-    k->blocks = k->plane_blocks * planes;
+    k->blocks = (dg + kBlock - 1) / kBlock;
     return GSR_OK;
 }
 gsr_status_t graph_rows(const void* graph_ptr, int32_t ptr_i64, int64_t graphs, int64_t n, GraphRows* g) {
@@ -1057,7 +1058,7 @@ gsr_status_t gsr_group_norm(const void* x, int64_t ldx, int64_t n, int32_t d, in
     if (!(eps > 0.0f) || std::isinf(eps)) return fail(GSR_ERR_INVALID_ARG, "eps=%g is not a positive number", (double)eps);
     if (x == y_out && ldx != ldy) return fail(GSR_ERR_INVALID_ARG, "in place, but with row strides of %lld and %lld", (long long)ldx, (long long)ldy);
     const bool save = codes_out || scales_out;
-    if (save) GSR_TRY(checkpoint_of(n, dg, planes, codes_out, scales_out, &ck));
+    if (save) GSR_TRY(checkpoint_of(n, dg, codes_out, scales_out, &ck));
     const PieceRule rule = piece_of(dg, groups, d / groups, dtype, x == y_out);
     const int V = rule.v;
     const NormShape s = norm_shape(n, d, planes, groups, V);
@@ -1110,7 +1111,7 @@ gsr_status_t gsr_group_norm_grad(const void* dy, int64_t lddy, const void* x, in
     const bool coded = codes || scales;
     if (coded && x) return fail(GSR_ERR_INVALID_ARG, "x and its checkpoint");
     GSR_TRY(row_plane("dy", dy, n, dg, lddy, dtype, &pd));
-    if (coded) GSR_TRY(checkpoint_of(n, dg, planes, codes, scales, &ck));
+    if (coded) GSR_TRY(checkpoint_of(n, dg, codes, scales, &ck));
     else GSR_TRY(row_plane("x", x, n, dg, ldx, dtype, &px));
     GSR_TRY(row_plane("dx_out", dx_out, n, dg, lddx, dtype, &po));
     GSR_TRY(graph_rows(graph_ptr, ptr_i64, graphs, n, &g));
@@ -1167,7 +1168,7 @@ gsr_status_t gsr_checkpoint_save(const void* x, int64_t ldx, int64_t n, int32_t 
     RowPlane p;
     Checkpoint ck;
     GSR_TRY(row_plane("x", x, n, dg, ldx, dtype, &p));
-    GSR_TRY(checkpoint_of(n, dg, planes, codes_out, scales_out, &ck));
+    GSR_TRY(checkpoint_of(n, dg, codes_out, scales_out, &ck));
     if (n == 0) return GSR_OK;
     const PieceRule rule = piece_of(dg, 1, dg, dtype, false);
     const NormShape s = apply_shape(norm_shape(n, d, planes, 1, rule.v), nullptr);
@@ -1186,7 +1187,7 @@ gsr_status_t gsr_checkpoint_load(const int8_t* codes, const float* scales, int64
     RowPlane p;
     Checkpoint ck;
     GSR_TRY(row_plane("x_out", x_out, n, dg, ldx, dtype, &p));
-    GSR_TRY(checkpoint_of(n, dg, planes, codes, scales, &ck));
+    GSR_TRY(checkpoint_of(n, dg, codes, scales, &ck));
     if (n == 0) return GSR_OK;
     const PieceRule rule = piece_of(dg, 1, dg, dtype, false);
     const NormShape s = apply_shape(norm_shape(n, d, planes, 1, rule.v), nullptr);

@@ -337,7 +337,7 @@ LARGEST = np.nextafter(np.finfo(np.float32).max / np.float32(127.0), np.float32(
 
 
 def codes_ref(x, c):
-    """codes [n, d] and scales of rows x (float32 or wider values) in max(c, 1) groups: exact products in 64 bits."""
+    """codes and scales of rows x (float32 or wider values) in max(c, 1) groups, group by group: exact products in 64 bits."""
     n, d = x.shape
     dg = d // max(c, 1)
     codes, scales = np.zeros((n, d), dtype=np.int8), []
@@ -351,7 +351,16 @@ def codes_ref(x, c):
             codes[:, lo:hi] = np.rint(127.0 * part / top[:, None]).astype(np.int8)       # 127 x is exact, the quotient rounded to 53 bits
             scale = np.minimum(top.astype(np.float32) / np.float32(127.0), LARGEST)
             scales.append(np.where(fine, scale, np.float32(np.nan)))
-    return codes, np.stack(scales, 1) if scales else np.zeros((n, 0), np.float32)
+    by_group = lambda v: np.ascontiguousarray(v.reshape(n, max(c, 1), v.shape[1] // max(c, 1)).transpose(1, 0, 2))         # noqa: E731
+    return by_group(codes), by_group(np.stack(scales, 1))
+
+
+def decoded(codes, scales, c):
+    """The rows [n, d] that codes and scales in the order of a plane of max(c, 1) groups stand for, in float32."""
+    (n, d), c = codes.shape, max(c, 1)
+    q, s = codes.view(c, n, d // c), scales.view(c, n, scales.shape[1] // c)
+    blocks = torch.arange(q.shape[2], device=dev()) // 64
+    return (q.float() * s[:, :, blocks]).permute(1, 0, 2).reshape(n, d)
 
 
 def save(x, n, d, c):
@@ -372,12 +381,10 @@ def test_checkpoint(n, d, c, dtype, pad, offset):
     _, x = plane(n, d, c, dtype, torch.from_numpy(values), pad, offset)
     codes, scales = save(x, n, d, c)
     want, want_scales = codes_ref(rows_of(x).float().cpu().numpy(), c)
-    assert np.array_equal(codes.cpu().numpy(), want) and np.array_equal(scales.cpu().numpy(), want_scales)
+    assert np.array_equal(codes.cpu().numpy().ravel(), want.ravel()) and np.array_equal(scales.cpu().numpy().ravel(), want_scales.ravel())
     buffer, back = plane(n, d, c, dtype, None, pad, offset)
     gsr.gsr_checkpoint_load(codes, scales, back)
-    dg = d // max(c, 1)
-    blocks = (torch.arange(d) // dg * -(-dg // 64) + torch.arange(d) % dg // 64).to(dev())
-    assert torch.equal(rows_of(back), (codes.float() * scales[:, blocks]).to(dtype)) and untouched(buffer, back)
+    assert torch.equal(rows_of(back), decoded(codes, scales, c).to(dtype)) and untouched(buffer, back)
 
 
 def test_checkpoint_at_the_borders_between_codes():
@@ -391,8 +398,8 @@ def test_checkpoint_at_the_borders_between_codes():
     x = np.array(rows, dtype=np.float32)
     codes, scales = save(put(x), *x.shape, 0)
     want, want_scales = codes_ref(x, 0)
-    assert np.array_equal(codes.cpu().numpy(), want) and np.array_equal(scales.cpu().numpy(), want_scales)
-    assert np.all(want[:, 1] == 64)
+    assert np.array_equal(codes.cpu().numpy(), want[0]) and np.array_equal(scales.cpu().numpy(), want_scales[0])
+    assert np.all(want[0, :, 1] == 64)
 
 
 def test_checkpoint_of_extreme_values():
@@ -407,7 +414,7 @@ def test_checkpoint_of_extreme_values():
     x[7] = torch.linspace(-1e30, 1e-30, 128)
     codes, scales = save(x, 8, 128, 0)
     want, want_scales = codes_ref(x.cpu().numpy(), 0)
-    assert np.array_equal(codes.cpu().numpy(), want) and np.array_equal(scales.cpu().numpy(), want_scales, equal_nan=True)
+    assert np.array_equal(codes.cpu().numpy(), want[0]) and np.array_equal(scales.cpu().numpy(), want_scales[0], equal_nan=True)
     back = torch.empty_like(x)
     gsr.gsr_checkpoint_load(codes, scales, back)
     assert bool(back[4, :64].isnan().all()) and bool((back[4, 64:] - 1.0).abs().max() <= 2.0 ** -23) and bool(back[5, 64:].isnan().all())
@@ -430,18 +437,14 @@ def test_norm_writes_the_checkpoint_and_its_gradient_reads_it(n, d, c, groups, d
     assert torch.equal(y, y8) and torch.equal(mean, mean8) and torch.equal(rstd, rstd8)
     whole_codes, whole_scales = save(px, n, d, c)
     a, b = int(ptr[0]), int(ptr[-1])
-    assert torch.equal(codes[a:b], whole_codes[a:b]) and torch.equal(scales[a:b], whole_scales[a:b])
-    for part in (codes[:a], codes[b:]):
-        assert bool((part == 77).all())
-    for part in (scales[:a], scales[b:]):
-        assert bool((part == GUARD).all())
+    by_rows = lambda v: v.view(max(c, 1), n, -1)                                                       # noqa: E731
+    for got, whole, guard in ((by_rows(codes), by_rows(whole_codes), 77), (by_rows(scales), by_rows(whole_scales), GUARD)):
+        assert torch.equal(got[:, a:b], whole[:, a:b]) and bool((got[:, :a] == guard).all()) and bool((got[:, b:] == guard).all())
     # the gradient from the codes is that of the values they stand for
     _, dy = plane(n, d, c, dtype, torch.from_numpy(rng.standard_normal((n, d))))
     dx, dgamma, dbeta = torch.full_like(px, GUARD), torch.empty(d, device=dev()), torch.empty(d, device=dev())
     gsr.gsr_group_norm_grad(dy, mean, rstd, dx, codes=codes, scales=scales, dgamma_out=dgamma, dbeta_out=dbeta, **args)
-    dg = d // max(c, 1)
-    blocks = (torch.arange(d) // dg * -(-dg // 64) + torch.arange(d) % dg // 64).to(dev())
-    stands_for = (whole_codes.float() * whole_scales[:, blocks]).double().cpu().numpy()
+    stands_for = decoded(whole_codes, whole_scales, c).double().cpu().numpy()
     ref = Reference(stands_for, ptr, groups, gamma, beta, "silu", mean.double().cpu().numpy(), rstd.double().cpu().numpy())
     want, off = ref.backward(host(dy))
     close(host(dx), want["dx"], off["dx"], dtype)
