@@ -528,24 +528,33 @@ __global__ __launch_bounds__(1024) void k_norm_small(NormShape s, GraphRows g, c
 }
 
 // ---- backward --------------------------------------------------------------------------------------------
-// dz = dy act'(z) for a lane's columns in a graph.  Which side of zero z lies on is decided in 64 bits (z = a x + b; 500k x 256 16-bit values: 113 -> 105 us for
-// the sums, 94 without an activation): in 32 one value in ten million falls on the other one.
+// dz = dy act'(z) for a lane's columns in a graph.  Which side of zero z = a x + b lies on is decided as in 64 bits (in 32 one value in ten million falls on the other
+// one): with x' = sign(a) x it is above where x' > -b / |a|, and so where x' is above the largest float that is not above -b / |a|, one comparison.
+// 500k x 256 16-bit values, sums and gradient: 110 and 133 us with it, 117 and 146 with z in 64 bits, 92 and 127 without an activation.
+__device__ __forceinline__ float float_below(double v) {               // the largest that is not above
+    const float f = (float)v;
+    if (!((double)f > v)) return f;
+    const uint32_t u = __float_as_uint(f);
+    return __uint_as_float(f > 0.0f ? u - 1 : f < 0.0f ? u + 1 : 0x80000001u);
+}
 template <int V, int ACT>
 struct BeforeActivation {
-    double a[ACT == GSR_ACT_RELU ? V : 1], b[ACT == GSR_ACT_RELU ? V : 1];
+    float edge[ACT == GSR_ACT_RELU ? V : 1];
+    uint32_t sign[ACT == GSR_ACT_RELU ? V : 1];
     __device__ __forceinline__ BeforeActivation(float m, float rs, const float (&gamma)[V], const float (&beta)[V]) {
         if constexpr (ACT == GSR_ACT_RELU) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                a[j] = (double)rs * (double)gamma[j];
-                b[j] = fma(-(double)m, a[j], (double)beta[j]);
+                const double a = (double)rs * (double)gamma[j], b = fma(-(double)m, a, (double)beta[j]);
+                sign[j] = a < 0.0 ? 0x80000000u : 0u;
+                edge[j] = a == 0.0 ? (b > 0.0 ? -INFINITY : INFINITY) : float_below(-b / fabs(a));
             }
         }
     }
+    // (a NaN comes to 0 here and is one again when it meets xh)
     __device__ __forceinline__ float operator()(int j, float dy, float x, float xh, const float (&gamma)[V], const float (&beta)[V]) const {
         if constexpr (ACT == GSR_ACT_RELU) {
-            const double z = fma((double)x, a[j], b[j]);
-            return z > 0.0 ? dy : z <= 0.0 ? 0.0f : (float)z;               // (NaN stays NaN)
+            return __uint_as_float(__float_as_uint(x) ^ sign[j]) > edge[j] ? dy : 0.0f;
         } else if constexpr (ACT == GSR_ACT_SILU) {
             const float z = xh * gamma[j] + beta[j], l = logistic(z);
             return dy * (l * (1.0f + z * (1.0f - l)));
@@ -873,9 +882,10 @@ constexpr int64_t kMaxPieces = (int64_t)1 << 31;
 
 bool aligned_to(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 
-// Rows of a wave: as many as make kChunks waves of all slabs together; eight pieces of every lane at least, and at most kMaxRows.
+// Rows of a wave: as many as make kChunks waves of all slabs together; at most kMaxRows, and eight pieces of every lane at least, two where a wave would meet many
+// graphs, which take their turns.
 constexpr int64_t kChunks = 4096, kMaxRows = 1024;
-int64_t least_rows(const NormShape& s) { return 8 * (64 >> s.lanes_log2); }
+int64_t least_rows(const NormShape& s, int64_t graphs) { return (graphs > 1 ? 2 : 8) * (64 >> s.lanes_log2); }
 
 // Pieces of 16 bytes of the plane's type where every lane's columns lie in one group; else single columns.  With a tail the last piece overlaps the one
 // before it, whose lane may have stored already where a pass works in place.
@@ -889,7 +899,7 @@ PieceRule piece_of(int32_t dg, int32_t groups, int32_t cg, int32_t dtype, bool i
     if (groups == 1 && dg > v && !in_place) return {v, dg % v != 0};
     return {1, false};
 }
-NormShape norm_shape(int64_t n, int32_t d, int32_t planes, int32_t groups, int V) {
+NormShape norm_shape(int64_t n, int64_t graphs, int32_t d, int32_t planes, int32_t groups, int V) {
     NormShape s{};
     s.n = n;
     s.d = d;
@@ -905,7 +915,7 @@ NormShape norm_shape(int64_t n, int32_t d, int32_t planes, int32_t groups, int V
     for (int k = 2; k <= 6; ++k) if (fits(k) && lanes_for(k) <= least + least / 4) s.lanes_log2 = k;
     s.group_slabs = lanes_for(s.lanes_log2) >> s.lanes_log2;
     s.slabs = s.group_slabs * planes;
-    s.rows = (int32_t)std::min(kMaxRows, std::max(least_rows(s), (n * s.slabs + kChunks - 1) / kChunks));
+    s.rows = (int32_t)std::min(kMaxRows, std::max(least_rows(s, graphs), (n * s.slabs + kChunks - 1) / kChunks));
     s.chunks = (n + s.rows - 1) / s.rows;
     return s;
 }
@@ -965,7 +975,7 @@ NormWs carve_norm(const NormShape& s, int64_t graphs) {
     NormWs w{};
     w.pieces = 0;
     // at least as many chunks as any number of rows up to n has, so that a workspace serves them all
-    const int64_t chunks = std::max((s.n + kMaxRows - 1) / kMaxRows, std::min((s.n + least_rows(s) - 1) / least_rows(s), kChunks / s.slabs + 1));
+    const int64_t chunks = std::max((s.n + kMaxRows - 1) / kMaxRows, std::min((s.n + least_rows(s, graphs) - 1) / least_rows(s, graphs), kChunks / s.slabs + 1));
     w.shifts = align_up((size_t)(chunks + graphs) * s.stride() * sizeof(double2));
     w.means = w.shifts + align_up((size_t)s.groups * sizeof(double));
     w.columns = w.means + align_up((size_t)graphs * s.groups * sizeof(float2));
@@ -986,8 +996,11 @@ gsr_status_t workspace_of(const NormWs& w, const NormShape& s, int64_t graphs, v
 // A pass that leaves no sums takes eight pieces of every lane a wave, so that the waves at work lie close together in memory, and with offsets to
 // look up 16.  1M x 256 floats with 2,048 waves of a plane / 8 / 16 pieces: forward with a checkpoint 517 / 391 / 403 us, gradient from it 527 / 399 / 419,
 // save 336 / 297 / 313; 500k x 256 16-bit values in 301 graphs, gradient: 143 / 154 / 144.
+// Fewer where that would make less than 2,048 waves (and fewer rows for the waves that leave sums): 524 rows of 381 floats, each its own graph, gradient
+// 59 -> 24 us; 3,960 rows of 96 in 635 graphs, forward 57 -> 29.
 NormShape apply_shape(NormShape s, const void* graph_ptr) {
-    s.rows = (graph_ptr ? 16 : 8) * (64 >> s.lanes_log2);
+    const int64_t subs = 64 >> s.lanes_log2, most = graph_ptr ? 16 : 8, least = graph_ptr ? 1 : 4, even = s.n * s.slabs / (2048 * subs);
+    s.rows = (int32_t)(std::min(most, std::max(least, even)) * subs);
     s.chunks = (s.n + s.rows - 1) / s.rows;
     return s;
 }
@@ -1038,7 +1051,7 @@ size_t gsr_group_norm_workspace(int64_t n, int64_t graphs, int32_t d, int32_t c,
     // in place, single columns may take the place of pieces
     size_t bytes = 0;
     for (bool in_place : {false, true})
-        bytes = std::max(bytes, carve_norm(norm_shape(n, d, planes, groups, piece_of(d / planes, groups, d / groups, dtype, in_place).v), graphs).total);
+        bytes = std::max(bytes, carve_norm(norm_shape(n, graphs, d, planes, groups, piece_of(d / planes, groups, d / groups, dtype, in_place).v), graphs).total);
     return bytes;
 }
 
@@ -1061,7 +1074,7 @@ gsr_status_t gsr_group_norm(const void* x, int64_t ldx, int64_t n, int32_t d, in
     if (save) GSR_TRY(checkpoint_of(n, dg, codes_out, scales_out, &ck));
     const PieceRule rule = piece_of(dg, groups, d / groups, dtype, x == y_out);
     const int V = rule.v;
-    const NormShape s = norm_shape(n, d, planes, groups, V);
+    const NormShape s = norm_shape(n, graphs, d, planes, groups, V);
     const NormWs ws = carve_norm(s, graphs);
     GSR_TRY(workspace_of(ws, s, graphs, workspace, workspace_bytes));
     if (graphs == 0) return GSR_OK;
@@ -1120,7 +1133,7 @@ gsr_status_t gsr_group_norm_grad(const void* dy, int64_t lddy, const void* x, in
     if (dy == dx_out && lddy != lddx) return fail(GSR_ERR_INVALID_ARG, "in place, but with row strides of %lld and %lld", (long long)lddy, (long long)lddx);
     const PieceRule rule = piece_of(dg, groups, d / groups, dtype, dy == dx_out);
     const int V = rule.v;
-    const NormShape s = norm_shape(n, d, planes, groups, V);
+    const NormShape s = norm_shape(n, graphs, d, planes, groups, V);
     const NormWs ws = carve_norm(s, graphs);
     GSR_TRY(workspace_of(ws, s, graphs, workspace, workspace_bytes));
     hipStream_t st = (hipStream_t)stream;
@@ -1171,7 +1184,7 @@ gsr_status_t gsr_checkpoint_save(const void* x, int64_t ldx, int64_t n, int32_t 
     GSR_TRY(checkpoint_of(n, dg, codes_out, scales_out, &ck));
     if (n == 0) return GSR_OK;
     const PieceRule rule = piece_of(dg, 1, dg, dtype, false);
-    const NormShape s = apply_shape(norm_shape(n, d, planes, 1, rule.v), nullptr);
+    const NormShape s = apply_shape(norm_shape(n, 1, d, planes, 1, rule.v), nullptr);
     by_piece(dtype, rule, [&](auto t, auto v, auto tail) {
         using T = decltype(t);
         hipLaunchKernelGGL((k_checkpoint_save<T, v.value, tail.value>), rows_grid(s), dim3(256), 0, (hipStream_t)stream, s, (const T*)x, p, ck);
@@ -1190,7 +1203,7 @@ gsr_status_t gsr_checkpoint_load(const int8_t* codes, const float* scales, int64
     GSR_TRY(checkpoint_of(n, dg, codes, scales, &ck));
     if (n == 0) return GSR_OK;
     const PieceRule rule = piece_of(dg, 1, dg, dtype, false);
-    const NormShape s = apply_shape(norm_shape(n, d, planes, 1, rule.v), nullptr);
+    const NormShape s = apply_shape(norm_shape(n, 1, d, planes, 1, rule.v), nullptr);
     by_piece(dtype, rule, [&](auto t, auto v, auto tail) {
         using T = decltype(t);
         hipLaunchKernelGGL((k_checkpoint_load<T, v.value, tail.value>), rows_grid(s), dim3(256), 0, (hipStream_t)stream, s, ck, (T*)x_out, p);
