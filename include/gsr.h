@@ -425,8 +425,8 @@ gsr_status_t gsr_checkpoint_load(const int8_t* codes, const float* scales, int64
  * A head on the output of a stack for tasks whose targets are classes (the type of a masked cell, say, with the table of the node embeddings):
  *   z_ij = x_i . E_j + b_j,  lse_i = log sum_j exp z_ij,  loss = mean over the rows with a class of lse_i - z_i,t_i  (0 if there are none).
  * x: a plane (device, n x d of `dtype`; ROW_MAJOR with row stride ldx, d at least; GROUP_PLANAR in c groups of d/c columns, row stride ldx, d/c at
- * least, group stride n * ldx).  E: `classes` rows of d values of the same dtype, row stride ldt.  bias: device, `classes` floats (-inf takes a class
- * out), or NULL.  ids: device, n classes, int32, or int64 with ids_i64 = 1; a row whose id lies outside [0, classes), such as -1, has no class: no part
+ * least, group stride n * ldx).  E: `classes` rows of d values of the same dtype, row stride ldt.  bias: device, `classes` floats, or NULL; -inf
+ * takes a class out (the loss of a row of that class is infinite).  ids: device, n classes, int32, or int64 with ids_i64 = 1; a row whose id lies outside [0, classes), such as -1, has no class: no part
  * in the loss or in any gradient, whatever its values, and a dx of 0.  z is never stored: neither call needs memory of the order n * classes.
  *
  * gsr_class_loss: loss_out (device, 1 float), lse_out (device, n floats, every row's).
@@ -436,9 +436,9 @@ gsr_status_t gsr_checkpoint_load(const int8_t* codes, const float* scales, int64
  * sum_i dz_ij (`classes` floats); any but not all of them may be NULL.  Every element is written.
  *
  * float32 values, |v| < 2^64, enter the products as multiples of 2^-22 of themselves or 2^-39 of the largest of 32 rows (aligned ones), dz as those of
- * 2^-22 of itself or 2^-36 of the largest in its sum; sums are taken in float32 (the loss and dbias: in float64 across tiles).  With 16-bit planes
+ * 2^-22 of itself or 2^-36 of the largest in its sum (below 2^-70 it may count as 0); sums are taken in float32 (the loss and dbias: in float64 across tiles).  With 16-bit planes
  * dz is rounded to 16 bits before the products with E and x.  Equal calls give equal bits.  Values must be finite: a row with infinities or NaN gets a
- * loss that is none, which then is the mean's.  1 <= d <= 512, c divides d, n and classes below 2^31 - 256; pointers aligned to their elements.
+ * loss that is none, which then is the mean's.  1 <= d <= 512, c divides d, n and classes below 2^28; pointers aligned to their elements.
  * workspace: device, 16-byte aligned, at least gsr_class_loss_workspace() / gsr_class_grad_workspace() bytes (0: sizes that are refused; never
  * fewer for more rows or classes, so that one serves any fewer), some copies of x and E; it holds nothing between calls.  What a call writes overlaps nothing that it reads.  Calls only launch kernels and may be captured;
  * calls with workspaces of their own may run side by side. */

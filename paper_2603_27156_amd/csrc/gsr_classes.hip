@@ -92,20 +92,27 @@ __device__ __forceinline__ void two_pieces(float v, uint32_t& h, uint32_t& l) {
     h = __builtin_bit_cast(uint16_t, top);
     l = f16_bits(v - static_cast<float>(top));
 }
-// 16-bit rows: four pieces by a workgroup
+// 16-bit rows: 16 pieces by a workgroup
+constexpr int kPieces = 16;
 __device__ __forceinline__ void lay_out(const RowSource& s, uint4* __restrict__ out, float*, int64_t pad, int ks, int64_t block, const ClassTokens* known, bf16_t) {
-    const int64_t piece = block * 4 + (threadIdx.x >> 6);
-    if (piece >= pad / 16 * ks) return;
     const int lane = lane_id();
-    const int64_t row = piece / ks * 16 + (lane & 15);
-    float v[8];
-    load_eight<bf16_t>(s, row, row < s.rows && (!known || known->at(row) >= 0), (int)(piece % ks) * 32 + (lane >> 4) * 8, v);
-    uint4 w;
-    w.x = __builtin_amdgcn_perm(__float_as_uint(v[1]), __float_as_uint(v[0]), 0x07060302u);
-    w.y = __builtin_amdgcn_perm(__float_as_uint(v[3]), __float_as_uint(v[2]), 0x07060302u);
-    w.z = __builtin_amdgcn_perm(__float_as_uint(v[5]), __float_as_uint(v[4]), 0x07060302u);
-    w.w = __builtin_amdgcn_perm(__float_as_uint(v[7]), __float_as_uint(v[6]), 0x07060302u);
-    out[piece * 64 + lane] = w;
+    float v[kPieces / 4][8];
+#pragma unroll
+    for (int i = 0; i < kPieces / 4; ++i) {
+        const int64_t piece = block * kPieces + i * 4 + (threadIdx.x >> 6), row = piece / ks * 16 + (lane & 15);
+        load_eight<bf16_t>(s, row, row < s.rows && (!known || known->at(row) >= 0), (int)(piece % ks) * 32 + (lane >> 4) * 8, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kPieces / 4; ++i) {
+        const int64_t piece = block * kPieces + i * 4 + (threadIdx.x >> 6);
+        if (piece >= pad / 16 * ks) return;
+        uint4 w;
+        w.x = __builtin_amdgcn_perm(__float_as_uint(v[i][1]), __float_as_uint(v[i][0]), 0x07060302u);
+        w.y = __builtin_amdgcn_perm(__float_as_uint(v[i][3]), __float_as_uint(v[i][2]), 0x07060302u);
+        w.z = __builtin_amdgcn_perm(__float_as_uint(v[i][5]), __float_as_uint(v[i][4]), 0x07060302u);
+        w.w = __builtin_amdgcn_perm(__float_as_uint(v[i][7]), __float_as_uint(v[i][6]), 0x07060302u);
+        out[piece * 64 + lane] = w;
+    }
 }
 // floats: 32 rows by a workgroup, all of them in its registers
 __device__ __forceinline__ void lay_out(const RowSource& s, uint4* __restrict__ out, float* __restrict__ exponents, int64_t pad, int ks, int64_t tile,
@@ -725,6 +732,7 @@ __global__ __launch_bounds__(256) void k_class_grad_join(ClassGradArgs by_row, C
 namespace {
 
 constexpr int kPadRows = 256;                   // operands are laid out to a multiple of what a workgroup keeps at most
+constexpr int64_t kMaxRows = (int64_t)1 << 28;  // of x and of E: a grid holds fewer than 2^32 threads
 constexpr int kMaxSplits = 512;
 constexpr int64_t kMaxPartRows = 1 << 17;       // rows of partial sums, of all parts together
 
@@ -829,9 +837,9 @@ struct ClassShape {
 gsr_status_t class_shape(const void* x, int64_t ldx, int64_t n, int32_t d, int32_t c, int32_t layout, int32_t dtype, const void* table, int64_t classes,
                          int64_t ldt, const float* bias, const void* ids, int32_t ids_i64, ClassShape* s) {
     if (n < 0) return fail(GSR_ERR_INVALID_ARG, "negative n");
-    if (n >= ((int64_t)1 << 31) - kPadRows) return fail(GSR_ERR_UNSUPPORTED, "n=%lld too large", (long long)n);
+    if (n >= kMaxRows) return fail(GSR_ERR_UNSUPPORTED, "n=%lld at or above 2^28", (long long)n);
     if (classes < 1) return fail(GSR_ERR_INVALID_ARG, "%lld classes", (long long)classes);
-    if (classes >= ((int64_t)1 << 31) - kPadRows) return fail(GSR_ERR_UNSUPPORTED, "%lld classes", (long long)classes);
+    if (classes >= kMaxRows) return fail(GSR_ERR_UNSUPPORTED, "%lld classes, 2^28 or more", (long long)classes);
     if (d < 1 || d > kMaxClassWidth) return fail(GSR_ERR_UNSUPPORTED, "d=%d outside [1, %d]", d, kMaxClassWidth);
     if (c < 1 || d % c) return fail(GSR_ERR_UNSUPPORTED, "c=%d does not divide d=%d", c, d);
     if (layout != GSR_LAYOUT_ROW_MAJOR && layout != GSR_LAYOUT_GROUP_PLANAR) return fail(GSR_ERR_INVALID_ARG, "layout %d", layout);
@@ -870,9 +878,9 @@ ClassSetup launch_setup(const ClassShape& s, const ClassPlan& p, const float* bi
     a.x_pad = p.x_pad;
     a.e_pad = p.e_pad;
     a.ks = p.ks;
-    const int64_t share = dtype == GSR_F32 ? kTileRows : 64;           // (padded rows are a multiple of both)
-    a.x_blocks = (unsigned)(p.x_pad * (dtype == GSR_F32 ? 1 : p.ks) / share);
-    a.e_blocks = (unsigned)(p.e_pad * (dtype == GSR_F32 ? 1 : p.ks) / share);
+    auto share = [&](int64_t pad) { return (unsigned)(dtype == GSR_F32 ? pad / kTileRows : pad / 16 * p.ks / kPieces); };        // (rows are padded to 256)
+    a.x_blocks = share(p.x_pad);
+    a.e_blocks = share(p.e_pad);
     a.row_blocks = (unsigned)((p.x_pad + 1023) / 1024);
     a.bias_blocks = (unsigned)((p.e_pad + 1023) / 1024);
     const dim3 grid(a.x_blocks + a.e_blocks + a.row_blocks + a.bias_blocks);
@@ -920,7 +928,7 @@ using namespace gsr;
 extern "C" {
 
 size_t gsr_class_loss_workspace(int64_t n, int64_t classes, int32_t d, int32_t dtype) {
-    if (n < 0 || n >= ((int64_t)1 << 31) - kPadRows || classes < 1 || classes >= ((int64_t)1 << 31) - kPadRows || d < 1 || d > kMaxClassWidth ||
+    if (n < 0 || n >= kMaxRows || classes < 1 || classes >= kMaxRows || d < 1 || d > kMaxClassWidth ||
         (dtype != GSR_F32 && dtype != GSR_BF16))
         return 0;
     return class_plan(n, classes, d, dtype).loss_bytes;

@@ -164,7 +164,8 @@ __device__ __forceinline__ double wave_total(double v) {
     for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
     return v;
 }
-// (graph, group) of this wave (WIDE: of this workgroup of 1,024) and the sums of its pieces, in every lane of (the first) wave; false: no task
+// (graph, group) of this wave (WIDE: of this workgroup of 1,024) and the sums of its pieces, in every lane of (the first) wave; false: no task, or not the wave
+// that has the sums
 template <bool WIDE>
 __device__ __forceinline__ bool joined(const NormShape& s, const GraphRows& g, int V, int64_t block, const double2* __restrict__ pieces,
                                        int64_t& task, double& u, double& v, int64_t& rows) {
@@ -175,6 +176,7 @@ __device__ __forceinline__ bool joined(const NormShape& s, const GraphRows& g, i
     v = wave_total(v);
     if constexpr (WIDE) {
         __shared__ double s_sum[16][2];
+        __syncthreads();                        // the task before has read its sums
         if (lane_id() == 0) {
             s_sum[threadIdx.x >> 6][0] = u;
             s_sum[threadIdx.x >> 6][1] = v;
@@ -388,16 +390,17 @@ __device__ __forceinline__ void statistics(double u, double v, double count, dou
 }
 template <bool WIDE>
 __global__ __launch_bounds__(1024) void k_norm_join(NormShape s, GraphRows g, int V, const double2* __restrict__ pieces,
-                                                    const double* __restrict__ shifts, double eps,
-                                                   float* __restrict__ mean, float* __restrict__ rstd) {
-    int64_t task, rows;
-    double u, v;
-    if (!joined<WIDE>(s, g, V, blockIdx.x, pieces, task, u, v, rows)) return;
-    if (lane_id()) return;
-    float m, r;
-    statistics(u, v, (double)rows * s.cg, rows ? shifts[task % s.groups] : 0.0, eps, m, r);
-    mean[task] = m;
-    rstd[task] = r;
+                                                    const double* __restrict__ shifts, int64_t task_blocks, double eps,
+                                                    float* __restrict__ mean, float* __restrict__ rstd) {
+    for (int64_t block = blockIdx.x; block < task_blocks; block += gridDim.x) {
+        int64_t task, rows;
+        double u, v;
+        if (!joined<WIDE>(s, g, V, block, pieces, task, u, v, rows) || lane_id()) continue;
+        float m, r;
+        statistics(u, v, (double)rows * s.cg, rows ? shifts[task % s.groups] : 0.0, eps, m, r);
+        mean[task] = m;
+        rstd[task] = r;
+    }
 }
 
 __device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
@@ -645,22 +648,24 @@ __global__ __launch_bounds__(256) void k_norm_grad_sums(NormShape s, GraphRows g
     }
 }
 
-// The first `task_blocks` workgroups join the pieces: means of h and of h xh of every (graph, group).  The others add up 16 columns of
+// The first `task_wgs` workgroups join the pieces: means of h and of h xh of every (graph, group).  The others add up 16 columns of
 // dgamma and dbeta each, with 64 threads a column.
 template <bool WIDE>
 __global__ __launch_bounds__(1024) void k_norm_grad_join(NormShape s, GraphRows g, int V, const double2* __restrict__ pieces, int64_t task_blocks,
-                                                        float2* __restrict__ means, const float* __restrict__ columns, int64_t parts,
+                                                        int64_t task_wgs, float2* __restrict__ means, const float* __restrict__ columns, int64_t parts,
                                                         float* __restrict__ dgamma, float* __restrict__ dbeta) {
-    if ((int64_t)blockIdx.x < task_blocks) {
-        int64_t task, rows;
-        double u, v;
-        if (!joined<WIDE>(s, g, V, blockIdx.x, pieces, task, u, v, rows) || lane_id()) return;
-        const double count = (double)rows * s.cg;
-        means[task] = rows ? make_float2((float)(u / count), (float)(v / count)) : make_float2(0.0f, 0.0f);
+    if ((int64_t)blockIdx.x < task_wgs) {
+        for (int64_t block = blockIdx.x; block < task_blocks; block += task_wgs) {
+            int64_t task, rows;
+            double u, v;
+            if (!joined<WIDE>(s, g, V, block, pieces, task, u, v, rows) || lane_id()) continue;
+            const double count = (double)rows * s.cg;
+            means[task] = rows ? make_float2((float)(u / count), (float)(v / count)) : make_float2(0.0f, 0.0f);
+        }
         return;
     }
     __shared__ double s_part[64][16];
-    const int64_t block = blockIdx.x - task_blocks;
+    const int64_t block = blockIdx.x - task_wgs;
     const int col = (int)(block * 16 + (threadIdx.x & 15)), k = threadIdx.x >> 4;       // of 2 d: dgamma's columns, then dbeta's
     double sum = 0.0;
     if (col < 2 * s.d) {
@@ -969,7 +974,7 @@ gsr_status_t norm_args(int32_t d, int32_t groups, int32_t act, const float* gamm
 struct NormWs {
     size_t pieces, shifts, means, columns, total;
     bool wide;
-    int64_t task_blocks;
+    int64_t task_blocks, task_wgs;
 };
 NormWs carve_norm(const NormShape& s, int64_t graphs) {
     NormWs w{};
@@ -983,6 +988,7 @@ NormWs carve_norm(const NormShape& s, int64_t graphs) {
     w.wide = s.chunks > 64 * graphs;
     const int64_t tasks = graphs * s.groups;
     w.task_blocks = w.wide ? tasks : (tasks + 15) / 16;
+    w.task_wgs = std::min<int64_t>(w.task_blocks, 1 << 20);
     return w;
 }
 gsr_status_t workspace_of(const NormWs& w, const NormShape& s, int64_t graphs, void* workspace, size_t bytes) {
@@ -1000,7 +1006,7 @@ gsr_status_t workspace_of(const NormWs& w, const NormShape& s, int64_t graphs, v
 // 59 -> 24 us; 3,960 rows of 96 in 635 graphs, forward 57 -> 29.
 NormShape apply_shape(NormShape s, const void* graph_ptr) {
     const int64_t subs = 64 >> s.lanes_log2, most = graph_ptr ? 16 : 8, least = graph_ptr ? 1 : 4, even = s.n * s.slabs / (2048 * subs);
-    s.rows = (int32_t)(std::min(most, std::max(least, even)) * subs);
+    s.rows = (int32_t)(std::max(std::min(most, std::max(least, even)), (s.n >> 25) / subs + 1) * subs);            // (a grid holds fewer than 2^32 threads)
     s.chunks = (s.n + s.rows - 1) / s.rows;
     return s;
 }
@@ -1097,8 +1103,8 @@ gsr_status_t gsr_group_norm(const void* x, int64_t ldx, int64_t n, int32_t d, in
             return;
         }
         if (n) hipLaunchKernelGGL((k_norm_sums<T, P, tail.value>), rows_grid(s), dim3(256), 0, st, s, g, (const T*)x, px, pieces, shifts);
-        if (ws.wide) hipLaunchKernelGGL((k_norm_join<true>), dim3((unsigned)ws.task_blocks), dim3(1024), 0, st, s, g, V, pieces, shifts, (double)eps, mean_out, rstd_out);
-        else hipLaunchKernelGGL((k_norm_join<false>), dim3((unsigned)ws.task_blocks), dim3(1024), 0, st, s, g, V, pieces, shifts, (double)eps, mean_out, rstd_out);
+        if (ws.wide) hipLaunchKernelGGL((k_norm_join<true>), dim3((unsigned)ws.task_wgs), dim3(1024), 0, st, s, g, V, pieces, shifts, ws.task_blocks, (double)eps, mean_out, rstd_out);
+        else hipLaunchKernelGGL((k_norm_join<false>), dim3((unsigned)ws.task_wgs), dim3(1024), 0, st, s, g, V, pieces, shifts, ws.task_blocks, (double)eps, mean_out, rstd_out);
         if (!n) return;
         const Affine f{gamma, beta, mean_out, rstd_out};
         const NormShape q = apply_shape(s, graph_ptr);
@@ -1154,12 +1160,12 @@ gsr_status_t gsr_group_norm_grad(const void* dy, int64_t lddy, const void* x, in
         }
         if (n) hipLaunchKernelGGL((k_norm_grad_sums<T, P, tail.value, ACT, Source>), rows_grid(s), dim3(256), 0, st, s, g, (const T*)dy, pd, source, f, pieces, columns);
         const int64_t column_blocks = dgamma_out || dbeta_out ? (2 * (int64_t)d + 15) / 16 : 0;
-        const dim3 grid((unsigned)(ws.task_blocks + column_blocks));
+        const dim3 grid((unsigned)(ws.task_wgs + column_blocks));
         const int64_t parts = (s.chunks + 3) / 4;
         if (grid.x && ws.wide)
-            hipLaunchKernelGGL((k_norm_grad_join<true>), grid, dim3(1024), 0, st, s, g, V, pieces, ws.task_blocks, means, columns, parts, dgamma_out, dbeta_out);
+            hipLaunchKernelGGL((k_norm_grad_join<true>), grid, dim3(1024), 0, st, s, g, V, pieces, ws.task_blocks, ws.task_wgs, means, columns, parts, dgamma_out, dbeta_out);
         else if (grid.x)
-            hipLaunchKernelGGL((k_norm_grad_join<false>), grid, dim3(1024), 0, st, s, g, V, pieces, ws.task_blocks, means, columns, parts, dgamma_out, dbeta_out);
+            hipLaunchKernelGGL((k_norm_grad_join<false>), grid, dim3(1024), 0, st, s, g, V, pieces, ws.task_blocks, ws.task_wgs, means, columns, parts, dgamma_out, dbeta_out);
         if (n && graphs) hipLaunchKernelGGL((k_norm_grad_apply<T, P, tail.value, ACT, Source>), rows_grid(q), dim3(256), 0, st, q, g, (const T*)dy, pd, source, f, means, (T*)dx_out, po);
     };
     by_piece(dtype, rule, [&](auto t, auto v, auto tail) {

@@ -17,7 +17,7 @@ def grad(x=P, ldx=8, n=4, d=8, c=2, layout=0, dtype=0, table=P, classes=10, ldt=
                                     None)
 
 
-SHARED = [(dict(n=-1), BAD), (dict(n=2 ** 31 - 256), UNSUPPORTED), (dict(classes=0), BAD), (dict(classes=2 ** 31 - 256), UNSUPPORTED), (dict(d=0), UNSUPPORTED),
+SHARED = [(dict(n=-1), BAD), (dict(n=2 ** 28), UNSUPPORTED), (dict(classes=0), BAD), (dict(classes=2 ** 28), UNSUPPORTED), (dict(d=0), UNSUPPORTED),
           (dict(d=513, ldx=513, ldt=513), UNSUPPORTED), (dict(c=0), UNSUPPORTED), (dict(c=3), UNSUPPORTED), (dict(layout=2), BAD), (dict(dtype=2), UNSUPPORTED),
           (dict(ldx=7), BAD), (dict(layout=1, ldx=3), BAD), (dict(ldx=2 ** 31), BAD), (dict(ldt=7), BAD), (dict(ldt=2 ** 31), BAD), (dict(x=None), BAD),
           (dict(table=None), BAD), (dict(ids=None), BAD), (dict(x=P + 2), BAD), (dict(table=P + 1, dtype=1), BAD), (dict(bias=P + 2), BAD), (dict(ids=P + 4, i64=1), BAD),
@@ -41,7 +41,7 @@ def test_workspaces():
         assert 0 < size(0, 1, 1, 0) <= size(2_000, 40, 64, 0)
         # some copies of x and of the table, and nothing of the order n * classes
         assert size(1_000_000, 50_000, 256, 1) < 8 * 1_050_000 * 256 * 4
-        for bad in ((-1, 1, 1, 0), (2 ** 31 - 256, 1, 1, 0), (1, 0, 1, 0), (1, 2 ** 31 - 256, 1, 0), (1, 1, 0, 0), (1, 1, 513, 0), (1, 1, 1, 2)):
+        for bad in ((-1, 1, 1, 0), (2 ** 28, 1, 1, 0), (1, 0, 1, 0), (1, 2 ** 28, 1, 0), (1, 1, 0, 0), (1, 1, 513, 0), (1, 1, 1, 2)):
             assert size(*bad) == 0
     assert loss(nbytes=lib.gsr_class_loss_workspace(4, 10, 8, 0) - 1) == SMALL and grad(nbytes=lib.gsr_class_grad_workspace(4, 10, 8, 0) - 1) == SMALL
 

@@ -216,6 +216,26 @@ def test_large_logits_stay_finite():
         assert bool(dx.isfinite().all()) and abs(loss.item() - ref.loss()[0]) <= ref.loss()[1]
 
 
+def test_a_class_that_is_taken_out():
+    """A bias of -inf: no part in lse, no gradient of its row of the table; a row of that class has an infinite loss and a finite gradient."""
+    x, e, b, ids, _ = inputs(60, 40, 64, 0, F32, torch.int32, "common", 0, 0, True)
+    ids[ids == 7] = 6
+    b[7] = float("-inf")
+    loss, lse = forward(x, e, b, ids, 60)
+    others = torch.arange(40, device=dev()) != 7
+    ids_without = torch.where(ids > 7, ids - 1, ids)
+    loss2, lse2 = forward(x, e[others].contiguous(), b[others].contiguous(), ids_without, 60)
+    assert torch.allclose(lse, lse2, rtol=1e-6, atol=0) and torch.allclose(loss, loss2, rtol=1e-6, atol=0)
+    de, db = torch.empty_like(e), torch.empty_like(b)
+    gsr.gsr_class_grad(x, e, ids, lse, dtable_out=de, bias=b, dbias_out=db)
+    assert not de[7].any() and db[7] == 0 and bool(de.isfinite().all())
+    ids[3] = 7
+    loss, lse = forward(x, e, b, ids, 60)
+    dx = torch.empty_like(x)
+    gsr.gsr_class_grad(x, e, ids, lse, dx_out=dx, dtable_out=de, bias=b, dbias_out=db)
+    assert loss.item() == float("inf") and bool(dx.isfinite().all()) and bool(de.isfinite().all()) and abs(db[7].item() + 1 / 60) <= 1e-7
+
+
 @pytest.mark.parametrize("spread", ["classes", "rows", "columns", "learnt"])
 def test_values_of_very_different_size(spread):
     """Classes of probabilities down to 1e-13, rows and columns of very different size, rows whose class is nearly certain.  Of the first two every row of

@@ -452,6 +452,25 @@ def test_norm_writes_the_checkpoint_and_its_gradient_reads_it(n, d, c, groups, d
     close(dbeta.double().cpu().numpy(), want["dbeta"], off["dbeta"])
 
 
+@pytest.mark.parametrize("n,d,groups,graphs", [(40_000, 16, 16, 30_000), (3_000, 2_048, 2_048, 600)])
+def test_many_graphs_and_groups(n, d, groups, graphs):
+    """More sums than workgroups are launched for, and groups of single columns."""
+    rng = np.random.default_rng(n)
+    x = rng.standard_normal((n, d)).astype(np.float32)
+    ptr = np.sort(np.concatenate([[0, n], rng.integers(0, n + 1, graphs - 1)]))
+    y, (mean, rstd) = torch.empty((n, d), device=dev()), stats(ptr, groups)
+    gsr.gsr_group_norm(put(x), y, mean, rstd, eps=EPS, graph_ptr=put(ptr, torch.int64))
+    graph = np.repeat(np.arange(graphs), np.diff(ptr))
+    sums = lambda v: np.add.reduceat(np.concatenate([v, np.zeros((1, d))]), ptr[:-1], axis=0) * (np.diff(ptr) > 0)[:, None]     # noqa: E731
+    count = np.maximum(np.diff(ptr), 1)[:, None]
+    x = x.astype(np.float64)
+    m = sums(x) / count
+    r = 1.0 / np.sqrt(sums((x - m[graph]) ** 2) / count + EPS)
+    close(mean.double().cpu().numpy(), m, 2 * U * np.abs(m) + 1e-15)
+    close(rstd.double().cpu().numpy(), r, 2 * U * r + 1e-13 * r ** 3)
+    assert torch.equal(y, (put(x) - mean[graph]) * rstd[graph]) or (y - (put(x) - mean[graph]) * rstd[graph]).abs().max() <= 4 * U * 320
+
+
 def test_captured_and_replayed():
     """Both directions and a checkpoint in one graph, replayed on other inputs with eager work between."""
     n, d, groups = 3000, 128, 4
