@@ -36,8 +36,9 @@ struct GraphRows {
 };
 
 // How rows and columns are dealt out.  Columns go to lanes in pieces of V; 2^lanes_log2 lanes hold a slab of a row and the wave 64 >> lanes_log2
-// rows at a time.  A slab never crosses the border of a plane of a GROUP_PLANAR tensor.  Where V does not divide a plane's columns (TAIL) the last
-// piece of a row begins before its own columns, in those of the lane before, which count there alone.
+// rows at a time.  A slab never crosses the border of a plane of a GROUP_PLANAR tensor.  Where V divides a plane's columns and a group's, every lane's columns lie
+// in one group.  Else (TAIL) the last piece of a row begins before its own columns, in those of the lane before, which count there alone, and a lane's
+// columns lie in two groups at most, no group being narrower than V.
 struct NormShape {
     int64_t n, chunks;              // chunks of `rows` rows, one per wave
     int32_t d, dg, cg, groups;
@@ -56,9 +57,10 @@ struct LaneColumns {
     int column;                     // the same in the whole row of d
     int own;                        // first column of its own: col + skip
     int skip;                       // TAIL: columns that are the lane's before
-    int group;                      // the group of all its columns; -1 for a lane without columns
-    bool on, head;                  // head: the first lane of its group in the slab
-    uint32_t joins;                 // bit k: the lane 2^k further holds columns of the same group
+    int group;                      // the group of its first own column; -1 for a lane without columns
+    int begin, split;               // TAIL: loaded columns before `begin` lie in the group before, those from `split` on in the next one (0, V: none do)
+    bool on, head, last;            // head: the first lane of its group in the slab; last: the last one with columns
+    uint32_t joins;                 // bit k: the lane 2^k further holds columns of the same group (begins with one)
 };
 template <int V>
 __device__ __forceinline__ LaneColumns lane_columns(const NormShape& s, int slab) {
@@ -80,6 +82,10 @@ __device__ __forceinline__ LaneColumns lane_columns(const NormShape& s, int slab
     c.column = c.plane * s.dg + c.col;
     c.group = group(li);
     c.head = c.on && group(li - 1) != c.group;
+    c.last = c.on && group(li + 1) < 0;
+    const int from = c.group * s.cg - c.column, to = from + s.cg;
+    c.begin = c.on && from > 0 ? from : 0;
+    c.split = c.on && to < V ? to : V;
     c.joins = 0;
     for (int k = 0; k < s.lanes_log2; ++k) c.joins |= (uint32_t)(c.on && group(li + (1 << k)) == c.group) << k;
     return c;
@@ -125,8 +131,27 @@ __device__ __forceinline__ void join_lanes(const NormShape& s, const LaneColumns
         }
     }
 }
-__device__ __forceinline__ void leave_piece(const NormShape& s, const LaneColumns& c, int slab, int64_t w, int64_t graph, double u, double v,
+// TAIL: u2, v2 are sums of columns in the group after; they go to the next lane, which begins in it, or are a piece of their own in the slab's last
+template <bool TAIL>
+__device__ __forceinline__ void hand_on(const NormShape& s, const LaneColumns& c, double& u, double& v, double& u2, double& v2) {
+    if constexpr (TAIL) {
+        const bool first = (lane_id() & ((1 << s.lanes_log2) - 1)) == 0;
+        const double a = __shfl_up(u2, 1), b = __shfl_up(v2, 1);
+        if (!first && c.on) {
+            u += a;
+            v += b;
+        }
+        for (int o = 1 << s.lanes_log2; o < 64; o <<= 1) {
+            u2 += __shfl_xor(u2, o);
+            v2 += __shfl_xor(v2, o);
+        }
+    }
+}
+template <bool TAIL, int V>
+__device__ __forceinline__ void leave_piece(const NormShape& s, const LaneColumns& c, int slab, int64_t w, int64_t graph, double u, double v, double u2, double v2,
                                             double2* __restrict__ pieces) {
+    hand_on<TAIL>(s, c, u, v, u2, v2);
+    if (TAIL && c.last && c.split < V && c.sub == 0) pieces[(w + graph) * s.stride() + slab + c.group + 1] = make_double2(u2, v2);
     join_lanes(s, c, u, v);
     // chunks and graphs both go up along the rows, slabs and groups along the columns: the sums of two indices name a piece
     if (c.head && c.sub == 0) pieces[(w + graph) * s.stride() + slab + c.group] = make_double2(u, v);
@@ -355,11 +380,16 @@ __global__ __launch_bounds__(256) void k_norm_sums(NormShape s, GraphRows g, con
     if (w >= s.chunks) return;
     const int slab = blockIdx.y;
     const LaneColumns c = lane_columns<V>(s, slab);
-    const double shift = group_shift(s, g, x, p, c.on ? c.group : 0);
-    if (w == 0 && c.head && c.sub == 0 && c.plane * s.dg + c.own == c.group * s.cg) shifts[c.group] = shift;
+    const double shift = group_shift(s, g, x, p, c.on ? c.group : 0), shift2 = TAIL && c.split < V ? group_shift(s, g, x, p, c.group + 1) : shift;
+    // by the lane in whose own columns the group begins
+    if (w == 0 && c.on && c.sub == 0 && c.plane * s.dg + c.own == c.group * s.cg) shifts[c.group] = shift;
+    if (TAIL && w == 0 && c.on && c.sub == 0 && c.split < V) shifts[c.group + 1] = shift2;
     over_graphs(s, g, w, [&](int64_t graph, int64_t a, int64_t b) {
         constexpr int U = 4;
-        double u = 0.0, v = 0.0;
+        constexpr int A = TAIL ? V : 1;             // sums of every column, or of all
+        double u[A], v[A];
+#pragma unroll
+        for (int j = 0; j < A; ++j) u[j] = v[j] = 0.0;
         for (int64_t r = a; r < b; r += U * c.subs) {
             PlaneSource<T, V, false> q[U];
 #pragma unroll
@@ -374,13 +404,22 @@ __global__ __launch_bounds__(256) void k_norm_sums(NormShape s, GraphRows g, con
                 const bool in = r + k * c.subs + c.sub < b;
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const double t = in && !(TAIL && j < c.skip) ? (double)q[k].at(j) - shift : 0.0;
-                    u += t;
-                    v = fma(t, t, v);
+                    const double t = in ? (double)q[k].at(j) - (TAIL && j >= c.split ? shift2 : shift) : 0.0;
+                    u[TAIL ? j : 0] += t;
+                    v[TAIL ? j : 0] = fma(t, t, v[TAIL ? j : 0]);
                 }
             }
         }
-        leave_piece(s, c, slab, w, graph, u, v, pieces);
+        double u1 = 0.0, v1 = 0.0, u2 = 0.0, v2 = 0.0;
+#pragma unroll
+        for (int j = 0; j < A; ++j) {
+            const bool next = TAIL && j >= c.split, none = TAIL && j < c.skip;
+            u1 += next || none ? 0.0 : u[j];
+            v1 += next || none ? 0.0 : v[j];
+            u2 += next ? u[j] : 0.0;
+            v2 += next ? v[j] : 0.0;
+        }
+        leave_piece<TAIL, V>(s, c, slab, w, graph, u1, v1, u2, v2, pieces);
     });
 }
 __device__ __forceinline__ void statistics(double u, double v, double count, double shift, double eps, float& mean, float& rstd) {
@@ -418,6 +457,21 @@ __device__ __forceinline__ void load_affine(const float* __restrict__ p, const L
 struct Affine {
     const float *gamma, *beta, *mean, *rstd;
 };
+// What a lane's columns have by their group: one value, or with TAIL each column one of three (those that are the lane's before it are written again).
+__device__ __forceinline__ float pick(bool which, float a, float b) { return which ? a : b; }         // of values: a conditional on members may become one on addresses
+template <int V, bool TAIL>
+struct ByGroup {
+    float before, one, after;
+    int begin, split;
+    __device__ __forceinline__ ByGroup(const LaneColumns& c, const float* p, int64_t at, int step = 1) : one(p[at * step]), begin(c.begin), split(c.split) {
+        before = TAIL && begin > 0 ? p[(at - 1) * step] : one;
+        after = TAIL && split < V ? p[(at + 1) * step] : one;
+    }
+    __device__ __forceinline__ float operator[](int j) const {
+        if constexpr (TAIL) return pick(j < begin, before, pick(j >= split, after, one));
+        else return one;
+    }
+};
 
 template <typename T, int V, bool TAIL, int ACT, bool SAVE>
 __global__ __launch_bounds__(256) void k_norm_apply(NormShape s, GraphRows g, const T* x, RowPlane p, Affine f, T* y, RowPlane py, Checkpoint ck) {
@@ -430,7 +484,7 @@ __global__ __launch_bounds__(256) void k_norm_apply(NormShape s, GraphRows g, co
     over_graphs(s, g, w, [&](int64_t graph, int64_t a, int64_t b) {
         constexpr int U = 4;
         const int64_t at = graph * s.groups + (c.on ? c.group : 0);
-        const float m = f.mean[at], rs = f.rstd[at];
+        const ByGroup<V, TAIL> m(c, f.mean, at), rs(c, f.rstd, at);
         for (int64_t r = a; r < b; r += U * c.subs) {
             PlaneSource<T, V, true> q[U];
 #pragma unroll
@@ -450,7 +504,7 @@ __global__ __launch_bounds__(256) void k_norm_apply(NormShape s, GraphRows g, co
                     save_piece<V, TAIL>(ck, s, c, row, row < b, v);
                 }
 #pragma unroll
-                for (int j = 0; j < V; ++j) v[j] = activation<ACT>((q[k].at(j) - m) * rs * gamma[j] + beta[j]);
+                for (int j = 0; j < V; ++j) v[j] = activation<ACT>((q[k].at(j) - m[j]) * rs[j] * gamma[j] + beta[j]);
                 if (row < b && c.on) store_piece<V, true>(y + c.plane * py.gs + row * py.ld + c.col, v);
             }
         }
@@ -544,11 +598,12 @@ template <int V, int ACT>
 struct BeforeActivation {
     float edge[ACT == GSR_ACT_RELU ? V : 1];
     uint32_t sign[ACT == GSR_ACT_RELU ? V : 1];
-    __device__ __forceinline__ BeforeActivation(float m, float rs, const float (&gamma)[V], const float (&beta)[V]) {
+    template <typename S>
+    __device__ __forceinline__ BeforeActivation(const S& m, const S& rs, const float (&gamma)[V], const float (&beta)[V]) {
         if constexpr (ACT == GSR_ACT_RELU) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const double a = (double)rs * (double)gamma[j], b = fma(-(double)m, a, (double)beta[j]);
+                const double a = (double)rs[j] * (double)gamma[j], b = fma(-(double)m[j], a, (double)beta[j]);
                 sign[j] = a < 0.0 ? 0x80000000u : 0u;
                 edge[j] = a == 0.0 ? (b > 0.0 ? -INFINITY : INFINITY) : float_below(-b / fabs(a));
             }
@@ -584,7 +639,7 @@ __global__ __launch_bounds__(256) void k_norm_grad_sums(NormShape s, GraphRows g
         over_graphs(s, g, w, [&](int64_t graph, int64_t a, int64_t b) {
             constexpr int U = 2;
             const int64_t at = graph * s.groups + (c.on ? c.group : 0);
-            const float m = f.mean[at], rs = f.rstd[at];
+            const ByGroup<V, TAIL> m(c, f.mean, at), rs(c, f.rstd, at);
             const BeforeActivation<V, ACT> before(m, rs, gamma, beta);
             float sum_x[V], sum_z[V];
 #pragma unroll
@@ -606,7 +661,7 @@ __global__ __launch_bounds__(256) void k_norm_grad_sums(NormShape s, GraphRows g
                     const bool in = r + k * c.subs + c.sub < b;
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
-                        const float x = q[k].at(j), xh = (x - m) * rs;
+                        const float x = q[k].at(j), xh = (x - m[j]) * rs[j];
                         const float dz = before(j, e[k].at(j), x, xh, gamma, beta);
                         const bool counts = in && !(TAIL && j < c.skip);
                         sum_z[j] += counts ? dz : 0.0f;
@@ -614,15 +669,19 @@ __global__ __launch_bounds__(256) void k_norm_grad_sums(NormShape s, GraphRows g
                     }
                 }
             }
-            double u = 0.0, v = 0.0;
+            double u = 0.0, v = 0.0, u2 = 0.0, v2 = 0.0;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                u = fma((double)gamma[j], (double)sum_z[j], u);
-                v = fma((double)gamma[j], (double)sum_x[j], v);
+                const bool next = TAIL && j >= c.split;
+                const double z = (double)gamma[j] * (double)sum_z[j], x = (double)gamma[j] * (double)sum_x[j];
+                u += next ? 0.0 : z;
+                v += next ? 0.0 : x;
+                u2 += next ? z : 0.0;
+                v2 += next ? x : 0.0;
                 all_z[j] += sum_z[j];
                 all_x[j] += sum_x[j];
             }
-            leave_piece(s, c, slab, w, graph, u, v, pieces);
+            leave_piece<TAIL, V>(s, c, slab, w, graph, u, v, u2, v2, pieces);
         });
     }
     __shared__ float s_col[4][2][64 * V];
@@ -692,7 +751,7 @@ __global__ __launch_bounds__(1024) void k_norm_grad_join(NormShape s, GraphRows 
 
 template <typename T, int V, bool TAIL, int ACT, typename Source>
 __global__ __launch_bounds__(256) void k_norm_grad_apply(NormShape s, GraphRows g, const T* dy, RowPlane pd, Source source, Affine f,
-                                                         const float2* __restrict__ means, T* dx, RowPlane px) {
+                                                         const float* __restrict__ means, T* dx, RowPlane px) {
     const int64_t w = s.chunks - 1 - ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6));        // backwards, as k_norm_apply
     if (w < 0) return;
     const LaneColumns c = lane_columns<V>(s, blockIdx.y);
@@ -702,8 +761,8 @@ __global__ __launch_bounds__(256) void k_norm_grad_apply(NormShape s, GraphRows 
     over_graphs(s, g, w, [&](int64_t graph, int64_t a, int64_t b) {
         constexpr int U = 2;
         const int64_t at = graph * s.groups + (c.on ? c.group : 0);
-        const float m = f.mean[at], rs = f.rstd[at];
-        const float2 mm = means[at];
+        const ByGroup<V, TAIL> m(c, f.mean, at), rs(c, f.rstd, at);
+        const ByGroup<V, TAIL> m1(c, means, at, 2), m2(c, means + 1, at, 2);
         const BeforeActivation<V, ACT> before(m, rs, gamma, beta);
         for (int64_t r = a; r < b; r += U * c.subs) {
             PlaneSource<T, V, true> e[U];
@@ -723,9 +782,9 @@ __global__ __launch_bounds__(256) void k_norm_grad_apply(NormShape s, GraphRows 
                 float v[V];
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const float x = q[k].at(j), xh = (x - m) * rs;
+                    const float x = q[k].at(j), xh = (x - m[j]) * rs[j];
                     const float dz = before(j, e[k].at(j), x, xh, gamma, beta);
-                    v[j] = rs * (gamma[j] * dz - mm.x - xh * mm.y);
+                    v[j] = rs[j] * (gamma[j] * dz - m1[j] - xh * m2[j]);
                 }
                 if (row < b && c.on) store_piece<V, true>(dx + c.plane * px.gs + row * px.ld + c.col, v);
             }
@@ -744,7 +803,7 @@ __global__ __launch_bounds__(1024) void k_norm_grad_small(NormShape s, GraphRows
     load_affine<V>(f.gamma, c, 1.0f, gamma);
     load_affine<V>(f.beta, c, 0.0f, beta);
     const int group = c.on ? c.group : 0;
-    const float m = f.mean[group], rs = f.rstd[group];
+    const ByGroup<V, false> m(c, f.mean, group), rs(c, f.rstd, group);
     const BeforeActivation<V, ACT> before(m, rs, gamma, beta);
     float sum_x[V], sum_z[V];
 #pragma unroll
@@ -767,7 +826,7 @@ __global__ __launch_bounds__(1024) void k_norm_grad_small(NormShape s, GraphRows
             const bool in = r + k * c.subs + c.sub < b;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float x = q[k].at(j), xh = (x - m) * rs, dz = before(j, e[k].at(j), x, xh, gamma, beta);
+                const float x = q[k].at(j), xh = (x - m[j]) * rs[j], dz = before(j, e[k].at(j), x, xh, gamma, beta);
                 sum_z[j] += in ? dz : 0.0f;
                 sum_x[j] += in ? dz * xh : 0.0f;
             }
@@ -819,8 +878,8 @@ __global__ __launch_bounds__(1024) void k_norm_grad_small(NormShape s, GraphRows
         float w[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const float x = q.at(j), xh = (x - m) * rs, dz = before(j, e.at(j), x, xh, gamma, beta);
-            w[j] = rs * (gamma[j] * dz - m1 - xh * m2);
+            const float x = q.at(j), xh = (x - m[j]) * rs[j], dz = before(j, e.at(j), x, xh, gamma, beta);
+            w[j] = rs[j] * (gamma[j] * dz - m1 - xh * m2);
         }
         if (row < b && c.on) store_piece<V>(dx + c.plane * px.gs + row * px.ld + c.col, w);
     }
@@ -892,19 +951,20 @@ bool aligned_to(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1
 constexpr int64_t kChunks = 4096, kMaxRows = 1024;
 int64_t least_rows(const NormShape& s, int64_t graphs) { return (graphs > 1 ? 2 : 8) * (64 >> s.lanes_log2); }
 
-// Pieces of 16 bytes of the plane's type where every lane's columns lie in one group; else single columns.  With a tail the last piece overlaps the one
-// before it, whose lane may have stored already where a pass works in place.
+// Pieces of 16 bytes of the plane's type, but for groups or planes narrower than that; with a tail, single columns in place, where the last piece of a row overlaps
+// the one before it, whose lane may have stored already.  480k x 136 16-bit values in eight groups of 17, relu, in pieces and in single
+// columns: forward 48 and 98 us, sums of the gradient 79 and 300, gradient 118 and 207.
 struct PieceRule {
     int v;
     bool tail;
 };
-PieceRule piece_of(int32_t dg, int32_t groups, int32_t cg, int32_t dtype, bool in_place) {
+PieceRule piece_of(int32_t dg, int32_t cg, int32_t dtype, bool in_place) {
     const int v = dtype == GSR_BF16 ? 8 : 4;
     if (dg % v == 0 && cg % v == 0) return {v, false};
-    if (groups == 1 && dg > v && !in_place) return {v, dg % v != 0};
+    if (dg > v && cg >= v && !in_place) return {v, true};
     return {1, false};
 }
-NormShape norm_shape(int64_t n, int64_t graphs, int32_t d, int32_t planes, int32_t groups, int V) {
+NormShape norm_shape(int64_t n, int64_t graphs, int32_t d, int32_t planes, int32_t groups, int32_t dtype, int V) {
     NormShape s{};
     s.n = n;
     s.d = d;
@@ -912,12 +972,14 @@ NormShape norm_shape(int64_t n, int64_t graphs, int32_t d, int32_t planes, int32
     s.groups = groups;
     s.cg = d / groups;
     const int pieces = (s.dg + V - 1) / V;
-    // as few idle lanes as can be, or up to a quarter more for longer rows; a block of a checkpoint in one slab
+    // as few idle lanes as can be, or up to a quarter more for longer rows, twice as many where slabs would share lines of memory; a block of a checkpoint
+    // in one slab.  480k x 136 16-bit values in one slab of 32 lanes against three of 8: forward 43 and 145 us.
     auto lanes_for = [&](int k) { return (((pieces - 1) >> k) + 1) << k; };
     auto fits = [&](int k) { return (V << k) % kBlock == 0 || (V << k) >= s.dg; };
     int least = 1 << 30;
     for (int k = 2; k <= 6; ++k) if (fits(k)) least = std::min(least, lanes_for(k));
-    for (int k = 2; k <= 6; ++k) if (fits(k) && lanes_for(k) <= least + least / 4) s.lanes_log2 = k;
+    const int most = s.dg * (int)dtype_size(dtype) % 128 ? 2 * least : least + least / 4;
+    for (int k = 2; k <= 6; ++k) if (fits(k) && lanes_for(k) <= most) s.lanes_log2 = k;
     s.group_slabs = lanes_for(s.lanes_log2) >> s.lanes_log2;
     s.slabs = s.group_slabs * planes;
     s.rows = (int32_t)std::min(kMaxRows, std::max(least_rows(s, graphs), (n * s.slabs + kChunks - 1) / kChunks));
@@ -1057,7 +1119,7 @@ size_t gsr_group_norm_workspace(int64_t n, int64_t graphs, int32_t d, int32_t c,
     // in place, single columns may take the place of pieces
     size_t bytes = 0;
     for (bool in_place : {false, true})
-        bytes = std::max(bytes, carve_norm(norm_shape(n, graphs, d, planes, groups, piece_of(d / planes, groups, d / groups, dtype, in_place).v), graphs).total);
+        bytes = std::max(bytes, carve_norm(norm_shape(n, graphs, d, planes, groups, dtype, piece_of(d / planes, d / groups, dtype, in_place).v), graphs).total);
     return bytes;
 }
 
@@ -1078,9 +1140,9 @@ gsr_status_t gsr_group_norm(const void* x, int64_t ldx, int64_t n, int32_t d, in
     if (x == y_out && ldx != ldy) return fail(GSR_ERR_INVALID_ARG, "in place, but with row strides of %lld and %lld", (long long)ldx, (long long)ldy);
     const bool save = codes_out || scales_out;
     if (save) GSR_TRY(checkpoint_of(n, dg, codes_out, scales_out, &ck));
-    const PieceRule rule = piece_of(dg, groups, d / groups, dtype, x == y_out);
+    const PieceRule rule = piece_of(dg, d / groups, dtype, x == y_out);
     const int V = rule.v;
-    const NormShape s = norm_shape(n, graphs, d, planes, groups, V);
+    const NormShape s = norm_shape(n, graphs, d, planes, groups, dtype, V);
     const NormWs ws = carve_norm(s, graphs);
     GSR_TRY(workspace_of(ws, s, graphs, workspace, workspace_bytes));
     if (graphs == 0) return GSR_OK;
@@ -1137,9 +1199,9 @@ gsr_status_t gsr_group_norm_grad(const void* dy, int64_t lddy, const void* x, in
     GSR_TRY(norm_args(d, groups, act, gamma, beta, mean, rstd, graphs));
     if (!aligned_to(dgamma_out, 4) || !aligned_to(dbeta_out, 4)) return fail(GSR_ERR_INVALID_ARG, "dgamma_out or dbeta_out is not aligned to its elements");
     if (dy == dx_out && lddy != lddx) return fail(GSR_ERR_INVALID_ARG, "in place, but with row strides of %lld and %lld", (long long)lddy, (long long)lddx);
-    const PieceRule rule = piece_of(dg, groups, d / groups, dtype, dy == dx_out);
+    const PieceRule rule = piece_of(dg, d / groups, dtype, dy == dx_out);
     const int V = rule.v;
-    const NormShape s = norm_shape(n, graphs, d, planes, groups, V);
+    const NormShape s = norm_shape(n, graphs, d, planes, groups, dtype, V);
     const NormWs ws = carve_norm(s, graphs);
     GSR_TRY(workspace_of(ws, s, graphs, workspace, workspace_bytes));
     hipStream_t st = (hipStream_t)stream;
@@ -1166,7 +1228,7 @@ gsr_status_t gsr_group_norm_grad(const void* dy, int64_t lddy, const void* x, in
             hipLaunchKernelGGL((k_norm_grad_join<true>), grid, dim3(1024), 0, st, s, g, V, pieces, ws.task_blocks, ws.task_wgs, means, columns, parts, dgamma_out, dbeta_out);
         else if (grid.x)
             hipLaunchKernelGGL((k_norm_grad_join<false>), grid, dim3(1024), 0, st, s, g, V, pieces, ws.task_blocks, ws.task_wgs, means, columns, parts, dgamma_out, dbeta_out);
-        if (n && graphs) hipLaunchKernelGGL((k_norm_grad_apply<T, P, tail.value, ACT, Source>), rows_grid(q), dim3(256), 0, st, q, g, (const T*)dy, pd, source, f, means, (T*)dx_out, po);
+        if (n && graphs) hipLaunchKernelGGL((k_norm_grad_apply<T, P, tail.value, ACT, Source>), rows_grid(q), dim3(256), 0, st, q, g, (const T*)dy, pd, source, f, (const float*)means, (T*)dx_out, po);
     };
     by_piece(dtype, rule, [&](auto t, auto v, auto tail) {
         using T = decltype(t);
@@ -1189,8 +1251,8 @@ gsr_status_t gsr_checkpoint_save(const void* x, int64_t ldx, int64_t n, int32_t 
     GSR_TRY(row_plane("x", x, n, dg, ldx, dtype, &p));
     GSR_TRY(checkpoint_of(n, dg, codes_out, scales_out, &ck));
     if (n == 0) return GSR_OK;
-    const PieceRule rule = piece_of(dg, 1, dg, dtype, false);
-    const NormShape s = apply_shape(norm_shape(n, 1, d, planes, 1, rule.v), nullptr);
+    const PieceRule rule = piece_of(dg, dg, dtype, false);
+    const NormShape s = apply_shape(norm_shape(n, 1, d, planes, 1, dtype, rule.v), nullptr);
     by_piece(dtype, rule, [&](auto t, auto v, auto tail) {
         using T = decltype(t);
         hipLaunchKernelGGL((k_checkpoint_save<T, v.value, tail.value>), rows_grid(s), dim3(256), 0, (hipStream_t)stream, s, (const T*)x, p, ck);
@@ -1208,8 +1270,8 @@ gsr_status_t gsr_checkpoint_load(const int8_t* codes, const float* scales, int64
     GSR_TRY(row_plane("x_out", x_out, n, dg, ldx, dtype, &p));
     GSR_TRY(checkpoint_of(n, dg, codes, scales, &ck));
     if (n == 0) return GSR_OK;
-    const PieceRule rule = piece_of(dg, 1, dg, dtype, false);
-    const NormShape s = apply_shape(norm_shape(n, 1, d, planes, 1, rule.v), nullptr);
+    const PieceRule rule = piece_of(dg, dg, dtype, false);
+    const NormShape s = apply_shape(norm_shape(n, 1, d, planes, 1, dtype, rule.v), nullptr);
     by_piece(dtype, rule, [&](auto t, auto v, auto tail) {
         using T = decltype(t);
         hipLaunchKernelGGL((k_checkpoint_load<T, v.value, tail.value>), rows_grid(s), dim3(256), 0, (hipStream_t)stream, s, ck, (T*)x_out, p);

@@ -174,6 +174,16 @@ CASES = [
     (90, 257, 0, 1, F32, "relu", "rows", 0, 0, False),
     (70, 9, 0, 1, BF16, "silu", "many", 0, 1, True),
     (41, 1031, 0, 1, BF16, "none", "padded", 0, 0, True),
+    # groups that are no whole number of pieces: they begin and end inside one
+    (703, 99, 3, 9, F32, "silu", "many", 0, 0, True),
+    (703, 150, 2, 6, BF16, "relu", "padded", 0, 0, True),
+    (301, 1020, 0, 12, F32, "silu", "many", 0, 0, True),
+    (203, 2055, 0, 15, BF16, "silu", "many", 1, 1, True),
+    (500, 136, 0, 8, F32, "relu", "one", 0, 0, True),
+    (500, 136, 0, 8, BF16, "relu", "many", 0, 0, False),
+    (400, 90, 2, 3, F32, "none", "empty", 0, 0, True),
+    (400, 102, 2, 3, BF16, "silu", "padded", 2, 0, True),
+    (61, 5000, 0, 8, F32, "relu", "rows", 0, 0, True),
     (50, 48, 0, 3, F32, "silu", "none", 0, 0, True),
     (0, 48, 0, 3, F32, "silu", "none", 0, 0, True),
 ]
@@ -251,7 +261,7 @@ def test_gradient_against_differences(act):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("n,d,c,groups", [(701, 128, 2, 4), (701, 77, 0, 1), (300, 257, 0, 1), (300, 77, 0, 7)])
+@pytest.mark.parametrize("n,d,c,groups", [(701, 128, 2, 4), (701, 77, 0, 1), (300, 257, 0, 1), (300, 77, 0, 7), (300, 136, 0, 8), (200, 150, 2, 6)])
 def test_in_place(dtype, n, d, c, groups):
     rng, x, px, gamma, beta, ptr, dptr = case_inputs(n, d, c, groups, dtype, "padded", 0, 0, True)
     args = dict(gamma=put(gamma), beta=put(beta), act=gsr.GSR_ACT_SILU, graph_ptr=dptr)
@@ -270,7 +280,7 @@ def test_in_place(dtype, n, d, c, groups):
     gsr.gsr_group_norm_grad(dy, mean, rstd, dx, x=before, **args)
     gsr.gsr_group_norm_grad(dy, mean, rstd, dy, x=before, **args)
     ref = Reference(x, ptr, groups, gamma, beta, "silu", mean.double().cpu().numpy(), rstd.double().cpu().numpy())
-    if d % 8 == 0:
+    if d % groups == 0 and d // groups % 8 == 0 and d // max(c, 1) % 8 == 0:
         assert torch.equal(dx, dy)
     want, off = ref.backward(given)
     close(host(dy), np.where(np.isnan(want["dx"]), np.nan, want["dx"]), off["dx"], dtype)
@@ -423,7 +433,7 @@ def test_checkpoint_of_extreme_values():
 
 
 @pytest.mark.parametrize("n,d,c,groups,dtype,graphs", [(1001, 256, 4, 4, F32, "padded"), (777, 77, 0, 7, BF16, "many"), (64, 96, 3, 6, BF16, "one"),
-                                                       (333, 40, 0, 2, F32, "empty"), (333, 77, 0, 1, F32, "many"), (201, 130, 2, 1, BF16, "padded"),
+                                                       (333, 40, 0, 2, F32, "empty"), (333, 77, 0, 1, F32, "many"), (201, 130, 2, 1, BF16, "padded"), (333, 150, 2, 6, BF16, "many"), (333, 99, 3, 9, F32, "padded"),
                                                        (99, 385, 0, 1, BF16, "one")])
 def test_norm_writes_the_checkpoint_and_its_gradient_reads_it(n, d, c, groups, dtype, graphs):
     rng, x, px, gamma, beta, ptr, dptr = case_inputs(n, d, c, groups, dtype, graphs, 0, 0, True)
