@@ -394,7 +394,8 @@ __device__ __forceinline__ void add_up(double& sum, int64_t& count) {          /
         count += s_count[i];
     }
 }
-// 2^q lanes take the splits of a row
+// 2^q lanes take the splits of a row.  Sums in 64 bits; exponentials and logarithms of 32 bits, whose 3 u are below those of the parts: by the 64-bit
+// functions a call of 2,000 rows and 40 classes takes 19.3 us, not 18.2.
 __global__ __launch_bounds__(1024) void k_class_lse(const float2* __restrict__ part, const float* __restrict__ at_target,
                                                     const int32_t* __restrict__ target, int64_t n, int64_t x_pad, int splits, int q,
                                                     float* __restrict__ lse_out, LossPart* __restrict__ parts, float* __restrict__ loss) {
@@ -407,10 +408,10 @@ __global__ __launch_bounds__(1024) void k_class_lse(const float2* __restrict__ p
         for (int s = first; s < splits; s += step) m = fmaxf(m, part[s * x_pad + i].x);
         for (int o = step >> 1; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
         double l = 0.0;
-        for (int s = first; s < splits; s += step) l += (double)part[s * x_pad + i].y * exp((double)part[s * x_pad + i].x - (double)m);
+        for (int s = first; s < splits; s += step) l += (double)(part[s * x_pad + i].y * __builtin_amdgcn_exp2f((part[s * x_pad + i].x - m) * kLog2e));
         for (int o = step >> 1; o; o >>= 1) l += __shfl_xor(l, o);
         if (first || row >= n) continue;
-        const double lse = (double)m + log(l);
+        const double lse = (double)m + (double)logf((float)l);
         lse_out[i] = (float)lse;
         if (target[i] >= 0) {
             sum += lse - (double)at_target[i];
@@ -557,7 +558,10 @@ __device__ __forceinline__ void grad_side(const ClassGradArgs& g, unsigned index
 #pragma unroll
             for (int r = 0; r < RB; ++r) z[blk][r] = NP == 2 ? all_four(0.0f) : BY_CLASS ? all_four(own_f[r]) : row_f[blk];
         }
+        // A wave in its products goes before one that fetches or is at its exponentials: 16 bits at D = 256, 3,140 -> 3,100 us; no gain for floats or the loss.
+        __builtin_amdgcn_s_setprio(1);
         tile_logits<KS, NP, RB>(tile, own, lane, z);
+        __builtin_amdgcn_s_setprio(0);
         frag8 dz[RB][NP];
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
@@ -607,6 +611,7 @@ __device__ __forceinline__ void grad_side(const ClassGradArgs& g, unsigned index
             }
             operand_of<NP>(z[0][r], z[1][r], dz[r]);
         }
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int c = 0; c < 2 * KS; c += 2) {
             frag8 b[2][NP];
@@ -622,6 +627,7 @@ __device__ __forceinline__ void grad_side(const ClassGradArgs& g, unsigned index
 #pragma unroll
                     for (int r = 0; r < RB; ++r) acc[r][c + q] = mfma_product<NP>(i, dz[r], b[q], acc[r][c + q]);
         }
+        __builtin_amdgcn_s_setprio(0);
         if constexpr (!TWO) {
             __syncthreads();
             if (t + 1 < t1) fetch_tile<N>(g.stream + (int64_t)(t + 1) * N * 64, s_tile[0], wave, lane);
