@@ -391,9 +391,10 @@ gsr_status_t gsr_adam_update_list(float* const* w, const void* const* dw, float*
  * float32 first, in an order that the sizes and the offsets alone fix.  Values are summed from the first value of their group
  * in the first graph on: a graph whose mean lies 2^20 standard deviations from it loses the variance.
  * y_out may be x and dx_out may be dy, with the same stride; apart from that what a call writes overlaps nothing that it reads.
- * eps > 0; 1 <= d <= 131072; n < 2^31; pointers aligned to their elements.  workspace: device, 16-byte aligned, at least
- * gsr_group_norm_workspace() bytes (0: sizes that are refused; never fewer for more rows or graphs, so that one serves any fewer); it holds nothing between
- * calls.  Calls only launch kernels and may be captured; calls with workspaces of their own may run side by side. */
+ * eps > 0; 1 <= d <= 131072; n < 2^31; pointers aligned to their elements; where graphs x (groups + d) is 2^30 or more a call may be refused.
+ * workspace: device, 16-byte aligned, at least gsr_group_norm_workspace() bytes (0: sizes outside these limits; never fewer for more rows or graphs, so
+ * that one serves any fewer); it holds nothing between calls.  Calls only launch kernels and may be captured; calls with workspaces of their own may run
+ * side by side. */
 typedef enum gsr_act { GSR_ACT_NONE = 0, GSR_ACT_RELU = 1, GSR_ACT_SILU = 2 } gsr_act_t;
 size_t gsr_group_norm_workspace(int64_t n, int64_t graphs, int32_t d, int32_t c, int32_t layout, int32_t dtype, int32_t groups);
 gsr_status_t gsr_group_norm(const void* x, int64_t ldx, int64_t n, int32_t d, int32_t c, int32_t layout, int32_t dtype, const void* graph_ptr,
