@@ -404,7 +404,7 @@ __global__ __launch_bounds__(256) void k_norm_sums(NormShape s, GraphRows g, con
                 const bool in = r + k * c.subs + c.sub < b;
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const double t = in ? (double)q[k].at(j) - (TAIL && j >= c.split ? shift2 : shift) : 0.0;
+                    const double from = TAIL && j >= c.split ? shift2 : shift, t = (double)(in ? q[k].at(j) : (float)from) - from;
                     u[TAIL ? j : 0] += t;
                     v[TAIL ? j : 0] = fma(t, t, v[TAIL ? j : 0]);
                 }
@@ -629,9 +629,11 @@ __global__ __launch_bounds__(256) void k_norm_grad_sums(NormShape s, GraphRows g
     const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     const int slab = blockIdx.y;
     const LaneColumns c = lane_columns<V>(s, slab);
-    float all_x[V], all_z[V];
+    __shared__ float s_col[4][2][V][64];            // every lane's sums of its columns over the graphs: in registers they would leave room for fewer waves
+    const int lane = lane_id();
+    float (&all)[2][V][64] = s_col[threadIdx.x >> 6];
 #pragma unroll
-    for (int j = 0; j < V; ++j) all_x[j] = all_z[j] = 0.0f;
+    for (int j = 0; j < V; ++j) all[0][j][lane] = all[1][j][lane] = 0.0f;
     if (w < s.chunks) {
         float gamma[V], beta[V];
         load_affine<V>(f.gamma, c, 1.0f, gamma);
@@ -678,32 +680,23 @@ __global__ __launch_bounds__(256) void k_norm_grad_sums(NormShape s, GraphRows g
                 v += next ? 0.0 : x;
                 u2 += next ? z : 0.0;
                 v2 += next ? x : 0.0;
-                all_z[j] += sum_z[j];
-                all_x[j] += sum_x[j];
+                all[0][j][lane] += sum_x[j];
+                all[1][j][lane] += sum_z[j];
             }
             leave_piece<TAIL, V>(s, c, slab, w, graph, u, v, u2, v2, pieces);
         });
     }
-    __shared__ float s_col[4][2][64 * V];
-    const int lanes = 1 << s.lanes_log2, li = lane_id() & (lanes - 1);
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        for (int o = lanes; o < 64; o <<= 1) {
-            all_x[j] += __shfl_xor(all_x[j], o);
-            all_z[j] += __shfl_xor(all_z[j], o);
-        }
-        if (c.sub == 0 && !(TAIL && j < c.skip)) {
-            s_col[threadIdx.x >> 6][0][li * V + j - c.skip] = all_x[j];
-            s_col[threadIdx.x >> 6][1][li * V + j - c.skip] = all_z[j];
-        }
-    }
     __syncthreads();
-    const int first = (slab % s.group_slabs) * lanes * V, plane = slab / s.group_slabs;
+    const int lanes = 1 << s.lanes_log2, first = (slab % s.group_slabs) * lanes * V, plane = slab / s.group_slabs;
     for (int i = threadIdx.x; i < 2 * lanes * V; i += 256) {
-        const int which = i >= lanes * V, k = which ? i - lanes * V : i;
-        if (first + k >= s.dg) continue;
-        columns[((int64_t)blockIdx.x * 2 + which) * s.d + plane * s.dg + first + k] =
-            (s_col[0][which][k] + s_col[1][which][k]) + (s_col[2][which][k] + s_col[3][which][k]);
+        const int li = i & (lanes - 1), which = (i >> s.lanes_log2) / V, own = (i >> s.lanes_log2) % V, col = first + li * V + own;
+        if (col >= s.dg) continue;
+        const int begin = first + li * V, j = own + (TAIL && begin + V > s.dg ? begin + V - s.dg : 0);       // (the columns before a tail's own come first)
+        double sum = 0.0;
+        for (int l = li; l < 64; l += lanes)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum += (double)s_col[k][which][j][l];
+        columns[((int64_t)blockIdx.x * 2 + which) * s.d + plane * s.dg + col] = (float)sum;
     }
 }
 
