@@ -688,13 +688,13 @@ template <typename V, typename Part, typename Store>
 __device__ __forceinline__ void join_parts(int64_t first, int64_t count, int splits, int q, V* s_sum, Part part, Store store) {
     const int each = 256 >> q, mine = threadIdx.x & (each - 1), lane = threadIdx.x >> (8 - q);
     const int64_t i = first + mine;
-    V v = 0;
+    V v{};
     if (i < count) {
         constexpr int U = 4;
         for (int s = lane; s < splits; s += U << q) {
             V t[U];
 #pragma unroll
-            for (int k = 0; k < U; ++k) t[k] = s + (k << q) < splits ? part(s + (k << q), i) : V(0);
+            for (int k = 0; k < U; ++k) t[k] = s + (k << q) < splits ? part(s + (k << q), i) : V{};
 #pragma unroll
             for (int k = 0; k < U; ++k) v += t[k];
         }
@@ -707,13 +707,21 @@ __device__ __forceinline__ void join_parts(int64_t first, int64_t count, int spl
     }
     if (i < count) store(i, v);
 }
+__host__ __device__ constexpr unsigned join_quads(int d) { return (unsigned)(d + 3) / 4; }
+__device__ __forceinline__ void store_four(float* p, f32x4 v) { *reinterpret_cast<u32x4a*>(p) = __builtin_bit_cast(u32x4a, v); }
+__device__ __forceinline__ void store_four(bf16_t* p, f32x4 v) {
+    u32x2h t;
+    t[0] = bf16_bits(v[0]) | bf16_bits(v[1]) << 16;
+    t[1] = bf16_bits(v[2]) | bf16_bits(v[3]) << 16;
+    *reinterpret_cast<u32x2h*>(p) = t;
+}
 struct JoinShape {
     unsigned row_blocks, class_blocks, bias_blocks;         // workgroups of each; 0: nothing to join
     int row_q, class_q, width;
 };
 template <typename T>
 __global__ __launch_bounds__(256) void k_class_grad_join(ClassGradArgs by_row, ClassGradArgs by_class, JoinShape j) {
-    __shared__ double s_sum[256];
+    __shared__ f32x4 s_sum[256];
     unsigned b = blockIdx.x;
     const bool rows = b < j.row_blocks;
     if (!rows) b -= j.row_blocks;
@@ -721,15 +729,22 @@ __global__ __launch_bounds__(256) void k_class_grad_join(ClassGradArgs by_row, C
     const int q = rows ? j.row_q : j.class_q;
     const float scale = gradient_scale(g.counts, g.count_blocks, g.scale);
     if (rows || b < j.class_blocks) {
-        join_parts<float>((int64_t)b * (256 >> q), g.rows * g.d, g.splits, q, reinterpret_cast<float*>(s_sum),
-            [&](int s, int64_t i) { return g.part[((int64_t)s * g.own_pad + i / g.d) * j.width + i % g.d]; },
-            [&](int64_t i, float v) {
-                const int64_t row = i / g.d;
-                const int col = (int)(i - row * g.d), plane = col / g.dg;
-                store_as(static_cast<T*>(g.out) + plane * g.gs + row * g.ld + (col - plane * g.dg), v * scale);
+        const unsigned quads = join_quads(g.d);         // four columns each; (there are fewer than 2^32 of them where a side is split)
+        join_parts<f32x4>((int64_t)b * (256 >> q), g.rows * quads, g.splits, q, s_sum,
+            [&](int s, int64_t i) { return four(g.part + ((int64_t)s * g.own_pad + (unsigned)i / quads) * j.width + (unsigned)i % quads * 4); },
+            [&](int64_t i, f32x4 v) {
+                const unsigned row = (unsigned)i / quads;
+                const int col = (int)((unsigned)i % quads) * 4, plane = col / g.dg;
+                T* to = static_cast<T*>(g.out) + plane * g.gs + row * g.ld + (col - plane * g.dg);
+                v *= scale;
+                if (g.dg % 4 == 0) return store_four(to, v);
+                for (int k = 0; k < 4 && col + k < g.d; ++k) {
+                    const int other = (col + k) / g.dg;
+                    store_as(static_cast<T*>(g.out) + other * g.gs + row * g.ld + (col + k - other * g.dg), v[k]);
+                }
             });
     } else {
-        join_parts<double>((int64_t)(b - j.class_blocks) * (256 >> q), g.rows, g.splits, q, s_sum,
+        join_parts<double>((int64_t)(b - j.class_blocks) * (256 >> q), g.rows, g.splits, q, reinterpret_cast<double*>(s_sum),
             [&](int s, int64_t i) { return g.bias_part[(int64_t)s * g.own_pad + i]; }, [&](int64_t i, double v) { g.dbias[i] = (float)(v * (double)scale); });
     }
 }
@@ -915,11 +930,11 @@ void launch_grad(ClassGradArgs by_row, ClassGradArgs by_class, hipStream_t st) {
     auto values = [](int64_t count, int q) { return (unsigned)((count + (256 >> q) - 1) / (256 >> q)); };
     if (by_row.splits > 1) {
         j.row_q = join_lanes(by_row.splits);
-        j.row_blocks = values(by_row.rows * by_row.d, j.row_q);
+        j.row_blocks = values(by_row.rows * join_quads(by_row.d), j.row_q);
     }
     if (by_class.splits > 1) {
         j.class_q = join_lanes(by_class.splits);
-        if (by_class.out) j.class_blocks = values(by_class.rows * by_class.d, j.class_q);
+        if (by_class.out) j.class_blocks = values(by_class.rows * join_quads(by_class.d), j.class_q);
         if (by_class.dbias) j.bias_blocks = values(by_class.rows, j.class_q);
     }
     const unsigned joins = j.row_blocks + j.class_blocks + j.bias_blocks;
