@@ -117,6 +117,9 @@ def borders(kind, n, rng):
         return np.array([0, 0, 0, n // 3, n // 3, n, n, n])
     if kind == "none":
         return np.array([n // 2])
+    if kind == "uneven":                            # two large graphs among small ones
+        sizes = [n // 500] * 13 + [n * 2 // 5] + [n // 250] * 14 + [n * 2 // 5] + [n // 500] * 10
+        return np.concatenate([[0], np.cumsum(sizes), [n]])
     assert kind == "many"
     return np.sort(np.concatenate([[0, n], rng.integers(0, n + 1, max(1, n // 6))]))
 
@@ -184,6 +187,9 @@ CASES = [
     (400, 90, 2, 3, F32, "none", "empty", 0, 0, True),
     (400, 102, 2, 3, BF16, "silu", "padded", 2, 0, True),
     (61, 5000, 0, 8, F32, "relu", "rows", 0, 0, True),
+    (5_000, 64, 0, 1, F32, "silu", "uneven", 0, 0, True),
+    (5_003, 96, 2, 4, BF16, "relu", "uneven", 0, 0, True),
+    (6_001, 99, 0, 3, F32, "none", "uneven", 1, 0, True),
     (50, 48, 0, 3, F32, "silu", "none", 0, 0, True),
     (0, 48, 0, 3, F32, "silu", "none", 0, 0, True),
 ]
