@@ -286,6 +286,7 @@ struct ClassLossArgs {
     int64_t x_pad;
     int32_t tiles, splits;
 };
+// 32,749 x 50,021 of 256 16-bit values: 666 us, 1,260 TFLOP/s (a large library product reaches 1,444 on the same card); matrix cores busy 55 % of the cycles.
 template <int KS, int NP, int RB>
 __global__ __launch_bounds__(256, loss_waves(KS, NP)) void k_class_loss(ClassLossArgs g) {
     constexpr int N = 2 * KS * NP;
@@ -685,7 +686,10 @@ __device__ __forceinline__ void grad_side(const ClassGradArgs& g, unsigned index
         }
     }
 }
-// dx and dE, or one of them, in one launch: what is left of the one's last round is filled by the other, and few rows and classes wait for one launch less
+// dx and dE, or one of them, in one launch: what is left of the one's last round is filled by the other, and few rows and classes wait for one launch less.
+// 32,749 x 50,021 of 256 16-bit values: four products (each side has the logits anew) in 2.97 ms, 1,130 TFLOP/s; 8,191 x 4,099 floats at D = 384, 284 us, 1,090.
+// Matrix cores busy 48 and 50 % of the cycles.  With a quarter fewer vector instructions (exponents in one multiply-add, classes looked for by tile) the cycles
+// fall by 2 % and the time grows by 3 %, since the clock falls; four blocks a wave, one wave a SIMD: 4.5 ms.
 template <int KS, int NP, int RB, typename T>
 __global__ __launch_bounds__(256, grad_waves(KS, NP)) void k_class_grad(ClassGradArgs by_row, ClassGradArgs by_class) {
     __shared__ uint4 s_tile[grad_two(KS, NP) ? 2 : 1][2 * KS * NP * 64];
