@@ -367,3 +367,19 @@ def test_calls_side_by_side_and_again_give_the_same_bits():
     torch.cuda.synchronize()
     for g in got:
         assert all(torch.equal(a, b) for a, b in zip(g, want))
+
+
+def test_row_strides_that_lead_beyond_2_to_the_32_values():
+    n, classes, d, stride = 35, 34, 64, 2 ** 27
+    x, e, b, ids, _ = inputs(n, classes, d, 0, BF16, torch.int32, "mixed", 0, 0, True)
+    memory = torch.empty(n * stride, dtype=BF16, device=dev())
+    wide_x, wide_dx, wide_e, wide_de = (memory.as_strided((n if k < 2 else classes, d), (stride, 1), k * d) for k in range(4))
+    wide_x.copy_(x)
+    wide_e.copy_(e)
+
+    def run(x, e, dx, de):
+        loss, lse = forward(x, e, b, ids, n)
+        gsr.gsr_class_grad(x, e, ids, lse, dx_out=dx, dtable_out=de, bias=b)
+        return loss, lse, dx, de
+    for got, want in zip(run(wide_x, wide_e, wide_dx, wide_de), run(x, e, torch.empty_like(x), torch.empty_like(e))):
+        assert torch.equal(got, want)

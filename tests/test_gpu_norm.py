@@ -545,3 +545,40 @@ def test_calls_side_by_side_and_again_give_the_same_bits():
     torch.cuda.synchronize()
     for g in got:
         assert all(torch.equal(a, b) for a, b in zip(g, want))
+
+
+@pytest.mark.parametrize("c", [0, 4])
+def test_planes_of_more_than_2_to_the_32_values(c):
+    """The last graph of a plane whose values, codes and their offsets pass 32 bits, against the same rows by themselves.
+
+    Sums of other chunks: means of h and h xh are off by 1,024 u of the mean of absolute values (below 1) in each call, so dx by 2 * 1,024 u * (1 + |xh|) r, below
+    2^-10 for |xh| < 7; and every 16-bit result by half a step in each, 2^-7 of the value for both."""
+    n, d, last = 17_000_001, 256, 1_003
+    torch.manual_seed(1)
+    x = torch.empty((n, d) if not c else (c, n, d // c), dtype=BF16, device=dev()).normal_()
+    blocks = gsr.gsr_checkpoint_blocks(d, max(1, c))
+    y, codes, scales = torch.empty_like(x), torch.empty(x.shape, dtype=torch.int8, device=dev()), torch.empty((*x.shape[:-1], blocks // max(1, c)), device=dev())
+    ptr = torch.tensor([0, n - last, n], device=dev())
+    mean, rstd = stats([0, 1, 2], 8)
+    gsr.gsr_group_norm(x, y, mean, rstd, graph_ptr=ptr, codes_out=codes, scales_out=scales)
+
+    def end(t):
+        return t[..., -last:, :].contiguous()
+    x2 = end(x)
+    y2, codes2, scales2 = torch.empty_like(x2), torch.empty(x2.shape, dtype=torch.int8, device=dev()), torch.empty((*x2.shape[:-1], blocks // max(1, c)), device=dev())
+    mean2, rstd2 = stats([0, 1], 8)
+    gsr.gsr_group_norm(x2, y2, mean2, rstd2, codes_out=codes2, scales_out=scales2)
+    assert torch.equal(end(codes), codes2) and torch.equal(end(scales), scales2)
+    assert torch.allclose(mean[1:], mean2, rtol=4 * U, atol=1e-12) and torch.allclose(rstd[1:], rstd2, rtol=4 * U)
+    assert torch.allclose(end(y).float(), y2.float(), rtol=2.0 ** -7, atol=16 * U * 8)
+    assert float(y[..., :1000, :].float().std()) > 0.9
+    back, back2 = torch.empty_like(x2), torch.empty_like(x2)
+    gsr.gsr_checkpoint_load(codes, scales, x)
+    gsr.gsr_checkpoint_load(codes2, scales2, back2)
+    back.copy_(end(x))
+    assert torch.equal(back, back2)
+    dy2 = end(y)
+    dx2 = torch.empty_like(dy2)
+    gsr.gsr_group_norm_grad(dy2, mean[1:].contiguous(), rstd[1:].contiguous(), dx2, codes=codes2, scales=scales2)
+    gsr.gsr_group_norm_grad(y, mean, rstd, y, codes=codes, scales=scales, graph_ptr=ptr)
+    assert torch.allclose(end(y).float(), dx2.float(), rtol=2.0 ** -7, atol=2.0 ** -10)
