@@ -441,7 +441,7 @@ gsr_status_t gsr_checkpoint_load(const int8_t* codes, const float* scales, int64
  * dz is rounded to 16 bits before the products with E and x.  Equal calls give equal bits.  Values must be finite: a row with infinities or NaN gets a
  * loss that is none, which then is the mean's.  1 <= d <= 512, c divides d, n and classes below 2^28; pointers aligned to their elements.
  * workspace: device, 16-byte aligned, at least gsr_class_loss_workspace() / gsr_class_grad_workspace() bytes (0: sizes that are refused; never
- * fewer for more rows or classes, so that one serves any fewer), some copies of x and E; it holds nothing between calls.  What a call writes overlaps nothing that it reads.  Calls only launch kernels and may be captured;
+ * fewer for more rows or classes, so that one serves any fewer), copies of x and E and up to 2^17 rows of d sums in float32 for each; it holds nothing between calls.  What a call writes overlaps nothing that it reads.  Calls only launch kernels and may be captured;
  * calls with workspaces of their own may run side by side. */
 size_t gsr_class_loss_workspace(int64_t n, int64_t classes, int32_t d, int32_t dtype);
 size_t gsr_class_grad_workspace(int64_t n, int64_t classes, int32_t d, int32_t dtype);

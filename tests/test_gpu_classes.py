@@ -118,6 +118,8 @@ CASES = [
     (300, 4_099, 256, 8, BF16, torch.int32, "mixed", 8, 8, True),
     (513, 700, 384, 2, F32, torch.int64, "common", 0, 0, True),
     (513, 700, 300, 0, BF16, torch.int32, "mixed", 0, 0, False),
+    (70_001, 23, 64, 2, F32, torch.int32, "mixed", 0, 0, True),
+    (70_001, 23, 40, 0, BF16, torch.int64, "mixed", 0, 0, True),
     (200, 333, 512, 2, F32, torch.int32, "mixed", 0, 0, True),
     (200, 333, 512, 8, BF16, torch.int32, "mixed", 0, 0, True),
     (65, 130, 511, 0, F32, torch.int32, "mixed", 1, 0, True),
