@@ -436,7 +436,7 @@ gsr_status_t gsr_checkpoint_load(const int8_t* codes, const float* scales, int64
  * class:  dx_out = dz E (a plane as x, row stride lddx), dtable_out = dz^T x (classes rows of d values of `dtype`, row stride lddt), dbias_out_j =
  * sum_i dz_ij (`classes` floats); any but not all of them may be NULL.  Every element is written.
  *
- * float32 values, |v| < 2^64, enter the products as multiples of 2^-22 of themselves or 2^-39 of the largest of 32 rows (aligned ones), dz as those of
+ * float32 values, |v| < 2^64, enter the products as multiples of 2^-22 of themselves or 2^-39 of the largest of their row, dz as those of
  * 2^-22 of itself or 2^-36 of the largest in its sum (below 2^-70 it may count as 0); sums are taken in float32 (the loss and dbias: in float64 across tiles).  With 16-bit planes
  * dz is rounded to 16 bits before the products with E and x.  Equal calls give equal bits.  Values must be finite: a row with infinities or NaN gets a
  * loss that is none, which then is the mean's.  1 <= d <= 512, c divides d, n and classes below 2^28; pointers aligned to their elements.

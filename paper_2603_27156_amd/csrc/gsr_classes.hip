@@ -11,9 +11,10 @@
 //
 // Operands are laid out once per call as the matrix instructions take them: rows in blocks of 16, columns in steps of 32, and of every (block, step)
 // 64 pieces of 16 bytes in lane order, zeros behind the last row and column.  So tiles are copied to LDS as they lie, from any layout, stride and
-// width.  bf16 planes go in as they are.  Floats go in as two fp16 pieces h + l of 11 bits each: 32 rows at a time are first multiplied by the power of two that
-// brings their largest value to 2^14 .. 2^15, which keeps both pieces in fp16's range (what is left out is below 2^-22 of a value, or 2^-39 of the
-// largest), and a product of floats is hh + hl + lh (l l is below 2^-24 of it), added up in float32.  Exact products of three bf16 pieces, which need no powers of two, are six:
+// width.  bf16 planes go in as they are.  Floats go in as two fp16 pieces h + l of 11 bits each: every row is first multiplied by the power of two that
+// brings its largest value to 2^14 .. 2^15, which keeps both pieces in fp16's range (what is left out is below 2^-22 of a value, or 2^-39 of the
+// largest; a power for 32 rows together would let one row, such as a padding one, take the others' bits), and a product of floats is hh + hl + lh
+// (l l is below 2^-24 of it), added up in float32.  Exact products of three bf16 pieces, which need no powers of two, are six:
 // 8,191 x 4,099 at D = 384, gradients 708 us instead of 362 (343 by now).
 #include "gsr_internal.h"
 #include "gsr_pieces.h"
@@ -55,7 +56,7 @@ struct ClassSetup {
     RowSource x, e;
     ClassTokens ids;
     uint4 *xf, *ef;                 // in pieces
-    float *x_exp, *e_exp;           // floats: exponents of the powers of two that the 32 rows of a tile have to be multiplied by
+    float *x_scale, *e_scale;       // floats: the power of two that a row's pieces have to be multiplied by
     const float *lse, *bias;        // lse: NULL in the forward
     float *lse_out, *bias_out;      // of all rows that the kernels read, padded ones too
     int32_t *target, *counts;       // class of every row; rows with a class of every block
@@ -114,8 +115,9 @@ __device__ __forceinline__ void lay_out(const RowSource& s, uint4* __restrict__ 
         out[piece * 64 + lane] = w;
     }
 }
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }         // of a normal one
 // floats: 32 rows by a workgroup, all of them in its registers
-__device__ __forceinline__ void lay_out(const RowSource& s, uint4* __restrict__ out, float* __restrict__ exponents, int64_t pad, int ks, int64_t tile,
+__device__ __forceinline__ void lay_out(const RowSource& s, uint4* __restrict__ out, float* __restrict__ scales, int64_t pad, int ks, int64_t tile,
                                         const ClassTokens* known, float) {
     constexpr int MOST = kMaxClassWidth / 32 * 2 / 4;           // of a wave
     const int lane = lane_id(), wave = threadIdx.x >> 6;
@@ -126,7 +128,7 @@ __device__ __forceinline__ void lay_out(const RowSource& s, uint4* __restrict__ 
         in[b] = row < s.rows && (!known || known->at(row) >= 0);
     }
     float v[MOST][8];
-    uint32_t top = 0;                   // bits of the largest finite value
+    uint32_t top[2] = {0, 0};           // of the lane's rows: bits of the largest finite value
 #pragma unroll
     for (int i = 0; i < MOST; ++i) {
         const int piece = i * 4 + wave, b = piece >= ks, k = b ? piece - ks : piece;
@@ -134,35 +136,49 @@ __device__ __forceinline__ void lay_out(const RowSource& s, uint4* __restrict__ 
     }
 #pragma unroll
     for (int i = 0; i < MOST; ++i) {
-        if (i * 4 + wave >= 2 * ks) continue;
+        const int piece = i * 4 + wave;
+        if (piece >= 2 * ks) continue;
+        uint32_t most = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const uint32_t u = __float_as_uint(v[i][j]) & 0x7FFFFFFFu;
-            if (u < 0x7F800000u) top = top > u ? top : u;
+            if (u < 0x7F800000u) most = most > u ? most : u;
         }
+        if (piece < ks) top[0] = top[0] > most ? top[0] : most;
+        else top[1] = top[1] > most ? top[1] : most;
     }
-    for (int o = 32; o; o >>= 1) {
-        const uint32_t u = __shfl_xor(top, o);
-        top = top > u ? top : u;
+    __shared__ uint32_t s_top[4][2][16];
+    float up[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        for (int o = 16; o < 64; o <<= 1) {
+            const uint32_t u = __shfl_xor(top[b], o);
+            top[b] = top[b] > u ? top[b] : u;
+        }
+        if (lane < 16) s_top[wave][b][lane] = top[b];
     }
-    __shared__ uint32_t s_top[4];
-    if (lane == 0) s_top[wave] = top;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < 4; ++w) top = top > s_top[w] ? top : s_top[w];
-    // rows of zeros, and rows below 2^-100, whose products are nothing beside the rounding of any logit
-    int e = (int)(top >> 23) - 127;
-    if (top == 0) e = 0;
-    if (e < -100) e = -100;
-    const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
-    if (threadIdx.x == 0) exponents[tile] = (float)(e - 14);
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const uint32_t u = s_top[w][b][lane & 15];
+            top[b] = top[b] > u ? top[b] : u;
+        }
+        // rows of zeros, and rows below 2^-100, whose products are nothing beside the rounding of any logit
+        int e = (int)(top[b] >> 23) - 127;
+        if (top[b] == 0) e = 0;
+        if (e < -100) e = -100;
+        up[b] = power_of_two(14 - e);
+        if (wave == 0 && lane < 16) scales[tile * kTileRows + b * 16 + lane] = power_of_two(e - 14);
+    }
 #pragma unroll
     for (int i = 0; i < MOST; ++i) {
         const int piece = i * 4 + wave;
         if (piece >= 2 * ks) continue;
         uint32_t h[8], l[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) two_pieces(v[i][j] * up, h[j], l[j]);
+        for (int j = 0; j < 8; ++j) two_pieces(v[i][j] * (piece < ks ? up[0] : up[1]), h[j], l[j]);
         uint4* to = out + (tile * 2 * ks + piece) * 128 + lane;
         to[0] = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
         to[64] = make_uint4(l[0] | l[1] << 16, l[2] | l[3] << 16, l[4] | l[5] << 16, l[6] | l[7] << 16);
@@ -173,12 +189,12 @@ __global__ __launch_bounds__(256) void k_class_setup(ClassSetup s) {
     unsigned b = blockIdx.x;
     const int wave = threadIdx.x >> 6;
     if (b < s.x_blocks) {
-        lay_out(s.x, s.xf, s.x_exp, s.x_pad, s.ks, b, s.lse ? &s.ids : nullptr, T{});
+        lay_out(s.x, s.xf, s.x_scale, s.x_pad, s.ks, b, s.lse ? &s.ids : nullptr, T{});
         return;
     }
     b -= s.x_blocks;
     if (b < s.e_blocks) {
-        lay_out(s.e, s.ef, s.e_exp, s.e_pad, s.ks, b, nullptr, T{});
+        lay_out(s.e, s.ef, s.e_scale, s.e_pad, s.ks, b, nullptr, T{});
         return;
     }
     b -= s.e_blocks;
@@ -278,7 +294,7 @@ __device__ __forceinline__ f32x4 all_four(float v) { return f32x4{v, v, v, v}; }
 // ---- forward ---------------------------------------------------------------------------------------------
 struct ClassLossArgs {
     const uint4 *xf, *ef;
-    const float *x_exp, *e_exp;             // floats only
+    const float *x_scale, *e_scale;         // floats only
     const float* bias;
     const int32_t* target;
     float2* part;                   // [splits][x_pad]: running maximum, sum of exp(z - maximum)
@@ -299,11 +315,11 @@ __global__ __launch_bounds__(256, loss_waves(KS, NP)) void k_class_loss(ClassLos
     frag8 own[RB][KS][NP];
     load_own<KS, NP, RB>(g.xf, block0, lane, own);
     int target[RB];
-    float top[RB], sum[RB], own_exp[RB];
+    float top[RB], sum[RB], own_scale[RB];
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
         target[r] = g.target[(block0 + r) * 16 + (lane & 15)];
-        own_exp[r] = NP == 2 ? g.x_exp[(block0 + r) >> 1] : 0.0f;
+        own_scale[r] = NP == 2 ? g.x_scale[(block0 + r) * 16 + (lane & 15)] : 0.0f;
         top[r] = kNoMax;
         sum[r] = 0.0f;
     }
@@ -321,14 +337,13 @@ __global__ __launch_bounds__(256, loss_waves(KS, NP)) void k_class_loss(ClassLos
         }
         tile_logits<KS, NP, RB>(tile, own, lane, z);
         if constexpr (NP == 2) {
-            const float e = g.e_exp[t];
 #pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                const float f = __builtin_amdgcn_exp2f(own_exp[r] + e);
+            for (int blk = 0; blk < 2; ++blk) {
+                const f32x4 scale = four(g.e_scale + (int64_t)t * kTileRows + blk * 16 + grp * 4);
 #pragma unroll
-                for (int blk = 0; blk < 2; ++blk)
+                for (int r = 0; r < RB; ++r)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) z[blk][r][i] = fmaf(z[blk][r][i], f, bias[blk][i]);
+                    for (int i = 0; i < 4; ++i) z[blk][r][i] = fmaf(z[blk][r][i] * scale[i], own_scale[r], bias[blk][i]);
             }
         }
 #pragma unroll
@@ -448,7 +463,7 @@ __global__ __launch_bounds__(1024) void k_class_loss_sum(const LossPart* __restr
 // ---- backward --------------------------------------------------------------------------------------------
 struct ClassGradArgs {
     const uint4 *own, *stream;      // in pieces: the rows that a workgroup keeps, and the tiles
-    const float *own_exp, *stream_exp;          // floats only: of their tiles
+    const float *own_scale, *stream_scale;      // floats only: of their rows
     const float *lse, *bias;
     const int32_t *target, *counts;
     void* out;                      // rows x d of T: a plane, or a table
@@ -504,15 +519,15 @@ __device__ __forceinline__ s16x4 column_of_lds(const uint4* tile, int blk, int c
 }
 
 // Two pieces of fp16 hold dz only in its range, and gradients of rare classes and of rows that are nearly learnt are far below 1.  So every own row has a power of
-// two 2^k by which its dz (times the streamed tile's power of two) and its sums are multiplied; k begins high, and whenever a value of the row would leave
-// fp16's range it goes down so far that the row may grow eightfold before it does again.  A dz is held to 2^-22 of itself or 2^-36 of the row's largest so far.
-constexpr float kFirstExponent = 60.0f, kLargestPiece = 32768.0f;
+// two k by which its dz (times the streamed row's power of two) and its sums are multiplied; k begins high, and whenever a value of the row would leave
+// fp16's range it goes down so far that the row may grow eightfold before it does again.  A dz is held to 2^-22 of itself, or its product with the streamed row's
+// largest value to 2^-36 of the largest so far.
+constexpr float kFirstScale = 0x1p60f, kLargestPiece = 32768.0f;
 template <int KS, int RB>
 __device__ __forceinline__ void fit_row(int r, float largest, float& k, f32x4 (&z)[2][RB], f32x4 (&acc)[RB][2 * KS], int grp) {
     const bool over = largest >= kLargestPiece;         // (not for NaN)
-    const float down = over ? (float)(14 - 3) - (float)((int)(__float_as_uint(largest) >> 23) - 127) : 0.0f;
-    const float f = __builtin_amdgcn_exp2f(down);
-    k += down;
+    const float f = over ? power_of_two(14 - 3 + 127 - (int)(__float_as_uint(largest) >> 23)) : 1.0f;
+    k *= f;
 #pragma unroll
     for (int blk = 0; blk < 2; ++blk)
 #pragma unroll
@@ -538,7 +553,7 @@ __device__ __forceinline__ void grad_side(const ClassGradArgs& g, unsigned index
     frag8 own[RB][KS][NP];
     load_own<KS, NP, RB>(g.own, block0, lane, own);
     // of this wave's rows: lse and class (BY_CLASS: bias and class number), and their powers of two; the same of streamed rows comes with the tile
-    float own_f[RB], own_exp[RB], k[RB];
+    float own_f[RB], own_scale[RB], k[RB];
     int own_c[RB];
     f32x4 acc[RB][2 * KS];
     double bias_sum[RB];
@@ -547,8 +562,8 @@ __device__ __forceinline__ void grad_side(const ClassGradArgs& g, unsigned index
         const int64_t i = (block0 + r) * 16 + (lane & 15);
         own_f[r] = BY_CLASS ? g.bias[i] : g.lse[i];
         own_c[r] = BY_CLASS ? (int)i : g.target[i];
-        own_exp[r] = NP == 2 ? g.own_exp[(block0 + r) >> 1] : 0.0f;
-        k[r] = NP == 2 ? kFirstExponent : 0.0f;
+        own_scale[r] = NP == 2 ? g.own_scale[i] : 0.0f;
+        k[r] = kFirstScale;
         bias_sum[r] = 0.0;
 #pragma unroll
         for (int c = 0; c < 2 * KS; ++c) acc[r][c] = all_four(0.0f);
@@ -557,12 +572,13 @@ __device__ __forceinline__ void grad_side(const ClassGradArgs& g, unsigned index
     for (int t = t0; t < t1; ++t) {
         const uint4* tile = s_tile[TWO ? (t - t0) & 1 : 0];
         if (TWO && t + 1 < t1) fetch_tile<N>(g.stream + (int64_t)(t + 1) * N * 64, s_tile[TWO ? (t - t0 + 1) & 1 : 0], wave, lane);
-        f32x4 z[2][RB], row_f[2];
+        f32x4 z[2][RB], row_f[2], row_scale[2];
         int row_c[2][4];
 #pragma unroll
         for (int blk = 0; blk < 2; ++blk) {
             const int64_t i = (int64_t)t * kTileRows + blk * 16 + grp * 4;
             row_f[blk] = four((BY_CLASS ? g.lse : g.bias) + i);
+            if constexpr (NP == 2) row_scale[blk] = four(g.stream_scale + i);
             int4 c = make_int4((int)i, (int)i + 1, (int)i + 2, (int)i + 3);
             if constexpr (BY_CLASS) c = *reinterpret_cast<const int4*>(g.target + i);
             row_c[blk][0] = c.x; row_c[blk][1] = c.y; row_c[blk][2] = c.z; row_c[blk][3] = c.w;
@@ -576,47 +592,27 @@ __device__ __forceinline__ void grad_side(const ClassGradArgs& g, unsigned index
         frag8 dz[RB][NP];
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
-            if constexpr (NP == 1) {
 #pragma unroll
-                for (int blk = 0; blk < 2; ++blk)
+            for (int blk = 0; blk < 2; ++blk)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float p = __builtin_amdgcn_exp2f((z[blk][r][i] - (BY_CLASS ? row_f[blk][i] : own_f[r])) * kLog2e);
-                        z[blk][r][i] = row_c[blk][i] == own_c[r] ? p - 1.0f : p;
-                    }
-                if constexpr (BY_CLASS) {
-                    const f32x4 s = z[0][r] + z[1][r];
-                    bias_sum[r] += (double)((s[0] + s[1]) + (s[2] + s[3]));
+                for (int i = 0; i < 4; ++i) {
+                    const float b = BY_CLASS ? own_f[r] : row_f[blk][i], l = BY_CLASS ? row_f[blk][i] : own_f[r];
+                    if constexpr (NP == 2) z[blk][r][i] = fmaf(z[blk][r][i] * row_scale[blk][i], own_scale[r], b);
+                    const float p = __builtin_amdgcn_exp2f((z[blk][r][i] - l) * kLog2e);
+                    z[blk][r][i] = row_c[blk][i] == own_c[r] ? p - 1.0f : p;
                 }
-            } else {
-                const float e = g.stream_exp[t], f = __builtin_amdgcn_exp2f(own_exp[r] + e), up = e + k[r];
-#pragma unroll
-                for (int blk = 0; blk < 2; ++blk)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float b = BY_CLASS ? own_f[r] : row_f[blk][i], l = BY_CLASS ? row_f[blk][i] : own_f[r];
-                        z[blk][r][i] = __builtin_amdgcn_exp2f(fmaf(fmaf(z[blk][r][i], f, b) - l, kLog2e, up));
-                    }
-                bool hit = false;
-#pragma unroll
-                for (int blk = 0; blk < 2; ++blk)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) hit |= row_c[blk][i] == own_c[r];
-                if (ballot(hit)) {
-                    const float one = __builtin_amdgcn_exp2f(up);
-#pragma unroll
-                    for (int blk = 0; blk < 2; ++blk)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (row_c[blk][i] == own_c[r]) z[blk][r][i] -= one;
-                }
-                if constexpr (BY_CLASS) {
-                    const f32x4 s = z[0][r] + z[1][r];
-                    bias_sum[r] += (double)((s[0] + s[1]) + (s[2] + s[3])) * (double)__builtin_amdgcn_exp2f(-up);
-                }
+            if constexpr (BY_CLASS) {
+                const f32x4 s = z[0][r] + z[1][r];
+                bias_sum[r] += (double)((s[0] + s[1]) + (s[2] + s[3]));
+            }
+            if constexpr (NP == 2) {
                 float largest = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) largest = fmaxf(largest, fmaxf(fabsf(z[0][r][i]), fabsf(z[1][r][i])));
+                for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                    for (int blk = 0; blk < 2; ++blk) z[blk][r][i] = z[blk][r][i] * k[r] * row_scale[blk][i];
+                    largest = fmaxf(largest, fmaxf(fabsf(z[0][r][i]), fabsf(z[1][r][i])));
+                }
                 largest = quarter_fmax(largest);
                 if (ballot(largest >= kLargestPiece)) fit_row<KS, RB>(r, largest, k[r], z, acc, grp);
             }
@@ -658,7 +654,7 @@ __device__ __forceinline__ void grad_side(const ClassGradArgs& g, unsigned index
         }
         if (!g.out) continue;                   // only the bias is asked for
         if constexpr (NP == 2) {
-            const float f = __builtin_amdgcn_exp2f(-k[r]);
+            const float f = __uint_as_float(0x7F000000u - __float_as_uint(k[r]));           // 1 / k
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float row = __shfl(f, grp * 4 + i);
@@ -807,7 +803,7 @@ struct ClassPlan {
     int ks, np, loss_rb, grad_rb;
     int64_t x_pad, e_pad;
     int loss_splits, x_splits, e_splits;
-    size_t xf, ef, x_exp, e_exp, lse, bias, target, counts, loss_bytes;         // the first of these are shared
+    size_t xf, ef, x_scale, e_scale, lse, bias, target, counts, loss_bytes;         // the first of these are shared
     size_t part, at_target, parts;                              // forward
     size_t x_part, e_part, bias_part, grad_bytes;               // backward
 };
@@ -832,8 +828,8 @@ ClassPlan class_plan(int64_t n, int64_t classes, int32_t d, int32_t dtype) {
     };
     p.xf = take((size_t)p.x_pad * p.ks * 64 * p.np);
     p.ef = take((size_t)p.e_pad * p.ks * 64 * p.np);
-    p.x_exp = take((size_t)p.x_pad / kTileRows * 4);
-    p.e_exp = take((size_t)p.e_pad / kTileRows * 4);
+    p.x_scale = take((size_t)p.x_pad * 4);
+    p.e_scale = take((size_t)p.e_pad * 4);
     p.lse = take((size_t)p.x_pad * 4);
     p.bias = take((size_t)p.e_pad * 4);
     p.target = take((size_t)p.x_pad * 4);
@@ -902,8 +898,8 @@ ClassSetup launch_setup(const ClassShape& s, const ClassPlan& p, const float* bi
     a.ids = s.ids;
     a.xf = (uint4*)(ws + p.xf);
     a.ef = (uint4*)(ws + p.ef);
-    a.x_exp = (float*)(ws + p.x_exp);
-    a.e_exp = (float*)(ws + p.e_exp);
+    a.x_scale = (float*)(ws + p.x_scale);
+    a.e_scale = (float*)(ws + p.e_scale);
     a.lse = lse;
     a.bias = bias;
     a.lse_out = (float*)(ws + p.lse);
@@ -993,7 +989,7 @@ gsr_status_t gsr_class_loss(const void* x, int64_t ldx, int64_t n, int32_t d, in
     LossPart* parts = (LossPart*)(ws + p.parts);
     if (n) {
         const ClassSetup a = launch_setup(s, p, bias, nullptr, ws, dtype, st);
-        const ClassLossArgs g{a.xf, a.ef, a.x_exp, a.e_exp, a.bias_out, a.target, (float2*)(ws + p.part), (float*)(ws + p.at_target), p.x_pad,
+        const ClassLossArgs g{a.xf, a.ef, a.x_scale, a.e_scale, a.bias_out, a.target, (float2*)(ws + p.part), (float*)(ws + p.at_target), p.x_pad,
                               (int32_t)((classes + kTileRows - 1) / kTileRows), p.loss_splits};
         by_steps(p.ks, [&](auto k) {
             constexpr int KS = k.value, R1 = loss_blocks(KS, 1), R2 = loss_blocks(KS, 2);
@@ -1038,8 +1034,8 @@ gsr_status_t gsr_class_grad(const void* x, int64_t ldx, int64_t n, int32_t d, in
     if (dx_out && n) {
         g.own = a.xf;
         g.stream = a.ef;
-        g.own_exp = a.x_exp;
-        g.stream_exp = a.e_exp;
+        g.own_scale = a.x_scale;
+        g.stream_scale = a.e_scale;
         g.out = dx_out;
         g.rows = n;
         g.ld = lddx;
@@ -1053,8 +1049,8 @@ gsr_status_t gsr_class_grad(const void* x, int64_t ldx, int64_t n, int32_t d, in
     if (dtable_out || dbias_out) {
         h.own = a.ef;
         h.stream = a.xf;
-        h.own_exp = a.e_exp;
-        h.stream_exp = a.x_exp;
+        h.own_scale = a.e_scale;
+        h.stream_scale = a.x_scale;
         h.out = dtable_out;
         h.dbias = dbias_out;
         h.rows = classes;
