@@ -519,25 +519,32 @@ __device__ __forceinline__ s16x4 column_of_lds(const uint4* tile, int blk, int c
 }
 
 // Two pieces of fp16 hold dz only in its range, and gradients of rare classes and of rows that are nearly learnt are far below 1.  So every own row has a power of
-// two k by which its dz (times the streamed row's power of two) and its sums are multiplied; k begins high, and whenever a value of the row would leave
+// two k by which its dz (times the streamed row's power of two) and its sums are multiplied; k begins so high that no dz above 2^-100 of a streamed row of its size
+// is lost, stays below 2^100 over the streamed rows' powers (so that a dz of 1 is finite), and whenever a value of the row would leave
 // fp16's range it goes down so far that the row may grow eightfold before it does again.  A dz is held to 2^-22 of itself, or its product with the streamed row's
 // largest value to 2^-36 of the largest so far.
-constexpr float kFirstScale = 0x1p60f, kLargestPiece = 32768.0f;
+constexpr float kLargestRow = 0x1p100f, kLargestPiece = 32768.0f;
+// room: what k already had to go down by for the tile's sake
 template <int KS, int RB>
-__device__ __forceinline__ void fit_row(int r, float largest, float& k, f32x4 (&z)[2][RB], f32x4 (&acc)[RB][2 * KS], int grp) {
+__device__ __forceinline__ void fit_row(int r, float room, float largest, float& k, f32x4 (&z)[2][RB], f32x4 (&acc)[RB][2 * KS], int grp) {
     const bool over = largest >= kLargestPiece;         // (not for NaN)
     const float f = over ? power_of_two(14 - 3 + 127 - (int)(__float_as_uint(largest) >> 23)) : 1.0f;
-    k *= f;
+    k = k * room * f;                                   // (room * f by itself may be below the smallest number)
 #pragma unroll
     for (int blk = 0; blk < 2; ++blk)
 #pragma unroll
         for (int i = 0; i < 4; ++i) z[blk][r][i] *= f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float row = __shfl(f, grp * 4 + i);       // sums lie by rows, values by columns
+        const float row = __shfl(room * f, grp * 4 + i);        // sums lie by rows, values by columns
 #pragma unroll
         for (int c = 0; c < 2 * KS; ++c) acc[r][c][i] *= row;
     }
+}
+// what brings k times `scale`, both powers of two, to kLargestRow at most
+__device__ __forceinline__ float room_for(float k, float scale) {
+    const int over = (int)(__float_as_uint(k) >> 23) + (int)(__float_as_uint(scale) >> 23) - 2 * 127 - 100;
+    return over > 0 ? power_of_two(-over) : 1.0f;
 }
 
 // Workgroup `index` of those of one side: a block of its rows and a part of the tiles.
@@ -563,7 +570,7 @@ __device__ __forceinline__ void grad_side(const ClassGradArgs& g, unsigned index
         own_f[r] = BY_CLASS ? g.bias[i] : g.lse[i];
         own_c[r] = BY_CLASS ? (int)i : g.target[i];
         own_scale[r] = NP == 2 ? g.own_scale[i] : 0.0f;
-        k[r] = kFirstScale;
+        k[r] = kLargestRow;
         bias_sum[r] = 0.0;
 #pragma unroll
         for (int c = 0; c < 2 * KS; ++c) acc[r][c] = all_four(0.0f);
@@ -606,15 +613,19 @@ __device__ __forceinline__ void grad_side(const ClassGradArgs& g, unsigned index
                 bias_sum[r] += (double)((s[0] + s[1]) + (s[2] + s[3]));
             }
             if constexpr (NP == 2) {
-                float largest = 0.0f;
+                float scale = 0.0f, largest = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) scale = fmaxf(scale, fmaxf(row_scale[0][i], row_scale[1][i]));
+                const bool high = ballot(scale > 1.0f);                 // (rows of values above 2^14 may leave k too little room)
+                const float room = high ? room_for(k[r], quarter_fmax(scale)) : 1.0f;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
 #pragma unroll
-                    for (int blk = 0; blk < 2; ++blk) z[blk][r][i] = z[blk][r][i] * k[r] * row_scale[blk][i];
+                    for (int blk = 0; blk < 2; ++blk) z[blk][r][i] = z[blk][r][i] * (k[r] * room) * row_scale[blk][i];
                     largest = fmaxf(largest, fmaxf(fabsf(z[0][r][i]), fabsf(z[1][r][i])));
                 }
                 largest = quarter_fmax(largest);
-                if (ballot(largest >= kLargestPiece)) fit_row<KS, RB>(r, largest, k[r], z, acc, grp);
+                if (high || ballot(largest >= kLargestPiece)) fit_row<KS, RB>(r, room, largest, k[r], z, acc, grp);
             }
             operand_of<NP>(z[0][r], z[1][r], dz[r]);
         }
