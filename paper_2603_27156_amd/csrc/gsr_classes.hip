@@ -292,12 +292,19 @@ __device__ __forceinline__ f32x4 four(const float* p) { return *reinterpret_cast
 __device__ __forceinline__ f32x4 all_four(float v) { return f32x4{v, v, v, v}; }
 
 // ---- forward ---------------------------------------------------------------------------------------------
+// A lane adds up exp(z - top) of its rows.  What a nearly learnt row's loss consists of, classes of 2^-24 and less of the largest's probability, is lost in a running
+// sum of 32 bits, so only the eight of a tile are added in 32 bits and the tiles in 64.  top follows the largest logit where it is left behind by more than 1: a few
+// times over any number of classes, each of which multiplies the sum by a rounded exponential; and a class 1 above the others is exactly 1 in the sum.
+struct alignas(16) SoftmaxSum {
+    double sum;
+    float top;
+};
 struct ClassLossArgs {
     const uint4 *xf, *ef;
     const float *x_scale, *e_scale;         // floats only
     const float* bias;
     const int32_t* target;
-    float2* part;                   // [splits][x_pad]: running maximum, sum of exp(z - maximum)
+    SoftmaxSum* part;               // [splits][x_pad]
     float* at_target;               // [x_pad]
     int64_t x_pad;
     int32_t tiles, splits;
@@ -315,13 +322,14 @@ __global__ __launch_bounds__(256, loss_waves(KS, NP)) void k_class_loss(ClassLos
     frag8 own[RB][KS][NP];
     load_own<KS, NP, RB>(g.xf, block0, lane, own);
     int target[RB];
-    float top[RB], sum[RB], own_scale[RB];
+    float top[RB], own_scale[RB];
+    double sum[RB];
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
         target[r] = g.target[(block0 + r) * 16 + (lane & 15)];
         own_scale[r] = NP == 2 ? g.x_scale[(block0 + r) * 16 + (lane & 15)] : 0.0f;
         top[r] = kNoMax;
-        sum[r] = 0.0f;
+        sum[r] = 0.0;
     }
     tile_arrived();
     for (int t = t0; t < t1; ++t) {
@@ -360,14 +368,16 @@ __global__ __launch_bounds__(256, loss_waves(KS, NP)) void k_class_loss(ClassLos
             for (int blk = 0; blk < 2; ++blk)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) m = fmaxf(m, z[blk][r][i]);
-            const float by = -m * kLog2e;               // rounded once for all: off by 2^-24 |m| in lse, as the logits are
-            float s = sum[r] * __builtin_amdgcn_exp2f((top[r] - m) * kLog2e);
+            m = m > top[r] + 1.0f ? m : top[r];
+            const float before = __builtin_amdgcn_exp2f((top[r] - m) * kLog2e);
+            top[r] = m;
+            f32x4 e[2];
 #pragma unroll
             for (int blk = 0; blk < 2; ++blk)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s += __builtin_amdgcn_exp2f(fmaf(z[blk][r][i], kLog2e, by));
-            top[r] = m;
-            sum[r] = s;
+                for (int i = 0; i < 4; ++i) e[blk][i] = __builtin_amdgcn_exp2f((z[blk][r][i] - m) * kLog2e);
+            const f32x4 pairs = e[0] + e[1];
+            sum[r] = fma((double)before, sum[r], (double)((pairs[0] + pairs[1]) + (pairs[2] + pairs[3])));
         }
         if constexpr (!TWO) {
             __syncthreads();
@@ -379,10 +389,10 @@ __global__ __launch_bounds__(256, loss_waves(KS, NP)) void k_class_loss(ClassLos
     for (int r = 0; r < RB; ++r) {
         float m = fmaxf(top[r], __shfl_xor(top[r], 16));
         m = fmaxf(m, __shfl_xor(m, 32));
-        float s = sum[r] * __builtin_amdgcn_exp2f((top[r] - m) * kLog2e);
+        double s = sum[r] * (double)__builtin_amdgcn_exp2f((top[r] - m) * kLog2e);
         s += __shfl_xor(s, 16);
         s += __shfl_xor(s, 32);
-        if (grp == 0) g.part[blockIdx.y * g.x_pad + (block0 + r) * 16 + lane] = make_float2(m, s);
+        if (grp == 0) g.part[blockIdx.y * g.x_pad + (block0 + r) * 16 + lane] = SoftmaxSum{s, m};
     }
 }
 // lse of rows and their part of the loss; a single workgroup writes the loss itself
@@ -410,9 +420,9 @@ __device__ __forceinline__ void add_up(double& sum, int64_t& count) {          /
         count += s_count[i];
     }
 }
-// 2^q lanes take the splits of a row.  Sums in 64 bits; exponentials and logarithms of 32 bits, whose 3 u are below those of the parts.  2,000 rows of two parts,
+// 2^q lanes take the splits of a row.  Sums in 64 bits; exponentials and logarithms of 32 bits, off by 3 u of themselves.  2,000 rows of two parts,
 // one workgroup: 3.6 us; with each part read twice and 64-bit functions 9.4.
-__global__ __launch_bounds__(1024) void k_class_lse(const float2* __restrict__ part, const float* __restrict__ at_target,
+__global__ __launch_bounds__(1024) void k_class_lse(const SoftmaxSum* __restrict__ part, const float* __restrict__ at_target,
                                                     const int32_t* __restrict__ target, int64_t n, int64_t x_pad, int splits, int q,
                                                     float* __restrict__ lse_out, LossPart* __restrict__ parts, float* __restrict__ loss) {
     double sum = 0.0;
@@ -423,24 +433,25 @@ __global__ __launch_bounds__(1024) void k_class_lse(const float2* __restrict__ p
         const int32_t t = target[i];
         const float at = at_target[i];
         constexpr int U = 4;                    // parts of a lane that stay in its registers: as many as it has, but for long sides
-        float2 p[U];
+        SoftmaxSum p[U];
 #pragma unroll
-        for (int k = 0; k < U; ++k) p[k] = first + k * step < splits ? part[(first + k * step) * x_pad + i] : make_float2(kNoMax, 0.0f);
+        for (int k = 0; k < U; ++k) p[k] = first + k * step < splits ? part[(first + k * step) * x_pad + i] : SoftmaxSum{0.0, kNoMax};
         float m = kNoMax;
 #pragma unroll
-        for (int k = 0; k < U; ++k) m = fmaxf(m, p[k].x);
-        for (int s = first + U * step; s < splits; s += step) m = fmaxf(m, part[s * x_pad + i].x);
+        for (int k = 0; k < U; ++k) m = fmaxf(m, p[k].top);
+        for (int s = first + U * step; s < splits; s += step) m = fmaxf(m, part[s * x_pad + i].top);
         for (int o = step >> 1; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+        auto to_top = [&](const SoftmaxSum& q) { return q.sum * (double)__builtin_amdgcn_exp2f((q.top - m) * kLog2e); };
         double l = 0.0;
 #pragma unroll
-        for (int k = 0; k < U; ++k) l += (double)(p[k].y * __builtin_amdgcn_exp2f((p[k].x - m) * kLog2e));
-        for (int s = first + U * step; s < splits; s += step) l += (double)(part[s * x_pad + i].y * __builtin_amdgcn_exp2f((part[s * x_pad + i].x - m) * kLog2e));
+        for (int k = 0; k < U; ++k) l += to_top(p[k]);
+        for (int s = first + U * step; s < splits; s += step) l += to_top(part[s * x_pad + i]);
         for (int o = step >> 1; o; o >>= 1) l += __shfl_xor(l, o);
         if (first || row >= n) continue;
-        const double lse = (double)m + (double)logf((float)l);
-        lse_out[i] = (float)lse;
+        const float above = l < 1.5 ? log1pf((float)(l - 1.0)) : logf((float)l);            // (l is 1 at least, or 0 if no class is left)
+        lse_out[i] = (float)((double)m + (double)above);
         if (t >= 0) {
-            sum += lse - (double)at;
+            sum += ((double)m - (double)at) + (double)above;
             ++count;
         }
     }
@@ -847,7 +858,7 @@ ClassPlan class_plan(int64_t n, int64_t classes, int32_t d, int32_t dtype) {
     p.counts = take((size_t)((p.x_pad + 1023) / 1024) * 4);
     const size_t shared = at;
     const int64_t x_parts = part_rows(e_tiles, p.x_pad), e_parts = part_rows(x_tiles, p.e_pad);
-    p.part = take((size_t)std::max(p.x_pad, x_parts) * sizeof(float2));
+    p.part = take((size_t)std::max(p.x_pad, x_parts) * sizeof(SoftmaxSum));
     p.at_target = take((size_t)p.x_pad * 4);
     p.parts = take((size_t)((n + 1023) / 1024 + 64) * sizeof(LossPart));       // (65,536 threads at most where a row has several)
     p.loss_bytes = at;
@@ -1000,7 +1011,7 @@ gsr_status_t gsr_class_loss(const void* x, int64_t ldx, int64_t n, int32_t d, in
     LossPart* parts = (LossPart*)(ws + p.parts);
     if (n) {
         const ClassSetup a = launch_setup(s, p, bias, nullptr, ws, dtype, st);
-        const ClassLossArgs g{a.xf, a.ef, a.x_scale, a.e_scale, a.bias_out, a.target, (float2*)(ws + p.part), (float*)(ws + p.at_target), p.x_pad,
+        const ClassLossArgs g{a.xf, a.ef, a.x_scale, a.e_scale, a.bias_out, a.target, (SoftmaxSum*)(ws + p.part), (float*)(ws + p.at_target), p.x_pad,
                               (int32_t)((classes + kTileRows - 1) / kTileRows), p.loss_splits};
         by_steps(p.ks, [&](auto k) {
             constexpr int KS = k.value, R1 = loss_blocks(KS, 1), R2 = loss_blocks(KS, 2);
