@@ -395,29 +395,33 @@ struct CodeSource {
 };
 
 // ---- forward ---------------------------------------------------------------------------------------------
-// Sums of x - k and (x - k)^2 in 64 bits, with the first value of the group in the first graph as k for all graphs: squares are all but exact there, and what
-// mean (x - k)^2 - (mean (x - k))^2 loses of the variance to cancellation is nothing unless a graph's mean lies some 2^20 standard deviations from k.
+// Sums of x - k and (x - k)^2 in 64 bits, with the first value of a graph's group as k: squares are all but exact there, and k, being one of `count` values, lies at
+// most sqrt(count) standard deviations from the mean, so that mean (x - k)^2 - (mean (x - k))^2 loses some count 2^-53 of the variance to cancellation.  k of another
+// graph would have no such bound.
 // 1M x 256 floats 178 us, 5.8 TB/s; 500k x 256 16-bit values 53 us, 4.8 TB/s, where the 64-bit sums take as long as the reads.  4,096 waves: with 2,048 or 16,384
 // the forward of the floats takes 498 or 495 us instead of 484, and its gradient from a checkpoint some 50 more.
 template <typename T>
-__device__ __forceinline__ double group_shift(const NormShape& s, const GraphRows& g, const T* x, const RowPlane& p, int group) {
+__device__ __forceinline__ float group_shift(const NormShape& s, const T* x, const RowPlane& p, int64_t first, int group) {
     const int column = group * s.cg, plane = column / s.dg;
-    const int64_t first = g.at(0), row = first < s.n ? first : s.n - 1;
-    const float v = to_float(x[plane * p.gs + row * p.ld + (column - plane * s.dg)]);
-    return fabsf(v) < INFINITY ? (double)v : 0.0;
+    const float v = to_float(x[plane * p.gs + first * p.ld + (column - plane * s.dg)]);
+    return fabsf(v) < INFINITY ? v : 0.0f;
 }
 template <typename T, int V, bool TAIL>
 __global__ __launch_bounds__(256) void k_norm_sums(NormShape s, GraphRows g, const T* __restrict__ x, RowPlane p, double2* __restrict__ pieces,
-                                                   double* __restrict__ shifts) {
+                                                   float* __restrict__ shifts) {
     const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (w >= s.chunks) return;
     const int slab = blockIdx.y;
     const LaneColumns c = lane_columns<V>(s, slab);
-    const double shift = group_shift(s, g, x, p, c.on ? c.group : 0), shift2 = TAIL && c.split < V ? group_shift(s, g, x, p, c.group + 1) : shift;
-    // by the lane in whose own columns the group begins
-    if (w == 0 && c.on && c.sub == 0 && c.plane * s.dg + c.own == c.group * s.cg) shifts[c.group] = shift;
-    if (TAIL && w == 0 && c.on && c.sub == 0 && c.split < V) shifts[c.group + 1] = shift2;
     over_graphs(s, g, w, [&](int64_t graph, int64_t a, int64_t b) {
+        const int64_t first = g.at(graph);
+        const float k1 = group_shift(s, x, p, first, c.on ? c.group : 0), k2 = TAIL && c.split < V ? group_shift(s, x, p, first, c.group + 1) : k1;
+        // by the lane in whose own columns the group begins, of the wave that has the graph's first row
+        if (a == first && c.on && c.sub == 0) {
+            if (c.plane * s.dg + c.own == c.group * s.cg) shifts[graph * s.groups + c.group] = k1;
+            if (TAIL && c.split < V) shifts[graph * s.groups + c.group + 1] = k2;
+        }
+        const double shift = k1, shift2 = k2;
         constexpr int U = 4;
         constexpr int A = TAIL ? V : 1;             // sums of every column, or of all
         double u[A], v[A];
@@ -462,14 +466,14 @@ __device__ __forceinline__ void statistics(double u, double v, double count, dou
 }
 template <int THREADS>
 __global__ __launch_bounds__(1024) void k_norm_join(NormShape s, GraphRows g, int V, const double2* __restrict__ pieces,
-                                                    const double* __restrict__ shifts, int64_t task_blocks, double eps,
+                                                    const float* __restrict__ shifts, int64_t task_blocks, double eps,
                                                     float* __restrict__ mean, float* __restrict__ rstd) {
     for (int64_t block = blockIdx.x; block < task_blocks; block += gridDim.x) {
         int64_t task, rows;
         double u, v;
         if (!joined<THREADS>(s, g, V, block, pieces, task, u, v, rows) || threadIdx.x % THREADS) continue;
         float m, r;
-        statistics(u, v, (double)rows * s.cg, rows ? shifts[task % s.groups] : 0.0, eps, m, r);
+        statistics(u, v, (double)rows * s.cg, rows ? (double)shifts[task] : 0.0, eps, m, r);
         mean[task] = m;
         rstd[task] = r;
     }
@@ -569,7 +573,7 @@ __global__ __launch_bounds__(1024) void k_norm_small(NormShape s, GraphRows g, c
     const int wave = threadIdx.x >> 6;
     const int64_t a = g.at(0), b = g.at(1) > a ? g.at(1) : a;
     constexpr int U = 4;
-    const double shift = group_shift(s, g, x, p, c.on ? c.group : 0);
+    const double shift = a < b ? (double)group_shift(s, x, p, a, c.on ? c.group : 0) : 0.0;
     double u = 0.0, v = 0.0;
     for (int64_t r = a + (int64_t)wave * U * c.subs; r < b; r += 16 * U * c.subs) {
         PlaneSource<T, V, false> q[U];
@@ -1064,9 +1068,9 @@ gsr_status_t norm_args(int32_t d, int32_t groups, int32_t act, const float* gamm
     return GSR_OK;
 }
 
-// The workspace of both directions: pieces; the groups' shifts; the means of the gradient, the columns' partial sums.
+// The workspace of both directions: pieces; what the sums of every (graph, group) are taken from, or in the gradient its means; the columns' partial sums.
 struct NormWs {
-    size_t pieces, shifts, means, columns, total;
+    size_t pieces, means, columns, total;
     int threads;                    // for a (graph, group) in the join
     int64_t task_blocks, task_wgs;
 };
@@ -1075,8 +1079,7 @@ NormWs carve_norm(const NormShape& s, int64_t graphs) {
     w.pieces = 0;
     // at least as many chunks as any number of rows up to n has, so that a workspace serves them all
     const int64_t chunks = std::max((s.n + kMaxRows - 1) / kMaxRows, std::min((s.n + least_rows(s, graphs) - 1) / least_rows(s, graphs), kChunks / s.slabs + 1));
-    w.shifts = align_up((size_t)(chunks + graphs) * s.stride() * sizeof(double2));
-    w.means = w.shifts + align_up((size_t)s.groups * sizeof(double));
+    w.means = align_up((size_t)(chunks + graphs) * s.stride() * sizeof(double2));
     w.columns = w.means + align_up((size_t)graphs * s.groups * sizeof(float2));
     w.total = w.columns + align_up((size_t)((chunks + 3) / 4) * 2 * s.d * 4);
     // (301 graphs of 32 groups, 500k x 256 16-bit values: the join 7.9 us with 16 threads, 13.7 with waves)
@@ -1187,7 +1190,7 @@ gsr_status_t gsr_group_norm(const void* x, int64_t ldx, int64_t n, int32_t d, in
     if (graphs == 0) return GSR_OK;
     hipStream_t st = (hipStream_t)stream;
     double2* pieces = (double2*)((char*)workspace + ws.pieces);
-    double* shifts = (double*)((char*)workspace + ws.shifts);
+    float* shifts = (float*)((char*)workspace + ws.means);
     by_piece(dtype, rule, [&](auto t, auto v, auto tail) {
         using T = decltype(t);
         constexpr int P = v.value;
