@@ -1,11 +1,11 @@
-"""Graphs of a batch stand by themselves: what one of them holds has no part in the others."""
+"""Graphs of a batch stand by themselves: what one of them holds, and how many of them are empty, has no part in the others."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2603_27156_amd as gsr
 from test_gpu_embed import BF16, F32, dev
-from test_gpu_norm import U, Reference, close, host, put
+from test_gpu_norm import ACTS, U, Reference, close, host, put
 
 pytestmark = pytest.mark.gpu
 
@@ -51,3 +51,56 @@ def test_graphs_of_very_different_size(far):
     ref = Reference(host(x), ptr.tolist(), 2, None, None, "none")
     close(mean.double().cpu().numpy(), ref.mean, 2 * U * np.abs(ref.mean))
     close(rstd.double().cpu().numpy(), ref.rstd, 2 * U * ref.rstd)
+
+
+def empty_runs(kind, empty):
+    """First rows of graphs in 300 rows, `empty` of them without a row at one offset inside a chunk of rows."""
+    at = {"middle": [0, 103] + [103] * empty + [203, 290], "padded": [0, 103, 203] + [203] * empty, "front": [11] * (empty + 1) + [103, 203],
+          "many": list(np.repeat([0, 5, 6, 7, 8, 103, 104, 203, 299], max(1, empty // 9)))}[kind]
+    return torch.tensor(at, dtype=torch.int32, device=dev())
+
+
+@pytest.mark.parametrize("kind", ["middle", "padded", "front", "many"])
+@pytest.mark.parametrize("empty", [1, 2, 63, 64, 65, 4_000])
+@pytest.mark.parametrize("d,groups,dtype,act", [(64, 4, F32, "silu"), (77, 7, BF16, "relu")])
+def test_empty_graphs_anywhere(d, groups, dtype, act, empty, kind):
+    rng = np.random.default_rng(empty)
+    ptr = empty_runs(kind, empty)
+    x, dy = put(rng.standard_normal((300, d)), dtype), put(rng.standard_normal((300, d)), dtype)
+    gamma, beta = put(1.0 + 0.3 * rng.standard_normal(d)), put(0.3 * rng.standard_normal(d))
+    y, mean, rstd = forward(x, ptr, groups, gamma=gamma, beta=beta, act=ACTS[act])
+    g64, b64 = gamma.double().cpu().numpy(), beta.double().cpu().numpy()
+    ref = Reference(host(x), ptr.tolist(), groups, g64, b64, act)
+    close(mean.double().cpu().numpy(), ref.mean, 2 * U * np.abs(ref.mean) + 2.0 ** -50)
+    close(rstd.double().cpu().numpy(), ref.rstd, 2 * U * ref.rstd)
+    ref = Reference(host(x), ptr.tolist(), groups, g64, b64, act, mean.double().cpu().numpy(), rstd.double().cpu().numpy())
+    close(host(y), *ref.forward(), dtype)
+    dx, dgamma, dbeta = torch.zeros_like(x), torch.empty(d, device=dev()), torch.empty(d, device=dev())
+    gsr.gsr_group_norm_grad(dy, mean, rstd, dx, x=x, gamma=gamma, beta=beta, act=ACTS[act], graph_ptr=ptr, dgamma_out=dgamma, dbeta_out=dbeta)
+    want, off = ref.backward(host(dy))
+    close(host(dx), want["dx"], off["dx"], dtype)
+    close(dgamma.double().cpu().numpy(), want["dgamma"], off["dgamma"])
+    close(dbeta.double().cpu().numpy(), want["dbeta"], off["dbeta"])
+    spare = torch.ones(300, dtype=torch.bool, device=dev())
+    spare[ptr[0]:ptr[-1]] = False
+    assert not y[spare].any() and not dx[spare].any()
+
+
+@pytest.mark.parametrize("kind", ["middle", "padded", "front"])
+def test_empty_graphs_are_not_walked_one_by_one(kind):
+    """A captured step has room for a fixed number of graphs, and most may be empty.  Two million of them at one offset: both directions end within 50 ms (a
+    wave that steps through them, two loads that depend on each other a graph, takes some two seconds; their statistics are 16 MB)."""
+    ptr = empty_runs(kind, 2_000_000)
+    x = torch.randn((300, 64), device=dev())
+    dx = torch.empty_like(x)
+    ws = torch.empty(gsr.gsr_group_norm_workspace(x, 1, ptr), dtype=torch.uint8, device=dev())
+    took = []
+    for _ in range(2):
+        start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        start.record()
+        y, mean, rstd = forward(x, ptr, 1, workspace=ws)
+        gsr.gsr_group_norm_grad(y, mean, rstd, dx, x=x, graph_ptr=ptr, workspace=ws)
+        end.record()
+        end.synchronize()
+        took.append(start.elapsed_time(end))
+    assert min(took) <= 50.0, took
