@@ -389,7 +389,7 @@ gsr_status_t gsr_adam_update_list(float* const* w, const void* const* dw, float*
  *                         m, r: as gsr_group_norm left them.  x, or with x = NULL its checkpoint, whose values then take the place of x.
  * RELU has the derivative 0 at 0.  SILU(z) = z / (1 + exp(-z)).  Sums over rows are taken in float64, those of a gradient over up to 1,024 rows in
  * float32 first, in an order that the sizes and the offsets alone fix.  What one graph holds has no part in another's results.
- * y_out may be x and dx_out may be dy, with the same stride; apart from that what a call writes overlaps nothing that it reads.
+ * y_out may be x and dx_out may be dy, with the same stride; apart from that what a call writes overlaps nothing that it reads (dx_out that is x is refused).
  * eps > 0; 1 <= d <= 131072; n < 2^31; pointers aligned to their elements; where graphs x (groups + d) is 2^30 or more a call may be refused.
  * workspace: device, 16-byte aligned, at least gsr_group_norm_workspace() bytes (0: sizes outside these limits; never fewer for more rows or graphs, so
  * that one serves any fewer); it holds nothing between calls.  Calls only launch kernels and may be captured; calls with workspaces of their own may run

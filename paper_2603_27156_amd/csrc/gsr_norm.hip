@@ -1247,6 +1247,7 @@ gsr_status_t gsr_group_norm_grad(const void* dy, int64_t lddy, const void* x, in
     GSR_TRY(graph_rows(graph_ptr, ptr_i64, graphs, n, &g));
     GSR_TRY(norm_args(d, groups, act, gamma, beta, mean, rstd, graphs));
     if (!aligned_to(dgamma_out, 4) || !aligned_to(dbeta_out, 4)) return fail(GSR_ERR_INVALID_ARG, "dgamma_out or dbeta_out is not aligned to its elements");
+    if (x && x == dx_out) return fail(GSR_ERR_INVALID_ARG, "dx_out is x, whose rows are read again while it is written");
     if (dy == dx_out && lddy != lddx) return fail(GSR_ERR_INVALID_ARG, "in place, but with row strides of %lld and %lld", (long long)lddy, (long long)lddx);
     const PieceRule rule = piece_of(dg, d / groups, dtype, dy == dx_out);
     const int V = rule.v;
