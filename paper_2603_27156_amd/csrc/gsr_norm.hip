@@ -1114,17 +1114,17 @@ NormShape apply_shape(NormShape s, const void* graph_ptr) {
     s.chunks = (s.n + s.rows - 1) / s.rows;
     return s;
 }
-// Workgroups for a slab of a graph that takes one launch, or 0.  One launch against three, floats, groups of 32 columns, in a captured graph: 200 rows 5.6 us /
-// 10.5, gradient 7.6 / 13.7; 2,000 rows (256 KB) 9.1 / 10.7 and 13.6 / 14.0; 4,000 rows 12.9 / 10.7 and 20.4 / 14.7.  Called from Python, where launches
-// wait for the host: 2,000 rows 12.2 / 16.4 and 13.7 / 18.2, 4,000 rows 12.8 / 16.4 and 20.2 / 18.2.
-constexpr int kSmallShares = 32;
-constexpr int64_t kSmallBytes = 256 << 10;
-unsigned small_shares(const NormShape& s, const PieceRule& rule, int64_t graphs, int32_t dtype, bool in_place) {
-    const int width = rule.v << s.lanes_log2;
+// Workgroups for a slab of a graph that takes one launch, or 0: a workgroup takes its slab's rows by rounds of 16 waves, 16 rounds at most and 32 of single columns.
+// One launch against three, silu, in a captured graph.  Floats, 64 columns in two groups, 8 rounds (512 rows): 8.0 us / 11.6, gradient 10.3 / 13.3; 16: 10.1 / 11.6
+// and 14.4 / 13.4; 32: 14.4 / 10.6 and 22.7 / 12.0.  One column, 16 rounds (4,096 rows): 9.3 / 9.6 and 11.4 / 10.4; 64: 22.8 / 11.2 and 33.0 / 12.3.  64 columns, each
+// its own group, 32 rounds (512 rows): 10.3 / 12.7 and 12.2 / 12.8; 64: 14.9 / 12.1 and 19.6 / 12.8.  Called from Python, where launches wait for the host: 2,000 rows of
+// 32 floats in two planes, 16 rounds, 12.2 / 16.4 and 13.7 / 18.2, 4,000 rows 12.8 / 16.4 and 20.2 / 18.2.
+constexpr int kSmallShares = 32, kSmallRounds = 16, kSmallColumnRounds = 32;
+unsigned small_shares(const NormShape& s, const PieceRule& rule, int64_t graphs, bool in_place) {
+    const int width = rule.v << s.lanes_log2, rows = 16 * (64 >> s.lanes_log2);
     const bool whole = s.dg % s.cg == 0 && (s.group_slabs == 1 || width % s.cg == 0);
-    if (graphs != 1 || rule.tail || !whole || s.n < 1 || s.n * std::min(width, s.dg) * (int64_t)dtype_size(dtype) > kSmallBytes) return 0;
+    if (graphs != 1 || rule.tail || !whole || s.n < 1 || s.n > (int64_t)rows * (rule.v == 1 ? kSmallColumnRounds : kSmallRounds)) return 0;
     if (in_place) return 1;                     // others would read what it has written
-    const int rows = 16 * (64 >> s.lanes_log2);
     return (unsigned)std::min<int64_t>(kSmallShares, (s.n + rows - 1) / rows);
 }
 dim3 rows_grid(const NormShape& s) { return dim3((unsigned)((s.chunks + 3) / 4), (unsigned)s.slabs); }
@@ -1200,7 +1200,7 @@ gsr_status_t gsr_group_norm(const void* x, int64_t ldx, int64_t n, int32_t d, in
     by_piece(dtype, rule, [&](auto t, auto v, auto tail) {
         using T = decltype(t);
         constexpr int P = v.value;
-        if (const unsigned shares = small_shares(s, rule, graphs, dtype, x == y_out)) {
+        if (const unsigned shares = small_shares(s, rule, graphs, x == y_out)) {
             const dim3 grid(shares, (unsigned)s.slabs);
             by_activation(act, [&](auto a) {
                 if (save)
@@ -1264,7 +1264,7 @@ gsr_status_t gsr_group_norm_grad(const void* dy, int64_t lddy, const void* x, in
         using T = decltype(t);
         using Source = decltype(source);
         constexpr int P = v.value, ACT = a.value;
-        if (const unsigned shares = small_shares(s, rule, graphs, dtype, dy == dx_out)) {
+        if (const unsigned shares = small_shares(s, rule, graphs, dy == dx_out)) {
             if constexpr (!tail.value)
                 hipLaunchKernelGGL((k_norm_grad_small<T, P, ACT, Source>), dim3(shares, (unsigned)s.slabs), dim3(1024), 0, st, s, g, (const T*)dy, pd, source, f,
                                    (T*)dx_out, po, dgamma_out, dbeta_out);

@@ -104,3 +104,26 @@ def test_empty_graphs_are_not_walked_one_by_one(kind):
         end.synchronize()
         took.append(start.elapsed_time(end))
     assert min(took) <= 50.0, took
+
+
+@pytest.mark.parametrize("d,groups,dtype,rows", [(1, 1, F32, 8192), (3, 3, F32, 8192), (4, 1, F32, 4096), (8, 1, BF16, 4096), (24, 24, BF16, 1024), (64, 2, F32, 1024),
+                                                 (256, 32, BF16, 512)])
+@pytest.mark.parametrize("more", [-1, 0, 1])
+def test_rows_about_the_single_launch(d, groups, dtype, rows, more):
+    """A single graph of as many rows as one launch takes, one fewer and one more."""
+    rng = np.random.default_rng(d)
+    n = rows + more
+    x, dy = put(rng.standard_normal((n, d)) + 3.0, dtype), put(rng.standard_normal((n, d)), dtype)
+    y, (mean, rstd) = torch.empty_like(x), (torch.empty((1, groups), device=dev()) for _ in range(2))
+    gsr.gsr_group_norm(x, y, mean, rstd, act=ACTS["silu"])
+    ref = Reference(host(x), [0, n], groups, None, None, "silu")
+    close(mean.double().cpu().numpy(), ref.mean, 2 * U * np.abs(ref.mean))
+    close(rstd.double().cpu().numpy(), ref.rstd, 2 * U * ref.rstd)
+    ref = Reference(host(x), [0, n], groups, None, None, "silu", mean.double().cpu().numpy(), rstd.double().cpu().numpy())
+    close(host(y), *ref.forward(), dtype)
+    dx, dgamma, dbeta = torch.empty_like(x), torch.empty(d, device=dev()), torch.empty(d, device=dev())
+    gsr.gsr_group_norm_grad(dy, mean, rstd, dx, x=x, act=ACTS["silu"], dgamma_out=dgamma, dbeta_out=dbeta)
+    want, off = ref.backward(host(dy))
+    close(host(dx), want["dx"], off["dx"], dtype)
+    close(dgamma.double().cpu().numpy(), want["dgamma"], off["dgamma"])
+    close(dbeta.double().cpu().numpy(), want["dbeta"], off["dbeta"])
