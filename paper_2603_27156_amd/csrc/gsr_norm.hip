@@ -107,19 +107,22 @@ __device__ __forceinline__ int64_t graph_of(const GraphRows& g, int64_t row) {
 
 // body(graph, a, b) for the rows [a, b) of every graph that has some in chunk w.  Of graphs without rows, of which a batch of fixed size may have any number at one
 // offset, the first is met and the others passed over.
+__device__ __forceinline__ int64_t uniform(int64_t v) {                // the same in every lane: kept in scalar registers
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)v) | (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(v >> 32)) << 32);
+}
 template <typename Body>
 __device__ __forceinline__ void over_graphs(const NormShape& s, const GraphRows& g, int64_t w, Body body) {
-    const int64_t r0 = w * s.rows, r1 = r0 + s.rows < s.n ? r0 + s.rows : s.n;
+    const int64_t r0 = uniform(w) * s.rows, r1 = r0 + s.rows < s.n ? r0 + s.rows : s.n;
     int64_t i = g.ptr ? graph_of(g, r0) : 0;
     if (i >= g.graphs) return;
-    for (int64_t first = g.at(i); first < r1;) {
-        const int64_t last = g.at(i + 1), a = first > r0 ? first : r0, b = last < r1 ? last : r1;
+    for (int64_t first = uniform(g.at(i)); first < r1;) {
+        const int64_t last = uniform(g.at(i + 1)), a = first > r0 ? first : r0, b = last < r1 ? last : r1;
         if (a < b) body(i, a, b);
         const bool empty = a >= b;
         const int64_t next = empty ? graph_of(g, a) : 0;
         i = next > i ? next : i + 1;                    // (goes on whatever the offsets)
         if (i >= g.graphs) break;
-        first = empty ? g.at(i) : last;
+        first = empty ? uniform(g.at(i)) : last;
     }
 }
 
