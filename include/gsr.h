@@ -422,7 +422,9 @@ gsr_status_t gsr_checkpoint_load(const int8_t* codes, const float* scales, int64
 
 /* ---- softmax cross entropy over many classes, without the logits ----
  *
- * A head on the output of a stack for tasks whose targets are classes (the type of a masked cell, say, with the table of the node embeddings):
+ * A head on the output of a stack for tasks whose targets are classes (the type of a masked cell, say, with the table of the node embeddings).  gsr_step has its
+ * own head and takes no gradient of its output: behind a stack these calls go with gsr_layer_forward and gsr_layer_backward, which keep no column sets (save_indices
+ * is gsr_step's), so that the gradient of a deep stack's input is that of save_indices 0.
  *   z_ij = x_i . E_j + b_j,  lse_i = log sum_j exp z_ij,  loss = mean over the rows with a class of lse_i - z_i,t_i  (0 if there are none).
  * x: a plane (device, n x d of `dtype`; ROW_MAJOR with row stride ldx, d at least; GROUP_PLANAR in c groups of d/c columns, row stride ldx, d/c at
  * least, group stride n * ldx).  E: `classes` rows of d values of the same dtype, row stride ldt.  bias: device, `classes` floats, or NULL; -inf

@@ -15,7 +15,7 @@
 // brings its largest value to 2^14 .. 2^15, which keeps both pieces in fp16's range (what is left out is below 2^-22 of a value, or 2^-39 of the
 // largest; a power for 32 rows together would let one row, such as a padding one, take the others' bits), and a product of floats is hh + hl + lh
 // (l l is below 2^-24 of it), added up in float32.  Exact products of three bf16 pieces, which need no powers of two, are six:
-// 8,191 x 4,099 at D = 384, gradients 708 us instead of 362 (343 by now).
+// 8,191 x 4,099 at D = 384, gradients 708 us instead of 362.
 #include "gsr_internal.h"
 #include "gsr_pieces.h"
 
@@ -309,7 +309,8 @@ struct ClassLossArgs {
     int64_t x_pad;
     int32_t tiles, splits;
 };
-// 32,749 x 50,021 of 256 16-bit values: 666 us, 1,260 TFLOP/s (a large library product reaches 1,444 on the same card); matrix cores busy 55 % of the cycles.
+// 32,749 x 50,021 of 256 16-bit values: 718 us, 1,170 TFLOP/s (a large library product reaches 1,444 on the same card); matrix cores busy 51 % of the cycles.  With sums of
+// 32 bits and exp by one multiply-add 4 % less, 12 % at 70,000 x 2,000 of 32 columns.
 template <int KS, int NP, int RB>
 __global__ __launch_bounds__(256, loss_waves(KS, NP)) void k_class_loss(ClassLossArgs g) {
     constexpr int N = 2 * KS * NP;
@@ -421,7 +422,7 @@ __device__ __forceinline__ void add_up(double& sum, int64_t& count) {          /
     }
 }
 // 2^q lanes take the splits of a row.  Sums in 64 bits; exponentials and logarithms of 32 bits, off by 3 u of themselves.  2,000 rows of two parts,
-// one workgroup: 3.6 us; with each part read twice and 64-bit functions 9.4.
+// one workgroup: 4.9 us; with each part read twice and 64-bit functions 9.4.
 __global__ __launch_bounds__(1024) void k_class_lse(const SoftmaxSum* __restrict__ part, const float* __restrict__ at_target,
                                                     const int32_t* __restrict__ target, int64_t n, int64_t x_pad, int splits, int q,
                                                     float* __restrict__ lse_out, LossPart* __restrict__ parts, float* __restrict__ loss) {
@@ -496,7 +497,11 @@ __device__ __forceinline__ float gradient_scale(const int32_t* __restrict__ coun
 __device__ __forceinline__ void store_as(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_as(bf16_t* p, float v) { p->bits = (uint16_t)bf16_bits(v); }
 
-// eight dz as the operand of the second product: rounded to bf16 (a relative 2^-9 of each, like the gradients that they are summed to), or in two pieces
+// Eight dz as the operand of the second product: rounded to bf16 (at most 2^-8 of each, as the gradients that they are summed to are), or in two pieces.  The first
+// rounding shows beside the second where sums are short: the error of dx and dE in norm is 0.0020 instead of 0.0017 with two or three terms a sum, 0.0017 either way with
+// 32,749 x 50,021.  It was left, since what takes it away costs every call more than it gives: fp16 operands with 11 bits of dz and a power of two for every row 3,270 us
+// instead of 2,880 there (fewer cycles, but the clock falls by 13 % with fp16 products), 72 -> 88 at 100,000 x 300 of 128 columns, 131 -> 167 at 70,000 x 2,000 of 32; two
+// bf16 pieces of dz 4,000, 83 and 174.
 template <int NP>
 __device__ __forceinline__ void operand_of(const f32x4& a, const f32x4& b, frag8 (&o)[NP]) {
     if constexpr (NP == 1) {
@@ -705,8 +710,8 @@ __device__ __forceinline__ void grad_side(const ClassGradArgs& g, unsigned index
     }
 }
 // dx and dE, or one of them, in one launch: what is left of the one's last round is filled by the other, and few rows and classes wait for one launch less.
-// 32,749 x 50,021 of 256 16-bit values: four products (each side has the logits anew) in 2.95 ms, 1,140 TFLOP/s; 8,191 x 4,099 floats at D = 384, 284 us, 1,090.
-// Matrix cores busy 48 and 50 % of the cycles.  With a quarter fewer vector instructions (exponents in one multiply-add, classes looked for by tile) the cycles
+// 32,749 x 50,021 of 256 16-bit values: four products (each side has the logits anew) in 2.91 ms, 1,150 TFLOP/s; 8,191 x 4,099 floats at D = 384, 308 us, 1,000.
+// Matrix cores busy 49 % of the cycles.  With a quarter fewer vector instructions (exponents in one multiply-add, classes looked for by tile) the cycles
 // fall by 2 % and the time grows by 3 %, since the clock falls; four blocks a wave, one wave a SIMD: 4.5 ms.
 template <int KS, int NP, int RB, typename T>
 __global__ __launch_bounds__(256, grad_waves(KS, NP)) void k_class_grad(ClassGradArgs by_row, ClassGradArgs by_class, unsigned row_from, unsigned class_from) {

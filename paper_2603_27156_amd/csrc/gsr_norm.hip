@@ -407,7 +407,7 @@ struct CodeSource {
 // Sums of x - k and (x - k)^2 in 64 bits, with the first value of a graph's group as k: squares are all but exact there, and k, being one of `count` values, lies at
 // most sqrt(count) standard deviations from the mean, so that mean (x - k)^2 - (mean (x - k))^2 loses some count 2^-53 of the variance to cancellation.  k of another
 // graph would have no such bound.
-// 1M x 256 floats 178 us, 5.8 TB/s; 500k x 256 16-bit values 53 us, 4.8 TB/s, where the 64-bit sums take as long as the reads.  4,096 waves: with 2,048 or 16,384
+// 1M x 256 floats 178 us, 5.8 TB/s; 500k x 256 16-bit values 57 us, 4.5 TB/s, where the 64-bit sums take as long as the reads.  4,096 waves: with 2,048 or 16,384
 // the forward of the floats takes 498 or 495 us instead of 484, and its gradient from a checkpoint some 50 more.
 template <typename T>
 __device__ __forceinline__ float group_shift(const NormShape& s, const T* x, const RowPlane& p, int64_t first, int group) {
@@ -522,7 +522,7 @@ struct ByGroup {
 // Bound by its reads and writes: 1M x 256 floats 299 us, 6.8 TB/s, with a checkpoint 390, 6.0; 500k x 256 16-bit values 78 us, 6.5 TB/s.
 template <typename T, int V, bool TAIL, int ACT, bool SAVE>
 __global__ __launch_bounds__(256) void k_norm_apply(NormShape s, GraphRows g, const T* x, RowPlane p, Affine f, T* y, RowPlane py, Checkpoint ck) {
-    const int64_t w = s.chunks - 1 - ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6));        // backwards: what was read last may still be cached
+    const int64_t w = s.chunks - 1 - ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6));        // rows backwards: of one slab what was read last may still be cached (several go in the order that they were read in)
     if (w < 0) return;
     const LaneColumns c = lane_columns<V>(s, blockIdx.y);
     float gamma[V], beta[V];
