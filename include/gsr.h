@@ -438,7 +438,8 @@ gsr_status_t gsr_checkpoint_load(const int8_t* codes, const float* scales, int64
  * sum_i dz_ij (`classes` floats); any but not all of them may be NULL.  Every element is written.
  *
  * float32 values, |v| < 2^64, enter the products as multiples of 2^-22 of themselves or 2^-39 of the largest of their row, dz as those of
- * 2^-22 of itself or, times the row of E or x that it meets, 2^-36 of the largest such product in its sum (a dz below 2^-100 may count as 0); sums are taken in float32, those over the classes in lse, of the loss and of dbias in float64 across tiles of 32.  With 16-bit planes
+ * 2^-22 of itself or, times the row of E or x that it meets, 2^-36 of the largest such product in its sum (products
+ * below 2^-88 keep fewer bits, below 2^-110 none); sums are taken in float32, those over the classes in lse, of the loss and of dbias in float64 across tiles of 32.  With 16-bit planes
  * dz is rounded to 16 bits before the products with E and x.  Equal calls give equal bits.  Values must be finite: a row with infinities or NaN gets a
  * loss that is none, which then is the mean's.  1 <= d <= 512, c divides d, n and classes below 2^28; pointers aligned to their elements.
  * workspace: device, 16-byte aligned, at least gsr_class_loss_workspace() / gsr_class_grad_workspace() bytes (0: sizes that are refused; never

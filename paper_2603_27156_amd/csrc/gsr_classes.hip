@@ -535,8 +535,8 @@ __device__ __forceinline__ s16x4 column_of_lds(const uint4* tile, int blk, int c
 }
 
 // Two pieces of fp16 hold dz only in its range, and gradients of rare classes and of rows that are nearly learnt are far below 1.  So every own row has a power of
-// two k by which its dz (times the streamed row's power of two) and its sums are multiplied; k begins so high that no dz above 2^-100 of a streamed row of its size
-// is lost, stays below 2^100 over the streamed rows' powers (so that a dz of 1 is finite), and whenever a value of the row would leave
+// two k by which its dz (times the streamed row's power of two) and its sums are multiplied; k begins so high that products of a dz and a streamed
+// value of 2^-88 and more keep all their bits, stays below 2^100 over the streamed rows' powers (so that a dz of 1 is finite), and whenever a value of the row would leave
 // fp16's range it goes down so far that the row may grow eightfold before it does again.  A dz is held to 2^-22 of itself, or its product with the streamed row's
 // largest value to 2^-36 of the largest so far.
 constexpr float kLargestRow = 0x1p100f, kLargestPiece = 32768.0f;
